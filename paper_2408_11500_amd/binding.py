@@ -48,7 +48,8 @@ EXPORTS = [
 ]
 
 PROF_KINDS = {0: "spmm", 1: "dense_fwd", 2: "dense_bwd", 3: "grad_reduce", 4: "concat", 5: "spmm_add",
-              6: "linear_fwd", 7: "linear_bwd", 8: "linear_grad", 9: "loss", 10: "accumulate"}
+              6: "linear_fwd", 7: "linear_bwd", 8: "linear_grad", 9: "loss", 10: "accumulate",
+              11: "embed", 12: "resnorm", 13: "clip"}
 
 
 class SliceGCNError(RuntimeError):
@@ -106,6 +107,43 @@ MAX_GROUP = 8
 
 class _Allocator(ctypes.Structure):
     _fields_ = [("ctx", ctypes.c_void_p), ("alloc", ctypes.c_void_p)]
+
+
+# slicegcn_train.h
+F32, BF16, F16 = 0, 1, 2
+VALUE_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+EMBED_IDS64, EMBED_PAD, EMBED_ACCUMULATE = 1, 2, 4
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+GATE_SIGMOID = 1
+RESNORM_MAX_WIDTH = 16384
+NORM_TWO, NORM_MAX = 0, 1
+
+
+class _EmbedDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("vocab", ctypes.c_int64), ("pad", ctypes.c_int64), ("scale", ctypes.c_double),
+                ("width", ctypes.c_int32), ("table_type", ctypes.c_int32), ("row_type", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class _ResnormDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("width", ctypes.c_int32), ("type", ctypes.c_int32), ("post", ctypes.c_int32),
+                ("pre", ctypes.c_int32), ("flags", ctypes.c_uint32), ("residual", ctypes.c_double), ("eps", ctypes.c_double)]
+
+
+class _ResnormParams(ctypes.Structure):  # slicegcn_resnorm_params and, for their gradients, slicegcn_resnorm_grads
+    _fields_ = [(name, ctypes.c_void_p) for name in ("post_w", "post_b", "pre_w", "pre_b", "gate")]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64)]
+
+
+class _ResnormIo(ctypes.Structure):
+    _fields_ = ([(name, _Rows) for name in ("x", "y", "gate", "h", "u")] + [("stats", ctypes.c_void_p)] +
+                [(name, _Rows) for name in ("dh", "du", "dx", "dy", "dgate")])
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_int64), ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -169,6 +207,22 @@ def lib() -> ctypes.CDLL:
         L.slicegcn_adam_step.argtypes = [vp, vp, vp, vp, i64, f64, f64, f64, f64, f64, i32, vp]
         L.slicegcn_cosine_lr.argtypes = [ctypes.c_double, ctypes.c_double, i32, i32]
         L.slicegcn_cosine_lr.restype = ctypes.c_double
+        L.slicegcn_embed_fwd.argtypes = [vp, vp, vp, i64, vp, i64, vp]
+        L.slicegcn_embed_sort_workspace_bytes.argtypes = [i64, i64]
+        L.slicegcn_embed_sort_workspace_bytes.restype = sz
+        L.slicegcn_embed_sort.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+        L.slicegcn_embed_bwd_workspace_bytes.argtypes = [i64, i32]
+        L.slicegcn_embed_bwd_workspace_bytes.restype = sz
+        L.slicegcn_embed_bwd.argtypes = [vp, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+        L.slicegcn_resnorm_fwd.argtypes = [vp, vp, vp, vp]
+        L.slicegcn_resnorm_bwd_workspace_bytes.argtypes = [i64, i32]
+        L.slicegcn_resnorm_bwd_workspace_bytes.restype = sz
+        L.slicegcn_resnorm_bwd.argtypes = [vp, vp, vp, vp, vp, sz, vp]
+        L.slicegcn_global_norm_workspace_bytes.argtypes = [vp, i32]
+        L.slicegcn_global_norm_workspace_bytes.restype = sz
+        L.slicegcn_global_norm.argtypes = [vp, i32, i32, f64, vp, vp, vp, sz, vp]
+        L.slicegcn_clip.argtypes = [vp, vp, i32, i32, f64, vp, vp, vp, sz, vp]
+        L.slicegcn_adam_step_scaled.argtypes = [vp, vp, vp, vp, vp, i64, f64, f64, f64, f64, f64, i32, vp]
         L.slicegcn_strerror.argtypes = [ctypes.c_int]
         L.slicegcn_strerror.restype = ctypes.c_char_p
         L.slicegcn_last_error.restype = ctypes.c_char_p
@@ -617,6 +671,182 @@ def slicegcn_softmax_ce(logits, labels, loss, dlogits, ws):
     _check(lib().slicegcn_softmax_ce(pl, ld, n, classes, _vec(labels, "labels", torch.int32),
                                      _vec(loss, "loss"), pd, ldd, pws, nws, _stream()))
     return loss
+
+
+# ---- slicegcn_train.h ---------------------------------------------------------------------
+def _value_type(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in VALUE_TYPES:
+        raise TypeError(f"{name}: expected fp32, bf16 or fp16, not {t.dtype}")
+    return VALUE_TYPES[t.dtype]
+
+
+def _embed_desc(n, vocab, width, table_type, row_type, scale, pad, flags):
+    if pad is not None:
+        flags |= EMBED_PAD
+    return _EmbedDesc(n, vocab, 0 if pad is None else pad, scale, width, table_type, row_type, flags)
+
+
+def _ids(ids: torch.Tensor):
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"ids: expected int32 or int64, not {ids.dtype}")
+    return _vec(ids, "ids", ids.dtype), EMBED_IDS64 if ids.dtype == torch.int64 else 0
+
+
+def slicegcn_embed_fwd(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0, pad: int | None = None):
+    """out[i] = scale * table[ids[i]].  ``ids``: int32 or int64, contiguous, one per row of ``out``; rows of the token ``pad`` are
+    zero, those of tokens outside the table NaN."""
+    pi, flags = _ids(ids)
+    pt, ldt = _mat(table, "table", table.dtype)
+    po, ldo = _mat(out, "out", out.dtype)
+    if out.shape != (ids.numel(), table.shape[1]):
+        raise ValueError("out must have a row per token, as wide as the table")
+    desc = _embed_desc(ids.numel(), table.shape[0], table.shape[1], _value_type(table, "table"), _value_type(out, "out"), scale, pad, flags)
+    _check(lib().slicegcn_embed_fwd(ctypes.byref(desc), pi, pt, ldt, po, ldo, _stream()))
+    return out
+
+
+def slicegcn_embed_sort_workspace_bytes(n: int, vocab: int) -> int:
+    return int(lib().slicegcn_embed_sort_workspace_bytes(n, vocab))
+
+
+def slicegcn_embed_sort(ids: torch.Tensor, vocab: int, order: torch.Tensor, starts: torch.Tensor, ws, pad: int | None = None):
+    """order[starts[t]:starts[t + 1]] = the positions of token t, ascending; ``pad`` and tokens outside the table are left out.
+    ``order``: int32, one per token; ``starts``: int32, vocab + 1."""
+    pi, flags = _ids(ids)
+    if order.numel() != ids.numel() or starts.numel() != vocab + 1:
+        raise ValueError("order must have an entry per token and starts vocab + 1")
+    desc = _embed_desc(ids.numel(), vocab, 1, F32, F32, 1.0, pad, flags)
+    _check(lib().slicegcn_embed_sort(ctypes.byref(desc), pi, _vec(order, "order", torch.int32), _vec(starts, "starts", torch.int32),
+                                     *_ws(ws), _stream()))
+    return order, starts
+
+
+def slicegcn_embed_bwd_workspace_bytes(n: int, width: int) -> int:
+    return int(lib().slicegcn_embed_bwd_workspace_bytes(n, width))
+
+
+def slicegcn_embed_bwd(order: torch.Tensor, starts: torch.Tensor, dout: torch.Tensor, dtable: torch.Tensor, ws, scale: float = 1.0,
+                       accumulate: bool = False):
+    """dtable[t] = (or, with ``accumulate``, +=) scale * the sum of dout over token t's positions.  ``order``, ``starts``: of
+    slicegcn_embed_sort."""
+    pd, ldo = _mat(dout, "dout", dout.dtype)
+    pt, ldt = _mat(dtable, "dtable", dtable.dtype)
+    vocab, width = dtable.shape
+    if dout.shape != (order.numel(), width) or starts.numel() != vocab + 1:
+        raise ValueError("dout must have a row per token, as wide as dtable, and starts an entry per token of the table and one more")
+    desc = _embed_desc(order.numel(), vocab, width, _value_type(dtable, "dtable"), _value_type(dout, "dout"), scale, None,
+                       EMBED_ACCUMULATE if accumulate else 0)
+    _check(lib().slicegcn_embed_bwd(ctypes.byref(desc), _vec(order, "order", torch.int32), _vec(starts, "starts", torch.int32), pd, ldo,
+                                    pt, ldt, *_ws(ws), _stream()))
+    return dtable
+
+
+def _resnorm_structs(x, y, gate, post, pre, post_w, post_b, pre_w, pre_b, sigmoid, residual, eps, stats, rows):
+    """Descriptor, parameters and rows of a call; ``rows``: its other matrices by name."""
+    first = x if x is not None else y
+    if first is None:
+        raise ValueError("neither x nor y")
+    shape, dtype = first.shape, first.dtype
+    io = _ResnormIo()
+    matrix_gate = gate is not None and gate.dim() == 2
+    for name, t in (("x", x), ("y", y), ("gate", gate if matrix_gate else None), *rows.items()):
+        if t is None:
+            continue
+        data, ld = _mat(t, name, dtype)
+        if t.shape != shape:
+            raise ValueError(f"{name} differs in shape from {'x' if first is x else 'y'}")
+        setattr(io, name, _Rows(data or 256, ld))  # an empty tensor has no address, and none of its rows is touched
+    n, width = shape
+    if stats is not None:
+        if tuple(stats.shape) != (n, 4):
+            raise ValueError("stats must be n x 4")
+        io.stats = _vec(stats, "stats")
+    params = _ResnormParams()
+    for name, t in (("post_w", post_w), ("post_b", post_b), ("pre_w", pre_w), ("pre_b", pre_b), ("gate", None if matrix_gate else gate)):
+        if t is not None:
+            if t.numel() != width:
+                raise ValueError(f"{name} must have an element per column")
+            setattr(params, name, _vec(t, name))
+    desc = _ResnormDesc(n, width, _value_type(first, "x"), post, pre, GATE_SIGMOID if sigmoid else 0, residual, eps)
+    return desc, params, io
+
+
+def slicegcn_resnorm_fwd(x, y, h, u, post: int = NORM_NONE, pre: int = NORM_NONE, post_w=None, post_b=None, pre_w=None, pre_b=None,
+                         gate=None, sigmoid: bool = False, residual: float = 1.0, eps: float = 1e-6, stats=None):
+    """h = residual * x + s * (post(y) * post_w + post_b);  u = pre(h) * pre_w + pre_b.  ``x`` or ``y``, ``h`` or ``u`` may be None.
+    ``gate`` (s; through a sigmoid with ``sigmoid``): fp32 [width], or one value per element in the rows' type.
+    ``stats``: fp32 [n, 4], filled for the backward pass."""
+    desc, params, io = _resnorm_structs(x, y, gate, post, pre, post_w, post_b, pre_w, pre_b, sigmoid, residual, eps, stats, dict(h=h, u=u))
+    _check(lib().slicegcn_resnorm_fwd(ctypes.byref(desc), ctypes.byref(params), ctypes.byref(io), _stream()))
+    return h, u
+
+
+def slicegcn_resnorm_bwd_workspace_bytes(n: int, width: int) -> int:
+    return int(lib().slicegcn_resnorm_bwd_workspace_bytes(n, width))
+
+
+def slicegcn_resnorm_bwd(x, y, stats, dh, du, dx, dy, ws, post: int = NORM_NONE, pre: int = NORM_NONE, post_w=None, post_b=None,
+                         pre_w=None, pre_b=None, gate=None, sigmoid: bool = False, residual: float = 1.0, eps: float = 1e-6,
+                         dpost_w=None, dpost_b=None, dpre_w=None, dpre_b=None, dgate=None):
+    """Gradients of slicegcn_resnorm_fwd with the same arguments, from ``dh`` and ``du`` (one of them may be None); gradients that are
+    None are not formed.  ``ws`` is needed for gradients of parameters (a gate per column is one)."""
+    matrix_gate = gate is not None and gate.dim() == 2
+    desc, params, io = _resnorm_structs(x, y, gate, post, pre, post_w, post_b, pre_w, pre_b, sigmoid, residual, eps, stats,
+                                        dict(dh=dh, du=du, dx=dx, dy=dy, dgate=dgate if matrix_gate else None))
+    grads = _ResnormParams()
+    for name, t in (("post_w", dpost_w), ("post_b", dpost_b), ("pre_w", dpre_w), ("pre_b", dpre_b), ("gate", None if matrix_gate else dgate)):
+        if t is not None:
+            if t.numel() != desc.width:
+                raise ValueError(f"d{name} must have an element per column")
+            setattr(grads, name, _vec(t, "d" + name))
+    _check(lib().slicegcn_resnorm_bwd(ctypes.byref(desc), ctypes.byref(params), ctypes.byref(io), ctypes.byref(grads), *_ws(ws), _stream()))
+
+
+class TensorList:
+    """Contiguous device tensors (fp32, bf16, fp16) as the list slicegcn_global_norm and slicegcn_clip take, laid out once for
+    tensors that stay where they are, like the gradients of a model."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.array = (_Tensor * max(len(self.tensors), 1))()
+        for i, (t, entry) in enumerate(zip(self.tensors, self.array)):
+            entry.data, entry.count, entry.type = _vec(t, f"tensor {i}", t.dtype), t.numel(), _value_type(t, f"tensor {i}")
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def slicegcn_global_norm_workspace_bytes(tensors: TensorList) -> int:
+    return int(lib().slicegcn_global_norm_workspace_bytes(tensors.array, len(tensors)))
+
+
+def slicegcn_global_norm(tensors: TensorList, norm: torch.Tensor, ws, max_norm: float = float("inf"), factor: torch.Tensor | None = None,
+                         kind: int = NORM_TWO):
+    """norm = the 2-norm (or with NORM_MAX the largest absolute value) over all elements; factor = what clips it to ``max_norm``.
+    ``norm``, ``factor``: fp32 [1]."""
+    _check(lib().slicegcn_global_norm(tensors.array, len(tensors), kind, max_norm, _vec(norm, "norm"), _vec(factor, "factor"), *_ws(ws),
+                                      _stream()))
+    return norm
+
+
+def slicegcn_clip(tensors: TensorList, outs: TensorList | None, max_norm: float, norm: torch.Tensor | None, ws,
+                  factor: torch.Tensor | None = None, kind: int = NORM_TWO):
+    """Scales ``tensors`` so that their norm is at most ``max_norm``, into ``outs`` (None: in place)."""
+    if outs is not None and len(outs) != len(tensors):
+        raise ValueError("outs must have as many tensors")
+    _check(lib().slicegcn_clip(tensors.array, outs.array if outs is not None else None, len(tensors), kind, max_norm, _vec(norm, "norm"),
+                               _vec(factor, "factor"), *_ws(ws), _stream()))
+    return norm
+
+
+def slicegcn_adam_step_scaled(param, grad, factor, m, v, lr: float, step: int, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0):
+    """slicegcn_adam_step on ``factor`` (fp32 [1] on the device) times ``grad``."""
+    n = param.numel()
+    for t, name in ((grad, "grad"), (m, "m"), (v, "v")):
+        if t.numel() != n:
+            raise ValueError(f"{name} differs in size from param")
+    _check(lib().slicegcn_adam_step_scaled(_vec(param, "param"), _vec(grad, "grad"), _vec(factor, "factor"), _vec(m, "m"), _vec(v, "v"), n,
+                                           lr, beta1, beta2, eps, weight_decay, step, _stream()))
 
 
 def slicegcn_profile_reserve(scopes: int):

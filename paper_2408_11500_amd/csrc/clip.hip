@@ -1,0 +1,360 @@
+// The norm over all elements of many tensors, and clipping to it.
+//
+//   norm = sqrt(sum g^2) or max |g|;   factor = norm <= max_norm ? 1 : max_norm / norm;   to = factor * from
+//
+// Tensors are cut into tiles of TILE_VECS 16-byte accesses; a workgroup takes consecutive tiles, adds the squares in fp64 (the square
+// of an fp32 number is exact there and cannot overflow) and stores one partial result, which are added in a fixed order: no atomics,
+// bitwise reproducible.  The workgroups of the scaling pass each form that last sum by themselves, which saves a launch between the two
+// passes.  The list of tensors travels in the kernel arguments (4 KB hold LIST tensors; a longer list takes several launches), so
+// that nothing has to be copied to the device and a call can be captured.  Bound by bytes.
+#include "common.h"
+#include "values.h"
+
+#include <cmath>
+
+namespace slicegcn {
+
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int TILE_VECS = 4 * THREADS; // 16-byte accesses per tile
+constexpr int LIST = 144;              // tensors per launch
+constexpr int MAX_BLOCKS = 2048;       // per call, rounded up to whole launches
+
+struct TensorRange { // the tensors of one launch; a tensor's tiles are [first[i], first[i + 1])
+    const void *from[LIST];
+    void *to[LIST];
+    uint64_t count[LIST]; // elements, type in the upper bits
+    uint32_t first[LIST + 1];
+};
+constexpr int TYPE_SHIFT = 56;
+
+struct LaunchPart {
+    int32_t tensors;
+    uint32_t tiles, tiles_per_block;
+};
+
+__device__ inline double wave_sum(double v)
+{
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) v += __shfl_xor(v, s, 64);
+    return v;
+}
+
+__device__ inline uint32_t wave_max(uint32_t v)
+{
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, s, 64));
+    return v;
+}
+
+// The running result of a thread: a sum of squares, or the largest |g| as bits (which order like the numbers, NaN above all of them)
+template <int KIND> struct Running;
+template <> struct Running<SLICEGCN_NORM_TWO> {
+    double v = 0.0;
+    __device__ void add(float g) { v = fma((double)g, (double)g, v); }
+    __device__ void join(uint64_t o) { v += __longlong_as_double((long long)o); }
+    __device__ uint64_t bits() const { return (uint64_t)__double_as_longlong(v); }
+    __device__ void over_wave() { v = wave_sum(v); }
+    __device__ double norm() const { return sqrt(v); }
+};
+template <> struct Running<SLICEGCN_NORM_MAX> {
+    uint32_t v = 0;
+    __device__ void add(float g) { v = max(v, __float_as_uint(g) & 0x7fffffffu); }
+    __device__ void join(uint64_t o) { v = max(v, (uint32_t)o); }
+    __device__ uint64_t bits() const { return v; }
+    __device__ void over_wave() { v = wave_max(v); }
+    __device__ double norm() const { return (double)__uint_as_float(v); }
+};
+
+// Over the workgroup, in every thread
+template <int KIND> __device__ inline void over_block(Running<KIND> &r, uint64_t *shared)
+{
+    r.over_wave();
+    if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = r.bits();
+    __syncthreads();
+    Running<KIND> all;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) all.join(shared[w]);
+    r = all;
+}
+
+// f(element type, tensor, first vector, end vector) for every piece of the workgroup's tiles, in order
+template <class F> __device__ inline void for_tiles(const TensorRange &list, const LaunchPart &part, F f)
+{
+    uint32_t tile = blockIdx.x * part.tiles_per_block;
+    const uint32_t end = min(tile + part.tiles_per_block, part.tiles);
+    int lo = 0, hi = part.tensors; // the tensor that holds the first tile: the last one that starts at or before it
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (list.first[mid] <= tile) lo = mid;
+        else hi = mid;
+    }
+    while (tile < end) {
+        while (list.first[lo + 1] <= tile) ++lo; // also past tensors without tiles
+        const uint32_t stop = min(end, list.first[lo + 1]);
+        const int64_t v0 = (int64_t)(tile - list.first[lo]) * TILE_VECS, v1 = (int64_t)(stop - list.first[lo]) * TILE_VECS;
+        const int type = (int)(list.count[lo] >> TYPE_SHIFT);
+        if (type == SLICEGCN_F32) f(float(), lo, v0, v1);
+        else if (type == SLICEGCN_BF16) f(bf16(), lo, v0, v1);
+        else f(f16(), lo, v0, v1);
+        tile = stop;
+    }
+}
+
+template <int KIND>
+__global__ __launch_bounds__(THREADS) void norm_partial_kernel(const TensorRange list, const LaunchPart part, uint64_t *__restrict__ partial)
+{
+    __shared__ uint64_t shared[THREADS / 64];
+    Running<KIND> r;
+    for_tiles(list, part, [&](auto zero, int t, int64_t v0, int64_t v1) {
+        using T = decltype(zero);
+        constexpr int V = 16 / sizeof(T);
+        const T *p = static_cast<const T *>(list.from[t]);
+        const int64_t count = (int64_t)(list.count[t] & (((uint64_t)1 << TYPE_SHIFT) - 1)), whole = count / V;
+        const int64_t stop = v1 < whole ? v1 : whole;
+        int64_t v = v0 + threadIdx.x;
+        for (; v + 3 * THREADS < stop; v += 4 * THREADS) {
+            typename VecOf<T, V>::type x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = load_vec<T, V>(p + (v + i * THREADS) * V);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) r.add((float)x[i][j]);
+        }
+        for (; v < stop; v += THREADS) {
+            const auto x = load_vec<T, V>(p + v * V);
+#pragma unroll
+            for (int j = 0; j < V; ++j) r.add((float)x[j]);
+        }
+        if (v1 > whole) // the tensor's last elements
+            for (int64_t i = whole * V + threadIdx.x; i < count; i += THREADS) r.add((float)p[i]);
+    });
+    over_block(r, shared);
+    if (threadIdx.x == 0) partial[blockIdx.x] = r.bits();
+}
+
+template <int KIND> __device__ inline Running<KIND> join_partials(const uint64_t *__restrict__ partial, int32_t partials, uint64_t *shared)
+{
+    Running<KIND> r;
+    for (int32_t i = threadIdx.x; i < partials; i += THREADS) r.join(partial[i]);
+    over_block(r, shared);
+    return r;
+}
+
+template <int KIND>
+__device__ inline float store_norm(const Running<KIND> &r, double max_norm, bool store, float *__restrict__ norm, float *__restrict__ factor)
+{
+    const double n = r.norm();
+    const float f = n <= max_norm ? 1.f : (float)(max_norm / n);
+    if (store) {
+        if (norm) *norm = (float)n;
+        if (factor) *factor = f;
+    }
+    return f;
+}
+
+template <int KIND>
+__global__ __launch_bounds__(THREADS) void norm_final_kernel(const uint64_t *__restrict__ partial, int32_t partials, double max_norm,
+                                                             float *__restrict__ norm, float *__restrict__ factor)
+{
+    __shared__ uint64_t shared[THREADS / 64];
+    const Running<KIND> r = join_partials<KIND>(partial, partials, shared);
+    store_norm<KIND>(r, max_norm, threadIdx.x == 0, norm, factor);
+}
+
+template <int KIND>
+__global__ __launch_bounds__(THREADS) void clip_kernel(const TensorRange list, const LaunchPart part, const uint64_t *__restrict__ partial,
+                                                       int32_t partials, double max_norm, float *__restrict__ norm, float *__restrict__ factor)
+{
+    __shared__ uint64_t shared[THREADS / 64];
+    const Running<KIND> r = join_partials<KIND>(partial, partials, shared);
+    const float f = store_norm<KIND>(r, max_norm, blockIdx.x == 0 && threadIdx.x == 0, norm, factor);
+    for_tiles(list, part, [&](auto zero, int t, int64_t v0, int64_t v1) {
+        using T = decltype(zero);
+        constexpr int V = 16 / sizeof(T);
+        const T *p = static_cast<const T *>(list.from[t]); // from and to may be the same tensor: a thread reads what it writes
+        T *q = static_cast<T *>(list.to[t]);
+        if (p == q && f == 1.f) return;
+        const int64_t count = (int64_t)(list.count[t] & (((uint64_t)1 << TYPE_SHIFT) - 1)), whole = count / V;
+        const int64_t stop = v1 < whole ? v1 : whole;
+        auto scaled = [&](const typename VecOf<T, V>::type &x, int64_t v) {
+            float o[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] = f * (float)x[j];
+            store_vec<T, V>(q + v * V, o);
+        };
+        int64_t v = v0 + threadIdx.x;
+        for (; v + 3 * THREADS < stop; v += 4 * THREADS) {
+            typename VecOf<T, V>::type x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = load_vec<T, V>(p + (v + i * THREADS) * V);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) scaled(x[i], v + i * THREADS);
+        }
+        for (; v < stop; v += THREADS) scaled(load_vec<T, V>(p + v * V), v);
+        if (v1 > whole)
+            for (int64_t i = whole * V + threadIdx.x; i < count; i += THREADS) q[i] = (T)(f * (float)p[i]);
+    });
+}
+
+int64_t tiles_of(const slicegcn_tensor &t)
+{
+    const int64_t per_tile = TILE_VECS * 16 / type_bytes(t.type);
+    return (t.count + per_tile - 1) / per_tile;
+}
+
+struct CallPlan {
+    int64_t tiles = 0;
+    int64_t tiles_per_block = 1;
+    int32_t partials = 0; // workgroups over all launches
+};
+
+int check_tensors(const char *what, const slicegcn_tensor *t, int32_t count)
+{
+    SG_REQUIRE(count >= 0 && (t || count == 0), SLICEGCN_EINVAL, "%s: no list of tensors", what);
+    for (int32_t i = 0; i < count; ++i) {
+        SG_REQUIRE(known_type(t[i].type), SLICEGCN_EINVAL, "%s: tensor %d has unknown type %d", what, i, t[i].type);
+        SG_REQUIRE(t[i].count >= 0 && t[i].count < ((int64_t)1 << 48), SLICEGCN_EINVAL, "%s: tensor %d has a bad number of elements", what, i);
+        SG_REQUIRE((t[i].data || t[i].count == 0) && aligned_for(t[i].data, t[i].type), SLICEGCN_EINVAL,
+                   "%s: tensor %d is NULL or misaligned", what, i);
+    }
+    return SLICEGCN_OK;
+}
+
+// Calls f(first tensor, tensors, tiles) for the tensors of each launch
+template <class F> int for_launches(const slicegcn_tensor *t, int32_t count, F f)
+{
+    for (int32_t i = 0; i < count;) {
+        int32_t n = 0;
+        int64_t tiles = 0;
+        while (i + n < count && n < LIST) tiles += tiles_of(t[i + n++]);
+        SG_REQUIRE(tiles <= UINT32_MAX, SLICEGCN_ERANGE, "global_norm: more than 2^32 tiles of 16 KB");
+        if (tiles > 0)
+            if (int rc = f(i, n, tiles)) return rc;
+        i += n;
+    }
+    return SLICEGCN_OK;
+}
+
+int plan_call(const slicegcn_tensor *t, int32_t count, CallPlan *plan)
+{
+    for (int32_t i = 0; i < count; ++i) plan->tiles += tiles_of(t[i]);
+    plan->tiles_per_block = plan->tiles <= MAX_BLOCKS ? 1 : (plan->tiles + MAX_BLOCKS - 1) / MAX_BLOCKS;
+    return for_launches(t, count, [&](int32_t, int32_t, int64_t tiles) {
+        plan->partials += (int32_t)((tiles + plan->tiles_per_block - 1) / plan->tiles_per_block);
+        return SLICEGCN_OK;
+    });
+}
+
+// Launches a kernel over all tensors: launch(list, part, blocks, first partial)
+template <class F> int launch_lists(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t count, const CallPlan &plan, F launch)
+{
+    int32_t slot = 0;
+    return for_launches(from, count, [&](int32_t first, int32_t n, int64_t tiles) {
+        TensorRange list;
+        uint32_t at = 0;
+        for (int32_t i = 0; i < n; ++i) {
+            list.from[i] = from[first + i].data;
+            list.to[i] = to ? to[first + i].data : from[first + i].data;
+            list.count[i] = (uint64_t)from[first + i].count | ((uint64_t)from[first + i].type << TYPE_SHIFT);
+            list.first[i] = at;
+            at += (uint32_t)tiles_of(from[first + i]);
+        }
+        for (int32_t i = n; i < LIST; ++i) list.from[i] = nullptr, list.to[i] = nullptr, list.count[i] = 0;
+        for (int32_t i = n; i <= LIST; ++i) list.first[i] = at;
+        const LaunchPart part{n, (uint32_t)tiles, (uint32_t)plan.tiles_per_block};
+        const int32_t blocks = (int32_t)((tiles + plan.tiles_per_block - 1) / plan.tiles_per_block);
+        launch(list, part, blocks, slot);
+        SG_LAUNCH_CHECK();
+        slot += blocks;
+        return SLICEGCN_OK;
+    });
+}
+
+int check_call(const char *what, const slicegcn_tensor *t, int32_t count, int32_t kind, double max_norm, CallPlan *plan, void *ws, size_t ws_bytes)
+{
+    if (int rc = check_tensors(what, t, count)) return rc;
+    SG_REQUIRE(kind == SLICEGCN_NORM_TWO || kind == SLICEGCN_NORM_MAX, SLICEGCN_EINVAL, "%s: unknown kind %d", what, kind);
+    SG_REQUIRE(max_norm >= 0.0, SLICEGCN_EINVAL, "%s: max_norm is negative or no number", what);
+    if (int rc = plan_call(t, count, plan)) return rc;
+    const size_t need = slicegcn_global_norm_workspace_bytes(t, count);
+    SG_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255u) == 0, SLICEGCN_EINVAL, "%s: misaligned workspace", what);
+    SG_REQUIRE(need == 0 || (ws && ws_bytes >= need), SLICEGCN_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need);
+    return SLICEGCN_OK;
+}
+
+template <int KIND>
+int partials(const slicegcn_tensor *t, int32_t count, const CallPlan &plan, uint64_t *ws, hipStream_t stream)
+{
+    return launch_lists(t, nullptr, count, plan, [&](const TensorRange &list, const LaunchPart &part, int32_t blocks, int32_t slot) {
+        norm_partial_kernel<KIND><<<blocks, THREADS, 0, stream>>>(list, part, ws + slot);
+    });
+}
+
+template <int KIND>
+int norm_call(const slicegcn_tensor *t, int32_t count, const CallPlan &plan, double max_norm, float *norm, float *factor, uint64_t *ws,
+              hipStream_t stream)
+{
+    if (int rc = partials<KIND>(t, count, plan, ws, stream)) return rc;
+    norm_final_kernel<KIND><<<1, THREADS, 0, stream>>>(ws, plan.partials, max_norm, norm, factor);
+    SG_LAUNCH_CHECK();
+    return SLICEGCN_OK;
+}
+
+template <int KIND>
+int clip_call(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t count, const CallPlan &plan, double max_norm, float *norm,
+              float *factor, uint64_t *ws, hipStream_t stream)
+{
+    if (int rc = partials<KIND>(from, count, plan, ws, stream)) return rc;
+    return launch_lists(from, to, count, plan, [&](const TensorRange &list, const LaunchPart &part, int32_t blocks, int32_t slot) {
+        clip_kernel<KIND><<<blocks, THREADS, 0, stream>>>(list, part, ws, plan.partials, max_norm, slot ? nullptr : norm, slot ? nullptr : factor);
+    });
+}
+
+} // namespace
+} // namespace slicegcn
+
+using namespace slicegcn;
+
+extern "C" size_t slicegcn_global_norm_workspace_bytes(const slicegcn_tensor *tensors, int32_t count)
+{
+    CallPlan plan;
+    if (check_tensors("global_norm_workspace_bytes", tensors, count) || plan_call(tensors, count, &plan)) return 0;
+    return (size_t)round_up(8 * (int64_t)plan.partials, 256);
+}
+
+extern "C" int slicegcn_global_norm(const slicegcn_tensor *tensors, int32_t count, int32_t kind, double max_norm, float *norm, float *factor,
+                                    void *ws, size_t ws_bytes, void *stream)
+{
+    CallPlan plan;
+    SG_REQUIRE(norm != nullptr, SLICEGCN_EINVAL, "global_norm: NULL norm");
+    if (int rc = check_call("global_norm", tensors, count, kind, factor ? max_norm : 0.0, &plan, ws, ws_bytes)) return rc;
+    ProfScope prof(SLICEGCN_PROF_CLIP, count, as_stream(stream));
+    auto *w = static_cast<uint64_t *>(ws);
+    return kind == SLICEGCN_NORM_TWO ? norm_call<SLICEGCN_NORM_TWO>(tensors, count, plan, max_norm, norm, factor, w, as_stream(stream))
+                                     : norm_call<SLICEGCN_NORM_MAX>(tensors, count, plan, max_norm, norm, factor, w, as_stream(stream));
+}
+
+extern "C" int slicegcn_clip(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t count, int32_t kind, double max_norm, float *norm,
+                             float *factor, void *ws, size_t ws_bytes, void *stream)
+{
+    CallPlan plan;
+    if (int rc = check_call("clip", from, count, kind, max_norm, &plan, ws, ws_bytes)) return rc;
+    if (to) {
+        if (int rc = check_tensors("clip", to, count)) return rc;
+        for (int32_t i = 0; i < count; ++i)
+            SG_REQUIRE(to[i].count == from[i].count && to[i].type == from[i].type, SLICEGCN_EINVAL,
+                       "clip: tensor %d differs in elements or type from what it is clipped from", i);
+    }
+    ProfScope prof(SLICEGCN_PROF_CLIP, count, as_stream(stream));
+    auto *w = static_cast<uint64_t *>(ws);
+    if (plan.tiles == 0) { // no elements: only the norm, zero
+        norm_final_kernel<SLICEGCN_NORM_TWO><<<1, THREADS, 0, as_stream(stream)>>>(w, 0, max_norm, norm, factor);
+        SG_LAUNCH_CHECK();
+        return SLICEGCN_OK;
+    }
+    return kind == SLICEGCN_NORM_TWO ? clip_call<SLICEGCN_NORM_TWO>(from, to, count, plan, max_norm, norm, factor, w, as_stream(stream))
+                                     : clip_call<SLICEGCN_NORM_MAX>(from, to, count, plan, max_norm, norm, factor, w, as_stream(stream));
+}

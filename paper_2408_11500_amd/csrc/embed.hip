@@ -1,0 +1,694 @@
+// Token embeddings: rows of a table looked up by token and scaled, and the table's gradient from sorted tokens.
+//
+//   out[i, :] = scale * table[ids[i], :]
+//   dTable[t, :] = scale * sum of dOut[i, :] over the positions i with ids[i] = t
+//
+// The gradient adds rows that lie apart; a stable sort of the tokens puts the positions of a token side by side, so that every row
+// of the gradient is formed by one owner in one fixed order: no floating-point atomics, bitwise reproducible.
+#include "common.h"
+#include "values.h"
+
+#include <cmath>
+
+namespace slicegcn {
+
+namespace {
+
+constexpr int THREADS = 256;
+
+// ---- lookup ---------------------------------------------------------------------------------------------------------------
+
+// A group of 2^log_lanes lanes moves ROWS rows at a time, V elements per lane and access; rows whose width is no multiple of V end with an access
+// that is moved left and overlaps the one before it (the same values twice).
+constexpr int LOOKUP_ROWS = 4;
+
+template <class ID, class TT, class TR, int V>
+__global__ __launch_bounds__(THREADS) void lookup_kernel(const ID *__restrict__ ids, int64_t n, int64_t vocab, int64_t pad, bool has_pad,
+                                                         const TT *__restrict__ table, int64_t ldt, int32_t width, float scale,
+                                                         TR *__restrict__ out, int64_t ldo, int log_lanes, int32_t tile)
+{
+    const int lane = threadIdx.x & ((1 << log_lanes) - 1), group = threadIdx.x >> log_lanes, groups = THREADS >> log_lanes;
+    const int32_t last = width - V, c0 = blockIdx.y * tile, c1 = min(c0 + tile, width);
+    for (int64_t r0 = (int64_t)blockIdx.x * groups * LOOKUP_ROWS + group; r0 < n; r0 += (int64_t)gridDim.x * groups * LOOKUP_ROWS) {
+        int64_t id[LOOKUP_ROWS];
+#pragma unroll
+        for (int i = 0; i < LOOKUP_ROWS; ++i) {
+            const int64_t r = r0 + i * groups;
+            id[i] = r < n ? (int64_t)ids[r] : -1;
+        }
+        for (int32_t c = c0 + lane * V; c < c1; c += V << log_lanes) {
+            const int32_t col = min(c, last);
+            typename VecOf<TT, V>::type x[LOOKUP_ROWS];
+#pragma unroll
+            for (int i = 0; i < LOOKUP_ROWS; ++i) {
+                const bool in = id[i] >= 0 && id[i] < vocab;
+                x[i] = load_vec<TT, V>(table + (in ? id[i] : 0) * ldt + col);
+            }
+#pragma unroll
+            for (int i = 0; i < LOOKUP_ROWS; ++i) {
+                const int64_t r = r0 + i * groups;
+                if (r >= n) break;
+                const bool in = id[i] >= 0 && id[i] < vocab, zero = has_pad && id[i] == pad;
+                float o[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) o[j] = zero ? 0.f : in ? scale * (float)x[i][j] : NAN;
+                store_vec<TR, V>(out + r * ldo + col, o);
+            }
+        }
+    }
+}
+
+// ---- sort -----------------------------------------------------------------------------------------------------------------
+
+// Stable sort by digits of at most DIGIT_BITS bits, lowest first.  Keys are tokens; padding and tokens outside the table get the key
+// `vocab` and end up behind all others.
+constexpr int DIGIT_BITS = 10, DIGITS = 1 << DIGIT_BITS;
+constexpr int SORT_THREADS = 512, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 8, SORT_TILE = SORT_THREADS * SORT_ITEMS;
+
+struct Tokens {
+    const void *ids;
+    int64_t n, vocab, pad;
+    bool wide, has_pad;
+};
+
+__device__ inline uint32_t token_key(const Tokens &t, int64_t i)
+{
+    const int64_t id = t.wide ? static_cast<const int64_t *>(t.ids)[i] : (int64_t)static_cast<const int32_t *>(t.ids)[i];
+    return id < 0 || id >= t.vocab || (t.has_pad && id == t.pad) ? (uint32_t)t.vocab : (uint32_t)id;
+}
+
+// Lanes of the wavefront that hold the same digit as this one, among the lanes in `active`
+__device__ inline uint64_t same_digit(uint32_t digit, int bits, uint64_t active)
+{
+    uint64_t same = active;
+    for (int b = 0; b < bits; ++b) {
+        const bool one = (digit >> b) & 1;
+        const uint64_t ones = __ballot(one);
+        same &= one ? ones : ~ones;
+    }
+    return same;
+}
+
+// Orders this wavefront's accesses to LDS among its lanes
+__device__ inline void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Exclusive prefix sum over the workgroup's threads
+__device__ inline uint32_t block_scan(uint32_t v, uint32_t *wave_sums)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t sum = v;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const uint32_t up = (uint32_t)__shfl_up((int)sum, s, 64);
+        if (lane >= s) sum += up;
+    }
+    if (lane == 63) wave_sums[wave] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int w = 0; w < wave; ++w) before += wave_sums[w];
+    __syncthreads(); // wave_sums may be written again
+    return before + sum - v;
+}
+
+// Ranks the workgroup's items (a wavefront's items are SORT_ITEMS runs of 64 in a row) by digit, stable: rank[i] is the item's place among the
+// wavefront's items of its digit.  counts[wave][digit] receives the wavefront's number of each digit.
+__device__ inline void rank_items(const uint32_t (&key)[SORT_ITEMS], const bool (&there)[SORT_ITEMS], int shift, int bits,
+                                  uint16_t (*counts)[DIGITS], uint32_t (&rank)[SORT_ITEMS])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t mask = (1u << bits) - 1;
+    for (int d = threadIdx.x; d < SORT_WAVES << bits; d += SORT_THREADS) counts[d >> bits][d & mask] = 0;
+    __syncthreads();
+    uint16_t *mine = counts[wave]; // other lanes change it between two reads of this one: hence the fences
+#pragma unroll
+    for (int i = 0; i < SORT_ITEMS; ++i) {
+        const uint32_t digit = (key[i] >> shift) & mask;
+        const uint64_t same = same_digit(digit, bits, __ballot(there[i]));
+        const uint32_t before = mine[digit];
+        const int lower = __popcll(same & (((uint64_t)1 << lane) - 1));
+        rank[i] = before + lower;
+        wave_fence(); // every lane has read before one of them writes
+        if (there[i] && lower == 0) mine[digit] = (uint16_t)(before + __popcll(same));
+        wave_fence();
+    }
+    __syncthreads();
+}
+
+// counts[wave][digit] -> number of the digit in the wavefronts before; returns the digit's total for thread = digit (two digits per thread)
+__device__ inline void counts_before(uint16_t (*counts)[DIGITS], int bits, uint32_t (&total)[DIGITS / SORT_THREADS])
+{
+#pragma unroll
+    for (int q = 0; q < DIGITS / SORT_THREADS; ++q) {
+        const int d = threadIdx.x * (DIGITS / SORT_THREADS) + q;
+        uint32_t sum = 0;
+        if (d < 1 << bits)
+            for (int w = 0; w < SORT_WAVES; ++w) {
+                const uint32_t c = counts[w][d];
+                counts[w][d] = (uint16_t)sum;
+                sum += c;
+            }
+        total[q] = sum;
+    }
+}
+
+// first place in sorted keys that holds a key of at least t
+__device__ inline uint32_t lower_bound(const uint32_t *keys, uint32_t count, uint32_t t)
+{
+    uint32_t lo = 0, len = count;
+    while (len > 0) {
+        const uint32_t half = len / 2;
+        const bool right = keys[lo + half] < t;
+        lo = right ? lo + half + 1 : lo;
+        len = right ? len - half - 1 : half;
+    }
+    return lo;
+}
+
+// Up to SORT_TILE tokens: every workgroup sorts all of them in LDS and writes its part of starts, the first one also the order: one launch
+constexpr int STARTS_PER_BLOCK = 8 * SORT_THREADS;
+__global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const Tokens t, int bits, int passes, int32_t *__restrict__ order, int32_t *__restrict__ starts)
+{
+    __shared__ uint16_t counts[SORT_WAVES][DIGITS];
+    __shared__ uint32_t base[DIGITS], wave_sums[SORT_WAVES];
+    __shared__ uint32_t keys[SORT_TILE];
+    __shared__ uint16_t from[SORT_TILE];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)t.n;
+    const int first = wave * 64 * SORT_ITEMS + lane;
+    uint32_t key[SORT_ITEMS], rank[SORT_ITEMS], index[SORT_ITEMS];
+    bool there[SORT_ITEMS];
+#pragma unroll
+    for (int i = 0; i < SORT_ITEMS; ++i) {
+        index[i] = first + i * 64;
+        there[i] = (int)index[i] < n;
+        key[i] = there[i] ? token_key(t, index[i]) : 0;
+    }
+    for (int p = 0; p < passes; ++p) {
+        rank_items(key, there, p * bits, bits, counts, rank);
+        uint32_t total[DIGITS / SORT_THREADS];
+        counts_before(counts, bits, total);
+        uint32_t sum = 0;
+#pragma unroll
+        for (int q = 0; q < DIGITS / SORT_THREADS; ++q) sum += total[q];
+        uint32_t at = block_scan(sum, wave_sums);
+#pragma unroll
+        for (int q = 0; q < DIGITS / SORT_THREADS; ++q) {
+            base[threadIdx.x * (DIGITS / SORT_THREADS) + q] = at;
+            at += total[q];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < SORT_ITEMS; ++i)
+            if (there[i]) {
+                const uint32_t digit = (key[i] >> (p * bits)) & ((1u << bits) - 1);
+                const uint32_t place = base[digit] + counts[wave][digit] + rank[i];
+                keys[place] = key[i];
+                from[place] = (uint16_t)index[i];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < SORT_ITEMS; ++i)
+            if (there[i]) {
+                key[i] = keys[first + i * 64];
+                index[i] = from[first + i * 64];
+            }
+    }
+    if (blockIdx.x == 0) {
+#pragma unroll
+        for (int i = 0; i < SORT_ITEMS; ++i)
+            if (there[i]) order[first + i * 64] = (int32_t)index[i];
+    }
+    const int64_t t0 = (int64_t)blockIdx.x * STARTS_PER_BLOCK;
+    for (int64_t v = t0 + threadIdx.x; v < t0 + STARTS_PER_BLOCK && v <= t.vocab; v += SORT_THREADS)
+        starts[v] = (int32_t)lower_bound(keys, (uint32_t)n, (uint32_t)v);
+}
+
+// More tokens: per digit, the tiles' histograms, their prefix sums, and the items to their places.
+__global__ __launch_bounds__(SORT_THREADS) void digit_count_kernel(const Tokens t, const uint32_t *__restrict__ keys, int shift, int bits, uint32_t *__restrict__ hist)
+{
+    __shared__ uint32_t counts[DIGITS];
+    const uint32_t mask = (1u << bits) - 1;
+    for (int d = threadIdx.x; d < 1 << bits; d += SORT_THREADS) counts[d] = 0;
+    __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * SORT_TILE + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < SORT_ITEMS; ++i) {
+        const int64_t at = first + i * SORT_THREADS;
+        if (at < t.n) atomicAdd(&counts[((keys ? keys[at] : token_key(t, at)) >> shift) & mask], 1u);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < 1 << bits; d += SORT_THREADS) hist[((int64_t)blockIdx.x << bits) + d] = counts[d];
+}
+
+// hist[tile][digit] -> number of the digit in the tiles before; total[digit].  A workgroup takes 64 digits, its wavefronts ranges of tiles.
+__global__ __launch_bounds__(1024) void digit_scan_kernel(uint32_t *__restrict__ hist, int64_t tiles, int bits, uint32_t *__restrict__ total)
+{
+    __shared__ uint32_t sums[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane, digits = 1 << bits;
+    const int64_t share = (tiles + 15) / 16, b = wave * share, e = min(b + share, tiles);
+    uint32_t sum = 0;
+    if (d < digits) {
+#pragma unroll 8
+        for (int64_t i = b; i < e; ++i) sum += hist[i * digits + d];
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+    for (int w = 0; w < 16; ++w) {
+        if (w == wave) before = all;
+        all += sums[w][lane];
+    }
+    if (d >= digits) return;
+    if (wave == 0) total[d] = all;
+#pragma unroll 8
+    for (int64_t i = b; i < e; ++i) {
+        const uint32_t c = hist[i * digits + d];
+        hist[i * digits + d] = before;
+        before += c;
+    }
+}
+
+__global__ __launch_bounds__(SORT_THREADS) void digit_scatter_kernel(const Tokens t, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ from,
+                                                                     int shift, int bits, const uint32_t *__restrict__ hist,
+                                                                     const uint32_t *__restrict__ total, uint32_t *__restrict__ out_keys,
+                                                                     uint32_t *__restrict__ out_from)
+{
+    __shared__ uint16_t counts[SORT_WAVES][DIGITS];
+    __shared__ uint32_t base[DIGITS], wave_sums[SORT_WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t first = (int64_t)blockIdx.x * SORT_TILE + wave * 64 * SORT_ITEMS + lane;
+    uint32_t key[SORT_ITEMS], index[SORT_ITEMS], rank[SORT_ITEMS];
+    bool there[SORT_ITEMS];
+#pragma unroll
+    for (int i = 0; i < SORT_ITEMS; ++i) {
+        const int64_t at = first + i * 64;
+        there[i] = at < t.n;
+        key[i] = there[i] ? keys ? keys[at] : token_key(t, at) : 0;
+        index[i] = there[i] && from ? from[at] : (uint32_t)at;
+    }
+    rank_items(key, there, shift, bits, counts, rank);
+    uint32_t inside[DIGITS / SORT_THREADS], all[DIGITS / SORT_THREADS], sum = 0;
+    counts_before(counts, bits, inside);
+#pragma unroll
+    for (int q = 0; q < DIGITS / SORT_THREADS; ++q) {
+        const int d = threadIdx.x * (DIGITS / SORT_THREADS) + q;
+        all[q] = d < 1 << bits ? total[d] : 0;
+        sum += all[q];
+    }
+    uint32_t at = block_scan(sum, wave_sums);
+#pragma unroll
+    for (int q = 0; q < DIGITS / SORT_THREADS; ++q) {
+        const int d = threadIdx.x * (DIGITS / SORT_THREADS) + q;
+        if (d < 1 << bits) base[d] = at + hist[((int64_t)blockIdx.x << bits) + d];
+        at += all[q];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < SORT_ITEMS; ++i)
+        if (there[i]) {
+            const uint32_t digit = (key[i] >> shift) & ((1u << bits) - 1);
+            const uint32_t place = base[digit] + counts[wave][digit] + rank[i];
+            out_keys[place] = key[i];
+            out_from[place] = index[i];
+        }
+}
+
+__global__ __launch_bounds__(THREADS) void starts_kernel(const uint32_t *__restrict__ keys, uint32_t n, int64_t vocab, int32_t *__restrict__ starts)
+{
+    for (int64_t t = (int64_t)blockIdx.x * THREADS + threadIdx.x; t <= vocab; t += (int64_t)gridDim.x * THREADS)
+        starts[t] = (int32_t)lower_bound(keys, n, (uint32_t)t);
+}
+
+// ---- gradient -------------------------------------------------------------------------------------------------------------
+
+// Tokens with at most CHUNK positions are summed by one lane group.  The positions of longer ones are cut at multiples of CHUNK (of the
+// places in the order): a wavefront sums each piece into a row of the workspace, and a second launch adds a token's pieces.
+// A piece's row is 2 * chunk, or 2 * chunk + 1 where the token starts inside the chunk (the chunk's first place is another token's).
+constexpr int CHUNK = 64;
+
+struct GradArgs {
+    const int32_t *order, *starts;
+    int64_t n, vocab, ldo, ldt;
+    int32_t width;
+    float scale;
+    bool accumulate;
+    int log_lanes;    // lanes of a group; a group's lanes hold V columns each
+    int64_t chunks;
+    float *pieces;    // [2 * chunks][width]
+};
+
+// The V columns of a lane.  The last ones of a row that is no multiple of V wide are moved left; the first `skip` of them belong to the lane before.
+struct Columns {
+    int32_t at, skip;
+    bool on; // false: past the end (`at` is valid all the same)
+};
+
+// acc += rows order[s], order[s + step], ... below e, in that order; AHEAD of them are requested before the first is used
+constexpr int AHEAD = 8;
+template <class TR, int V>
+__device__ inline void add_rows(const GradArgs &a, const TR *__restrict__ dOut, int32_t col, uint32_t s, uint32_t e, uint32_t step, float (&acc)[V])
+{
+    for (uint32_t p = s; p < e; p += AHEAD * step) {
+        int32_t row[AHEAD];
+        typename VecOf<TR, V>::type x[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const uint32_t at = p + i * step;
+            row[i] = at < e ? a.order[at] : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (row[i] < 0 || row[i] >= a.n) row[i] = -1;
+            if (row[i] >= 0) x[i] = load_vec<TR, V>(dOut + row[i] * a.ldo + col);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (row[i] >= 0) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] += (float)x[i][j];
+            }
+    }
+}
+
+// Each element has one owner (with ACCUMULATE a second one would add twice)
+template <class TT, int V> __device__ inline void store_sum(const GradArgs &a, TT *__restrict__ dTable, int64_t t, const Columns &c, float (&sum)[V])
+{
+    TT *p = dTable + t * a.ldt + c.at;
+    if (a.accumulate) {
+        const auto old = load_vec<TT, V>(p);
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += (float)old[j];
+    }
+    if (c.skip == 0) {
+        store_vec<TT, V>(p, sum);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j >= c.skip) p[j] = (TT)sum[j];
+    }
+}
+
+// The token whose positions hold place p (p < starts[vocab]): the last t with starts[t] <= p.  The whole wavefront looks for one.
+__device__ inline int64_t token_at(const GradArgs &a, int32_t p)
+{
+    int64_t lo = 0, hi = a.vocab; // starts[lo] <= p < starts[hi]
+    const int lane = threadIdx.x & 63;
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 63) / 64, at = lo + (lane + 1) * step;
+        const int c = __popcll(__ballot(at < hi && a.starts[at < hi ? at : lo] <= p));
+        lo += c * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
+__device__ inline int32_t place(const GradArgs &a, int64_t t) // starts[t] within the order
+{
+    const int32_t s = a.starts[t];
+    return s < 0 ? 0 : s > a.n ? (int32_t)a.n : s;
+}
+
+template <int V> __device__ inline Columns lane_columns(const GradArgs &a)
+{
+    const int lane = threadIdx.x & ((1 << a.log_lanes) - 1);
+    const int32_t c = ((int32_t)blockIdx.y << a.log_lanes) * V + lane * V, at = min(c, a.width - V);
+    return Columns{at, c - at, c < a.width};
+}
+
+template <class TR, class TT, int V>
+__global__ __launch_bounds__(THREADS) void embed_grad_kernel(const GradArgs a, const TR *__restrict__ dOut, TT *__restrict__ dTable, uint32_t first_block,
+                                                             uint32_t chunk_blocks)
+{
+    const Columns col = lane_columns<V>(a);
+    const uint32_t block = first_block + blockIdx.x;
+    if (block < chunk_blocks) { // pieces of long tokens, a wavefront per chunk
+        const int64_t chunk = (int64_t)block * (THREADS / 64) + threadIdx.x / 64;
+        const int32_t valid = place(a, a.vocab);
+        if (chunk >= a.chunks || chunk * CHUNK >= valid) return;
+        const int32_t p0 = (int32_t)chunk * CHUNK, p1 = valid - p0 < CHUNK ? valid : p0 + CHUNK;
+        const int64_t head = token_at(a, p0), tail = token_at(a, p1 - 1);
+        const int lanes = 1 << a.log_lanes, sub = (threadIdx.x & 63) >> a.log_lanes, subs = 64 >> a.log_lanes;
+        for (int which = 0; which < 2; ++which) {
+            const int64_t t = which ? tail : head;
+            if (which && tail == head) break;
+            const int32_t s = max(place(a, t), p0), e = min(place(a, t + 1), p1);
+            if ((int64_t)place(a, t + 1) - place(a, t) <= CHUNK || e <= s) continue;
+            float acc[V] = {};
+            add_rows<TR, V>(a, dOut, col.at, (uint32_t)s + sub, (uint32_t)e, subs, acc);
+            for (int step = lanes; step < 64; step <<= 1) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] += __shfl_xor(acc[j], step, 64);
+            }
+            if (sub == 0 && col.on) store_vec<float, V>(a.pieces + (2 * chunk + which) * a.width + col.at, acc);
+        }
+        return;
+    }
+    const int64_t t = ((int64_t)(block - chunk_blocks) * THREADS + threadIdx.x) >> a.log_lanes;
+    if (t >= a.vocab || !col.on) return;
+    const int32_t s = place(a, t), e = place(a, t + 1);
+    if ((int64_t)e - s > CHUNK || (a.accumulate && e <= s)) return;
+    float acc[V] = {};
+    if (e > s) add_rows<TR, V>(a, dOut, col.at, (uint32_t)s, (uint32_t)e, 1, acc);
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] *= a.scale;
+    store_sum<TT, V>(a, dTable, t, col, acc);
+}
+
+// The pieces of the long token that starts in this workgroup's chunk, if there is one
+template <class TT, int V>
+__global__ __launch_bounds__(THREADS) void embed_join_kernel(const GradArgs a, TT *__restrict__ dTable, uint32_t first_block)
+{
+    __shared__ double sums[THREADS][V];
+    const Columns col = lane_columns<V>(a);
+    const int64_t chunk = (int64_t)first_block + blockIdx.x;
+    const int32_t valid = place(a, a.vocab);
+    if (chunk * CHUNK >= valid) return;
+    const int32_t p0 = (int32_t)chunk * CHUNK, p1 = valid - p0 < CHUNK ? valid : p0 + CHUNK;
+    const int64_t t = token_at(a, p1 - 1); // a long token that starts in the chunk holds its last place
+    const int32_t s = place(a, t), e = place(a, t + 1);
+    if (s < p0 || (int64_t)e - s <= CHUNK) return; // the same for the whole workgroup
+    const int64_t last = (e - 1) / CHUNK;
+    const int lanes = 1 << a.log_lanes, sub = threadIdx.x >> a.log_lanes, subs = THREADS >> a.log_lanes;
+    double acc[V] = {};
+    for (int64_t c = chunk + sub; c <= last; c += subs) {
+        const int64_t slot = 2 * c + (c == chunk && s > p0);
+        const auto x = load_vec<float, V>(a.pieces + slot * a.width + col.at);
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += (double)x[j];
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) sums[threadIdx.x][j] = acc[j];
+    __syncthreads();
+    if (sub != 0 || !col.on) return;
+    float out[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        double total = 0.0;
+        for (int i = 0; i < subs; ++i) total += sums[threadIdx.x + i * lanes][j];
+        out[j] = (float)((double)a.scale * total);
+    }
+    store_sum<TT, V>(a, dTable, t, col, out);
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+
+// A pair of types that differ has fp32 on one side
+template <class F> auto with_types(int32_t table, int32_t rows, F f)
+{
+    return with_type(table, [&](auto t) {
+        return with_type(rows, [&](auto r) {
+            using TT = decltype(t);
+            using TR = decltype(r);
+            if constexpr (std::is_same_v<TT, TR> || std::is_same_v<TT, float> || std::is_same_v<TR, float>) return f(t, r);
+            else return (int)SLICEGCN_EINVAL; // refused before
+        });
+    });
+}
+
+int check_desc(const char *what, const slicegcn_embed_desc *d, bool rows)
+{
+    SG_REQUIRE(d != nullptr, SLICEGCN_EINVAL, "%s: NULL descriptor", what);
+    SG_REQUIRE(d->n >= 0 && d->vocab >= 1, SLICEGCN_EINVAL, "%s: need n >= 0 and vocab >= 1", what);
+    SG_REQUIRE(d->n <= INT32_MAX && d->vocab < INT32_MAX, SLICEGCN_ERANGE, "%s: n = %lld or vocab = %lld too large", what, (long long)d->n, (long long)d->vocab);
+    SG_REQUIRE((d->flags & ~(SLICEGCN_EMBED_IDS64 | SLICEGCN_EMBED_PAD | SLICEGCN_EMBED_ACCUMULATE)) == 0, SLICEGCN_EINVAL, "%s: unknown flag", what);
+    if (!rows) return SLICEGCN_OK;
+    SG_REQUIRE(d->width >= 1, SLICEGCN_EINVAL, "%s: width < 1", what);
+    SG_REQUIRE(known_type(d->table_type) && known_type(d->row_type), SLICEGCN_EINVAL, "%s: unknown type", what);
+    SG_REQUIRE(d->table_type == d->row_type || d->table_type == SLICEGCN_F32 || d->row_type == SLICEGCN_F32, SLICEGCN_EINVAL,
+               "%s: a table and rows in two different 16-bit types", what);
+    SG_REQUIRE(std::isfinite((float)d->scale), SLICEGCN_EINVAL, "%s: scale is not finite", what);
+    return SLICEGCN_OK;
+}
+
+int check_ids(const char *what, const slicegcn_embed_desc *d, const void *ids)
+{
+    SG_REQUIRE(ids || d->n == 0, SLICEGCN_EINVAL, "%s: NULL ids", what);
+    SG_REQUIRE((reinterpret_cast<uintptr_t>(ids) & (d->flags & SLICEGCN_EMBED_IDS64 ? 7u : 3u)) == 0, SLICEGCN_EINVAL, "%s: misaligned ids", what);
+    return SLICEGCN_OK;
+}
+
+// log2 of the lanes that hold a row's accesses, 8 to 64
+int log_lanes_for(int32_t accesses)
+{
+    int l = 3;
+    while (l < 6 && (1 << l) < accesses) ++l;
+    return l;
+}
+
+struct SortPlan {
+    int bits, passes; // per digit
+    int64_t tiles;
+    SortPlan(int64_t n, int64_t vocab)
+    {
+        int all = 1;
+        while ((vocab >> all) != 0) ++all; // keys 0 to vocab
+        passes = (all + DIGIT_BITS - 1) / DIGIT_BITS;
+        bits = (all + passes - 1) / passes;
+        tiles = (n + SORT_TILE - 1) / SORT_TILE;
+    }
+    int64_t hist_words() const { return round_up(tiles << bits, 64); }
+};
+
+} // namespace
+} // namespace slicegcn
+
+using namespace slicegcn;
+
+extern "C" int slicegcn_embed_fwd(const slicegcn_embed_desc *d, const void *ids, const void *table, int64_t ldt, void *out, int64_t ldo,
+                                  void *stream)
+{
+    if (int rc = check_desc("embed_fwd", d, true)) return rc;
+    if (int rc = check_ids("embed_fwd", d, ids)) return rc;
+    SG_REQUIRE(table && (out || d->n == 0), SLICEGCN_EINVAL, "embed_fwd: NULL pointer");
+    SG_REQUIRE(ldt >= d->width && ldo >= d->width, SLICEGCN_EINVAL, "embed_fwd: leading dimension smaller than the width");
+    SG_REQUIRE(aligned_for(table, d->table_type) && aligned_for(out, d->row_type), SLICEGCN_EINVAL, "embed_fwd: misaligned base");
+    if (d->n == 0) return SLICEGCN_OK;
+    ProfScope prof(SLICEGCN_PROF_EMBED, d->width, as_stream(stream));
+    const bool has_pad = d->flags & SLICEGCN_EMBED_PAD;
+    return with_types(d->table_type, d->row_type, [&](auto t, auto r) {
+        using TT = decltype(t);
+        using TR = decltype(r);
+        auto launch = [&](auto access) {
+            constexpr int V = decltype(access)::value;
+            const int32_t accesses = (d->width + V - 1) / V;
+            const int log_lanes = log_lanes_for(accesses), groups = THREADS >> log_lanes;
+            const int64_t blocks = (d->n + groups * LOOKUP_ROWS - 1) / (groups * LOOKUP_ROWS);
+            const int32_t tile = (V << log_lanes) * 4;
+            const int64_t tiles = ((int64_t)d->width + tile - 1) / tile;
+            SG_REQUIRE(tiles < 65536, SLICEGCN_ERANGE, "embed_fwd: width = %d too large", d->width);
+            const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), (unsigned)tiles);
+            if (d->flags & SLICEGCN_EMBED_IDS64)
+                lookup_kernel<int64_t, TT, TR, V><<<grid, THREADS, 0, as_stream(stream)>>>(
+                    static_cast<const int64_t *>(ids), d->n, d->vocab, d->pad, has_pad, static_cast<const TT *>(table), ldt, d->width,
+                    (float)d->scale, static_cast<TR *>(out), ldo, log_lanes, tile);
+            else
+                lookup_kernel<int32_t, TT, TR, V><<<grid, THREADS, 0, as_stream(stream)>>>(
+                    static_cast<const int32_t *>(ids), d->n, d->vocab, d->pad, has_pad, static_cast<const TT *>(table), ldt, d->width,
+                    (float)d->scale, static_cast<TR *>(out), ldo, log_lanes, tile);
+            SG_LAUNCH_CHECK();
+            return (int)SLICEGCN_OK;
+        };
+        constexpr int V = 16 / (int)sizeof(TR);
+        if (d->width >= V) return launch(std::integral_constant<int, V>());
+        return launch(std::integral_constant<int, 1>());
+    });
+}
+
+extern "C" size_t slicegcn_embed_sort_workspace_bytes(int64_t n, int64_t vocab)
+{
+    if (n < 0 || vocab < 1 || n > INT32_MAX || vocab >= INT32_MAX || n <= SORT_TILE) return 0;
+    const SortPlan plan(n, vocab);
+    return (size_t)round_up(4 * (plan.hist_words() + DIGITS + 4 * round_up(n, 64)), 256);
+}
+
+extern "C" int slicegcn_embed_sort(const slicegcn_embed_desc *d, const void *ids, int32_t *order, int32_t *starts, void *ws, size_t ws_bytes,
+                                   void *stream)
+{
+    if (int rc = check_desc("embed_sort", d, false)) return rc;
+    if (int rc = check_ids("embed_sort", d, ids)) return rc;
+    SG_REQUIRE((order || d->n == 0) && starts, SLICEGCN_EINVAL, "embed_sort: NULL pointer");
+    SG_REQUIRE((reinterpret_cast<uintptr_t>(order) & 3u) == 0 && (reinterpret_cast<uintptr_t>(starts) & 3u) == 0 &&
+                   (reinterpret_cast<uintptr_t>(ws) & 255u) == 0, SLICEGCN_EINVAL, "embed_sort: misaligned array or workspace");
+    const size_t need = slicegcn_embed_sort_workspace_bytes(d->n, d->vocab);
+    SG_REQUIRE(need == 0 || (ws && ws_bytes >= need), SLICEGCN_EWORKSPACE, "embed_sort: workspace of %zu bytes, %zu needed", ws_bytes, need);
+    ProfScope prof(SLICEGCN_PROF_EMBED, 0, as_stream(stream));
+    const Tokens t{ids, d->n, d->vocab, d->pad, (d->flags & SLICEGCN_EMBED_IDS64) != 0, (d->flags & SLICEGCN_EMBED_PAD) != 0};
+    const SortPlan plan(d->n, d->vocab);
+    hipStream_t s = as_stream(stream);
+    if (d->n <= SORT_TILE)
+        return launch_parts((d->vocab + STARTS_PER_BLOCK) / STARTS_PER_BLOCK, [&](unsigned, unsigned count) { // below 2^19 workgroups: one part
+            sort_small_kernel<<<count, SORT_THREADS, 0, s>>>(t, plan.bits, plan.passes, order, starts);
+        });
+    uint32_t *hist = static_cast<uint32_t *>(ws), *total = hist + plan.hist_words(), *buf = total + DIGITS;
+    const int64_t stride = round_up(d->n, 64);
+    uint32_t *keys[2] = {buf, buf + stride}, *from[2] = {buf + 2 * stride, buf + 3 * stride};
+    const uint32_t *in_keys = nullptr, *in_from = nullptr;
+    for (int p = 0; p < plan.passes; ++p) {
+        uint32_t *out_keys = keys[p & 1], *out_from = p == plan.passes - 1 ? reinterpret_cast<uint32_t *>(order) : from[p & 1];
+        const int shift = p * plan.bits;
+        digit_count_kernel<<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, shift, plan.bits, hist);
+        SG_LAUNCH_CHECK();
+        digit_scan_kernel<<<(unsigned)(((1 << plan.bits) + 63) / 64), 1024, 0, s>>>(hist, plan.tiles, plan.bits, total);
+        SG_LAUNCH_CHECK();
+        digit_scatter_kernel<<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, total, out_keys, out_from);
+        SG_LAUNCH_CHECK();
+        in_keys = out_keys;
+        in_from = out_from;
+    }
+    const int64_t blocks = (d->vocab + 1 + THREADS - 1) / THREADS;
+    starts_kernel<<<(unsigned)(blocks < 65536 ? blocks : 65536), THREADS, 0, s>>>(in_keys, (uint32_t)d->n, d->vocab, starts);
+    SG_LAUNCH_CHECK();
+    return SLICEGCN_OK;
+}
+
+extern "C" size_t slicegcn_embed_bwd_workspace_bytes(int64_t n, int32_t width)
+{
+    if (n <= CHUNK || n > INT32_MAX || width < 1) return 0; // no token can have more than CHUNK positions
+    return (size_t)round_up(2 * ((n + CHUNK - 1) / CHUNK) * (int64_t)width * 4, 256);
+}
+
+extern "C" int slicegcn_embed_bwd(const slicegcn_embed_desc *d, const int32_t *order, const int32_t *starts, const void *dOut, int64_t ldo,
+                                  void *dTable, int64_t ldt, void *ws, size_t ws_bytes, void *stream)
+{
+    if (int rc = check_desc("embed_bwd", d, true)) return rc;
+    SG_REQUIRE(starts && dTable && ((order && dOut) || d->n == 0), SLICEGCN_EINVAL, "embed_bwd: NULL pointer");
+    SG_REQUIRE(ldt >= d->width && ldo >= d->width, SLICEGCN_EINVAL, "embed_bwd: leading dimension smaller than the width");
+    SG_REQUIRE(aligned_for(dTable, d->table_type) && aligned_for(dOut, d->row_type) && (reinterpret_cast<uintptr_t>(order) & 3u) == 0 &&
+                   (reinterpret_cast<uintptr_t>(starts) & 3u) == 0 && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0, SLICEGCN_EINVAL,
+               "embed_bwd: misaligned array or workspace");
+    const size_t need = slicegcn_embed_bwd_workspace_bytes(d->n, d->width);
+    SG_REQUIRE(need == 0 || (ws && ws_bytes >= need), SLICEGCN_EWORKSPACE, "embed_bwd: workspace of %zu bytes, %zu needed", ws_bytes, need);
+    ProfScope prof(SLICEGCN_PROF_EMBED, d->width, as_stream(stream));
+    return with_types(d->table_type, d->row_type, [&](auto t, auto r) {
+        using TT = decltype(t);
+        using TR = decltype(r);
+        auto launch = [&](auto access) {
+            constexpr int V = decltype(access)::value;
+            const int32_t accesses = (d->width + V - 1) / V;
+            GradArgs a{order, starts, d->n, d->vocab, ldo, ldt, d->width, (float)d->scale, (d->flags & SLICEGCN_EMBED_ACCUMULATE) != 0,
+                       log_lanes_for(accesses), d->n > CHUNK ? (d->n + CHUNK - 1) / CHUNK : 0, static_cast<float *>(ws)};
+            const unsigned tiles = (unsigned)((accesses + (1 << a.log_lanes) - 1) >> a.log_lanes);
+            const uint32_t chunk_blocks = (uint32_t)((a.chunks + THREADS / 64 - 1) / (THREADS / 64));
+            const int64_t groups = THREADS >> a.log_lanes, blocks = chunk_blocks + (d->vocab + groups - 1) / groups;
+            SG_REQUIRE(tiles < 65536, SLICEGCN_ERANGE, "embed_bwd: width = %d too large", d->width);
+            if (int rc = launch_parts(blocks, [&](unsigned first, unsigned count) {
+                    embed_grad_kernel<TR, TT, V><<<dim3(count, tiles), THREADS, 0, as_stream(stream)>>>(
+                        a, static_cast<const TR *>(dOut), static_cast<TT *>(dTable), first, chunk_blocks);
+                }))
+                return rc;
+            if (a.chunks) {
+                if (int rc = launch_parts(a.chunks, [&](unsigned first, unsigned count) {
+                        embed_join_kernel<TT, V><<<dim3(count, tiles), THREADS, 0, as_stream(stream)>>>(a, static_cast<TT *>(dTable), first);
+                    }))
+                    return rc;
+            }
+            return (int)SLICEGCN_OK;
+        };
+        constexpr int V = 16 / (int)sizeof(TR);
+        if (d->width >= V) return launch(std::integral_constant<int, V>());
+        return launch(std::integral_constant<int, 1>());
+    });
+}

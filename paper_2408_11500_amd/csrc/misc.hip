@@ -1,6 +1,7 @@
 // Host-side slice strategy, direct feature slicing, slice encoding + concatenation and the
 // error-text plumbing of the C ABI.
 #include "common.h"
+#include "slicegcn_train.h"
 
 #include <cmath>
 
@@ -151,14 +152,17 @@ __global__ __launch_bounds__(256) void accumulate_kernel(float *__restrict__ dst
 }
 
 // One Adam step on `count` contiguous parameters (bias-corrected, optional L2 weight decay).
-// c1 = 1 - beta1^t and c2 = 1 - beta2^t are computed on the host in fp64.
+// c1 = 1 - beta1^t and c2 = 1 - beta2^t are computed on the host in fp64.  SCALED: the gradient times *factor.
+template <bool SCALED>
 __global__ __launch_bounds__(256) void adam_kernel(float *__restrict__ p, const float *__restrict__ g, float *__restrict__ m,
                                                    float *__restrict__ v, int64_t count, float lr, float beta1, float omb1,
-                                                   float beta2, float omb2, float eps, float wd, float inv_c1, float inv_c2)
+                                                   float beta2, float omb2, float eps, float wd, float inv_c1, float inv_c2,
+                                                   const float *__restrict__ factor)
 {
+    const float f = SCALED ? *factor : 1.f;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
         const float pi = p[i];
-        const float gi = g[i] + wd * pi;
+        const float gi = (SCALED ? f * g[i] : g[i]) + wd * pi;
         const float mi = beta1 * m[i] + omb1 * gi; // omb = 1 - beta, rounded from fp64 on the host
         const float vi = beta2 * v[i] + omb2 * gi * gi;
         m[i] = mi;
@@ -216,19 +220,36 @@ extern "C" int slicegcn_accumulate(float *dst, int64_t ldd, const float *src, in
     return slicegcn_accumulate_many(dst, ldd, &src, 1, lds_, n, w, stream);
 }
 
-extern "C" int slicegcn_adam_step(float *param, const float *grad, float *m, float *v, int64_t count, double lr, double beta1,
-                                  double beta2, double eps, double weight_decay, int32_t step, void *stream)
+static int adam_call(float *param, const float *grad, const float *factor, float *m, float *v, int64_t count, double lr, double beta1,
+                     double beta2, double eps, double weight_decay, int32_t step, void *stream)
 {
     SG_REQUIRE(param && grad && m && v, SLICEGCN_EINVAL, "adam_step: NULL pointer");
     SG_REQUIRE(count >= 1 && step >= 1, SLICEGCN_EINVAL, "adam_step: count and step must be >= 1");
     SG_REQUIRE(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0 && eps >= 0.0, SLICEGCN_EINVAL,
                "adam_step: betas must lie in [0, 1) and eps must not be negative");
     const double c1 = 1.0 - pow(beta1, (double)step), c2 = 1.0 - pow(beta2, (double)step);
-    adam_kernel<<<grid_for(count), 256, 0, as_stream(stream)>>>(param, grad, m, v, count, (float)lr, (float)beta1,
-                                                                (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps,
-                                                                (float)weight_decay, (float)(1.0 / c1), (float)(1.0 / c2));
+    auto launch = [&](auto kernel) {
+        kernel<<<grid_for(count), 256, 0, as_stream(stream)>>>(param, grad, m, v, count, (float)lr, (float)beta1, (float)(1.0 - beta1),
+                                                               (float)beta2, (float)(1.0 - beta2), (float)eps, (float)weight_decay,
+                                                               (float)(1.0 / c1), (float)(1.0 / c2), factor);
+    };
+    if (factor) launch(adam_kernel<true>);
+    else launch(adam_kernel<false>);
     SG_LAUNCH_CHECK();
     return SLICEGCN_OK;
+}
+
+extern "C" int slicegcn_adam_step(float *param, const float *grad, float *m, float *v, int64_t count, double lr, double beta1,
+                                  double beta2, double eps, double weight_decay, int32_t step, void *stream)
+{
+    return adam_call(param, grad, nullptr, m, v, count, lr, beta1, beta2, eps, weight_decay, step, stream);
+}
+
+extern "C" int slicegcn_adam_step_scaled(float *param, const float *grad, const float *factor, float *m, float *v, int64_t count, double lr,
+                                         double beta1, double beta2, double eps, double weight_decay, int32_t step, void *stream)
+{
+    SG_REQUIRE(factor != nullptr, SLICEGCN_EINVAL, "adam_step_scaled: NULL factor");
+    return adam_call(param, grad, factor, m, v, count, lr, beta1, beta2, eps, weight_decay, step, stream);
 }
 
 extern "C" double slicegcn_cosine_lr(double lr_max, double lr_min, int32_t t, int32_t t_max)

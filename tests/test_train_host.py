@@ -1,0 +1,162 @@
+"""The operators of slicegcn_train.h without a GPU: exported symbols, workspace sizes, and refusals before any device work."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2408_11500_amd import binding as B
+from test_abi_host import L, declared_symbols  # noqa: F401  (L is a fixture)
+
+ONE = 1 << 20  # an aligned non-NULL address: validation must fail before anything dereferences it
+
+
+def test_every_declared_symbol_is_exported(L):  # noqa: F811
+    names = declared_symbols("slicegcn_train.h")
+    assert {"slicegcn_embed_fwd", "slicegcn_embed_sort", "slicegcn_embed_bwd", "slicegcn_resnorm_fwd", "slicegcn_resnorm_bwd",
+            "slicegcn_global_norm", "slicegcn_clip", "slicegcn_adam_step_scaled"} <= set(names)
+    for n in names:
+        assert getattr(L, n).argtypes is not None, n
+
+
+def embed(n=4, vocab=4, width=4, table=B.F32, rows=B.F32, scale=1.0, pad=0, flags=0):
+    return B._EmbedDesc(n, vocab, pad, scale, width, table, rows, flags)
+
+
+BAD_EMBED = [(dict(n=-1), B.EINVAL), (dict(vocab=0), B.EINVAL), (dict(n=2**31), B.ERANGE), (dict(vocab=2**31 - 1), B.ERANGE), (dict(flags=8), B.EINVAL)]
+BAD_ROWS = [(dict(width=0), B.EINVAL), (dict(table=3), B.EINVAL), (dict(rows=-1), B.EINVAL), (dict(table=B.BF16, rows=B.F16), B.EINVAL),
+            (dict(scale=float("inf")), B.EINVAL), (dict(scale=float("nan")), B.EINVAL), (dict(scale=1e39), B.EINVAL), (dict(width=5), B.EINVAL)]
+
+
+@pytest.mark.parametrize("change,status", BAD_EMBED + BAD_ROWS)
+def test_embed_fwd_refuses(L, change, status):  # noqa: F811
+    assert L.slicegcn_embed_fwd(ctypes.byref(embed(**change)), ONE, ONE, 4, ONE, 4, None) == status
+
+
+def test_embed_calls_refuse_bad_pointers(L):  # noqa: F811
+    d = ctypes.byref(embed())
+    wide = ctypes.byref(embed(flags=B.EMBED_IDS64))
+    half = ctypes.byref(embed(table=B.BF16, rows=B.F32))
+    for args in ((None, ONE, ONE, 4, ONE, 4), (d, None, ONE, 4, ONE, 4), (d, ONE, None, 4, ONE, 4), (d, ONE, ONE, 4, None, 4), (d, ONE + 2, ONE, 4, ONE, 4),
+                 (wide, ONE + 4, ONE, 4, ONE, 4), (d, ONE, ONE + 2, 4, ONE, 4), (half, ONE, ONE + 1, 4, ONE, 4), (d, ONE, ONE, 3, ONE, 4), (d, ONE, ONE, 4, ONE, 3)):
+        assert L.slicegcn_embed_fwd(*args, None) == B.EINVAL
+    for args in ((None, ONE, ONE, ONE), (d, None, ONE, ONE), (d, ONE, None, ONE), (d, ONE, ONE, None), (d, ONE, ONE + 2, ONE), (d, ONE, ONE, ONE + 1)):
+        assert L.slicegcn_embed_sort(*args, None, 0, None) == B.EINVAL
+    big = embed(n=5000)
+    need = L.slicegcn_embed_sort_workspace_bytes(5000, 4)
+    assert need > 0
+    assert L.slicegcn_embed_sort(ctypes.byref(big), ONE, ONE, ONE, None, 0, None) == B.EWORKSPACE
+    assert L.slicegcn_embed_sort(ctypes.byref(big), ONE, ONE, ONE, ONE, need - 1, None) == B.EWORKSPACE
+    assert L.slicegcn_embed_sort(ctypes.byref(big), ONE, ONE, ONE, ONE + 64, need, None) == B.EINVAL
+    for args in ((None, ONE, ONE, ONE, 4, ONE, 4), (d, None, ONE, ONE, 4, ONE, 4), (d, ONE, None, ONE, 4, ONE, 4), (d, ONE, ONE, None, 4, ONE, 4),
+                 (d, ONE, ONE, ONE, 4, None, 4), (d, ONE, ONE, ONE, 3, ONE, 4), (d, ONE, ONE, ONE, 4, ONE, 3), (d, ONE + 2, ONE, ONE, 4, ONE, 4)):
+        assert L.slicegcn_embed_bwd(*args, None, 0, None) == B.EINVAL
+    need = L.slicegcn_embed_bwd_workspace_bytes(5000, 4)
+    assert L.slicegcn_embed_bwd(ctypes.byref(big), ONE, ONE, ONE, 4, ONE, 4, ONE, need - 1, None) == B.EWORKSPACE
+    for change, status in BAD_EMBED + BAD_ROWS:
+        assert L.slicegcn_embed_bwd(ctypes.byref(embed(**change)), ONE, ONE, ONE, 4, ONE, 4, ONE, 1 << 30, None) == status
+
+
+def test_embed_workspaces(L):  # noqa: F811
+    sort, grad = L.slicegcn_embed_sort_workspace_bytes, L.slicegcn_embed_bwd_workspace_bytes
+    assert sort(-1, 5) == sort(5, 0) == sort(2**31, 5) == sort(5, 2**31 - 1) == 0
+    assert sort(1_000_000, 50_000) >= 16_000_000
+    assert grad(-1, 4) == grad(100, 0) == grad(2**31, 4) == grad(0, 4) == grad(1, 4) == 0
+    assert grad(100_000, 64) > 0
+
+
+def resnorm(n=4, width=4, type=B.F32, post=B.NORM_RMS, pre=B.NORM_RMS, flags=0, residual=1.0, eps=1e-6):
+    return B._ResnormDesc(n, width, type, post, pre, flags, residual, eps)
+
+
+def io(**kw):
+    r = B._ResnormIo()
+    for k, v in dict(dict(x=ONE, y=ONE, h=ONE, u=ONE, dh=ONE, du=ONE, stats=ONE), **kw).items():
+        setattr(r, k, v if k == "stats" else B._Rows(*(v if isinstance(v, tuple) else (v, 4))))
+    return r
+
+
+def params(**kw):
+    return B._ResnormParams(**kw)
+
+
+BAD_RESNORM = [
+    (dict(n=-1), {}, {}, B.EINVAL), (dict(width=0), {}, {}, B.EINVAL), (dict(width=16385), {}, {}, B.EUNSUPPORTED), (dict(type=3), {}, {}, B.EINVAL),
+    (dict(post=3), {}, {}, B.EINVAL), (dict(pre=-1), {}, {}, B.EINVAL), (dict(flags=2), {}, {}, B.EINVAL), (dict(residual=float("nan")), {}, {}, B.EINVAL),
+    (dict(eps=0.0), {}, {}, B.EINVAL), (dict(eps=-1e-6), {}, {}, B.EINVAL), (dict(eps=1e-60), {}, {}, B.EINVAL), (dict(eps=float("nan")), {}, {}, B.EINVAL),
+    (dict(flags=1), {}, {}, B.EINVAL),                                   # sigmoid without gate
+    ({}, dict(gate=ONE), dict(gate=ONE), B.EINVAL),                      # two gates
+    (dict(post=0), dict(post_w=ONE), {}, B.EINVAL), (dict(pre=0), dict(pre_b=ONE), {}, B.EINVAL), ({}, dict(pre_w=ONE + 2), {}, B.EINVAL),
+    ({}, {}, dict(x=None, y=None), B.EINVAL), ({}, {}, dict(y=None), B.EINVAL), (dict(post=0), dict(gate=ONE), dict(y=None), B.EINVAL),
+    ({}, {}, dict(x=(ONE, 3)), B.EINVAL), ({}, {}, dict(y=ONE + 2), B.EINVAL), (dict(type=B.BF16), {}, dict(x=ONE + 1), B.EINVAL), ({}, {}, dict(stats=ONE + 8), B.EINVAL)]
+
+
+@pytest.mark.parametrize("desc,p,rows,status", BAD_RESNORM)
+def test_resnorm_refuses(L, desc, p, rows, status):  # noqa: F811
+    d, q, r = resnorm(**desc), params(**p), io(**rows)
+    assert L.slicegcn_resnorm_fwd(ctypes.byref(d), ctypes.byref(q), ctypes.byref(r), None) == status
+    assert L.slicegcn_resnorm_bwd(ctypes.byref(d), ctypes.byref(q), ctypes.byref(r), None, None, 0, None) == status
+
+
+def test_resnorm_directions_refuse(L):  # noqa: F811
+    d, none = ctypes.byref(resnorm()), ctypes.byref(params())
+    fwd = lambda **rows: L.slicegcn_resnorm_fwd(d, none, ctypes.byref(io(**rows)), None)
+    assert fwd(h=None, u=None) == fwd(u=None) == fwd(h=(ONE, 2)) == B.EINVAL
+    assert L.slicegcn_resnorm_fwd(None, none, ctypes.byref(io()), None) == L.slicegcn_resnorm_fwd(d, None, ctypes.byref(io()), None) == B.EINVAL
+    assert L.slicegcn_resnorm_fwd(d, none, None, None) == B.EINVAL
+
+    def bwd(grads=None, p=None, ws=None, nbytes=0, **rows):
+        return L.slicegcn_resnorm_bwd(d, ctypes.byref(params(**(p or {}))), ctypes.byref(io(**rows)), ctypes.byref(params(**(grads or {}))), ws, nbytes, None)
+    assert bwd(dh=None, du=None) == bwd(stats=None) == bwd(dx=ONE, x=None) == bwd(dgate=ONE) == bwd(dy=(ONE, 3)) == B.EINVAL
+    assert bwd(grads=dict(pre_w=ONE)) == B.EINVAL                        # gradient of an absent parameter
+    assert bwd(grads=dict(pre_w=ONE + 1), p=dict(pre_w=ONE)) == B.EINVAL
+    need = L.slicegcn_resnorm_bwd_workspace_bytes(4, 4)
+    assert bwd(grads=dict(pre_w=ONE), p=dict(pre_w=ONE)) == bwd(dict(pre_w=ONE), dict(pre_w=ONE), ONE, need - 1) == B.EWORKSPACE
+    assert bwd(dict(pre_w=ONE), dict(pre_w=ONE), ONE + 4, need) == B.EINVAL
+    ws = L.slicegcn_resnorm_bwd_workspace_bytes
+    assert ws(-1, 4) == ws(4, 0) == ws(4, 16385) == 0 and ws(4, 4) > 0
+
+
+def tensor_list(*entries):
+    return (B._Tensor * max(len(entries), 1))(*[B._Tensor(*e) for e in entries])
+
+
+@pytest.mark.parametrize("entries,count", [([(None, 4, 0, 0)], 1), ([(ONE, -1, 0, 0)], 1), ([(ONE, 4, 5, 0)], 1), ([(ONE + 2, 4, 0, 0)], 1), ([(ONE + 1, 4, 1, 0)], 1),
+                                           ([], -1), ([(ONE, 1 << 48, 0, 0)], 1)])
+def test_bad_tensors_are_refused(L, entries, count):  # noqa: F811
+    a = tensor_list(*entries)
+    assert L.slicegcn_global_norm_workspace_bytes(a, count) == 0
+    assert L.slicegcn_global_norm(a, count, 0, 1.0, ONE, None, ONE, 1 << 20, None) == B.EINVAL
+    assert L.slicegcn_clip(a, None, count, 0, 1.0, ONE, None, ONE, 1 << 20, None) == B.EINVAL
+    assert L.slicegcn_clip(tensor_list((ONE, 4, 0, 0)), a, 1 if count == 1 else count, 0, 1.0, ONE, None, ONE, 1 << 20, None) == B.EINVAL
+
+
+def test_norm_and_clip_refuse(L):  # noqa: F811
+    a = tensor_list((ONE, 5000, 0, 0), (None, 0, 1, 0))
+    need = L.slicegcn_global_norm_workspace_bytes(a, 2)
+    assert need > 0
+    assert L.slicegcn_global_norm(a, 2, 0, 1.0, None, None, ONE, need, None) == B.EINVAL
+    assert L.slicegcn_global_norm(a, 2, 2, 1.0, ONE, None, ONE, need, None) == B.EINVAL
+    assert L.slicegcn_global_norm(a, 2, 0, -1.0, ONE, ONE, ONE, need, None) == B.EINVAL
+    assert L.slicegcn_global_norm(a, 2, 0, float("nan"), ONE, ONE, ONE, need, None) == B.EINVAL
+    assert L.slicegcn_global_norm(None, 2, 0, 1.0, ONE, None, ONE, need, None) == B.EINVAL
+    assert L.slicegcn_global_norm(a, 2, 0, 1.0, ONE, None, ONE, need - 1, None) == B.EWORKSPACE
+    assert L.slicegcn_global_norm(a, 2, 0, 1.0, ONE, None, None, 0, None) == B.EWORKSPACE
+    assert L.slicegcn_global_norm(a, 2, 0, 1.0, ONE, None, ONE + 8, need, None) == B.EINVAL
+    assert L.slicegcn_clip(a, tensor_list((ONE, 4999, 0, 0), (None, 0, 1, 0)), 2, 0, 1.0, ONE, None, ONE, need, None) == B.EINVAL
+    assert L.slicegcn_clip(a, tensor_list((ONE, 5000, 1, 0), (None, 0, 1, 0)), 2, 0, 1.0, ONE, None, ONE, need, None) == B.EINVAL
+    assert L.slicegcn_adam_step_scaled(ONE, ONE, None, ONE, ONE, 4, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1, None) == B.EINVAL
+    assert L.slicegcn_adam_step_scaled(ONE, ONE, ONE, ONE, ONE, 4, 1e-3, 0.9, 0.999, 1e-8, 0.0, 0, None) == B.EINVAL
+
+
+def test_binding_refuses_what_is_no_device_tensor(L):  # noqa: F811
+    t = torch.zeros(4, 4)
+    with pytest.raises(TypeError):
+        B.slicegcn_embed_fwd(torch.zeros(4, dtype=torch.int16), t, t)
+    with pytest.raises(TypeError):
+        B.slicegcn_embed_fwd(torch.zeros(4, dtype=torch.int64), t, t)
+    with pytest.raises(TypeError):
+        B.slicegcn_resnorm_fwd(t, None, t, None)
+    with pytest.raises(ValueError):
+        B.slicegcn_resnorm_fwd(None, None, t, None)
+    with pytest.raises(TypeError):
+        B.TensorList([t])
