@@ -22,7 +22,7 @@ constexpr int THREADS = 256;
 // that is moved left and overlaps the one before it (the same values twice).
 constexpr int LOOKUP_ROWS = 4;
 
-template <class ID, class TT, class TR, int V>
+template <class ID, class TT, class TR, int V, bool PAST>
 __global__ __launch_bounds__(THREADS) void lookup_kernel(const ID *__restrict__ ids, int64_t n, int64_t vocab, int64_t pad, bool has_pad,
                                                          const TT *__restrict__ table, int64_t ldt, int32_t width, float scale,
                                                          TR *__restrict__ out, int64_t ldo, int log_lanes, int32_t tile)
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(THREADS) void lookup_kernel(const ID *__restrict__ 
                 float o[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) o[j] = zero ? 0.f : in ? scale * (float)x[i][j] : NAN;
-                store_vec<TR, V>(out + r * ldo + col, o);
+                store_result<PAST, TR, V>(out + r * ldo + col, o);
             }
         }
     }
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(THREADS) void lookup_kernel(const ID *__restrict__ 
 // Stable sort by digits of at most DIGIT_BITS bits, lowest first.  Keys are tokens; padding and tokens outside the table get the key
 // `vocab` and end up behind all others.
 constexpr int DIGIT_BITS = 10, DIGITS = 1 << DIGIT_BITS;
-constexpr int SORT_THREADS = 512, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 8, SORT_TILE = SORT_THREADS * SORT_ITEMS;
+constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 4, SORT_TILE = SORT_THREADS * SORT_ITEMS;
 
 struct Tokens {
     const void *ids;
@@ -81,10 +81,13 @@ __device__ inline uint32_t token_key(const Tokens &t, int64_t i)
 __device__ inline uint64_t same_digit(uint32_t digit, int bits, uint64_t active)
 {
     uint64_t same = active;
-    for (int b = 0; b < bits; ++b) {
-        const bool one = (digit >> b) & 1;
-        const uint64_t ones = __ballot(one);
-        same &= one ? ones : ~ones;
+#pragma unroll
+    for (int b = 0; b < DIGIT_BITS; ++b) {
+        if (b < bits) {
+            const bool one = (digit >> b) & 1;
+            const uint64_t ones = __ballot(one);
+            same &= one ? ones : ~ones;
+        }
     }
     return same;
 }
@@ -145,12 +148,16 @@ __device__ inline void counts_before(uint16_t (*counts)[DIGITS], int bits, uint3
     for (int q = 0; q < DIGITS / SORT_THREADS; ++q) {
         const int d = threadIdx.x * (DIGITS / SORT_THREADS) + q;
         uint32_t sum = 0;
-        if (d < 1 << bits)
+        if (d < 1 << bits) {
+            uint32_t c[SORT_WAVES];
+#pragma unroll
+            for (int w = 0; w < SORT_WAVES; ++w) c[w] = counts[w][d];
+#pragma unroll
             for (int w = 0; w < SORT_WAVES; ++w) {
-                const uint32_t c = counts[w][d];
                 counts[w][d] = (uint16_t)sum;
-                sum += c;
+                sum += c[w];
             }
+        }
         total[q] = sum;
     }
 }
@@ -169,7 +176,7 @@ __device__ inline uint32_t lower_bound(const uint32_t *keys, uint32_t count, uin
 }
 
 // Up to SORT_TILE tokens: every workgroup sorts all of them in LDS and writes its part of starts, the first one also the order: one launch
-constexpr int STARTS_PER_BLOCK = 8 * SORT_THREADS;
+constexpr int STARTS_PER_BLOCK = 4 * SORT_THREADS;
 __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const Tokens t, int bits, int passes, int32_t *__restrict__ order, int32_t *__restrict__ starts)
 {
     __shared__ uint16_t counts[SORT_WAVES][DIGITS];
@@ -271,9 +278,12 @@ __global__ __launch_bounds__(1024) void digit_scan_kernel(uint32_t *__restrict__
     }
 }
 
+// Up to FEW_TILES tiles a workgroup adds up the tiles' histograms by itself: the scan's launch costs more.
+constexpr int FEW_TILES = 64;
+template <bool FEW>
 __global__ __launch_bounds__(SORT_THREADS) void digit_scatter_kernel(const Tokens t, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ from,
                                                                      int shift, int bits, const uint32_t *__restrict__ hist,
-                                                                     const uint32_t *__restrict__ total, uint32_t *__restrict__ out_keys,
+                                                                     const uint32_t *__restrict__ total, int tiles, uint32_t *__restrict__ out_keys,
                                                                      uint32_t *__restrict__ out_from)
 {
     __shared__ uint16_t counts[SORT_WAVES][DIGITS];
@@ -289,20 +299,37 @@ __global__ __launch_bounds__(SORT_THREADS) void digit_scatter_kernel(const Token
         key[i] = there[i] ? keys ? keys[at] : token_key(t, at) : 0;
         index[i] = there[i] && from ? from[at] : (uint32_t)at;
     }
+    // a digit's items in the tiles before this one, and in all tiles
+    constexpr int Q = DIGITS / SORT_THREADS;
+    const int digits = 1 << bits, d0 = threadIdx.x * Q;
+    uint32_t before[Q] = {}, all[Q] = {}, sum = 0;
+    if (d0 < digits) {
+        if (FEW) {
+#pragma unroll 8
+            for (int i = 0; i < tiles; ++i) {
+                const auto c = load_vec<uint32_t, Q>(hist + i * digits + d0);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    before[q] += i < (int)blockIdx.x ? c[q] : 0;
+                    all[q] += c[q];
+                }
+            }
+        } else {
+            const auto b = load_vec<uint32_t, Q>(hist + (int64_t)blockIdx.x * digits + d0), c = load_vec<uint32_t, Q>(total + d0);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) before[q] = b[q], all[q] = c[q];
+        }
+    }
     rank_items(key, there, shift, bits, counts, rank);
-    uint32_t inside[DIGITS / SORT_THREADS], all[DIGITS / SORT_THREADS], sum = 0;
+    uint32_t inside[Q];
     counts_before(counts, bits, inside);
 #pragma unroll
-    for (int q = 0; q < DIGITS / SORT_THREADS; ++q) {
-        const int d = threadIdx.x * (DIGITS / SORT_THREADS) + q;
-        all[q] = d < 1 << bits ? total[d] : 0;
-        sum += all[q];
-    }
+    for (int q = 0; q < Q; ++q) sum += all[q];
     uint32_t at = block_scan(sum, wave_sums);
 #pragma unroll
     for (int q = 0; q < DIGITS / SORT_THREADS; ++q) {
         const int d = threadIdx.x * (DIGITS / SORT_THREADS) + q;
-        if (d < 1 << bits) base[d] = at + hist[((int64_t)blockIdx.x << bits) + d];
+        if (d < digits) base[d] = at + before[q];
         at += all[q];
     }
     __syncthreads();
@@ -324,10 +351,13 @@ __global__ __launch_bounds__(THREADS) void starts_kernel(const uint32_t *__restr
 
 // ---- gradient -------------------------------------------------------------------------------------------------------------
 
-// Tokens with at most CHUNK positions are summed by one lane group.  The positions of longer ones are cut at multiples of CHUNK (of the
-// places in the order): a wavefront sums each piece into a row of the workspace, and a second launch adds a token's pieces.
-// A piece's row is 2 * chunk, or 2 * chunk + 1 where the token starts inside the chunk (the chunk's first place is another token's).
-constexpr int CHUNK = 64;
+// The order is cut into chunks of positions, whatever tokens they hold, so that work is even however tokens repeat.  A lane group adds up its
+// chunk's rows token by token.  Tokens that lie within the chunk are finished there; the sums of a token that it shares with a neighbour go
+// to the workspace as pieces, and a second launch adds those: row 2 * chunk holds the piece of a token that started before the chunk,
+// row 2 * chunk + 1 that of one that starts in it and goes on behind it.  That launch also zeroes the rows of
+// tokens without positions.
+constexpr int CHUNK = 64; // positions, at most
+constexpr int AHEAD = 4;  // rows that are requested at a time, a batch ahead
 
 struct GradArgs {
     const int32_t *order, *starts;
@@ -336,8 +366,11 @@ struct GradArgs {
     float scale;
     bool accumulate;
     int log_lanes;    // lanes of a group; a group's lanes hold V columns each
+    int log_chunk;
+    uint32_t tiles;   // tiles of a row: workgroups beside each other hold the same rows
     int64_t chunks;
     float *pieces;    // [2 * chunks][width]
+    int32_t *tails;   // [chunks] the token that starts in the chunk and goes on behind it, or -1
 };
 
 // The V columns of a lane.  The last ones of a row that is no multiple of V wide are moved left; the first `skip` of them belong to the lane before.
@@ -346,36 +379,17 @@ struct Columns {
     bool on; // false: past the end (`at` is valid all the same)
 };
 
-// acc += rows order[s], order[s + step], ... below e, in that order; AHEAD of them are requested before the first is used
-constexpr int AHEAD = 8;
-template <class TR, int V>
-__device__ inline void add_rows(const GradArgs &a, const TR *__restrict__ dOut, int32_t col, uint32_t s, uint32_t e, uint32_t step, float (&acc)[V])
+template <int V> __device__ inline Columns lane_columns(const GradArgs &a, int32_t tile)
 {
-    for (uint32_t p = s; p < e; p += AHEAD * step) {
-        int32_t row[AHEAD];
-        typename VecOf<TR, V>::type x[AHEAD];
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const uint32_t at = p + i * step;
-            row[i] = at < e ? a.order[at] : -1;
-        }
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            if (row[i] < 0 || row[i] >= a.n) row[i] = -1;
-            if (row[i] >= 0) x[i] = load_vec<TR, V>(dOut + row[i] * a.ldo + col);
-        }
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (row[i] >= 0) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) acc[j] += (float)x[i][j];
-            }
-    }
+    const int lane = threadIdx.x & ((1 << a.log_lanes) - 1);
+    const int32_t c = (tile << a.log_lanes) * V + lane * V, at = min(c, a.width - V);
+    return Columns{at, c - at, c < a.width};
 }
 
 // Each element has one owner (with ACCUMULATE a second one would add twice)
-template <class TT, int V> __device__ inline void store_sum(const GradArgs &a, TT *__restrict__ dTable, int64_t t, const Columns &c, float (&sum)[V])
+template <bool PAST, class TT, int V> __device__ inline void store_sum(const GradArgs &a, TT *__restrict__ dTable, int64_t t, const Columns &c, float (&sum)[V])
 {
+    if (!c.on) return;
     TT *p = dTable + t * a.ldt + c.at;
     if (a.accumulate) {
         const auto old = load_vec<TT, V>(p);
@@ -383,26 +397,12 @@ template <class TT, int V> __device__ inline void store_sum(const GradArgs &a, T
         for (int j = 0; j < V; ++j) sum[j] += (float)old[j];
     }
     if (c.skip == 0) {
-        store_vec<TT, V>(p, sum);
+        store_result<PAST, TT, V>(p, sum);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
             if (j >= c.skip) p[j] = (TT)sum[j];
     }
-}
-
-// The token whose positions hold place p (p < starts[vocab]): the last t with starts[t] <= p.  The whole wavefront looks for one.
-__device__ inline int64_t token_at(const GradArgs &a, int32_t p)
-{
-    int64_t lo = 0, hi = a.vocab; // starts[lo] <= p < starts[hi]
-    const int lane = threadIdx.x & 63;
-    while (hi - lo > 1) {
-        const int64_t step = (hi - lo + 63) / 64, at = lo + (lane + 1) * step;
-        const int c = __popcll(__ballot(at < hi && a.starts[at < hi ? at : lo] <= p));
-        lo += c * step;
-        hi = min(hi, lo + step);
-    }
-    return lo;
 }
 
 __device__ inline int32_t place(const GradArgs &a, int64_t t) // starts[t] within the order
@@ -411,86 +411,208 @@ __device__ inline int32_t place(const GradArgs &a, int64_t t) // starts[t] withi
     return s < 0 ? 0 : s > a.n ? (int32_t)a.n : s;
 }
 
-template <int V> __device__ inline Columns lane_columns(const GradArgs &a)
+// The tokens that hold places p and q (below starts[vocab]): the last t with starts[t] <= p.  The lanes of a group look for them together.
+__device__ inline void tokens_at(const GradArgs &a, int32_t p, int32_t q, uint32_t *tp, uint32_t *tq)
 {
-    const int lane = threadIdx.x & ((1 << a.log_lanes) - 1);
-    const int32_t c = ((int32_t)blockIdx.y << a.log_lanes) * V + lane * V, at = min(c, a.width - V);
-    return Columns{at, c - at, c < a.width};
+    const int lanes = 1 << a.log_lanes, lane = threadIdx.x & (lanes - 1), shift = (threadIdx.x & 63) - lane;
+    const uint64_t mask = lanes == 64 ? ~(uint64_t)0 : ((uint64_t)1 << lanes) - 1;
+    uint32_t lo[2] = {0, 0}, hi[2] = {(uint32_t)a.vocab, (uint32_t)a.vocab}; // starts[lo] <= place < starts[hi]
+    while (hi[0] - lo[0] > 1 || hi[1] - lo[1] > 1) {
+        uint32_t step[2];
+        bool below[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            step[i] = (hi[i] - lo[i] + lanes - 1) >> a.log_lanes;
+            const uint32_t at = lo[i] + (lane + 1) * step[i];
+            below[i] = at < hi[i] && a.starts[at < hi[i] ? at : lo[i]] <= (i ? q : p);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            lo[i] += (uint32_t)__popcll(__ballot(below[i]) >> shift & mask) * step[i];
+            hi[i] = min(hi[i], lo[i] + step[i]);
+        }
+    }
+    *tp = lo[0];
+    *tq = lo[1];
 }
 
-template <class TR, class TT, int V>
-__global__ __launch_bounds__(THREADS) void embed_grad_kernel(const GradArgs a, const TR *__restrict__ dOut, TT *__restrict__ dTable, uint32_t first_block,
-                                                             uint32_t chunk_blocks)
+// Rows of tokens without positions.  A wavefront looks at so many of them (wide rows are long work).
+__host__ __device__ inline int zero_tokens(int log_lanes) { return log_lanes == 6 ? 16 : 64; }
+template <bool PAST, class TT, int V> __device__ inline void zero_rows(const GradArgs &a, TT *__restrict__ dTable, int64_t block)
 {
-    const Columns col = lane_columns<V>(a);
-    const uint32_t block = first_block + blockIdx.x;
-    if (block < chunk_blocks) { // pieces of long tokens, a wavefront per chunk
-        const int64_t chunk = (int64_t)block * (THREADS / 64) + threadIdx.x / 64;
-        const int32_t valid = place(a, a.vocab);
-        if (chunk >= a.chunks || chunk * CHUNK >= valid) return;
-        const int32_t p0 = (int32_t)chunk * CHUNK, p1 = valid - p0 < CHUNK ? valid : p0 + CHUNK;
-        const int64_t head = token_at(a, p0), tail = token_at(a, p1 - 1);
-        const int lanes = 1 << a.log_lanes, sub = (threadIdx.x & 63) >> a.log_lanes, subs = 64 >> a.log_lanes;
-        for (int which = 0; which < 2; ++which) {
-            const int64_t t = which ? tail : head;
-            if (which && tail == head) break;
-            const int32_t s = max(place(a, t), p0), e = min(place(a, t + 1), p1);
-            if ((int64_t)place(a, t + 1) - place(a, t) <= CHUNK || e <= s) continue;
-            float acc[V] = {};
-            add_rows<TR, V>(a, dOut, col.at, (uint32_t)s + sub, (uint32_t)e, subs, acc);
-            for (int step = lanes; step < 64; step <<= 1) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) acc[j] += __shfl_xor(acc[j], step, 64);
-            }
-            if (sub == 0 && col.on) store_vec<float, V>(a.pieces + (2 * chunk + which) * a.width + col.at, acc);
-        }
+    const int tokens = zero_tokens(a.log_lanes), lane = threadIdx.x & 63, sub = lane >> a.log_lanes, subs = 64 >> a.log_lanes;
+    const int64_t t0 = (block * (THREADS / 64) + threadIdx.x / 64) * tokens, t = t0 + lane;
+    const uint64_t empty = __ballot(lane < tokens && t < a.vocab && a.starts[t < a.vocab ? t + 1 : 0] <= a.starts[t < a.vocab ? t : 0]);
+    const float zero[V] = {};
+    for (int i = sub; i < tokens; i += subs) {
+        if (!(empty >> i & 1)) continue;
+        TT *row = dTable + (t0 + i) * a.ldt;
+        for (int32_t c = (lane & ((1 << a.log_lanes) - 1)) * V; c < a.width; c += V << a.log_lanes)
+            store_result<PAST, TT, V>(row + min(c, a.width - V), zero);
+    }
+}
+
+template <class TR, class TT, int V, bool PAST>
+__global__ __launch_bounds__(THREADS) void embed_grad_kernel(const GradArgs a, const TR *__restrict__ dOut, TT *__restrict__ dTable, uint32_t first_block)
+{
+    __shared__ int2 list[THREADS / 8][CHUNK + 2 * AHEAD]; // token and row of every position of a group's chunk
+    const int lanes = 1 << a.log_lanes, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.log_lanes, len = 1 << a.log_chunk;
+    const uint32_t block = first_block + blockIdx.x, tile = block % a.tiles;
+    const Columns col = lane_columns<V>(a, tile);
+    const int64_t chunk = ((int64_t)(block / a.tiles) * THREADS >> a.log_lanes) + group;
+    const int32_t valid = place(a, a.vocab);
+    if (chunk >= a.chunks) return;
+    const int64_t p0l = chunk << a.log_chunk;
+    if (p0l >= valid) {
+        if (lane == 0 && tile == 0 && a.chunks > 1) a.tails[chunk] = -1;
         return;
     }
-    const int64_t t = ((int64_t)(block - chunk_blocks) * THREADS + threadIdx.x) >> a.log_lanes;
-    if (t >= a.vocab || !col.on) return;
-    const int32_t s = place(a, t), e = place(a, t + 1);
-    if ((int64_t)e - s > CHUNK || (a.accumulate && e <= s)) return;
+    const int32_t p0 = (int32_t)p0l, count = min(valid - p0, len);
+    uint32_t head, tail;
+    tokens_at(a, p0, p0 + count - 1, &head, &tail);
+    for (int i = lane; i < len + 2 * AHEAD; i += lanes) {
+        int2 e = make_int2(-1, -1);
+        if (i < count) {
+            e.y = a.order[p0 + i];
+            if (e.y >= a.n) e.y = -1;
+            uint32_t lo = head, hi = max(head, tail) + 1;
+            while (hi - lo > 1) {
+                const uint32_t mid = lo + (hi - lo) / 2;
+                const bool right = a.starts[mid] <= p0 + i;
+                lo = right ? mid : lo;
+                hi = right ? hi : mid;
+            }
+            e.x = (int32_t)lo;
+        }
+        list[group][i] = e;
+    }
+    const bool starts_before = place(a, head) < p0, goes_on = (int64_t)place(a, (int64_t)tail + 1) > (int64_t)p0 + count;
+    wave_fence();
+    int32_t now = (int32_t)head;
+    bool first = starts_before; // the token `now` started before the chunk
     float acc[V] = {};
-    if (e > s) add_rows<TR, V>(a, dOut, col.at, (uint32_t)s, (uint32_t)e, 1, acc);
+    typename VecOf<TR, V>::type x[AHEAD];
+    int2 e[AHEAD];
+    auto request = [&](int b) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] *= a.scale;
-    store_sum<TT, V>(a, dTable, t, col, acc);
+        for (int i = 0; i < AHEAD; ++i) e[i] = list[group][b + i];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (e[i].y >= 0) {
+                x[i] = load_vec<TR, V>(dOut + e[i].y * a.ldo + col.at);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[i][j] = (TR)0.f;
+            }
+        }
+    };
+    request(0);
+    for (int b = 0; b < count; b += AHEAD) {
+        // Sums of tokens that end in this batch are set aside and stored once all of its rows are used and the next ones are requested: a store
+        // between uses of loads would have every later use wait for the store (loads and stores are counted together).
+        float done[AHEAD][V];
+        int32_t token[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const bool same = e[i].x == now || e[i].x < 0;
+            token[i] = same ? -1 : now;
+            now = same ? now : e[i].x;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                done[i][j] = acc[j];
+                acc[j] = (same ? acc[j] : 0.f) + (float)x[i][j];
+            }
+        }
+        if (b + AHEAD < count) request(b + AHEAD);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (token[i] < 0) continue;
+            if (first) {
+                if (col.on) store_vec<float, V>(a.pieces + 2 * chunk * a.width + col.at, done[i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) done[i][j] *= a.scale;
+                store_sum<PAST, TT, V>(a, dTable, token[i], col, done[i]);
+            }
+            first = false;
+        }
+    }
+    if (first || goes_on) {
+        if (col.on) store_vec<float, V>(a.pieces + (2 * chunk + (first ? 0 : 1)) * a.width + col.at, acc);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] *= a.scale;
+        store_sum<PAST, TT, V>(a, dTable, now, col, acc);
+    }
+    if (lane == 0 && tile == 0 && a.chunks > 1) a.tails[chunk] = goes_on && !first ? now : -1;
 }
 
-// The pieces of the long token that starts in this workgroup's chunk, if there is one
-template <class TT, int V>
-__global__ __launch_bounds__(THREADS) void embed_join_kernel(const GradArgs a, TT *__restrict__ dTable, uint32_t first_block)
+// Tokens that several chunks share: the pieces are added where the token starts.  A wavefront takes a chunk; what has many pieces is
+// added by the whole workgroup.
+constexpr int JOIN_CHUNKS = THREADS / 64, JOIN_MANY = 64;
+template <class TT, int V, bool PAST>
+__global__ __launch_bounds__(THREADS) void embed_join_kernel(const GradArgs a, TT *__restrict__ dTable, uint32_t first_block, uint32_t join_blocks)
 {
-    __shared__ double sums[THREADS][V];
-    const Columns col = lane_columns<V>(a);
-    const int64_t chunk = (int64_t)first_block + blockIdx.x;
-    const int32_t valid = place(a, a.vocab);
-    if (chunk * CHUNK >= valid) return;
-    const int32_t p0 = (int32_t)chunk * CHUNK, p1 = valid - p0 < CHUNK ? valid : p0 + CHUNK;
-    const int64_t t = token_at(a, p1 - 1); // a long token that starts in the chunk holds its last place
-    const int32_t s = place(a, t), e = place(a, t + 1);
-    if (s < p0 || (int64_t)e - s <= CHUNK) return; // the same for the whole workgroup
-    const int64_t last = (e - 1) / CHUNK;
-    const int lanes = 1 << a.log_lanes, sub = threadIdx.x >> a.log_lanes, subs = THREADS >> a.log_lanes;
-    double acc[V] = {};
-    for (int64_t c = chunk + sub; c <= last; c += subs) {
-        const int64_t slot = 2 * c + (c == chunk && s > p0);
-        const auto x = load_vec<float, V>(a.pieces + slot * a.width + col.at);
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] += (double)x[j];
+    __shared__ double sums[THREADS / 64][64][V];
+    const int wave = threadIdx.x / 64, sub = (threadIdx.x & 63) >> a.log_lanes, subs = 64 >> a.log_lanes, lanes = 1 << a.log_lanes;
+    const uint32_t block = first_block + blockIdx.x;
+    if (block >= join_blocks) {
+        zero_rows<PAST, TT, V>(a, dTable, block - join_blocks);
+        return;
     }
+    const int64_t chunk0 = (int64_t)(block / a.tiles) * JOIN_CHUNKS;
+    const Columns col = lane_columns<V>(a, block % a.tiles);
+    // the sum over every step-th piece of the token that starts in chunk c, from the first-th on; then over the lanes of a wavefront
+    auto add = [&](int64_t c, int64_t last, int64_t first, int64_t step, double (&acc)[V]) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) sums[threadIdx.x][j] = acc[j];
-    __syncthreads();
-    if (sub != 0 || !col.on) return;
-    float out[V];
+        for (int j = 0; j < V; ++j) acc[j] = 0.0;
+#pragma unroll 4
+        for (int64_t k = c + first; k <= last; k += step) {
+            const auto x = load_vec<float, V>(a.pieces + (2 * k + (k == c)) * a.width + col.at);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        double total = 0.0;
-        for (int i = 0; i < subs; ++i) total += sums[threadIdx.x + i * lanes][j];
-        out[j] = (float)((double)a.scale * total);
+            for (int j = 0; j < V; ++j) acc[j] += (double)x[j];
+        }
+        for (int s = lanes; s < 64; s <<= 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] += __shfl_xor(acc[j], s, 64);
+        }
+    };
+    auto store = [&](int64_t t, const double (&acc)[V]) {
+        float out[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) out[j] = (float)((double)a.scale * acc[j]);
+        store_sum<PAST, TT, V>(a, dTable, t, col, out);
+    };
+    auto token = [&](int64_t c) { return c < a.chunks ? a.tails[c] : -1; };
+    auto last_chunk = [&](int32_t t) { return (int64_t)(place(a, (int64_t)t + 1) - 1) >> a.log_chunk; };
+    int32_t t[JOIN_CHUNKS];
+    int64_t last[JOIN_CHUNKS];
+#pragma unroll
+    for (int w = 0; w < JOIN_CHUNKS; ++w) t[w] = token(chunk0 + w);
+#pragma unroll
+    for (int w = 0; w < JOIN_CHUNKS; ++w) last[w] = t[w] >= 0 ? last_chunk(t[w]) : -1;
+#pragma unroll
+    for (int w = 0; w < JOIN_CHUNKS; ++w) {
+        const int64_t c = chunk0 + w, pieces = last[w] - c + 1;
+        if (t[w] < 0) continue;
+        double acc[V];
+        if (pieces <= JOIN_MANY) {
+            if (wave != w) continue;
+            add(c, last[w], sub, subs, acc);
+            if (sub == 0) store(t[w], acc);
+        } else { // the same for the whole workgroup
+            add(c, last[w], wave * subs + sub, JOIN_CHUNKS * subs, acc);
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < V; ++j) sums[wave][threadIdx.x & 63][j] = acc[j];
+            __syncthreads();
+            if (wave == 0 && sub == 0) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[j] = ((sums[0][threadIdx.x][j] + sums[1][threadIdx.x][j]) + sums[2][threadIdx.x][j]) + sums[3][threadIdx.x][j];
+                store(t[w], acc);
+            }
+        }
     }
-    store_sum<TT, V>(a, dTable, t, col, out);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------------
@@ -538,6 +660,31 @@ int log_lanes_for(int32_t accesses)
     return l;
 }
 
+// How the gradient is cut: accesses of a row over lanes (and tiles of lanes), positions over chunks.
+struct GradPlan {
+    int log_lanes, log_chunk;
+    int64_t chunks;
+    int32_t tiles;
+    GradPlan(int64_t n, int32_t width, int v)
+    {
+        const int32_t accesses = (width + v - 1) / v;
+        log_lanes = log_lanes_for(accesses);
+        tiles = (accesses + (1 << log_lanes) - 1) >> log_lanes;
+        // as many wavefronts as keep the chip busy before chunks get longer: a longer chunk leaves fewer pieces
+        log_chunk = 3;
+        while (log_chunk < log_lanes + 1 && (1 << log_chunk) < CHUNK && (n * tiles << log_lanes >> (log_chunk + 1)) >= 64 * 2048) ++log_chunk;
+        chunks = (n + (1 << log_chunk) - 1) >> log_chunk;
+    }
+    size_t piece_bytes(int32_t width) const { return (size_t)round_up(2 * chunks * (int64_t)width * 4, 256); }
+    size_t bytes(int32_t width) const { return chunks <= 1 ? 0 : piece_bytes(width) + (size_t)round_up(4 * chunks, 256); }
+};
+
+int grad_access(int32_t width, int32_t row_type)
+{
+    const int v = 16 / type_bytes(row_type);
+    return width < v ? 1 : v;
+}
+
 struct SortPlan {
     int bits, passes; // per digit
     int64_t tiles;
@@ -580,14 +727,14 @@ extern "C" int slicegcn_embed_fwd(const slicegcn_embed_desc *d, const void *ids,
             const int64_t tiles = ((int64_t)d->width + tile - 1) / tile;
             SG_REQUIRE(tiles < 65536, SLICEGCN_ERANGE, "embed_fwd: width = %d too large", d->width);
             const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), (unsigned)tiles);
-            if (d->flags & SLICEGCN_EMBED_IDS64)
-                lookup_kernel<int64_t, TT, TR, V><<<grid, THREADS, 0, as_stream(stream)>>>(
-                    static_cast<const int64_t *>(ids), d->n, d->vocab, d->pad, has_pad, static_cast<const TT *>(table), ldt, d->width,
-                    (float)d->scale, static_cast<TR *>(out), ldo, log_lanes, tile);
-            else
-                lookup_kernel<int32_t, TT, TR, V><<<grid, THREADS, 0, as_stream(stream)>>>(
-                    static_cast<const int32_t *>(ids), d->n, d->vocab, d->pad, has_pad, static_cast<const TT *>(table), ldt, d->width,
-                    (float)d->scale, static_cast<TR *>(out), ldo, log_lanes, tile);
+            with_flag(past_cache(d->n, ldo, d->row_type), [&](auto past) {
+                with_flag(d->flags & SLICEGCN_EMBED_IDS64, [&](auto wide) {
+                    using ID = std::conditional_t<decltype(wide)::value, int64_t, int32_t>;
+                    lookup_kernel<ID, TT, TR, V, decltype(past)::value><<<grid, THREADS, 0, as_stream(stream)>>>(
+                        static_cast<const ID *>(ids), d->n, d->vocab, d->pad, has_pad, static_cast<const TT *>(table), ldt, d->width,
+                        (float)d->scale, static_cast<TR *>(out), ldo, log_lanes, tile);
+                });
+            });
             SG_LAUNCH_CHECK();
             return (int)SLICEGCN_OK;
         };
@@ -631,9 +778,14 @@ extern "C" int slicegcn_embed_sort(const slicegcn_embed_desc *d, const void *ids
         const int shift = p * plan.bits;
         digit_count_kernel<<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, shift, plan.bits, hist);
         SG_LAUNCH_CHECK();
-        digit_scan_kernel<<<(unsigned)(((1 << plan.bits) + 63) / 64), 1024, 0, s>>>(hist, plan.tiles, plan.bits, total);
-        SG_LAUNCH_CHECK();
-        digit_scatter_kernel<<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, total, out_keys, out_from);
+        if (plan.tiles <= FEW_TILES) {
+            digit_scatter_kernel<true><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, nullptr, (int)plan.tiles,
+                                                                                    out_keys, out_from);
+        } else {
+            digit_scan_kernel<<<(unsigned)(((1 << plan.bits) + 63) / 64), 1024, 0, s>>>(hist, plan.tiles, plan.bits, total);
+            SG_LAUNCH_CHECK();
+            digit_scatter_kernel<false><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, total, 0, out_keys, out_from);
+        }
         SG_LAUNCH_CHECK();
         in_keys = out_keys;
         in_from = out_from;
@@ -646,8 +798,9 @@ extern "C" int slicegcn_embed_sort(const slicegcn_embed_desc *d, const void *ids
 
 extern "C" size_t slicegcn_embed_bwd_workspace_bytes(int64_t n, int32_t width)
 {
-    if (n <= CHUNK || n > INT32_MAX || width < 1) return 0; // no token can have more than CHUNK positions
-    return (size_t)round_up(2 * ((n + CHUNK - 1) / CHUNK) * (int64_t)width * 4, 256);
+    if (n < 1 || n > INT32_MAX || width < 1) return 0;
+    const size_t a = GradPlan(n, width, grad_access(width, SLICEGCN_F32)).bytes(width), b = GradPlan(n, width, grad_access(width, SLICEGCN_BF16)).bytes(width);
+    return a > b ? a : b;
 }
 
 extern "C" int slicegcn_embed_bwd(const slicegcn_embed_desc *d, const int32_t *order, const int32_t *starts, const void *dOut, int64_t ldo,
@@ -667,25 +820,26 @@ extern "C" int slicegcn_embed_bwd(const slicegcn_embed_desc *d, const int32_t *o
         using TR = decltype(r);
         auto launch = [&](auto access) {
             constexpr int V = decltype(access)::value;
-            const int32_t accesses = (d->width + V - 1) / V;
+            const GradPlan plan(d->n, d->width, V);
             GradArgs a{order, starts, d->n, d->vocab, ldo, ldt, d->width, (float)d->scale, (d->flags & SLICEGCN_EMBED_ACCUMULATE) != 0,
-                       log_lanes_for(accesses), d->n > CHUNK ? (d->n + CHUNK - 1) / CHUNK : 0, static_cast<float *>(ws)};
-            const unsigned tiles = (unsigned)((accesses + (1 << a.log_lanes) - 1) >> a.log_lanes);
-            const uint32_t chunk_blocks = (uint32_t)((a.chunks + THREADS / 64 - 1) / (THREADS / 64));
-            const int64_t groups = THREADS >> a.log_lanes, blocks = chunk_blocks + (d->vocab + groups - 1) / groups;
-            SG_REQUIRE(tiles < 65536, SLICEGCN_ERANGE, "embed_bwd: width = %d too large", d->width);
-            if (int rc = launch_parts(blocks, [&](unsigned first, unsigned count) {
-                    embed_grad_kernel<TR, TT, V><<<dim3(count, tiles), THREADS, 0, as_stream(stream)>>>(
-                        a, static_cast<const TR *>(dOut), static_cast<TT *>(dTable), first, chunk_blocks);
-                }))
-                return rc;
-            if (a.chunks) {
-                if (int rc = launch_parts(a.chunks, [&](unsigned first, unsigned count) {
-                        embed_join_kernel<TT, V><<<dim3(count, tiles), THREADS, 0, as_stream(stream)>>>(a, static_cast<TT *>(dTable), first);
+                       plan.log_lanes, plan.log_chunk, (uint32_t)plan.tiles, plan.chunks, static_cast<float *>(ws),
+                       reinterpret_cast<int32_t *>(static_cast<char *>(ws) + plan.piece_bytes(d->width))};
+            const int64_t groups = THREADS >> a.log_lanes;
+            const int64_t chunk_blocks = (a.chunks + groups - 1) / groups * plan.tiles, per_block = (int64_t)zero_tokens(a.log_lanes) * (THREADS / 64);
+            const int64_t join_blocks = a.chunks > 1 ? (a.chunks + JOIN_CHUNKS - 1) / JOIN_CHUNKS * plan.tiles : 0;
+            const int64_t zero_blocks = a.accumulate ? 0 : (d->vocab + per_block - 1) / per_block;
+            SG_REQUIRE(chunk_blocks < ((int64_t)1 << 31) && join_blocks + zero_blocks < ((int64_t)1 << 31), SLICEGCN_ERANGE,
+                       "embed_bwd: %lld rows of %d columns are too many for a call", (long long)d->n, d->width);
+            return with_flag(past_cache(d->vocab, ldt, d->table_type), [&](auto past) {
+                constexpr bool PAST = decltype(past)::value;
+                if (int rc = launch_parts(chunk_blocks, [&](unsigned first, unsigned count) {
+                        embed_grad_kernel<TR, TT, V, PAST><<<count, THREADS, 0, as_stream(stream)>>>(a, static_cast<const TR *>(dOut), static_cast<TT *>(dTable), first);
                     }))
                     return rc;
-            }
-            return (int)SLICEGCN_OK;
+                return launch_parts(join_blocks + zero_blocks, [&](unsigned first, unsigned count) {
+                    embed_join_kernel<TT, V, PAST><<<count, THREADS, 0, as_stream(stream)>>>(a, static_cast<TT *>(dTable), first, (uint32_t)join_blocks);
+                });
+            });
         };
         constexpr int V = 16 / (int)sizeof(TR);
         if (d->width >= V) return launch(std::integral_constant<int, V>());

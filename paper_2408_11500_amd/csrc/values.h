@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "slicegcn_train.h"
 
@@ -16,6 +17,11 @@ inline int type_bytes(int32_t type) { return type == SLICEGCN_F32 ? 4 : 2; }
 inline bool known_type(int32_t type) { return type == SLICEGCN_F32 || type == SLICEGCN_BF16 || type == SLICEGCN_F16; }
 // every element on a boundary of its size: accesses of 16 bytes start at any such boundary
 inline bool aligned_for(const void *p, int32_t type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
+
+// Whether rows are stored past the caches: where they exceed the last-level cache (256 MB).  A lookup of 128-wide fp32 rows alone / with a
+// pass that reads its output, through / past the caches: 64 MB 20.8 / 20.5 and 40.5 / 42.6 us, 192 MB 57.7 / 56.1 and 129.7 / 131.7, 256 MB
+// 74.8 / 73.6 and 176.7 / 170.6, 1 GB 304 / 288 and 665 / 648; 2.4 M rows of 100 columns that lie 128 apart (lines written in part) 397 / 292 alone.
+inline bool past_cache(int64_t rows, int64_t ld, int32_t type) { return rows * ld * type_bytes(type) >= (int64_t)256 << 20; }
 
 // V elements that one access moves (16 bytes at most), at any element boundary
 template <class T, int V> struct VecOf {
@@ -38,6 +44,26 @@ template <class T, int V> __device__ inline void store_vec(T *p, const float (&v
 #pragma unroll
     for (int i = 0; i < V; ++i) r[i] = (T)v[i]; // to nearest, ties to even: the one rounding of a result
     *reinterpret_cast<typename VecOf<T, V>::packed *>(p) = r;
+}
+
+// The same past the caches, for results too large to be found there by whoever reads them next: see past_cache.  (Which of the two is a
+// template argument: of a branch between them the compiler makes one plain store.)
+template <class T, int V> __device__ inline void store_vec_past_cache(T *p, const float (&v)[V])
+{
+    if constexpr (V == 1) {
+        store_vec<T, V>(p, v);
+    } else {
+        typename VecOf<T, V>::type r;
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = (T)v[i];
+        __builtin_nontemporal_store(r, reinterpret_cast<typename VecOf<T, V>::packed *>(p));
+    }
+}
+
+template <bool PAST, class T, int V> __device__ inline void store_result(T *p, const float (&v)[V])
+{
+    if constexpr (PAST) store_vec_past_cache<T, V>(p, v);
+    else store_vec<T, V>(p, v);
 }
 
 template <int CTRL> __device__ inline float dpp(float v)
@@ -63,6 +89,9 @@ __device__ inline float group_sum(float v, int lanes)
     }
     return v;
 }
+
+// Calls f with std::true_type or std::false_type
+template <class F> inline auto with_flag(bool flag, F f) { return flag ? f(std::true_type()) : f(std::false_type()); }
 
 // Calls f with a value of the element type `type`
 template <class F> inline auto with_type(int32_t type, F f)
