@@ -1,0 +1,433 @@
+// Norms before and after a block, fused with the block's gate and the residual, forward and backward.
+//
+//   p = post(y) * post_w + post_b;   h = residual * x + s * p;   u = pre(h) * pre_w + pre_b
+//
+// With yn, hn the normalised rows, ry, rh the factors 1 / sqrt(...) they were multiplied by, and means over a row's columns:
+//   dun = du * pre_w;    dH = dh + rh * (dun - [mean dun] - hn * mean(dun * hn))          [..]: layer norm only
+//   dx = residual * dH;  dgate = dH * p (times s (1 - s) through a sigmoid)
+//   dyn = dH * s * post_w;  dy = ry * (dyn - [mean dyn] - yn * mean(dyn * yn))
+//   dpre_w = sum du * hn;  dpre_b = sum du;  dpost_w = sum dH * s * yn;  dpost_b = sum dH * s     (sums over rows)
+// A gate per column has dgate = post_w * sum dH * yn + post_b * sum dH, so that two sums per norm serve all parameters.
+//
+// A row lies in the registers of a group of lanes from its one read to its one write, and h is formed again in the backward pass instead of
+// being read: bound by bytes.
+#pragma once
+
+#include "resnorm.h"
+
+namespace slicegcn {
+namespace resnorm {
+
+namespace {
+
+template <int V> struct Lane { // K accesses of V columns; the last access of a row that is no multiple of V wide is moved left
+    int32_t col;
+    int skip; // leading columns that the access before it holds too
+    bool on;
+};
+
+template <class T, int V, int K> struct Raw { typename VecOf<T, V>::type v[K]; }; // a lane's part of a row, as it lies in memory
+
+template <class T, int V, int K, bool MULTI, bool FULL> struct Row {
+    const Args &a;
+    float *shared; // MULTI: [2][16][2]
+    int lane, slot; // lane within the row, row within the workgroup
+    int turn = 0;
+    Lane<V> at[K];
+
+    __device__ Row(const Args &args, float *sh) : a(args), shared(sh)
+    {
+        lane = threadIdx.x & (a.lanes - 1);
+        slot = threadIdx.x / a.lanes;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int32_t c = (lane + k * a.lanes) * V;
+            at[k].on = FULL || c < a.width;
+            at[k].col = FULL ? c : min(c, a.width - V);
+            at[k].skip = FULL ? 0 : c - at[k].col;
+        }
+    }
+
+    // sum of the lane's columns; f(k, j) is the summand
+    template <class F> __device__ float lane_sum(F f) const
+    {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (!at[k].on) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float v = f(k, j);
+                s += FULL || j >= at[k].skip ? v : 0.f;
+            }
+        }
+        return s;
+    }
+
+    // N sums over the row's lanes, in every lane
+    template <int N> __device__ void over_lanes(float (&s)[N])
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = group_sum(s[i], MULTI ? 64 : a.lanes);
+        if (!MULTI) return;
+        float *buf = shared + turn * 32; // written again two sums later, when every wavefront has read it
+        turn ^= 1;
+        const int wave = threadIdx.x / 64, waves = a.lanes / 64, first = slot * waves;
+        if (threadIdx.x % 64 == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) buf[2 * wave + i] = s[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = 0.f;
+        for (int w = 0; w < waves; ++w) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[i] += buf[2 * (first + w) + i];
+        }
+    }
+
+    __device__ Raw<T, V, K> load(const RowPtr &p, int64_t row, bool there) const
+    {
+        Raw<T, V, K> r;
+        const T *q = reinterpret_cast<const T *>(p.data) + row * p.ld;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (there && at[k].on) {
+                r.v[k] = load_vec<T, V>(q + at[k].col);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) r.v[k][j] = (T)0.f;
+            }
+        }
+        return r;
+    }
+
+    __device__ void store(const RowPtr &p, int64_t row, const float (&v)[K][V]) const
+    {
+        T *q = reinterpret_cast<T *>(p.data) + row * p.ld;
+        if (a.past_cache) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (at[k].on) store_vec_past_cache<T, V>(q + at[k].col, v[k]);
+            asm volatile(""); // keeps the two kinds of stores apart: made into one they would be plain ones
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (at[k].on) store_vec<T, V>(q + at[k].col, v[k]);
+        }
+    }
+
+    // the lane's columns of a parameter, or `absent`
+    __device__ void param(const float *p, float absent, float (&v)[K][V]) const
+    {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (p) {
+                const auto w = load_vec<float, V>(p + at[k].col);
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[k][j] = w[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[k][j] = absent;
+            }
+        }
+    }
+
+    template <class F> __device__ void each(F f) const
+    {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) f(k, j);
+    }
+
+    // mean and 1 / sqrt(...) of a row
+    __device__ void moments(const float (&v)[K][V], int kind, float *mean, float *factor)
+    {
+        float s[1];
+        *mean = 0.f;
+        if (kind == LAYER) {
+            s[0] = lane_sum([&](int k, int j) { return v[k][j]; });
+            over_lanes(s);
+            *mean = s[0] * a.inv_width;
+        }
+        const float m = *mean;
+        s[0] = lane_sum([&](int k, int j) { const float d = v[k][j] - m; return d * d; });
+        over_lanes(s);
+        *factor = 1.f / sqrtf(s[0] * a.inv_width + a.eps);
+    }
+
+    // s, the factor of p, from a gate
+    __device__ float opened(float g) const { return a.sigmoid ? 1.f / (1.f + expf(-g)) : g; }
+};
+
+// Parameters of the lane's columns, held over all rows.  With a gate per column (or none) s * p is one product: yn * (s * post_w) + s * post_b.
+// A workgroup of 1024 threads has registers for one row only: there the parameters are read again for every row, from the caches.
+template <int V, int K> struct Held {
+    float w[K][V], b[K][V], pre_w[K][V], pre_b[K][V];
+    template <bool MATRIX, bool FWD, class R> __device__ void load(const R &r, const Args &a)
+    {
+        r.param(a.post_w, 1.f, w);
+        r.param(a.post_b, 0.f, b);
+        r.param(a.pre_w, 1.f, pre_w);
+        if (FWD) r.param(a.pre_b, 0.f, pre_b);
+        if (!MATRIX && a.gate_col) {
+            float g[K][V];
+            r.param(a.gate_col, 1.f, g);
+            r.each([&](int k, int j) {
+                const float s = r.opened(g[k][j]);
+                w[k][j] *= s;
+                b[k][j] *= s;
+            });
+        }
+    }
+};
+
+// EXTRA: a layer norm or a bias anywhere
+template <class T, int V, int K, bool MULTI, bool FULL, int THREADS, bool MATRIX, bool EXTRA>
+__global__ __launch_bounds__(THREADS) void resnorm_fwd_kernel(const Args a)
+{
+    __shared__ float shared[MULTI ? 64 : 1];
+    Row<T, V, K, MULTI, FULL> r(a, shared);
+    constexpr bool HOLD = THREADS < 1024;
+    Held<V, K> p;
+    if (HOLD) p.template load<MATRIX, true>(r, a);
+    const int rows = THREADS / a.lanes;
+    for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < a.n; r0 += (int64_t)gridDim.x * rows) {
+        const int64_t row = r0 + r.slot;
+        const bool there = row < a.n;
+        float h[K][V], st[4] = {0.f, 1.f, 0.f, 1.f};
+        Raw<T, V, K> x, y, g;
+        if (a.x.data) x = r.load(a.x, row, there);
+        if (a.y.data) y = r.load(a.y, row, there);
+        if (MATRIX) g = r.load(a.gate, row, there);
+        if (!HOLD) p.template load<MATRIX, true>(r, a);
+        if (a.x.data) r.each([&](int k, int j) { h[k][j] = a.residual * (float)x.v[k][j]; });
+        else r.each([&](int k, int j) { h[k][j] = 0.f; });
+        if (a.y.data) {
+            float v[K][V];
+            r.each([&](int k, int j) { v[k][j] = (float)y.v[k][j]; });
+            if (a.post != NONE) {
+                r.moments(v, a.post, &st[0], &st[1]);
+                r.each([&](int k, int j) { v[k][j] = EXTRA ? (v[k][j] - st[0]) * st[1] : v[k][j] * st[1]; });
+            }
+            r.each([&](int k, int j) {
+                if (MATRIX) {
+                    const float q = EXTRA ? fmaf(v[k][j], p.w[k][j], p.b[k][j]) : v[k][j] * p.w[k][j];
+                    h[k][j] = fmaf(r.opened((float)g.v[k][j]), q, h[k][j]);
+                } else {
+                    if (EXTRA) h[k][j] += p.b[k][j];
+                    h[k][j] = fmaf(v[k][j], p.w[k][j], h[k][j]);
+                }
+            });
+        }
+        // rows in place: all of a row is read before any of it is written (a sum over the row sees to that too)
+        if (MULTI && !FULL && !(a.y.data && a.post != NONE)) __syncthreads();
+        if (a.h.data && there) r.store(a.h, row, h);
+        if (a.u.data) {
+            if (a.pre != NONE) {
+                r.moments(h, a.pre, &st[2], &st[3]);
+                r.each([&](int k, int j) {
+                    h[k][j] = EXTRA ? fmaf((h[k][j] - st[2]) * st[3], p.pre_w[k][j], p.pre_b[k][j]) : h[k][j] * st[3] * p.pre_w[k][j];
+                });
+            }
+            if (there) r.store(a.u, row, h);
+        }
+        if (a.stats && there && r.lane == 0) *reinterpret_cast<float4 *>(a.stats + 4 * row) = make_float4(st[0], st[1], st[2], st[3]);
+    }
+}
+
+// The rows that the backward pass reads of one row: requested a row ahead
+template <class T, int V, int K> struct Operands {
+    Raw<T, V, K> x, y, g, dh, du;
+    float4 st;
+    template <bool MATRIX, class R> __device__ void request(const R &r, const Args &a, int64_t row, bool there)
+    {
+        if (a.x.data) x = r.load(a.x, row, there);
+        if (a.y.data) y = r.load(a.y, row, there);
+        if (MATRIX) g = r.load(a.gate, row, there);
+        if (a.dh.data) dh = r.load(a.dh, row, there);
+        if (a.du.data) du = r.load(a.du, row, there);
+        st = there ? *reinterpret_cast<const float4 *>(a.stats + 4 * row) : make_float4(0.f, 1.f, 0.f, 1.f);
+    }
+};
+
+template <class T, int V, int K, bool MULTI, bool FULL, int THREADS, bool MATRIX, bool EXTRA>
+__global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
+{
+    __shared__ float shared[MULTI ? 64 : 1];
+    __shared__ float sums[THREADS <= 256 ? SUM_COLS : 1];
+    Row<T, V, K, MULTI, FULL> r(a, shared);
+    constexpr bool HOLD = THREADS < 1024;
+    Held<V, K> p;
+    if (HOLD) p.template load<MATRIX, false>(r, a);
+    const int rows = THREADS / a.lanes;
+    const int64_t stride = (int64_t)gridDim.x * rows;
+    float acc[PLANES][K][V] = {};
+    Operands<T, V, K> next;
+    if (HOLD && (int64_t)blockIdx.x * rows < a.n) next.template request<MATRIX>(r, a, (int64_t)blockIdx.x * rows + r.slot, (int64_t)blockIdx.x * rows + r.slot < a.n);
+    for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < a.n; r0 += stride) {
+        const int64_t row = r0 + r.slot;
+        const bool there = row < a.n;
+        if (!HOLD) {
+            next.template request<MATRIX>(r, a, row, there);
+            p.template load<MATRIX, false>(r, a);
+        }
+        const Operands<T, V, K> o = next;
+        if (HOLD && r0 + stride < a.n) next.template request<MATRIX>(r, a, row + stride, row + stride < a.n);
+        float h[K][V], yn[K][V], dH[K][V], q[K][V], s[K][V];
+        if (a.x.data) r.each([&](int k, int j) { h[k][j] = a.residual * (float)o.x.v[k][j]; });
+        else r.each([&](int k, int j) { h[k][j] = 0.f; });
+        if (a.y.data) { // h again, from what it was formed of
+            r.each([&](int k, int j) {
+                yn[k][j] = EXTRA ? ((float)o.y.v[k][j] - o.st.x) * o.st.y : (float)o.y.v[k][j] * o.st.y;
+                if (MATRIX) {
+                    s[k][j] = r.opened((float)o.g.v[k][j]);
+                    q[k][j] = EXTRA ? fmaf(yn[k][j], p.w[k][j], p.b[k][j]) : yn[k][j] * p.w[k][j];
+                    h[k][j] = fmaf(s[k][j], q[k][j], h[k][j]);
+                } else {
+                    if (EXTRA) h[k][j] += p.b[k][j];
+                    h[k][j] = fmaf(yn[k][j], p.w[k][j], h[k][j]);
+                }
+            });
+        }
+        if (a.dh.data) r.each([&](int k, int j) { dH[k][j] = (float)o.dh.v[k][j]; });
+        else r.each([&](int k, int j) { dH[k][j] = 0.f; });
+        if (a.du.data) {
+            if (a.pre == NONE) {
+                r.each([&](int k, int j) { dH[k][j] += (float)o.du.v[k][j]; });
+            } else {
+                float d[K][V];
+                r.each([&](int k, int j) { h[k][j] = EXTRA ? (h[k][j] - o.st.z) * o.st.w : h[k][j] * o.st.w; }); // hn
+                if (a.planes & 1) r.each([&](int k, int j) { acc[0][k][j] = fmaf((float)o.du.v[k][j], h[k][j], acc[0][k][j]); });
+                if (EXTRA && (a.planes & 2)) r.each([&](int k, int j) { acc[1][k][j] += (float)o.du.v[k][j]; });
+                r.each([&](int k, int j) { d[k][j] = (float)o.du.v[k][j] * p.pre_w[k][j]; });
+                float c[2] = {r.lane_sum([&](int k, int j) { return d[k][j] * h[k][j]; }), 0.f};
+                if (EXTRA && a.pre == LAYER) {
+                    c[1] = r.lane_sum([&](int k, int j) { return d[k][j]; });
+                    r.over_lanes(c);
+                } else {
+                    float one[1] = {c[0]};
+                    r.over_lanes(one);
+                    c[0] = one[0];
+                }
+                c[0] *= a.inv_width;
+                c[1] *= a.inv_width;
+                r.each([&](int k, int j) { dH[k][j] = fmaf(o.st.w, fmaf(-h[k][j], c[0], EXTRA ? d[k][j] - c[1] : d[k][j]), dH[k][j]); });
+            }
+        }
+        if (MULTI && !FULL && !(a.du.data && a.pre != NONE)) __syncthreads(); // rows in place, as in the forward pass
+        if (a.dx.data && there) {
+            r.each([&](int k, int j) { h[k][j] = a.residual * dH[k][j]; });
+            r.store(a.dx, row, h);
+        }
+        if (!a.y.data) continue;
+        if (MATRIX) {
+            if (a.dgate.data && there) {
+                r.each([&](int k, int j) { q[k][j] *= a.sigmoid ? dH[k][j] * (s[k][j] * (1.f - s[k][j])) : dH[k][j]; });
+                r.store(a.dgate, row, q);
+            }
+            r.each([&](int k, int j) { dH[k][j] *= s[k][j]; });
+        }
+        if (a.planes & 4) r.each([&](int k, int j) { acc[2][k][j] = fmaf(dH[k][j], yn[k][j], acc[2][k][j]); });
+        if (EXTRA && (a.planes & 8)) r.each([&](int k, int j) { acc[3][k][j] += dH[k][j]; });
+        if (!a.dy.data) continue;
+        r.each([&](int k, int j) { dH[k][j] *= p.w[k][j]; });
+        if (a.post != NONE) {
+            float d[2] = {r.lane_sum([&](int k, int j) { return dH[k][j] * yn[k][j]; }), 0.f};
+            if (EXTRA && a.post == LAYER) {
+                d[1] = r.lane_sum([&](int k, int j) { return dH[k][j]; });
+                r.over_lanes(d);
+            } else {
+                float one[1] = {d[0]};
+                r.over_lanes(one);
+                d[0] = one[0];
+            }
+            d[0] *= a.inv_width;
+            d[1] *= a.inv_width;
+            r.each([&](int k, int j) { dH[k][j] = o.st.y * fmaf(-yn[k][j], d[0], EXTRA ? dH[k][j] - d[1] : dH[k][j]); });
+        }
+        if (there) r.store(a.dy, row, dH);
+    }
+    if (!a.planes) return;
+    // the workgroup's sums: over the rows of a wavefront, then over wavefronts (or over the rows beside each other), in order
+    const int span = a.lanes < 64 ? 64 : a.lanes, part = threadIdx.x / span, parts = THREADS / span;
+    float *out = a.partial + (int64_t)blockIdx.x * PLANES * a.width;
+#pragma unroll
+    for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2) {
+        if (!(a.planes >> q & 1)) continue;
+        for (int step = a.lanes; step < 64; step <<= 1) r.each([&](int k, int j) { acc[q][k][j] += __shfl_xor(acc[q][k][j], step, 64); });
+        const bool mine = a.lanes >= 64 || (threadIdx.x & 63) < a.lanes;
+        if (parts > 1) {
+            for (int w = 0; w < parts; ++w) {
+                if (part == w && mine) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+#pragma unroll
+                        for (int j = 0; j < V; ++j)
+                            if (r.at[k].on && j >= r.at[k].skip) {
+                                float *to = sums + r.at[k].col + j;
+                                *to = w ? *to + acc[q][k][j] : acc[q][k][j];
+                            }
+                }
+                __syncthreads();
+            }
+            for (int c = threadIdx.x; c < a.width; c += THREADS) out[q * a.width + c] = sums[c];
+            __syncthreads();
+        } else if (mine) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (r.at[k].on) store_vec<float, V>(out + q * a.width + r.at[k].col, acc[q][k]);
+        }
+    }
+}
+
+template <bool BWD, class T, int V, int K, bool MULTI, bool FULL, int THREADS> void launch_kernel(const Args &a, int64_t blocks, hipStream_t s)
+{
+    with_flag(a.gate.data != nullptr, [&](auto matrix) {
+        with_flag(a.post == LAYER || a.pre == LAYER || a.post_b || a.pre_b, [&](auto extra) {
+            constexpr bool MATRIX = decltype(matrix)::value, EXTRA = decltype(extra)::value;
+            if constexpr (BWD) resnorm_bwd_kernel<T, V, K, MULTI, FULL, THREADS, MATRIX, EXTRA><<<(unsigned)blocks, THREADS, 0, s>>>(a);
+            else resnorm_fwd_kernel<T, V, K, MULTI, FULL, THREADS, MATRIX, EXTRA><<<(unsigned)blocks, THREADS, 0, s>>>(a);
+        });
+    });
+}
+
+template <bool BWD, class T, int V, int K> void launch_lanes(const Args &a, const Shape &s, int64_t blocks, hipStream_t stream)
+{
+    if constexpr (V == 1) { // rows narrower than an access
+        launch_kernel<BWD, T, V, K, false, false, 256>(a, blocks, stream);
+    } else if constexpr (K * V > ELEMS) { // the widest rows
+        launch_kernel<BWD, T, V, K, true, false, 1024>(a, blocks, stream);
+    } else if (s.lanes <= 64) {
+        if (s.full(a.width, V)) launch_kernel<BWD, T, V, K, false, true, 256>(a, blocks, stream);
+        else launch_kernel<BWD, T, V, K, false, false, 256>(a, blocks, stream);
+    } else if constexpr (2 * K * V > ELEMS) { // rows of fewer elements per lane take fewer lanes
+        if (s.lanes <= 256) launch_kernel<BWD, T, V, K, true, false, 256>(a, blocks, stream);
+        else if (s.lanes == 512) launch_kernel<BWD, T, V, K, true, false, 512>(a, blocks, stream);
+        else launch_kernel<BWD, T, V, K, true, false, 1024>(a, blocks, stream);
+    }
+}
+
+template <bool BWD, class T> void launch_type(const Args &a, const Shape &s, int64_t blocks, hipStream_t stream)
+{
+    constexpr int V = 16 / (int)sizeof(T);
+    if (a.width < V) return launch_lanes<BWD, T, 1, 1>(a, s, blocks, stream);
+    switch (s.accesses) {
+    case 1: return launch_lanes<BWD, T, V, 1>(a, s, blocks, stream);
+    case 2: return launch_lanes<BWD, T, V, 2>(a, s, blocks, stream);
+    default:
+        if constexpr (V == 4) {
+            if (s.accesses == 3) return launch_lanes<BWD, T, V, 3>(a, s, blocks, stream);
+            return launch_lanes<BWD, T, V, 4>(a, s, blocks, stream);
+        }
+    }
+}
+
+} // namespace
+
+template <class T> void launch_fwd(const Args &a, const Shape &s, int64_t blocks, hipStream_t stream) { launch_type<false, T>(a, s, blocks, stream); }
+template <class T> void launch_bwd(const Args &a, const Shape &s, int64_t blocks, hipStream_t stream) { launch_type<true, T>(a, s, blocks, stream); }
+
+} // namespace resnorm
+} // namespace slicegcn
