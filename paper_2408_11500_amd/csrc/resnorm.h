@@ -11,7 +11,6 @@ constexpr int NONE = SLICEGCN_NORM_NONE, LAYER = SLICEGCN_NORM_LAYER;
 constexpr int ELEMS = 8;              // elements of a row per lane, at most: the backward pass holds two rows' operands, parameters and sums
 constexpr int WIDE = 1024 * ELEMS;    // wider rows: twice as many
 constexpr int FWD_BLOCKS = 4096;      // workgroups of the forward pass, at most: parameters are read once per workgroup
-constexpr int SUM_COLS = 2048;        // widest row of which a workgroup holds several
 constexpr int PLANES = 4;             // sums over rows: du * hn, du, dH * s * yn, dH * s (without s where the gate is per column)
 
 struct RowPtr {

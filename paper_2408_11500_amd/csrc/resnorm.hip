@@ -49,11 +49,16 @@ __global__ __launch_bounds__(FINAL_THREADS) void resnorm_params_kernel(const Arg
 
 // ---- host -----------------------------------------------------------------------------------------------------------------
 
-// Workgroups of the backward pass: each leaves one set of sums.
-int64_t bwd_blocks(int64_t n, int32_t width, int32_t type)
+// Workgroups of the backward pass: each leaves one set of sums.  A CU takes one where that has the operands of a row ahead in 32 KB, else (16-bit or
+// narrow rows) two, and two where a gate per element makes the wavefronts compute for longer.  169 343 rows of 256 fp32 columns with one /
+// two / three a CU 190 / 209 / 206 us, 60 000 of 1000 bf16 columns 196 / 146 / 153, 232 965 of 602 fp32 columns with such a gate 1375 / 864 / 1092.
+int64_t bwd_blocks(int64_t n, int32_t width, int32_t type, bool matrix)
 {
-    const Shape s(width, access_elems(width, type));
-    const int64_t rows = s.threads() / s.lanes, want = (n + rows - 1) / rows, most = s.threads() > 512 ? 256 : s.threads() > 256 ? 512 : 1024;
+    constexpr int64_t CUS = 256, AHEAD = 32 << 10;
+    const int v = access_elems(width, type);
+    const Shape s(width, v);
+    const int64_t rows = s.threads() / s.lanes, want = (n + rows - 1) / rows, ahead = (int64_t)s.threads() * s.accesses * v * type_bytes(type) * 4;
+    const int64_t most = s.threads() <= 256 && (matrix || ahead < AHEAD) ? 2 * CUS : CUS;
     return want < most ? want : most;
 }
 
@@ -61,8 +66,9 @@ template <bool BWD> int launch(Args &a, int32_t type, hipStream_t stream)
 {
     const Shape s(a.width, access_elems(a.width, type));
     a.lanes = s.lanes;
+    a.past_cache = past_cache(a.n * (BWD ? (a.dx.data != nullptr) + (a.dy.data != nullptr) + (a.dgate.data != nullptr) : (a.h.data != nullptr) + (a.u.data != nullptr)), a.width, type);
     const int64_t rows = s.threads() / s.lanes, want = (a.n + rows - 1) / rows;
-    const int64_t blocks = BWD ? bwd_blocks(a.n, a.width, type) : want < FWD_BLOCKS ? want : FWD_BLOCKS;
+    const int64_t most = s.lanes > 64 ? FWD_BLOCKS : 1 << 20, blocks = BWD ? bwd_blocks(a.n, a.width, type, a.gate.data != nullptr) : want < most ? want : most;
     with_type(type, [&](auto t) {
         if (BWD) launch_bwd<decltype(t)>(a, s, blocks, stream);
         else launch_fwd<decltype(t)>(a, s, blocks, stream);
@@ -122,7 +128,6 @@ Args make_args(const slicegcn_resnorm_desc *d, const slicegcn_resnorm_params *p,
     a.post = d->post; a.pre = d->pre;
     a.residual = (float)d->residual; a.eps = (float)d->eps; a.inv_width = 1.f / (float)d->width;
     a.sigmoid = (d->flags & SLICEGCN_GATE_SIGMOID) != 0;
-    a.past_cache = past_cache(d->n, d->width, d->type);
     return a;
 }
 
@@ -143,7 +148,7 @@ extern "C" int slicegcn_resnorm_fwd(const slicegcn_resnorm_desc *d, const sliceg
 extern "C" size_t slicegcn_resnorm_bwd_workspace_bytes(int64_t n, int32_t width)
 {
     if (n < 0 || width < 1 || width > SLICEGCN_RESNORM_MAX_WIDTH) return 0;
-    const int64_t a = bwd_blocks(n, width, SLICEGCN_F32), b = bwd_blocks(n, width, SLICEGCN_BF16);
+    const int64_t a = bwd_blocks(n, width, SLICEGCN_F32, true), b = bwd_blocks(n, width, SLICEGCN_BF16, true);
     return (size_t)round_up((a > b ? a : b) * PLANES * (int64_t)width * 4, 256);
 }
 
@@ -170,7 +175,7 @@ extern "C" int slicegcn_resnorm_bwd(const slicegcn_resnorm_desc *d, const sliceg
     if (d->n > 0)
         if (int rc = launch<true>(a, d->type, as_stream(stream))) return rc;
     if (any) {
-        const int32_t blocks = d->n > 0 ? (int32_t)bwd_blocks(d->n, d->width, d->type) : 0;
+        const int32_t blocks = d->n > 0 ? (int32_t)bwd_blocks(d->n, d->width, d->type, a.gate.data != nullptr) : 0;
         resnorm_params_kernel<<<(d->width + FINAL_COLS - 1) / FINAL_COLS, FINAL_THREADS, 0, as_stream(stream)>>>(a, blocks, g);
         SG_LAUNCH_CHECK();
     }

@@ -256,9 +256,10 @@ template <class T, int V, int K, bool MULTI, bool FULL, int THREADS, bool MATRIX
 __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
 {
     __shared__ float shared[MULTI ? 64 : 1];
-    __shared__ float sums[THREADS <= 256 ? SUM_COLS : 1];
+    __shared__ float sums[THREADS <= 256 ? (EXTRA ? PLANES : PLANES / 2) * THREADS * ELEMS : 1];
     Row<T, V, K, MULTI, FULL> r(a, shared);
-    constexpr bool HOLD = THREADS < 1024;
+    // a workgroup of 1024 threads has registers for a row ahead only where elements are small and sums few
+    constexpr bool HOLD = THREADS < 1024 || (sizeof(T) == 2 && K == 1 && !EXTRA && !MATRIX);
     Held<V, K> p;
     if (HOLD) p.template load<MATRIX, false>(r, a);
     const int rows = THREADS / a.lanes;
@@ -350,34 +351,37 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
         if (there) r.store(a.dy, row, dH);
     }
     if (!a.planes) return;
-    // the workgroup's sums: over the rows of a wavefront, then over wavefronts (or over the rows beside each other), in order
-    const int span = a.lanes < 64 ? 64 : a.lanes, part = threadIdx.x / span, parts = THREADS / span;
+    // the workgroup's sums: over the rows it holds beside each other, in order
     float *out = a.partial + (int64_t)blockIdx.x * PLANES * a.width;
+    if (rows == 1) {
 #pragma unroll
-    for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2) {
-        if (!(a.planes >> q & 1)) continue;
-        for (int step = a.lanes; step < 64; step <<= 1) r.each([&](int k, int j) { acc[q][k][j] += __shfl_xor(acc[q][k][j], step, 64); });
-        const bool mine = a.lanes >= 64 || (threadIdx.x & 63) < a.lanes;
-        if (parts > 1) {
-            for (int w = 0; w < parts; ++w) {
-                if (part == w && mine) {
-#pragma unroll
-                    for (int k = 0; k < K; ++k)
-#pragma unroll
-                        for (int j = 0; j < V; ++j)
-                            if (r.at[k].on && j >= r.at[k].skip) {
-                                float *to = sums + r.at[k].col + j;
-                                *to = w ? *to + acc[q][k][j] : acc[q][k][j];
-                            }
-                }
-                __syncthreads();
-            }
-            for (int c = threadIdx.x; c < a.width; c += THREADS) out[q * a.width + c] = sums[c];
-            __syncthreads();
-        } else if (mine) {
+        for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2) {
+            if (!(a.planes >> q & 1)) continue;
 #pragma unroll
             for (int k = 0; k < K; ++k)
                 if (r.at[k].on) store_vec<float, V>(out + q * a.width + r.at[k].col, acc[q][k]);
+        }
+        return;
+    }
+    if constexpr (THREADS <= 256) {
+        const int plane = rows * a.width; // THREADS * ELEMS at most
+#pragma unroll
+        for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2) {
+            if (!(a.planes >> q & 1)) continue;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (r.at[k].on) store_vec<float, V>(sums + (EXTRA ? q : q / 2) * plane + r.slot * a.width + r.at[k].col, acc[q][k]);
+        }
+        __syncthreads();
+        for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2) {
+            if (!(a.planes >> q & 1)) continue;
+            for (int c = threadIdx.x; c < a.width; c += THREADS) {
+                const float *from = sums + (EXTRA ? q : q / 2) * plane + c;
+                float sum = 0.f;
+#pragma unroll 8
+                for (int i = 0; i < rows; ++i) sum += from[i * a.width];
+                out[q * a.width + c] = sum;
+            }
         }
     }
 }
