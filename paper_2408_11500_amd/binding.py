@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 from dataclasses import dataclass
 
@@ -119,27 +120,11 @@ RESNORM_MAX_WIDTH = 16384
 NORM_TWO, NORM_MAX = 0, 1
 
 
-class _EmbedDesc(ctypes.Structure):
-    _fields_ = [("n", ctypes.c_int64), ("vocab", ctypes.c_int64), ("pad", ctypes.c_int64), ("scale", ctypes.c_double),
-                ("width", ctypes.c_int32), ("table_type", ctypes.c_int32), ("row_type", ctypes.c_int32), ("flags", ctypes.c_uint32)]
-
-
-class _ResnormDesc(ctypes.Structure):
-    _fields_ = [("n", ctypes.c_int64), ("width", ctypes.c_int32), ("type", ctypes.c_int32), ("post", ctypes.c_int32),
-                ("pre", ctypes.c_int32), ("flags", ctypes.c_uint32), ("residual", ctypes.c_double), ("eps", ctypes.c_double)]
-
-
-class _ResnormParams(ctypes.Structure):  # slicegcn_resnorm_params and, for their gradients, slicegcn_resnorm_grads
-    _fields_ = [(name, ctypes.c_void_p) for name in ("post_w", "post_b", "pre_w", "pre_b", "gate")]
-
-
-class _Rows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64)]
-
-
-class _ResnormIo(ctypes.Structure):
-    _fields_ = ([(name, _Rows) for name in ("x", "y", "gate", "h", "u")] + [("stats", ctypes.c_void_p)] +
-                [(name, _Rows) for name in ("dh", "du", "dx", "dy", "dgate")])
+# Descriptors of slicegcn_train.h as packed bytes (a third of what filling ctypes structures takes, which is what small calls cost)
+_EMBED_DESC = struct.Struct("@qqqdiiiI")        # n, vocab, pad, scale, width, table_type, row_type, flags
+_RESNORM_DESC = struct.Struct("@qiiiiI4xdd")    # n, width, type, post, pre, flags, residual, eps
+_RESNORM_PARAMS = struct.Struct("@5P")          # post_w, post_b, pre_w, pre_b, gate; of their gradients too
+_RESNORM_IO = struct.Struct("@" + 5 * "Pq" + "P" + 5 * "Pq")  # x, y, gate, h, u; stats; dh, du, dx, dy, dgate
 
 
 class _Tensor(ctypes.Structure):
@@ -681,9 +666,11 @@ def _value_type(t: torch.Tensor, name: str) -> int:
 
 
 def _embed_desc(n, vocab, width, table_type, row_type, scale, pad, flags):
-    if pad is not None:
+    if pad is None:
+        pad = 0
+    else:
         flags |= EMBED_PAD
-    return _EmbedDesc(n, vocab, 0 if pad is None else pad, scale, width, table_type, row_type, flags)
+    return _EMBED_DESC.pack(n, vocab, pad, scale, width, table_type, row_type, flags)
 
 
 def _ids(ids: torch.Tensor):
@@ -701,7 +688,7 @@ def slicegcn_embed_fwd(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor
     if out.shape != (ids.numel(), table.shape[1]):
         raise ValueError("out must have a row per token, as wide as the table")
     desc = _embed_desc(ids.numel(), table.shape[0], table.shape[1], _value_type(table, "table"), _value_type(out, "out"), scale, pad, flags)
-    _check(lib().slicegcn_embed_fwd(ctypes.byref(desc), pi, pt, ldt, po, ldo, _stream()))
+    _check(lib().slicegcn_embed_fwd(desc, pi, pt, ldt, po, ldo, _stream()))
     return out
 
 
@@ -716,7 +703,7 @@ def slicegcn_embed_sort(ids: torch.Tensor, vocab: int, order: torch.Tensor, star
     if order.numel() != ids.numel() or starts.numel() != vocab + 1:
         raise ValueError("order must have an entry per token and starts vocab + 1")
     desc = _embed_desc(ids.numel(), vocab, 1, F32, F32, 1.0, pad, flags)
-    _check(lib().slicegcn_embed_sort(ctypes.byref(desc), pi, _vec(order, "order", torch.int32), _vec(starts, "starts", torch.int32),
+    _check(lib().slicegcn_embed_sort(desc, pi, _vec(order, "order", torch.int32), _vec(starts, "starts", torch.int32),
                                      *_ws(ws), _stream()))
     return order, starts
 
@@ -736,39 +723,61 @@ def slicegcn_embed_bwd(order: torch.Tensor, starts: torch.Tensor, dout: torch.Te
         raise ValueError("dout must have a row per token, as wide as dtable, and starts an entry per token of the table and one more")
     desc = _embed_desc(order.numel(), vocab, width, _value_type(dtable, "dtable"), _value_type(dout, "dout"), scale, None,
                        EMBED_ACCUMULATE if accumulate else 0)
-    _check(lib().slicegcn_embed_bwd(ctypes.byref(desc), _vec(order, "order", torch.int32), _vec(starts, "starts", torch.int32), pd, ldo,
+    _check(lib().slicegcn_embed_bwd(desc, _vec(order, "order", torch.int32), _vec(starts, "starts", torch.int32), pd, ldo,
                                     pt, ldt, *_ws(ws), _stream()))
     return dtable
 
 
-def _resnorm_structs(x, y, gate, post, pre, post_w, post_b, pre_w, pre_b, sigmoid, residual, eps, stats, rows):
-    """Descriptor, parameters and rows of a call; ``rows``: its other matrices by name."""
+def _rows(t, name: str, shape, dtype):
+    """(address, leading dimension) of a matrix that may be absent, as _mat of one of this shape and type."""
+    if t is None:
+        return 0, 0
+    if t.shape != shape or len(shape) != 2:
+        raise ValueError(f"{name}: expected a matrix like the call's others, {tuple(shape)}, not {tuple(t.shape)}")
+    strides = t.stride()
+    if t.dtype is not dtype or not t.is_cuda or (strides[1] != 1 and shape[1] > 1):
+        raise TypeError(f"{name}: expected a 2-D {dtype} device tensor with unit column stride")
+    # an empty tensor has no address, and none of its rows is touched
+    return t.data_ptr() or 256, strides[0] if shape[0] > 1 else max(strides[0], shape[1])
+
+
+def _columns(t, name: str, width: int):
+    """Address of an fp32 vector with an element per column that may be absent."""
+    if t is None:
+        return 0
+    if t.numel() != width:
+        raise ValueError(f"{name} must have an element per column")
+    if t.dtype is not torch.float32 or not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous fp32 device tensor")
+    return t.data_ptr()
+
+
+def _stats(stats, n: int):
+    if stats is None:
+        return 0
+    if tuple(stats.shape) != (n, 4):
+        raise ValueError("stats must be n x 4")
+    return _vec(stats, "stats") or 0
+
+
+def _resnorm_call(x, y, gate, post, pre, post_w, post_b, pre_w, pre_b, sigmoid, residual, eps):
+    """(shape, type, packed descriptor, packed parameters, addresses of x, y and the gate's rows) of a call."""
     first = x if x is not None else y
     if first is None:
         raise ValueError("neither x nor y")
     shape, dtype = first.shape, first.dtype
-    io = _ResnormIo()
-    matrix_gate = gate is not None and gate.dim() == 2
-    for name, t in (("x", x), ("y", y), ("gate", gate if matrix_gate else None), *rows.items()):
-        if t is None:
-            continue
-        data, ld = _mat(t, name, dtype)
-        if t.shape != shape:
-            raise ValueError(f"{name} differs in shape from {'x' if first is x else 'y'}")
-        setattr(io, name, _Rows(data or 256, ld))  # an empty tensor has no address, and none of its rows is touched
-    n, width = shape
-    if stats is not None:
-        if tuple(stats.shape) != (n, 4):
-            raise ValueError("stats must be n x 4")
-        io.stats = _vec(stats, "stats")
-    params = _ResnormParams()
-    for name, t in (("post_w", post_w), ("post_b", post_b), ("pre_w", pre_w), ("pre_b", pre_b), ("gate", None if matrix_gate else gate)):
-        if t is not None:
-            if t.numel() != width:
-                raise ValueError(f"{name} must have an element per column")
-            setattr(params, name, _vec(t, name))
-    desc = _ResnormDesc(n, width, _value_type(first, "x"), post, pre, GATE_SIGMOID if sigmoid else 0, residual, eps)
-    return desc, params, io
+    rows = (*_rows(x, "x", shape, dtype), *_rows(y, "y", shape, dtype))
+    width = shape[1]
+    if gate is None:
+        gate, rows = 0, rows + (0, 0)
+    elif gate.dim() == 2:
+        gate, rows = 0, rows + _rows(gate, "gate", shape, dtype)
+    else:
+        gate, rows = _columns(gate, "gate", width), rows + (0, 0)
+    desc = _RESNORM_DESC.pack(shape[0], width, _value_type(first, "x"), post, pre, GATE_SIGMOID if sigmoid else 0, residual, eps)
+    params = _RESNORM_PARAMS.pack(_columns(post_w, "post_w", width), _columns(post_b, "post_b", width), _columns(pre_w, "pre_w", width),
+                                  _columns(pre_b, "pre_b", width), gate)
+    return shape, dtype, desc, params, rows
 
 
 def slicegcn_resnorm_fwd(x, y, h, u, post: int = NORM_NONE, pre: int = NORM_NONE, post_w=None, post_b=None, pre_w=None, pre_b=None,
@@ -776,8 +785,9 @@ def slicegcn_resnorm_fwd(x, y, h, u, post: int = NORM_NONE, pre: int = NORM_NONE
     """h = residual * x + s * (post(y) * post_w + post_b);  u = pre(h) * pre_w + pre_b.  ``x`` or ``y``, ``h`` or ``u`` may be None.
     ``gate`` (s; through a sigmoid with ``sigmoid``): fp32 [width], or one value per element in the rows' type.
     ``stats``: fp32 [n, 4], filled for the backward pass."""
-    desc, params, io = _resnorm_structs(x, y, gate, post, pre, post_w, post_b, pre_w, pre_b, sigmoid, residual, eps, stats, dict(h=h, u=u))
-    _check(lib().slicegcn_resnorm_fwd(ctypes.byref(desc), ctypes.byref(params), ctypes.byref(io), _stream()))
+    shape, dtype, desc, params, rows = _resnorm_call(x, y, gate, post, pre, post_w, post_b, pre_w, pre_b, sigmoid, residual, eps)
+    io = _RESNORM_IO.pack(*rows, *_rows(h, "h", shape, dtype), *_rows(u, "u", shape, dtype), _stats(stats, shape[0]), *(10 * (0,)))
+    _check(lib().slicegcn_resnorm_fwd(desc, params, io, _stream()))
     return h, u
 
 
@@ -790,16 +800,14 @@ def slicegcn_resnorm_bwd(x, y, stats, dh, du, dx, dy, ws, post: int = NORM_NONE,
                          dpost_w=None, dpost_b=None, dpre_w=None, dpre_b=None, dgate=None):
     """Gradients of slicegcn_resnorm_fwd with the same arguments, from ``dh`` and ``du`` (one of them may be None); gradients that are
     None are not formed.  ``ws`` is needed for gradients of parameters (a gate per column is one)."""
-    matrix_gate = gate is not None and gate.dim() == 2
-    desc, params, io = _resnorm_structs(x, y, gate, post, pre, post_w, post_b, pre_w, pre_b, sigmoid, residual, eps, stats,
-                                        dict(dh=dh, du=du, dx=dx, dy=dy, dgate=dgate if matrix_gate else None))
-    grads = _ResnormParams()
-    for name, t in (("post_w", dpost_w), ("post_b", dpost_b), ("pre_w", dpre_w), ("pre_b", dpre_b), ("gate", None if matrix_gate else dgate)):
-        if t is not None:
-            if t.numel() != desc.width:
-                raise ValueError(f"d{name} must have an element per column")
-            setattr(grads, name, _vec(t, "d" + name))
-    _check(lib().slicegcn_resnorm_bwd(ctypes.byref(desc), ctypes.byref(params), ctypes.byref(io), ctypes.byref(grads), *_ws(ws), _stream()))
+    shape, dtype, desc, params, rows = _resnorm_call(x, y, gate, post, pre, post_w, post_b, pre_w, pre_b, sigmoid, residual, eps)
+    n, width = shape
+    of_rows = gate is not None and gate.dim() == 2
+    io = _RESNORM_IO.pack(*rows, 0, 0, 0, 0, _stats(stats, n), *_rows(dh, "dh", shape, dtype), *_rows(du, "du", shape, dtype),
+                          *_rows(dx, "dx", shape, dtype), *_rows(dy, "dy", shape, dtype), *_rows(dgate if of_rows else None, "dgate", shape, dtype))
+    grads = _RESNORM_PARAMS.pack(_columns(dpost_w, "dpost_w", width), _columns(dpost_b, "dpost_b", width), _columns(dpre_w, "dpre_w", width),
+                                 _columns(dpre_b, "dpre_b", width), 0 if of_rows else _columns(dgate, "dgate", width))
+    _check(lib().slicegcn_resnorm_bwd(desc, params, io, grads, *_ws(ws), _stream()))
 
 
 class TensorList:

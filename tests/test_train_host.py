@@ -19,7 +19,7 @@ def test_every_declared_symbol_is_exported(L):  # noqa: F811
 
 
 def embed(n=4, vocab=4, width=4, table=B.F32, rows=B.F32, scale=1.0, pad=0, flags=0):
-    return B._EmbedDesc(n, vocab, pad, scale, width, table, rows, flags)
+    return B._EMBED_DESC.pack(n, vocab, pad, scale, width, table, rows, flags)
 
 
 BAD_EMBED = [(dict(n=-1), B.EINVAL), (dict(vocab=0), B.EINVAL), (dict(n=2**31), B.ERANGE), (dict(vocab=2**31 - 1), B.ERANGE), (dict(flags=8), B.EINVAL)]
@@ -29,13 +29,13 @@ BAD_ROWS = [(dict(width=0), B.EINVAL), (dict(table=3), B.EINVAL), (dict(rows=-1)
 
 @pytest.mark.parametrize("change,status", BAD_EMBED + BAD_ROWS)
 def test_embed_fwd_refuses(L, change, status):  # noqa: F811
-    assert L.slicegcn_embed_fwd(ctypes.byref(embed(**change)), ONE, ONE, 4, ONE, 4, None) == status
+    assert L.slicegcn_embed_fwd(embed(**change), ONE, ONE, 4, ONE, 4, None) == status
 
 
 def test_embed_calls_refuse_bad_pointers(L):  # noqa: F811
-    d = ctypes.byref(embed())
-    wide = ctypes.byref(embed(flags=B.EMBED_IDS64))
-    half = ctypes.byref(embed(table=B.BF16, rows=B.F32))
+    d = embed()
+    wide = embed(flags=B.EMBED_IDS64)
+    half = embed(table=B.BF16, rows=B.F32)
     for args in ((None, ONE, ONE, 4, ONE, 4), (d, None, ONE, 4, ONE, 4), (d, ONE, None, 4, ONE, 4), (d, ONE, ONE, 4, None, 4), (d, ONE + 2, ONE, 4, ONE, 4),
                  (wide, ONE + 4, ONE, 4, ONE, 4), (d, ONE, ONE + 2, 4, ONE, 4), (half, ONE, ONE + 1, 4, ONE, 4), (d, ONE, ONE, 3, ONE, 4), (d, ONE, ONE, 4, ONE, 3)):
         assert L.slicegcn_embed_fwd(*args, None) == B.EINVAL
@@ -44,16 +44,16 @@ def test_embed_calls_refuse_bad_pointers(L):  # noqa: F811
     big = embed(n=5000)
     need = L.slicegcn_embed_sort_workspace_bytes(5000, 4)
     assert need > 0
-    assert L.slicegcn_embed_sort(ctypes.byref(big), ONE, ONE, ONE, None, 0, None) == B.EWORKSPACE
-    assert L.slicegcn_embed_sort(ctypes.byref(big), ONE, ONE, ONE, ONE, need - 1, None) == B.EWORKSPACE
-    assert L.slicegcn_embed_sort(ctypes.byref(big), ONE, ONE, ONE, ONE + 64, need, None) == B.EINVAL
+    assert L.slicegcn_embed_sort(big, ONE, ONE, ONE, None, 0, None) == B.EWORKSPACE
+    assert L.slicegcn_embed_sort(big, ONE, ONE, ONE, ONE, need - 1, None) == B.EWORKSPACE
+    assert L.slicegcn_embed_sort(big, ONE, ONE, ONE, ONE + 64, need, None) == B.EINVAL
     for args in ((None, ONE, ONE, ONE, 4, ONE, 4), (d, None, ONE, ONE, 4, ONE, 4), (d, ONE, None, ONE, 4, ONE, 4), (d, ONE, ONE, None, 4, ONE, 4),
                  (d, ONE, ONE, ONE, 4, None, 4), (d, ONE, ONE, ONE, 3, ONE, 4), (d, ONE, ONE, ONE, 4, ONE, 3), (d, ONE + 2, ONE, ONE, 4, ONE, 4)):
         assert L.slicegcn_embed_bwd(*args, None, 0, None) == B.EINVAL
     need = L.slicegcn_embed_bwd_workspace_bytes(5000, 4)
-    assert L.slicegcn_embed_bwd(ctypes.byref(big), ONE, ONE, ONE, 4, ONE, 4, ONE, need - 1, None) == B.EWORKSPACE
+    assert L.slicegcn_embed_bwd(big, ONE, ONE, ONE, 4, ONE, 4, ONE, need - 1, None) == B.EWORKSPACE
     for change, status in BAD_EMBED + BAD_ROWS:
-        assert L.slicegcn_embed_bwd(ctypes.byref(embed(**change)), ONE, ONE, ONE, 4, ONE, 4, ONE, 1 << 30, None) == status
+        assert L.slicegcn_embed_bwd(embed(**change), ONE, ONE, ONE, 4, ONE, 4, ONE, 1 << 30, None) == status
 
 
 def test_embed_workspaces(L):  # noqa: F811
@@ -65,18 +65,17 @@ def test_embed_workspaces(L):  # noqa: F811
 
 
 def resnorm(n=4, width=4, type=B.F32, post=B.NORM_RMS, pre=B.NORM_RMS, flags=0, residual=1.0, eps=1e-6):
-    return B._ResnormDesc(n, width, type, post, pre, flags, residual, eps)
+    return B._RESNORM_DESC.pack(n, width, type, post, pre, flags, residual, eps)
 
 
 def io(**kw):
-    r = B._ResnormIo()
-    for k, v in dict(dict(x=ONE, y=ONE, h=ONE, u=ONE, dh=ONE, du=ONE, stats=ONE), **kw).items():
-        setattr(r, k, v if k == "stats" else B._Rows(*(v if isinstance(v, tuple) else (v, 4))))
-    return r
+    given = dict(dict(x=ONE, y=ONE, h=ONE, u=ONE, dh=ONE, du=ONE, stats=ONE), **kw)
+    rows = lambda *names: [f for n in names for v in [given.get(n)] for f in (v if isinstance(v, tuple) else (v or 0, 4))]
+    return B._RESNORM_IO.pack(*rows("x", "y", "gate", "h", "u"), given["stats"] or 0, *rows("dh", "du", "dx", "dy", "dgate"))
 
 
 def params(**kw):
-    return B._ResnormParams(**kw)
+    return B._RESNORM_PARAMS.pack(*(kw.get(n, 0) for n in ("post_w", "post_b", "pre_w", "pre_b", "gate")))
 
 
 BAD_RESNORM = [
@@ -93,19 +92,19 @@ BAD_RESNORM = [
 @pytest.mark.parametrize("desc,p,rows,status", BAD_RESNORM)
 def test_resnorm_refuses(L, desc, p, rows, status):  # noqa: F811
     d, q, r = resnorm(**desc), params(**p), io(**rows)
-    assert L.slicegcn_resnorm_fwd(ctypes.byref(d), ctypes.byref(q), ctypes.byref(r), None) == status
-    assert L.slicegcn_resnorm_bwd(ctypes.byref(d), ctypes.byref(q), ctypes.byref(r), None, None, 0, None) == status
+    assert L.slicegcn_resnorm_fwd(d, q, r, None) == status
+    assert L.slicegcn_resnorm_bwd(d, q, r, None, None, 0, None) == status
 
 
 def test_resnorm_directions_refuse(L):  # noqa: F811
-    d, none = ctypes.byref(resnorm()), ctypes.byref(params())
-    fwd = lambda **rows: L.slicegcn_resnorm_fwd(d, none, ctypes.byref(io(**rows)), None)
+    d, none = resnorm(), params()
+    fwd = lambda **rows: L.slicegcn_resnorm_fwd(d, none, io(**rows), None)
     assert fwd(h=None, u=None) == fwd(u=None) == fwd(h=(ONE, 2)) == B.EINVAL
-    assert L.slicegcn_resnorm_fwd(None, none, ctypes.byref(io()), None) == L.slicegcn_resnorm_fwd(d, None, ctypes.byref(io()), None) == B.EINVAL
+    assert L.slicegcn_resnorm_fwd(None, none, io(), None) == L.slicegcn_resnorm_fwd(d, None, io(), None) == B.EINVAL
     assert L.slicegcn_resnorm_fwd(d, none, None, None) == B.EINVAL
 
     def bwd(grads=None, p=None, ws=None, nbytes=0, **rows):
-        return L.slicegcn_resnorm_bwd(d, ctypes.byref(params(**(p or {}))), ctypes.byref(io(**rows)), ctypes.byref(params(**(grads or {}))), ws, nbytes, None)
+        return L.slicegcn_resnorm_bwd(d, params(**(p or {})), io(**rows), params(**(grads or {})), ws, nbytes, None)
     assert bwd(dh=None, du=None) == bwd(stats=None) == bwd(dx=ONE, x=None) == bwd(dgate=ONE) == bwd(dy=(ONE, 3)) == B.EINVAL
     assert bwd(grads=dict(pre_w=ONE)) == B.EINVAL                        # gradient of an absent parameter
     assert bwd(grads=dict(pre_w=ONE + 1), p=dict(pre_w=ONE)) == B.EINVAL
