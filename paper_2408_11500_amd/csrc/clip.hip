@@ -2,7 +2,7 @@
 //
 //   norm = sqrt(sum g^2) or max |g|;   factor = norm <= max_norm ? 1 : max_norm / norm;   to = factor * from
 //
-// Tensors are cut into tiles of TILE_VECS 16-byte accesses; a workgroup takes consecutive tiles, adds the squares in fp64 (the square
+// Tensors are cut into tiles of TILE_VECS 16-byte accesses; a workgroup takes every so-manieth tile, adds the squares in fp64 (the square
 // of an fp32 number is exact there and cannot overflow) and stores one partial result, which are added in a fixed order: no atomics,
 // bitwise reproducible.  The workgroups of the scaling pass each form that last sum by themselves, which saves a launch between the two
 // passes.  The list of tensors travels in the kernel arguments (4 KB hold LIST tensors; a longer list takes several launches), so
@@ -31,7 +31,7 @@ constexpr int TYPE_SHIFT = 56;
 
 struct LaunchPart {
     int32_t tensors;
-    uint32_t tiles, tiles_per_block;
+    uint32_t tiles;
 };
 
 __device__ inline double wave_sum(double v)
@@ -67,39 +67,90 @@ template <> struct Running<SLICEGCN_NORM_MAX> {
     __device__ double norm() const { return (double)__uint_as_float(v); }
 };
 
-// Over the workgroup, in every thread
-template <int KIND> __device__ inline void over_block(Running<KIND> &r, uint64_t *shared)
+// Over the workgroup's WAVES wavefronts, in every thread
+template <int WAVES, int KIND> __device__ inline void over_block(Running<KIND> &r, uint64_t *shared)
 {
     r.over_wave();
     if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = r.bits();
     __syncthreads();
     Running<KIND> all;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) all.join(shared[w]);
+    for (int w = 0; w < WAVES; ++w) all.join(shared[w]);
     r = all;
 }
 
-// f(element type, tensor, first vector, end vector) for every piece of the workgroup's tiles, in order
-template <class F> __device__ inline void for_tiles(const TensorRange &list, const LaunchPart &part, F f)
+// f(element type, tensor, its first vector) for the tiles first, first + step, ... below `tiles`, the last one first where BACK
+template <bool BACK, class F> __device__ inline void for_tiles(const TensorRange &list, int tensors, uint32_t first, uint32_t step, uint32_t tiles, F f)
 {
-    uint32_t tile = blockIdx.x * part.tiles_per_block;
-    const uint32_t end = min(tile + part.tiles_per_block, part.tiles);
-    int lo = 0, hi = part.tensors; // the tensor that holds the first tile: the last one that starts at or before it
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (list.first[mid] <= tile) lo = mid;
+    if (first >= tiles) return;
+    const uint32_t count = (tiles - first + step - 1) / step, from = BACK ? first + (count - 1) * step : first;
+    int t = 0, hi = tensors; // the tensor that holds the tile: the last one that starts at or before it
+    while (hi - t > 1) {
+        const int mid = (t + hi) / 2;
+        if (list.first[mid] <= from) t = mid;
         else hi = mid;
     }
-    while (tile < end) {
-        while (list.first[lo + 1] <= tile) ++lo; // also past tensors without tiles
-        const uint32_t stop = min(end, list.first[lo + 1]);
-        const int64_t v0 = (int64_t)(tile - list.first[lo]) * TILE_VECS, v1 = (int64_t)(stop - list.first[lo]) * TILE_VECS;
-        const int type = (int)(list.count[lo] >> TYPE_SHIFT);
-        if (type == SLICEGCN_F32) f(float(), lo, v0, v1);
-        else if (type == SLICEGCN_BF16) f(bf16(), lo, v0, v1);
-        else f(f16(), lo, v0, v1);
-        tile = stop;
+    for (uint32_t k = 0; k < count; ++k) {
+        const uint32_t tile = BACK ? from - k * step : from + k * step;
+        if (BACK)
+            while (list.first[t] > tile) --t;
+        else
+            while (list.first[t + 1] <= tile) ++t; // also past tensors without tiles
+        const int64_t v0 = (int64_t)(tile - list.first[t]) * TILE_VECS;
+        const int type = (int)(list.count[t] >> TYPE_SHIFT);
+        if (type == SLICEGCN_F32) f(float(), t, v0);
+        else if (type == SLICEGCN_BF16) f(bf16(), t, v0);
+        else f(f16(), t, v0);
     }
+}
+
+__device__ inline int64_t elements(const TensorRange &list, int t) { return (int64_t)(list.count[t] & (((uint64_t)1 << TYPE_SHIFT) - 1)); }
+
+// The accesses of a tile by `threads` threads, of which this is the thread-th: whole(vector index, value) and rest(element index) for the last few
+template <class T, int THREADS_, class W, class R>
+__device__ inline void tile_accesses(const T *p, int64_t count, int64_t v0, int thread, W whole, R rest)
+{
+    constexpr int V = 16 / sizeof(T), N = TILE_VECS / THREADS_;
+    const int64_t vecs = count / V;
+    if (v0 + TILE_VECS <= vecs) {
+        typename VecOf<T, V>::type x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = load_vec<T, V>(p + (v0 + thread + i * THREADS_) * V);
+#pragma unroll
+        for (int i = 0; i < N; ++i) whole(v0 + thread + i * THREADS_, x[i]);
+        return;
+    }
+    for (int64_t v = v0 + thread; v < vecs; v += THREADS_) whole(v, load_vec<T, V>(p + v * V));
+    for (int64_t i = vecs * V + thread; i < count; i += THREADS_) rest(i);
+}
+
+template <class T, int THREADS_, int KIND>
+__device__ inline void add_tile(const TensorRange &list, int t, int64_t v0, int thread, Running<KIND> &r)
+{
+    const T *p = static_cast<const T *>(list.from[t]);
+    tile_accesses<T, THREADS_>(p, elements(list, t), v0, thread,
+                               [&](int64_t, const auto &x) {
+#pragma unroll
+                                   for (int j = 0; j < 16 / (int)sizeof(T); ++j) r.add((float)x[j]);
+                               },
+                               [&](int64_t i) { r.add((float)p[i]); });
+}
+
+template <bool PAST, class T, int THREADS_>
+__device__ inline void scale_tile(const TensorRange &list, int t, int64_t v0, int thread, float f)
+{
+    constexpr int V = 16 / sizeof(T);
+    const T *p = static_cast<const T *>(list.from[t]); // from and to may be the same tensor: a thread reads what it writes
+    T *q = static_cast<T *>(list.to[t]);
+    if (p == q && f == 1.f) return;
+    tile_accesses<T, THREADS_>(p, elements(list, t), v0, thread,
+                               [&](int64_t v, const auto &x) {
+                                   float o[V];
+#pragma unroll
+                                   for (int j = 0; j < V; ++j) o[j] = f * (float)x[j];
+                                   store_result<PAST, T, V>(q + v * V, o);
+                               },
+                               [&](int64_t i) { q[i] = (T)(f * (float)p[i]); });
 }
 
 template <int KIND>
@@ -107,31 +158,9 @@ __global__ __launch_bounds__(THREADS) void norm_partial_kernel(const TensorRange
 {
     __shared__ uint64_t shared[THREADS / 64];
     Running<KIND> r;
-    for_tiles(list, part, [&](auto zero, int t, int64_t v0, int64_t v1) {
-        using T = decltype(zero);
-        constexpr int V = 16 / sizeof(T);
-        const T *p = static_cast<const T *>(list.from[t]);
-        const int64_t count = (int64_t)(list.count[t] & (((uint64_t)1 << TYPE_SHIFT) - 1)), whole = count / V;
-        const int64_t stop = v1 < whole ? v1 : whole;
-        int64_t v = v0 + threadIdx.x;
-        for (; v + 3 * THREADS < stop; v += 4 * THREADS) {
-            typename VecOf<T, V>::type x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = load_vec<T, V>(p + (v + i * THREADS) * V);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) r.add((float)x[i][j]);
-        }
-        for (; v < stop; v += THREADS) {
-            const auto x = load_vec<T, V>(p + v * V);
-#pragma unroll
-            for (int j = 0; j < V; ++j) r.add((float)x[j]);
-        }
-        if (v1 > whole) // the tensor's last elements
-            for (int64_t i = whole * V + threadIdx.x; i < count; i += THREADS) r.add((float)p[i]);
-    });
-    over_block(r, shared);
+    for_tiles<false>(list, part.tensors, blockIdx.x, gridDim.x, part.tiles,
+                     [&](auto zero, int t, int64_t v0) { add_tile<decltype(zero), THREADS>(list, t, v0, threadIdx.x, r); });
+    over_block<THREADS / 64>(r, shared);
     if (threadIdx.x == 0) partial[blockIdx.x] = r.bits();
 }
 
@@ -139,7 +168,7 @@ template <int KIND> __device__ inline Running<KIND> join_partials(const uint64_t
 {
     Running<KIND> r;
     for (int32_t i = threadIdx.x; i < partials; i += THREADS) r.join(partial[i]);
-    over_block(r, shared);
+    over_block<THREADS / 64>(r, shared);
     return r;
 }
 
@@ -164,39 +193,35 @@ __global__ __launch_bounds__(THREADS) void norm_final_kernel(const uint64_t *__r
     store_norm<KIND>(r, max_norm, threadIdx.x == 0, norm, factor);
 }
 
-template <int KIND>
+// The tiles in the opposite order of the pass before: what that read last may still lie in the last-level cache (256 MB).
+template <int KIND, bool PAST>
 __global__ __launch_bounds__(THREADS) void clip_kernel(const TensorRange list, const LaunchPart part, const uint64_t *__restrict__ partial,
                                                        int32_t partials, double max_norm, float *__restrict__ norm, float *__restrict__ factor)
 {
     __shared__ uint64_t shared[THREADS / 64];
     const Running<KIND> r = join_partials<KIND>(partial, partials, shared);
     const float f = store_norm<KIND>(r, max_norm, blockIdx.x == 0 && threadIdx.x == 0, norm, factor);
-    for_tiles(list, part, [&](auto zero, int t, int64_t v0, int64_t v1) {
-        using T = decltype(zero);
-        constexpr int V = 16 / sizeof(T);
-        const T *p = static_cast<const T *>(list.from[t]); // from and to may be the same tensor: a thread reads what it writes
-        T *q = static_cast<T *>(list.to[t]);
-        if (p == q && f == 1.f) return;
-        const int64_t count = (int64_t)(list.count[t] & (((uint64_t)1 << TYPE_SHIFT) - 1)), whole = count / V;
-        const int64_t stop = v1 < whole ? v1 : whole;
-        auto scaled = [&](const typename VecOf<T, V>::type &x, int64_t v) {
-            float o[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) o[j] = f * (float)x[j];
-            store_vec<T, V>(q + v * V, o);
-        };
-        int64_t v = v0 + threadIdx.x;
-        for (; v + 3 * THREADS < stop; v += 4 * THREADS) {
-            typename VecOf<T, V>::type x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = load_vec<T, V>(p + (v + i * THREADS) * V);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) scaled(x[i], v + i * THREADS);
-        }
-        for (; v < stop; v += THREADS) scaled(load_vec<T, V>(p + v * V), v);
-        if (v1 > whole)
-            for (int64_t i = whole * V + threadIdx.x; i < count; i += THREADS) q[i] = (T)(f * (float)p[i]);
-    });
+    for_tiles<true>(list, part.tensors, blockIdx.x, gridDim.x, part.tiles,
+                    [&](auto zero, int t, int64_t v0) { scale_tile<PAST, decltype(zero), THREADS>(list, t, v0, threadIdx.x, f); });
+}
+
+// Few tiles: one workgroup, a wavefront per tile, does all of it in one launch.
+constexpr int SMALL_THREADS = 1024, SMALL_TILES = 2 * SMALL_THREADS / 64;
+template <int KIND>
+__global__ __launch_bounds__(SMALL_THREADS) void clip_small_kernel(const TensorRange list, int tensors, uint32_t tiles, double max_norm,
+                                                                   float *__restrict__ norm, float *__restrict__ factor, bool scale)
+{
+    __shared__ uint64_t shared[SMALL_THREADS / 64];
+    const int lane = threadIdx.x & 63;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    Running<KIND> r;
+    for_tiles<false>(list, tensors, wave, SMALL_THREADS / 64, tiles,
+                     [&](auto zero, int t, int64_t v0) { add_tile<decltype(zero), 64>(list, t, v0, lane, r); });
+    over_block<SMALL_THREADS / 64>(r, shared);
+    const float f = store_norm<KIND>(r, max_norm, threadIdx.x == 0, norm, factor);
+    if (!scale) return;
+    for_tiles<false>(list, tensors, wave, SMALL_THREADS / 64, tiles,
+                     [&](auto zero, int t, int64_t v0) { scale_tile<false, decltype(zero), 64>(list, t, v0, lane, f); });
 }
 
 int64_t tiles_of(const slicegcn_tensor &t)
@@ -209,6 +234,7 @@ struct CallPlan {
     int64_t tiles = 0;
     int64_t tiles_per_block = 1;
     int32_t partials = 0; // workgroups over all launches
+    bool small = false;   // one launch does everything
 };
 
 int check_tensors(const char *what, const slicegcn_tensor *t, int32_t count)
@@ -223,17 +249,17 @@ int check_tensors(const char *what, const slicegcn_tensor *t, int32_t count)
     return SLICEGCN_OK;
 }
 
-// Calls f(first tensor, tensors, tiles) for the tensors of each launch
-template <class F> int for_launches(const slicegcn_tensor *t, int32_t count, F f)
+// Calls f(first tensor, tensors, tiles) for the tensors of each launch, the last launch first where `back`
+template <class F> int for_launches(const slicegcn_tensor *t, int32_t count, bool back, F f)
 {
-    for (int32_t i = 0; i < count;) {
-        int32_t n = 0;
+    const int32_t launches = (count + LIST - 1) / LIST;
+    for (int32_t k = 0; k < launches; ++k) {
+        const int32_t first = (back ? launches - 1 - k : k) * LIST, n = count - first < LIST ? count - first : LIST;
         int64_t tiles = 0;
-        while (i + n < count && n < LIST) tiles += tiles_of(t[i + n++]);
+        for (int32_t i = 0; i < n; ++i) tiles += tiles_of(t[first + i]);
         SG_REQUIRE(tiles <= UINT32_MAX, SLICEGCN_ERANGE, "global_norm: more than 2^32 tiles of 16 KB");
         if (tiles > 0)
-            if (int rc = f(i, n, tiles)) return rc;
-        i += n;
+            if (int rc = f(first, n, tiles)) return rc;
     }
     return SLICEGCN_OK;
 }
@@ -242,33 +268,41 @@ int plan_call(const slicegcn_tensor *t, int32_t count, CallPlan *plan)
 {
     for (int32_t i = 0; i < count; ++i) plan->tiles += tiles_of(t[i]);
     plan->tiles_per_block = plan->tiles <= MAX_BLOCKS ? 1 : (plan->tiles + MAX_BLOCKS - 1) / MAX_BLOCKS;
-    return for_launches(t, count, [&](int32_t, int32_t, int64_t tiles) {
+    plan->small = plan->tiles <= SMALL_TILES && count <= LIST;
+    if (plan->small) return SLICEGCN_OK;
+    return for_launches(t, count, false, [&](int32_t, int32_t, int64_t tiles) {
         plan->partials += (int32_t)((tiles + plan->tiles_per_block - 1) / plan->tiles_per_block);
         return SLICEGCN_OK;
     });
 }
 
-// Launches a kernel over all tensors: launch(list, part, blocks, first partial)
-template <class F> int launch_lists(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t count, const CallPlan &plan, F launch)
+// Tensors [first, first + n) as a kernel argument
+TensorRange make_list(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t first, int32_t n)
 {
-    int32_t slot = 0;
-    return for_launches(from, count, [&](int32_t first, int32_t n, int64_t tiles) {
-        TensorRange list;
-        uint32_t at = 0;
-        for (int32_t i = 0; i < n; ++i) {
-            list.from[i] = from[first + i].data;
-            list.to[i] = to ? to[first + i].data : from[first + i].data;
-            list.count[i] = (uint64_t)from[first + i].count | ((uint64_t)from[first + i].type << TYPE_SHIFT);
-            list.first[i] = at;
-            at += (uint32_t)tiles_of(from[first + i]);
-        }
-        for (int32_t i = n; i < LIST; ++i) list.from[i] = nullptr, list.to[i] = nullptr, list.count[i] = 0;
-        for (int32_t i = n; i <= LIST; ++i) list.first[i] = at;
-        const LaunchPart part{n, (uint32_t)tiles, (uint32_t)plan.tiles_per_block};
+    TensorRange list;
+    uint32_t at = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        list.from[i] = from[first + i].data;
+        list.to[i] = to ? to[first + i].data : from[first + i].data;
+        list.count[i] = (uint64_t)from[first + i].count | ((uint64_t)from[first + i].type << TYPE_SHIFT);
+        list.first[i] = at;
+        at += (uint32_t)tiles_of(from[first + i]);
+    }
+    for (int32_t i = n; i < LIST; ++i) list.from[i] = nullptr, list.to[i] = nullptr, list.count[i] = 0;
+    for (int32_t i = n; i <= LIST; ++i) list.first[i] = at;
+    return list;
+}
+
+// Launches a kernel over all tensors: launch(list, part, blocks, blocks launched before)
+template <class F> int launch_lists(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t count, const CallPlan &plan, bool back, F launch)
+{
+    int32_t before = 0;
+    return for_launches(from, count, back, [&](int32_t first, int32_t n, int64_t tiles) {
+        const LaunchPart part{n, (uint32_t)tiles};
         const int32_t blocks = (int32_t)((tiles + plan.tiles_per_block - 1) / plan.tiles_per_block);
-        launch(list, part, blocks, slot);
+        launch(make_list(from, to, first, n), part, blocks, before);
         SG_LAUNCH_CHECK();
-        slot += blocks;
+        before += blocks;
         return SLICEGCN_OK;
     });
 }
@@ -286,30 +320,28 @@ int check_call(const char *what, const slicegcn_tensor *t, int32_t count, int32_
 }
 
 template <int KIND>
-int partials(const slicegcn_tensor *t, int32_t count, const CallPlan &plan, uint64_t *ws, hipStream_t stream)
+int call(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t count, bool scale, const CallPlan &plan, double max_norm, float *norm,
+         float *factor, uint64_t *ws, hipStream_t stream)
 {
-    return launch_lists(t, nullptr, count, plan, [&](const TensorRange &list, const LaunchPart &part, int32_t blocks, int32_t slot) {
-        norm_partial_kernel<KIND><<<blocks, THREADS, 0, stream>>>(list, part, ws + slot);
-    });
-}
-
-template <int KIND>
-int norm_call(const slicegcn_tensor *t, int32_t count, const CallPlan &plan, double max_norm, float *norm, float *factor, uint64_t *ws,
-              hipStream_t stream)
-{
-    if (int rc = partials<KIND>(t, count, plan, ws, stream)) return rc;
-    norm_final_kernel<KIND><<<1, THREADS, 0, stream>>>(ws, plan.partials, max_norm, norm, factor);
-    SG_LAUNCH_CHECK();
-    return SLICEGCN_OK;
-}
-
-template <int KIND>
-int clip_call(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t count, const CallPlan &plan, double max_norm, float *norm,
-              float *factor, uint64_t *ws, hipStream_t stream)
-{
-    if (int rc = partials<KIND>(from, count, plan, ws, stream)) return rc;
-    return launch_lists(from, to, count, plan, [&](const TensorRange &list, const LaunchPart &part, int32_t blocks, int32_t slot) {
-        clip_kernel<KIND><<<blocks, THREADS, 0, stream>>>(list, part, ws, plan.partials, max_norm, slot ? nullptr : norm, slot ? nullptr : factor);
+    if (plan.small) {
+        clip_small_kernel<KIND><<<1, SMALL_THREADS, 0, stream>>>(make_list(from, to, 0, count), count, (uint32_t)plan.tiles, max_norm, norm, factor, scale);
+        SG_LAUNCH_CHECK();
+        return SLICEGCN_OK;
+    }
+    if (int rc = launch_lists(from, nullptr, count, plan, false, [&](const TensorRange &list, const LaunchPart &part, int32_t blocks, int32_t before) {
+            norm_partial_kernel<KIND><<<blocks, THREADS, 0, stream>>>(list, part, ws + before);
+        }))
+        return rc;
+    if (!scale || plan.tiles == 0) {
+        norm_final_kernel<KIND><<<1, THREADS, 0, stream>>>(ws, plan.partials, max_norm, norm, factor);
+        SG_LAUNCH_CHECK();
+        return SLICEGCN_OK;
+    }
+    return launch_lists(from, to, count, plan, true, [&](const TensorRange &list, const LaunchPart &part, int32_t blocks, int32_t before) {
+        with_flag(past_cache(plan.tiles, TILE_VECS * 4, SLICEGCN_F32), [&](auto past) {
+            clip_kernel<KIND, decltype(past)::value><<<blocks, THREADS, 0, stream>>>(list, part, ws, plan.partials, max_norm, before ? nullptr : norm,
+                                                                                    before ? nullptr : factor);
+        });
     });
 }
 
@@ -333,8 +365,8 @@ extern "C" int slicegcn_global_norm(const slicegcn_tensor *tensors, int32_t coun
     if (int rc = check_call("global_norm", tensors, count, kind, factor ? max_norm : 0.0, &plan, ws, ws_bytes)) return rc;
     ProfScope prof(SLICEGCN_PROF_CLIP, count, as_stream(stream));
     auto *w = static_cast<uint64_t *>(ws);
-    return kind == SLICEGCN_NORM_TWO ? norm_call<SLICEGCN_NORM_TWO>(tensors, count, plan, max_norm, norm, factor, w, as_stream(stream))
-                                     : norm_call<SLICEGCN_NORM_MAX>(tensors, count, plan, max_norm, norm, factor, w, as_stream(stream));
+    return kind == SLICEGCN_NORM_TWO ? call<SLICEGCN_NORM_TWO>(tensors, nullptr, count, false, plan, max_norm, norm, factor, w, as_stream(stream))
+                                     : call<SLICEGCN_NORM_MAX>(tensors, nullptr, count, false, plan, max_norm, norm, factor, w, as_stream(stream));
 }
 
 extern "C" int slicegcn_clip(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t count, int32_t kind, double max_norm, float *norm,
@@ -350,11 +382,6 @@ extern "C" int slicegcn_clip(const slicegcn_tensor *from, const slicegcn_tensor 
     }
     ProfScope prof(SLICEGCN_PROF_CLIP, count, as_stream(stream));
     auto *w = static_cast<uint64_t *>(ws);
-    if (plan.tiles == 0) { // no elements: only the norm, zero
-        norm_final_kernel<SLICEGCN_NORM_TWO><<<1, THREADS, 0, as_stream(stream)>>>(w, 0, max_norm, norm, factor);
-        SG_LAUNCH_CHECK();
-        return SLICEGCN_OK;
-    }
-    return kind == SLICEGCN_NORM_TWO ? clip_call<SLICEGCN_NORM_TWO>(from, to, count, plan, max_norm, norm, factor, w, as_stream(stream))
-                                     : clip_call<SLICEGCN_NORM_MAX>(from, to, count, plan, max_norm, norm, factor, w, as_stream(stream));
+    return kind == SLICEGCN_NORM_TWO ? call<SLICEGCN_NORM_TWO>(from, to, count, true, plan, max_norm, norm, factor, w, as_stream(stream))
+                                     : call<SLICEGCN_NORM_MAX>(from, to, count, true, plan, max_norm, norm, factor, w, as_stream(stream));
 }
