@@ -566,7 +566,7 @@ __global__ __launch_bounds__(THREADS) void embed_join_kernel(const GradArgs a, T
     auto add = [&](int64_t c, int64_t last, int64_t first, int64_t step, double (&acc)[V]) {
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] = 0.0;
-#pragma unroll 4
+#pragma unroll 8
         for (int64_t k = c + first; k <= last; k += step) {
             const auto x = load_vec<float, V>(a.pieces + (2 * k + (k == c)) * a.width + col.at);
 #pragma unroll
@@ -672,7 +672,7 @@ struct GradPlan {
         tiles = (accesses + (1 << log_lanes) - 1) >> log_lanes;
         // as many wavefronts as keep the chip busy before chunks get longer: a longer chunk leaves fewer pieces
         log_chunk = 3;
-        while (log_chunk < log_lanes + 1 && (1 << log_chunk) < CHUNK && (n * tiles << log_lanes >> (log_chunk + 1)) >= 64 * 2048) ++log_chunk;
+        while ((1 << log_chunk) < CHUNK && (n * tiles << log_lanes >> (log_chunk + 1)) >= 64 * 2048) ++log_chunk;
         chunks = (n + (1 << log_chunk) - 1) >> log_chunk;
     }
     size_t piece_bytes(int32_t width) const { return (size_t)round_up(2 * chunks * (int64_t)width * 4, 256); }
@@ -830,7 +830,11 @@ extern "C" int slicegcn_embed_bwd(const slicegcn_embed_desc *d, const int32_t *o
             const int64_t zero_blocks = a.accumulate ? 0 : (d->vocab + per_block - 1) / per_block;
             SG_REQUIRE(chunk_blocks < ((int64_t)1 << 31) && join_blocks + zero_blocks < ((int64_t)1 << 31), SLICEGCN_ERANGE,
                        "embed_bwd: %lld rows of %d columns are too many for a call", (long long)d->n, d->width);
-            return with_flag(past_cache(d->vocab, ldt, d->table_type), [&](auto past) {
+            // Past the caches only whole lines, or parts of a line reach the memory one by one: a gradient of 500 000 rows of 300 fp32 columns 213 us,
+            // through the caches 180; 128 000 rows of 2048 bf16 columns 183 and 219
+            const int64_t row_bytes = (int64_t)d->width * type_bytes(d->table_type);
+            const bool whole_lines = row_bytes % 128 == 0 && ldt * type_bytes(d->table_type) % 128 == 0 && (reinterpret_cast<uintptr_t>(dTable) & 127u) == 0;
+            return with_flag(whole_lines && past_cache(d->vocab, ldt, d->table_type), [&](auto past) {
                 constexpr bool PAST = decltype(past)::value;
                 if (int rc = launch_parts(chunk_blocks, [&](unsigned first, unsigned count) {
                         embed_grad_kernel<TR, TT, V, PAST><<<count, THREADS, 0, as_stream(stream)>>>(a, static_cast<const TR *>(dOut), static_cast<TT *>(dTable), first);
