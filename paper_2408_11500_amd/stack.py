@@ -459,10 +459,11 @@ class FeatureFusion:
         B.slicegcn_linear_fwd(self.A, self.W2, self.b2, self.Xff[:, :self.s], None, act=B.ACT_NONE)
         return self.Xff
 
-    def backward(self, X: torch.Tensor, dXff: torch.Tensor):
-        """dXff: n x out_width gradient of the fused features (the sum over the slice models)."""
+    def backward(self, X: torch.Tensor, dXff: torch.Tensor, dX: torch.Tensor | None = None):
+        """dXff: n x out_width gradient of the fused features (the sum over the slice models).  ``dX``: receives the gradient
+        of X where that is learned too; raw features need none."""
         B.slicegcn_linear_bwd(self.A, self.W2, None, dXff, self.dA, self.dW2, self.db2, self.ws, act=B.ACT_NONE)
-        B.slicegcn_linear_bwd(X, self.W1, self.mask, self.dA, None, self.dW1, self.db1, self.ws, act=B.ACT_RELU)
+        B.slicegcn_linear_bwd(X, self.W1, self.mask, self.dA, dX, self.dW1, self.db1, self.ws, act=B.ACT_RELU)
 
 
 def _dense_slots(obj):
@@ -476,12 +477,14 @@ FeatureFusion.parameter_slots = _dense_slots
 class Optimizer:
     """Adam with a cosine-annealed learning rate (the paper's experimental settings) over all learnable
     tensors of the given models.  The tensors are moved into one flat buffer (gradients into another) and
-    the models' attributes rebound to views of it, so one library call updates every parameter."""
+    the models' attributes rebound to views of it, so one library call updates every parameter.
+    ``max_norm``: the gradients of all models together are scaled to at most this 2-norm; the update takes the factor along, so
+    they stay as they are in ``G``, and ``norm`` holds their norm (device scalar)."""
 
     ALIGN = 64  # floats: every tensor starts on a 256-byte boundary, so vector paths stay usable
 
     def __init__(self, models, lr_max: float, lr_min: float = 0.0, t_max: int = 1, beta1: float = 0.9,
-                 beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0):
+                 beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0, max_norm: float | None = None):
         slots = [s for m in models for s in m.parameter_slots()]
         get = lambda o, k: o[k] if isinstance(o, dict) else getattr(o, k)
         offs, total = [], 0
@@ -503,13 +506,22 @@ class Optimizer:
         self.hyper = (beta1, beta2, eps, weight_decay)
         self.lr_max, self.lr_min, self.t_max = lr_max, lr_min, t_max
         self.t = 0
+        self.max_norm = max_norm
+        if max_norm is not None:
+            self.norm, self.factor = (torch.zeros(1, dtype=torch.float32, device=dev) for _ in range(2))
+            self.gradients = B.TensorList([self.G])
+            self.norm_ws = torch.empty(B.slicegcn_global_norm_workspace_bytes(self.gradients), dtype=torch.uint8, device=dev)
 
     def step(self, epoch: int) -> float:
         """One update with the learning rate of ``epoch`` (0-based); returns that rate."""
         self.t += 1
         lr = B.slicegcn_cosine_lr(self.lr_max, self.lr_min, epoch, self.t_max)
         b1, b2, eps, wd = self.hyper
-        B.slicegcn_adam_step(self.P, self.G, self.M, self.V, lr, self.t, b1, b2, eps, wd)
+        if self.max_norm is None:
+            B.slicegcn_adam_step(self.P, self.G, self.M, self.V, lr, self.t, b1, b2, eps, wd)
+        else:
+            B.slicegcn_global_norm(self.gradients, self.norm, self.norm_ws, max_norm=self.max_norm, factor=self.factor)
+            B.slicegcn_adam_step_scaled(self.P, self.G, self.factor, self.M, self.V, lr, self.t, b1, b2, eps, wd)
         return lr
 
 

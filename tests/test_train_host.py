@@ -130,9 +130,9 @@ def test_bad_tensors_are_refused(L, entries, count):  # noqa: F811
 
 
 def test_norm_and_clip_refuse(L):  # noqa: F811
-    a = tensor_list((ONE, 5000, 0, 0), (None, 0, 1, 0))
+    a = tensor_list((ONE, 5_000_000, 0, 0), (None, 0, 1, 0))
     need = L.slicegcn_global_norm_workspace_bytes(a, 2)
-    assert need > 0
+    assert need > 0 and L.slicegcn_global_norm_workspace_bytes(tensor_list((ONE, 5000, 0, 0)), 1) == 0  # few elements: one launch, no workspace
     assert L.slicegcn_global_norm(a, 2, 0, 1.0, None, None, ONE, need, None) == B.EINVAL
     assert L.slicegcn_global_norm(a, 2, 2, 1.0, ONE, None, ONE, need, None) == B.EINVAL
     assert L.slicegcn_global_norm(a, 2, 0, -1.0, ONE, ONE, ONE, need, None) == B.EINVAL
@@ -141,8 +141,8 @@ def test_norm_and_clip_refuse(L):  # noqa: F811
     assert L.slicegcn_global_norm(a, 2, 0, 1.0, ONE, None, ONE, need - 1, None) == B.EWORKSPACE
     assert L.slicegcn_global_norm(a, 2, 0, 1.0, ONE, None, None, 0, None) == B.EWORKSPACE
     assert L.slicegcn_global_norm(a, 2, 0, 1.0, ONE, None, ONE + 8, need, None) == B.EINVAL
-    assert L.slicegcn_clip(a, tensor_list((ONE, 4999, 0, 0), (None, 0, 1, 0)), 2, 0, 1.0, ONE, None, ONE, need, None) == B.EINVAL
-    assert L.slicegcn_clip(a, tensor_list((ONE, 5000, 1, 0), (None, 0, 1, 0)), 2, 0, 1.0, ONE, None, ONE, need, None) == B.EINVAL
+    assert L.slicegcn_clip(a, tensor_list((ONE, 4_999_999, 0, 0), (None, 0, 1, 0)), 2, 0, 1.0, ONE, None, ONE, need, None) == B.EINVAL
+    assert L.slicegcn_clip(a, tensor_list((ONE, 5_000_000, 1, 0), (None, 0, 1, 0)), 2, 0, 1.0, ONE, None, ONE, need, None) == B.EINVAL
     assert L.slicegcn_adam_step_scaled(ONE, ONE, None, ONE, ONE, 4, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1, None) == B.EINVAL
     assert L.slicegcn_adam_step_scaled(ONE, ONE, ONE, ONE, ONE, 4, 1e-3, 0.9, 0.999, 1e-8, 0.0, 0, None) == B.EINVAL
 
