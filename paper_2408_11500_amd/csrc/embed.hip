@@ -63,7 +63,8 @@ __global__ __launch_bounds__(THREADS) void lookup_kernel(const ID *__restrict__ 
 // Stable sort by digits of at most DIGIT_BITS bits, lowest first.  Keys are tokens; padding and tokens outside the table get the key
 // `vocab` and end up behind all others.
 constexpr int DIGIT_BITS = 10, DIGITS = 1 << DIGIT_BITS;
-constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 4, SORT_TILE = SORT_THREADS * SORT_ITEMS;
+constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 4; // items of a thread, at most: fewer where that keeps more CUs busy
+constexpr int SMALL_SORT = SORT_THREADS * SORT_ITEMS;
 
 struct Tokens {
     const void *ids;
@@ -117,10 +118,11 @@ __device__ inline uint32_t block_scan(uint32_t v, uint32_t *wave_sums)
     return before + sum - v;
 }
 
-// Ranks the workgroup's items (a wavefront's items are SORT_ITEMS runs of 64 in a row) by digit, stable: rank[i] is the item's place among the
+// Ranks the workgroup's items (a wavefront's items are ITEMS runs of 64 in a row) by digit, stable: rank[i] is the item's place among the
 // wavefront's items of its digit.  counts[wave][digit] receives the wavefront's number of each digit.
-__device__ inline void rank_items(const uint32_t (&key)[SORT_ITEMS], const bool (&there)[SORT_ITEMS], int shift, int bits,
-                                  uint16_t (*counts)[DIGITS], uint32_t (&rank)[SORT_ITEMS])
+template <int ITEMS>
+__device__ inline void rank_items(const uint32_t (&key)[ITEMS], const bool (&there)[ITEMS], int shift, int bits,
+                                  uint16_t (*counts)[DIGITS], uint32_t (&rank)[ITEMS])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t mask = (1u << bits) - 1;
@@ -128,7 +130,7 @@ __device__ inline void rank_items(const uint32_t (&key)[SORT_ITEMS], const bool 
     __syncthreads();
     uint16_t *mine = counts[wave]; // other lanes change it between two reads of this one: hence the fences
 #pragma unroll
-    for (int i = 0; i < SORT_ITEMS; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         const uint32_t digit = (key[i] >> shift) & mask;
         const uint64_t same = same_digit(digit, bits, __ballot(there[i]));
         const uint32_t before = mine[digit];
@@ -177,18 +179,19 @@ __device__ inline uint32_t lower_bound(const uint32_t *keys, uint32_t count, uin
 
 // Up to SORT_TILE tokens: every workgroup sorts all of them in LDS and writes its part of starts, the first one also the order: one launch
 constexpr int STARTS_PER_BLOCK = 4 * SORT_THREADS;
+template <int ITEMS>
 __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const Tokens t, int bits, int passes, int32_t *__restrict__ order, int32_t *__restrict__ starts)
 {
     __shared__ uint16_t counts[SORT_WAVES][DIGITS];
     __shared__ uint32_t base[DIGITS], wave_sums[SORT_WAVES];
-    __shared__ uint32_t keys[SORT_TILE];
-    __shared__ uint16_t from[SORT_TILE];
+    __shared__ uint32_t keys[SORT_THREADS * ITEMS];
+    __shared__ uint16_t from[SORT_THREADS * ITEMS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)t.n;
-    const int first = wave * 64 * SORT_ITEMS + lane;
-    uint32_t key[SORT_ITEMS], rank[SORT_ITEMS], index[SORT_ITEMS];
-    bool there[SORT_ITEMS];
+    const int first = wave * 64 * ITEMS + lane;
+    uint32_t key[ITEMS], rank[ITEMS], index[ITEMS];
+    bool there[ITEMS];
 #pragma unroll
-    for (int i = 0; i < SORT_ITEMS; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         index[i] = first + i * 64;
         there[i] = (int)index[i] < n;
         key[i] = there[i] ? token_key(t, index[i]) : 0;
@@ -208,7 +211,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const Tokens t
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < SORT_ITEMS; ++i)
+        for (int i = 0; i < ITEMS; ++i)
             if (there[i]) {
                 const uint32_t digit = (key[i] >> (p * bits)) & ((1u << bits) - 1);
                 const uint32_t place = base[digit] + counts[wave][digit] + rank[i];
@@ -217,7 +220,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const Tokens t
             }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < SORT_ITEMS; ++i)
+        for (int i = 0; i < ITEMS; ++i)
             if (there[i]) {
                 key[i] = keys[first + i * 64];
                 index[i] = from[first + i * 64];
@@ -225,7 +228,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const Tokens t
     }
     if (blockIdx.x == 0) {
 #pragma unroll
-        for (int i = 0; i < SORT_ITEMS; ++i)
+        for (int i = 0; i < ITEMS; ++i)
             if (there[i]) order[first + i * 64] = (int32_t)index[i];
     }
     const int64_t t0 = (int64_t)blockIdx.x * STARTS_PER_BLOCK;
@@ -234,15 +237,16 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const Tokens t
 }
 
 // More tokens: per digit, the tiles' histograms, their prefix sums, and the items to their places.
+template <int ITEMS>
 __global__ __launch_bounds__(SORT_THREADS) void digit_count_kernel(const Tokens t, const uint32_t *__restrict__ keys, int shift, int bits, uint32_t *__restrict__ hist)
 {
     __shared__ uint32_t counts[DIGITS];
     const uint32_t mask = (1u << bits) - 1;
     for (int d = threadIdx.x; d < 1 << bits; d += SORT_THREADS) counts[d] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * SORT_TILE + threadIdx.x;
+    const int64_t first = (int64_t)blockIdx.x * (SORT_THREADS * ITEMS) + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < SORT_ITEMS; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         const int64_t at = first + i * SORT_THREADS;
         if (at < t.n) atomicAdd(&counts[((keys ? keys[at] : token_key(t, at)) >> shift) & mask], 1u);
     }
@@ -278,69 +282,78 @@ __global__ __launch_bounds__(1024) void digit_scan_kernel(uint32_t *__restrict__
     }
 }
 
-// Up to FEW_TILES tiles a workgroup adds up the tiles' histograms by itself: the scan's launch costs more.
-constexpr int FEW_TILES = 64;
-template <bool FEW>
+// Up to FEW_TILES tiles a workgroup adds up the tiles' histograms by itself: the scan's launch costs more (with the gradient, 83 tiles 62.8 us, scanned
+// 65.3; 123 tiles 61.7 and 56.7).
+constexpr int FEW_TILES = 96;
+template <bool FEW, int ITEMS>
 __global__ __launch_bounds__(SORT_THREADS) void digit_scatter_kernel(const Tokens t, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ from,
                                                                      int shift, int bits, const uint32_t *__restrict__ hist,
                                                                      const uint32_t *__restrict__ total, int tiles, uint32_t *__restrict__ out_keys,
                                                                      uint32_t *__restrict__ out_from)
 {
-    __shared__ uint16_t counts[SORT_WAVES][DIGITS];
-    __shared__ uint32_t base[DIGITS], wave_sums[SORT_WAVES];
+    __shared__ uint4 shared[SORT_WAVES * DIGITS / 8]; // the wavefronts' counts, then the items
+    __shared__ uint32_t local[DIGITS], delta[DIGITS], wave_sums[SORT_WAVES];
+    static_assert(sizeof(shared) >= sizeof(uint16_t[SORT_WAVES][DIGITS]) && sizeof(shared) >= sizeof(uint2[(SORT_THREADS * ITEMS)]), "room for either");
+    auto *counts = reinterpret_cast<uint16_t(*)[DIGITS]>(shared);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t first = (int64_t)blockIdx.x * SORT_TILE + wave * 64 * SORT_ITEMS + lane;
-    uint32_t key[SORT_ITEMS], index[SORT_ITEMS], rank[SORT_ITEMS];
-    bool there[SORT_ITEMS];
+    const int64_t first = (int64_t)blockIdx.x * (SORT_THREADS * ITEMS) + wave * 64 * ITEMS + lane;
+    uint32_t key[ITEMS], index[ITEMS], rank[ITEMS];
+    bool there[ITEMS];
 #pragma unroll
-    for (int i = 0; i < SORT_ITEMS; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         const int64_t at = first + i * 64;
         there[i] = at < t.n;
         key[i] = there[i] ? keys ? keys[at] : token_key(t, at) : 0;
         index[i] = there[i] && from ? from[at] : (uint32_t)at;
     }
-    // a digit's items in the tiles before this one, and in all tiles
-    constexpr int Q = DIGITS / SORT_THREADS;
-    const int digits = 1 << bits, d0 = threadIdx.x * Q;
-    uint32_t before[Q] = {}, all[Q] = {}, sum = 0;
-    if (d0 < digits) {
+    // a digit's items in the tiles before this one, and in all tiles: a thread per digit
+    static_assert(DIGITS == SORT_THREADS, "a thread per digit");
+    const int digits = 1 << bits, d = threadIdx.x;
+    uint32_t before = 0, all = 0;
+    if (d < digits) {
         if (FEW) {
-#pragma unroll 8
+#pragma unroll 16
             for (int i = 0; i < tiles; ++i) {
-                const auto c = load_vec<uint32_t, Q>(hist + i * digits + d0);
-#pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    before[q] += i < (int)blockIdx.x ? c[q] : 0;
-                    all[q] += c[q];
-                }
+                const uint32_t c = hist[i * digits + d];
+                before += i < (int)blockIdx.x ? c : 0;
+                all += c;
             }
         } else {
-            const auto b = load_vec<uint32_t, Q>(hist + (int64_t)blockIdx.x * digits + d0), c = load_vec<uint32_t, Q>(total + d0);
-#pragma unroll
-            for (int q = 0; q < Q; ++q) before[q] = b[q], all[q] = c[q];
+            before = hist[(int64_t)blockIdx.x * digits + d];
+            all = total[d];
         }
     }
     rank_items(key, there, shift, bits, counts, rank);
-    uint32_t inside[Q];
+    uint32_t inside[1];
     counts_before(counts, bits, inside);
+    const uint32_t here = block_scan(inside[0], wave_sums), everywhere = block_scan(all, wave_sums);
+    local[d] = here;
+    delta[d] = everywhere + before - here;
+    __syncthreads();
+    // The items in the order of their digits first: neighbouring lanes then store to neighbouring places.  Stored as they come, every item costs an
+    // access of its own (2.4 M tokens, 10 bits: 42 us; so 23).
+    const uint32_t mask = digits - 1;
+    uint32_t place[ITEMS];
 #pragma unroll
-    for (int q = 0; q < Q; ++q) sum += all[q];
-    uint32_t at = block_scan(sum, wave_sums);
-#pragma unroll
-    for (int q = 0; q < DIGITS / SORT_THREADS; ++q) {
-        const int d = threadIdx.x * (DIGITS / SORT_THREADS) + q;
-        if (d < digits) base[d] = at + before[q];
-        at += all[q];
+    for (int i = 0; i < ITEMS; ++i) {
+        const uint32_t digit = (key[i] >> shift) & mask;
+        place[i] = local[digit] + counts[wave][digit] + rank[i];
     }
+    __syncthreads(); // the items take the place of the counts
+    uint2 *items = reinterpret_cast<uint2 *>(shared);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+        if (there[i]) items[place[i]] = make_uint2(key[i], index[i]);
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < SORT_ITEMS; ++i)
-        if (there[i]) {
-            const uint32_t digit = (key[i] >> shift) & ((1u << bits) - 1);
-            const uint32_t place = base[digit] + counts[wave][digit] + rank[i];
-            out_keys[place] = key[i];
-            out_from[place] = index[i];
-        }
+    for (int i = 0; i < ITEMS; ++i) {
+        const uint32_t p = threadIdx.x + i * SORT_THREADS;
+        if ((int64_t)blockIdx.x * (SORT_THREADS * ITEMS) + p >= t.n) break;
+        const uint2 e = items[p];
+        const uint32_t to = delta[(e.x >> shift) & mask] + p;
+        out_keys[to] = e.x;
+        out_from[to] = e.y;
+    }
 }
 
 __global__ __launch_bounds__(THREADS) void starts_kernel(const uint32_t *__restrict__ keys, uint32_t n, int64_t vocab, int32_t *__restrict__ starts)
@@ -685,8 +698,18 @@ int grad_access(int32_t width, int32_t row_type)
     return width < v ? 1 : v;
 }
 
+// Calls f with the number of items of a thread
+template <class F> auto with_items(int items, F f)
+{
+    return items == 1 ? f(std::integral_constant<int, 1>()) : items == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, SORT_ITEMS>());
+}
+
+// Tokens up to which a thread of the sort takes one, two of them (else SORT_ITEMS): sort and gradient of 16 columns, 16 000 tokens with one, two, four
+// 32.9, 38.0, 39.5 us, 120 000 with two, four 48.6, 53.7, 500 000 65.8, 69.0, 1 M 126.6, 118.4.
+constexpr int64_t FEW_ITEMS[2] = {65536, 524288};
 struct SortPlan {
     int bits, passes; // per digit
+    int items;        // per thread
     int64_t tiles;
     SortPlan(int64_t n, int64_t vocab)
     {
@@ -694,7 +717,8 @@ struct SortPlan {
         while ((vocab >> all) != 0) ++all; // keys 0 to vocab
         passes = (all + DIGIT_BITS - 1) / DIGIT_BITS;
         bits = (all + passes - 1) / passes;
-        tiles = (n + SORT_TILE - 1) / SORT_TILE;
+        items = n <= FEW_ITEMS[0] ? 1 : n <= FEW_ITEMS[1] ? 2 : SORT_ITEMS;
+        tiles = (n + SORT_THREADS * items - 1) / (SORT_THREADS * items);
     }
     int64_t hist_words() const { return round_up(tiles << bits, 64); }
 };
@@ -746,7 +770,7 @@ extern "C" int slicegcn_embed_fwd(const slicegcn_embed_desc *d, const void *ids,
 
 extern "C" size_t slicegcn_embed_sort_workspace_bytes(int64_t n, int64_t vocab)
 {
-    if (n < 0 || vocab < 1 || n > INT32_MAX || vocab >= INT32_MAX || n <= SORT_TILE) return 0;
+    if (n < 0 || vocab < 1 || n > INT32_MAX || vocab >= INT32_MAX || n <= SMALL_SORT) return 0;
     const SortPlan plan(n, vocab);
     return (size_t)round_up(4 * (plan.hist_words() + DIGITS + 4 * round_up(n, 64)), 256);
 }
@@ -765,9 +789,11 @@ extern "C" int slicegcn_embed_sort(const slicegcn_embed_desc *d, const void *ids
     const Tokens t{ids, d->n, d->vocab, d->pad, (d->flags & SLICEGCN_EMBED_IDS64) != 0, (d->flags & SLICEGCN_EMBED_PAD) != 0};
     const SortPlan plan(d->n, d->vocab);
     hipStream_t s = as_stream(stream);
-    if (d->n <= SORT_TILE)
+    if (d->n <= SMALL_SORT)
         return launch_parts((d->vocab + STARTS_PER_BLOCK) / STARTS_PER_BLOCK, [&](unsigned, unsigned count) { // below 2^19 workgroups: one part
-            sort_small_kernel<<<count, SORT_THREADS, 0, s>>>(t, plan.bits, plan.passes, order, starts);
+            with_items(d->n <= SORT_THREADS ? 1 : d->n <= 2 * SORT_THREADS ? 2 : SORT_ITEMS, [&](auto items) {
+                sort_small_kernel<decltype(items)::value><<<count, SORT_THREADS, 0, s>>>(t, plan.bits, plan.passes, order, starts);
+            });
         });
     uint32_t *hist = static_cast<uint32_t *>(ws), *total = hist + plan.hist_words(), *buf = total + DIGITS;
     const int64_t stride = round_up(d->n, 64);
@@ -776,17 +802,23 @@ extern "C" int slicegcn_embed_sort(const slicegcn_embed_desc *d, const void *ids
     for (int p = 0; p < plan.passes; ++p) {
         uint32_t *out_keys = keys[p & 1], *out_from = p == plan.passes - 1 ? reinterpret_cast<uint32_t *>(order) : from[p & 1];
         const int shift = p * plan.bits;
-        digit_count_kernel<<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, shift, plan.bits, hist);
-        SG_LAUNCH_CHECK();
-        if (plan.tiles <= FEW_TILES) {
-            digit_scatter_kernel<true><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, nullptr, (int)plan.tiles,
-                                                                                    out_keys, out_from);
-        } else {
-            digit_scan_kernel<<<(unsigned)(((1 << plan.bits) + 63) / 64), 1024, 0, s>>>(hist, plan.tiles, plan.bits, total);
-            SG_LAUNCH_CHECK();
-            digit_scatter_kernel<false><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, total, 0, out_keys, out_from);
-        }
-        SG_LAUNCH_CHECK();
+        if (int rc = with_items(plan.items, [&](auto items) {
+                constexpr int ITEMS = decltype(items)::value;
+                digit_count_kernel<ITEMS><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, shift, plan.bits, hist);
+                SG_LAUNCH_CHECK();
+                if (plan.tiles <= FEW_TILES) {
+                    digit_scatter_kernel<true, ITEMS><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, nullptr,
+                                                                                                   (int)plan.tiles, out_keys, out_from);
+                } else {
+                    digit_scan_kernel<<<(unsigned)(((1 << plan.bits) + 63) / 64), 1024, 0, s>>>(hist, plan.tiles, plan.bits, total);
+                    SG_LAUNCH_CHECK();
+                    digit_scatter_kernel<false, ITEMS><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, total, 0,
+                                                                                                    out_keys, out_from);
+                }
+                SG_LAUNCH_CHECK();
+                return (int)SLICEGCN_OK;
+            }))
+            return rc;
         in_keys = out_keys;
         in_from = out_from;
     }
