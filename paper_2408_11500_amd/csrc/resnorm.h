@@ -10,7 +10,6 @@ namespace resnorm {
 constexpr int NONE = SLICEGCN_NORM_NONE, LAYER = SLICEGCN_NORM_LAYER;
 constexpr int ELEMS = 8;              // elements of a row per lane, at most: the backward pass holds two rows' operands, parameters and sums
 constexpr int WIDE = 1024 * ELEMS;    // wider rows: twice as many
-constexpr int FWD_BLOCKS = 4096;      // workgroups of the forward pass, at most: parameters are read once per workgroup
 constexpr int PLANES = 4;             // sums over rows: du * hn, du, dH * s * yn, dH * s (without s where the gate is per column)
 
 struct RowPtr {
@@ -31,13 +30,13 @@ struct Args {
     uint32_t planes; // bit p: the sums of plane p are wanted
 };
 
-// A row's accesses over lanes: as few lanes as the registers of a row allow (8 at least: a whole line), so that a sum over the row takes few steps.
+// A row's accesses over lanes: as few lanes as the registers of a row allow (8 at least, 4 for rows of four accesses), so that a sum over the row takes few steps.
 struct Shape {
     int lanes, accesses; // per row, per lane
     Shape(int32_t width, int v)
     {
         const int all = (width + v - 1) / v, most = v == 1 ? 1 : (width <= WIDE ? ELEMS : 2 * ELEMS) / v;
-        lanes = 8;
+        lanes = all <= 4 ? 4 : 8;
         while (lanes * most < all) lanes *= 2;
         accesses = (all + lanes - 1) / lanes;
     }
@@ -50,6 +49,12 @@ inline int access_elems(int32_t width, int32_t type)
     const int v = 16 / type_bytes(type);
     return width < v ? 1 : v;
 }
+
+// Whether the workgroups of the forward pass take many rows each, one requested ahead, with parameters and columns found out once: rows of several
+// wavefronts, whose wavefronts wait for each other, and 16-bit rows that do not fill their lanes, which are bound by instructions.  Others
+// are as fast or faster with a row to each group of lanes.  TB/s of rows read and written, looping / not: bf16 rows of 100 with layer norms
+// 4.7 / 3.3, of 256 with RMS norms 5.0 / 5.7, of 4096 (several wavefronts) 5.5 / 5.0, fp32 rows of 256 5.3 / 5.6.
+constexpr bool fwd_loops(bool multi, bool full, int bytes) { return multi || (bytes == 2 && !full); }
 
 // Launches a direction for one element type
 template <class T> void launch_fwd(const Args &a, const Shape &s, int64_t blocks, hipStream_t stream);

@@ -68,7 +68,10 @@ template <bool BWD> int launch(Args &a, int32_t type, hipStream_t stream)
     a.lanes = s.lanes;
     a.past_cache = past_cache(a.n * (BWD ? (a.dx.data != nullptr) + (a.dy.data != nullptr) + (a.dgate.data != nullptr) : (a.h.data != nullptr) + (a.u.data != nullptr)), a.width, type);
     const int64_t rows = s.threads() / s.lanes, want = (a.n + rows - 1) / rows;
-    const int64_t most = s.lanes > 64 ? FWD_BLOCKS : 1 << 20, blocks = BWD ? bwd_blocks(a.n, a.width, type, a.gate.data != nullptr) : want < most ? want : most;
+    const int v = access_elems(a.width, type);
+    const bool loops = v > 1 && fwd_loops(s.lanes > 64, s.full(a.width, v), type_bytes(type));
+    const int64_t most = BWD ? 0 : !loops ? 1 << 20 : s.lanes > 64 ? 4096 : 2048;
+    const int64_t blocks = BWD ? bwd_blocks(a.n, a.width, type, a.gate.data != nullptr) : want < most ? want : most;
     with_type(type, [&](auto t) {
         if (BWD) launch_bwd<decltype(t)>(a, s, blocks, stream);
         else launch_fwd<decltype(t)>(a, s, blocks, stream);

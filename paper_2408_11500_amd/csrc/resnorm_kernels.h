@@ -28,12 +28,14 @@ template <int V> struct Lane { // K accesses of V columns; the last access of a 
 
 template <class T, int V, int K> struct Raw { typename VecOf<T, V>::type v[K]; }; // a lane's part of a row, as it lies in memory
 
-template <class T, int V, int K, bool MULTI, bool FULL> struct Row {
+// COUNTS: which columns count in sums is held as factors over all rows, or found out each time
+template <class T, int V, int K, bool MULTI, bool FULL, bool COUNTS> struct Row {
     const Args &a;
     float *shared; // MULTI: [2][16][2]
     int lane, slot; // lane within the row, row within the workgroup
     int turn = 0;
     Lane<V> at[K];
+    float counts[COUNTS ? K : 1][COUNTS ? V : 1]; // 1 where the column counts in the lane's sums, 0 where another lane holds it too or it lies past the end
 
     __device__ Row(const Args &args, float *sh) : a(args), shared(sh)
     {
@@ -45,20 +47,41 @@ template <class T, int V, int K, bool MULTI, bool FULL> struct Row {
             at[k].on = FULL || c < a.width;
             at[k].col = FULL ? c : min(c, a.width - V);
             at[k].skip = FULL ? 0 : c - at[k].col;
+            if constexpr (COUNTS) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) counts[k][j] = at[k].on && j >= at[k].skip ? 1.f : 0.f;
+            }
         }
     }
 
-    // sum of the lane's columns; f(k, j) is the summand
+    // sum of f(k, j) * g(k, j) over the lane's columns
+    template <class F, class G> __device__ float lane_dot(F f, G g) const
+    {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (!COUNTS && !at[k].on) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if constexpr (FULL) s = fmaf(f(k, j), g(k, j), s);
+                else if constexpr (COUNTS) s = fmaf(f(k, j) * counts[k][j], g(k, j), s);
+                else s = fmaf(j >= at[k].skip ? f(k, j) : 0.f, g(k, j), s);
+            }
+        }
+        return s;
+    }
+
     template <class F> __device__ float lane_sum(F f) const
     {
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (!at[k].on) continue;
+            if (!COUNTS && !at[k].on) continue;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float v = f(k, j);
-                s += FULL || j >= at[k].skip ? v : 0.f;
+                if constexpr (FULL) s += f(k, j);
+                else if constexpr (COUNTS) s = fmaf(f(k, j), counts[k][j], s);
+                else s += j >= at[k].skip ? f(k, j) : 0.f;
             }
         }
         return s;
@@ -152,9 +175,10 @@ template <class T, int V, int K, bool MULTI, bool FULL> struct Row {
             *mean = s[0] * a.inv_width;
         }
         const float m = *mean;
-        s[0] = lane_sum([&](int k, int j) { const float d = v[k][j] - m; return d * d; });
+        const auto apart = [&](int k, int j) { return v[k][j] - m; };
+        s[0] = lane_dot(apart, apart);
         over_lanes(s);
-        *factor = 1.f / sqrtf(s[0] * a.inv_width + a.eps);
+        *factor = rsqrtf(s[0] * a.inv_width + a.eps); // one operation, off by a unit in the last place at most
     }
 
     // s, the factor of p, from a gate
@@ -165,19 +189,19 @@ template <class T, int V, int K, bool MULTI, bool FULL> struct Row {
 // A workgroup of 1024 threads has registers for one row only: there the parameters are read again for every row, from the caches.
 template <int V, int K> struct Held {
     float w[K][V], b[K][V], pre_w[K][V], pre_b[K][V];
-    template <bool MATRIX, bool FWD, class R> __device__ void load(const R &r, const Args &a)
+    template <bool MATRIX, bool EXTRA, bool FWD, class R> __device__ void load(const R &r, const Args &a)
     {
         r.param(a.post_w, 1.f, w);
-        r.param(a.post_b, 0.f, b);
+        if (EXTRA) r.param(a.post_b, 0.f, b);
         r.param(a.pre_w, 1.f, pre_w);
-        if (FWD) r.param(a.pre_b, 0.f, pre_b);
+        if (EXTRA && FWD) r.param(a.pre_b, 0.f, pre_b);
         if (!MATRIX && a.gate_col) {
             float g[K][V];
             r.param(a.gate_col, 1.f, g);
             r.each([&](int k, int j) {
                 const float s = r.opened(g[k][j]);
                 w[k][j] *= s;
-                b[k][j] *= s;
+                if (EXTRA) b[k][j] *= s;
             });
         }
     }
@@ -188,27 +212,35 @@ template <class T, int V, int K, bool MULTI, bool FULL, int THREADS, bool MATRIX
 __global__ __launch_bounds__(THREADS) void resnorm_fwd_kernel(const Args a)
 {
     __shared__ float shared[MULTI ? 64 : 1];
-    Row<T, V, K, MULTI, FULL> r(a, shared);
-    constexpr bool HOLD = THREADS < 1024;
+    constexpr bool HOLD = THREADS < 1024, LOOP = HOLD && fwd_loops(MULTI, FULL, sizeof(T));
+    Row<T, V, K, MULTI, FULL, LOOP && !MULTI> r(a, shared);
     Held<V, K> p;
-    if (HOLD) p.template load<MATRIX, true>(r, a);
+    if (HOLD) p.template load<MATRIX, EXTRA, true>(r, a);
     const int rows = THREADS / a.lanes;
-    for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < a.n; r0 += (int64_t)gridDim.x * rows) {
+    const int64_t stride = (int64_t)gridDim.x * rows;
+    Raw<T, V, K> next_x, next_y, next_g;
+    auto request = [&](int64_t row) {
+        const bool there = row < a.n;
+        if (a.x.data) next_x = r.load(a.x, row, there);
+        if (a.y.data) next_y = r.load(a.y, row, there);
+        if (MATRIX) next_g = r.load(a.gate, row, there);
+    };
+    if (LOOP) request((int64_t)blockIdx.x * rows + r.slot);
+    for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < a.n; r0 += stride) {
         const int64_t row = r0 + r.slot;
         const bool there = row < a.n;
         float h[K][V], st[4] = {0.f, 1.f, 0.f, 1.f};
-        Raw<T, V, K> x, y, g;
-        if (a.x.data) x = r.load(a.x, row, there);
-        if (a.y.data) y = r.load(a.y, row, there);
-        if (MATRIX) g = r.load(a.gate, row, there);
-        if (!HOLD) p.template load<MATRIX, true>(r, a);
+        if (!LOOP) request(row);
+        if (!HOLD) p.template load<MATRIX, EXTRA, true>(r, a);
+        const Raw<T, V, K> x = next_x, y = next_y, g = next_g;
+        if (LOOP && r0 + stride < a.n) request(row + stride);
         if (a.x.data) r.each([&](int k, int j) { h[k][j] = a.residual * (float)x.v[k][j]; });
         else r.each([&](int k, int j) { h[k][j] = 0.f; });
         if (a.y.data) {
             float v[K][V];
             r.each([&](int k, int j) { v[k][j] = (float)y.v[k][j]; });
             if (a.post != NONE) {
-                r.moments(v, a.post, &st[0], &st[1]);
+                r.moments(v, EXTRA ? a.post : (int)SLICEGCN_NORM_RMS, &st[0], &st[1]);
                 r.each([&](int k, int j) { v[k][j] = EXTRA ? (v[k][j] - st[0]) * st[1] : v[k][j] * st[1]; });
             }
             r.each([&](int k, int j) {
@@ -226,7 +258,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_fwd_kernel(const Args a)
         if (a.h.data && there) r.store(a.h, row, h);
         if (a.u.data) {
             if (a.pre != NONE) {
-                r.moments(h, a.pre, &st[2], &st[3]);
+                r.moments(h, EXTRA ? a.pre : (int)SLICEGCN_NORM_RMS, &st[2], &st[3]);
                 r.each([&](int k, int j) {
                     h[k][j] = EXTRA ? fmaf((h[k][j] - st[2]) * st[3], p.pre_w[k][j], p.pre_b[k][j]) : h[k][j] * st[3] * p.pre_w[k][j];
                 });
@@ -257,11 +289,11 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
 {
     __shared__ float shared[MULTI ? 64 : 1];
     __shared__ float sums[THREADS <= 256 ? (EXTRA ? PLANES : PLANES / 2) * THREADS * ELEMS : 1];
-    Row<T, V, K, MULTI, FULL> r(a, shared);
+    Row<T, V, K, MULTI, FULL, !FULL && THREADS < 1024> r(a, shared);
     // a workgroup of 1024 threads has registers for a row ahead only where elements are small and sums few
     constexpr bool HOLD = THREADS < 1024 || (sizeof(T) == 2 && K == 1 && !EXTRA && !MATRIX);
     Held<V, K> p;
-    if (HOLD) p.template load<MATRIX, false>(r, a);
+    if (HOLD) p.template load<MATRIX, EXTRA, false>(r, a);
     const int rows = THREADS / a.lanes;
     const int64_t stride = (int64_t)gridDim.x * rows;
     float acc[PLANES][K][V] = {};
@@ -272,7 +304,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
         const bool there = row < a.n;
         if (!HOLD) {
             next.template request<MATRIX>(r, a, row, there);
-            p.template load<MATRIX, false>(r, a);
+            p.template load<MATRIX, EXTRA, false>(r, a);
         }
         const Operands<T, V, K> o = next;
         if (HOLD && r0 + stride < a.n) next.template request<MATRIX>(r, a, row + stride, row + stride < a.n);
@@ -303,7 +335,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
                 if (a.planes & 1) r.each([&](int k, int j) { acc[0][k][j] = fmaf((float)o.du.v[k][j], h[k][j], acc[0][k][j]); });
                 if (EXTRA && (a.planes & 2)) r.each([&](int k, int j) { acc[1][k][j] += (float)o.du.v[k][j]; });
                 r.each([&](int k, int j) { d[k][j] = (float)o.du.v[k][j] * p.pre_w[k][j]; });
-                float c[2] = {r.lane_sum([&](int k, int j) { return d[k][j] * h[k][j]; }), 0.f};
+                float c[2] = {r.lane_dot([&](int k, int j) { return d[k][j]; }, [&](int k, int j) { return h[k][j]; }), 0.f};
                 if (EXTRA && a.pre == LAYER) {
                     c[1] = r.lane_sum([&](int k, int j) { return d[k][j]; });
                     r.over_lanes(c);
@@ -335,7 +367,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
         if (!a.dy.data) continue;
         r.each([&](int k, int j) { dH[k][j] *= p.w[k][j]; });
         if (a.post != NONE) {
-            float d[2] = {r.lane_sum([&](int k, int j) { return dH[k][j] * yn[k][j]; }), 0.f};
+            float d[2] = {r.lane_dot([&](int k, int j) { return dH[k][j]; }, [&](int k, int j) { return yn[k][j]; }), 0.f};
             if (EXTRA && a.post == LAYER) {
                 d[1] = r.lane_sum([&](int k, int j) { return dH[k][j]; });
                 r.over_lanes(d);
