@@ -289,7 +289,9 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
 {
     __shared__ float shared[MULTI ? 64 : 1];
     __shared__ float sums[THREADS <= 256 ? (EXTRA ? PLANES : PLANES / 2) * THREADS * ELEMS : 1];
-    Row<T, V, K, MULTI, FULL, !FULL && THREADS < 1024> r(a, shared);
+    // with a gate per element fp32 rows have no registers for the factors too: 232 965 rows of 602 with both 927 us, without the factors 855 (with a gate
+    // per column 824 and 884)
+    Row<T, V, K, MULTI, FULL, !FULL && THREADS < 1024 && !(MATRIX && sizeof(T) == 4)> r(a, shared);
     // a workgroup of 1024 threads has registers for a row ahead only where elements are small and sums few
     constexpr bool HOLD = THREADS < 1024 || (sizeof(T) == 2 && K == 1 && !EXTRA && !MATRIX);
     Held<V, K> p;
