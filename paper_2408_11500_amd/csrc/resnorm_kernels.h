@@ -15,8 +15,8 @@
 // a row's sums go round its lanes.  Counters: every kernel moves its operands once (2 % more where rows are no whole lines).
 // Measured (a 4 GiB copy moves 6.2 TB/s): forward 169 343 rows of 256 fp32 columns 120 us, 5.8 TB/s; 16 384 of 4096 bf16 84 us, 6.4 TB/s.
 // Backward 16 384 of 4096 bf16 150 us, 5.4 TB/s; 232 965 of 602 fp32 with layer norms and a sigmoid gate per element 855 us, 5.3 TB/s; above 4096
-// columns 4.6 (bf16) and 3.9 (fp32) TB/s with RMS norms and 1.9 to 2.5 with layer norms or a gate per element, whose registers do not fit 1024
-// threads; above 8192 0.6 to 1.3 TB/s for the same reason.
+// columns 4.6 to 4.8 TB/s with RMS norms and 3.4 to 4.1 with layer norms or a gate per element (1024 threads have 128 registers each; their sums over rows lie in
+// LDS, in registers they spilled: 1.4 to 2.4); above 8192 0.5 to 2.6 TB/s, where twice the elements do not fit the registers.
 #pragma once
 
 #include "resnorm.h"
@@ -298,13 +298,43 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
     // with a gate per element fp32 rows have no registers for the factors too: 232 965 rows of 602 with both 927 us, without the factors 855 (with a gate
     // per column 824 and 884)
     Row<T, V, K, MULTI, FULL, !FULL && THREADS < 1024 && !(MATRIX && sizeof(T) == 4)> r(a, shared);
-    // a workgroup of 1024 threads has registers for a row ahead only where elements are small and sums few
-    constexpr bool HOLD = THREADS < 1024 || (sizeof(T) == 2 && K == 1 && !EXTRA && !MATRIX);
+    // A workgroup of 1024 threads has registers for the parameters and a row ahead only without a gate per element, and in fp32 without layer norms and
+    // biases.  TB/s at 8192 columns with / without: bf16 layer norms 4.1 / 2.9, with a gate per element 3.4 / 3.6; fp32 RMS norms 4.6 / 4.5, layer
+    // norms 3.2 / 3.7.
+    constexpr bool HOLD = THREADS < 1024 || (K * V == ELEMS && !MATRIX && (sizeof(T) == 2 || !EXTRA));
     Held<V, K> p;
     if (HOLD) p.template load<MATRIX, EXTRA, false>(r, a);
     const int rows = THREADS / a.lanes;
     const int64_t stride = (int64_t)gridDim.x * rows;
-    float acc[PLANES][K][V] = {};
+    // the sums over rows: in registers, or, where 1024 threads have none to spare, in LDS (a lane's own places, so that nothing has to wait)
+    constexpr int HELD_PLANES = EXTRA ? PLANES : PLANES / 2;
+    constexpr bool IN_LDS = THREADS == 1024 && HELD_PLANES * K * V <= PLANES * ELEMS;
+    __shared__ float own[IN_LDS ? HELD_PLANES * K * THREADS * V : 1];
+    float acc[IN_LDS ? 1 : PLANES][IN_LDS ? 1 : K][IN_LDS ? 1 : V] = {};
+    const auto place = [&](int q, int k) { return own + (((EXTRA ? q : q / 2) * K + k) * THREADS + threadIdx.x) * V; };
+    if constexpr (IN_LDS) {
+        const float zero[V] = {};
+        for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2)
+#pragma unroll
+            for (int k = 0; k < K; ++k) store_vec<float, V>(place(q, k), zero);
+    }
+    // plane q += f(k, j) * g(k, j)
+    const auto add = [&](int q, auto f, auto g) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if constexpr (IN_LDS) {
+                const auto old = load_vec<float, V>(place(q, k));
+                float sum[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] = fmaf(f(k, j), g(k, j), old[j]);
+                store_vec<float, V>(place(q, k), sum);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[q][k][j] = fmaf(f(k, j), g(k, j), acc[q][k][j]);
+            }
+        }
+    };
+    const auto one = [](int, int) { return 1.f; };
     Operands<T, V, K> next;
     if (HOLD && (int64_t)blockIdx.x * rows < a.n) next.template request<MATRIX>(r, a, (int64_t)blockIdx.x * rows + r.slot, (int64_t)blockIdx.x * rows + r.slot < a.n);
     for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < a.n; r0 += stride) {
@@ -340,17 +370,18 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
             } else {
                 float d[K][V];
                 r.each([&](int k, int j) { h[k][j] = EXTRA ? (h[k][j] - o.st.z) * o.st.w : h[k][j] * o.st.w; }); // hn
-                if (a.planes & 1) r.each([&](int k, int j) { acc[0][k][j] = fmaf((float)o.du.v[k][j], h[k][j], acc[0][k][j]); });
-                if (EXTRA && (a.planes & 2)) r.each([&](int k, int j) { acc[1][k][j] += (float)o.du.v[k][j]; });
+                const auto du = [&](int k, int j) { return (float)o.du.v[k][j]; };
+                if (a.planes & 1) add(0, du, [&](int k, int j) { return h[k][j]; });
+                if (EXTRA && (a.planes & 2)) add(1, du, one);
                 r.each([&](int k, int j) { d[k][j] = (float)o.du.v[k][j] * p.pre_w[k][j]; });
                 float c[2] = {r.lane_dot([&](int k, int j) { return d[k][j]; }, [&](int k, int j) { return h[k][j]; }), 0.f};
                 if (EXTRA && a.pre == LAYER) {
                     c[1] = r.lane_sum([&](int k, int j) { return d[k][j]; });
                     r.over_lanes(c);
                 } else {
-                    float one[1] = {c[0]};
-                    r.over_lanes(one);
-                    c[0] = one[0];
+                    float first[1] = {c[0]};
+                    r.over_lanes(first);
+                    c[0] = first[0];
                 }
                 c[0] *= a.inv_width;
                 c[1] *= a.inv_width;
@@ -370,8 +401,9 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
             }
             r.each([&](int k, int j) { dH[k][j] *= s[k][j]; });
         }
-        if (a.planes & 4) r.each([&](int k, int j) { acc[2][k][j] = fmaf(dH[k][j], yn[k][j], acc[2][k][j]); });
-        if (EXTRA && (a.planes & 8)) r.each([&](int k, int j) { acc[3][k][j] += dH[k][j]; });
+        const auto dp = [&](int k, int j) { return dH[k][j]; };
+        if (a.planes & 4) add(2, dp, [&](int k, int j) { return yn[k][j]; });
+        if (EXTRA && (a.planes & 8)) add(3, dp, one);
         if (!a.dy.data) continue;
         r.each([&](int k, int j) { dH[k][j] *= p.w[k][j]; });
         if (a.post != NONE) {
@@ -380,9 +412,9 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
                 d[1] = r.lane_sum([&](int k, int j) { return dH[k][j]; });
                 r.over_lanes(d);
             } else {
-                float one[1] = {d[0]};
-                r.over_lanes(one);
-                d[0] = one[0];
+                float first[1] = {d[0]};
+                r.over_lanes(first);
+                d[0] = first[0];
             }
             d[0] *= a.inv_width;
             d[1] *= a.inv_width;
@@ -398,8 +430,12 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
         for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2) {
             if (!(a.planes >> q & 1)) continue;
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (r.at[k].on) store_vec<float, V>(out + q * a.width + r.at[k].col, acc[q][k]);
+            for (int k = 0; k < K; ++k) {
+                if (!r.at[k].on) continue;
+                float *to = out + q * a.width + r.at[k].col;
+                if constexpr (IN_LDS) *reinterpret_cast<typename VecOf<float, V>::packed *>(to) = load_vec<float, V>(place(q, k));
+                else store_vec<float, V>(to, acc[q][k]);
+            }
         }
         return;
     }
