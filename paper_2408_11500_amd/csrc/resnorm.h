@@ -30,14 +30,18 @@ struct Args {
     uint32_t planes; // bit p: the sums of plane p are wanted
 };
 
-// A row's accesses over lanes: as few lanes as the registers of a row allow (8 at least, 4 for rows of four accesses), so that a sum over the row takes few steps.
+// A row's accesses over lanes: as few lanes as the registers of a row allow, so that a sum over the row takes few steps.  A power of two up to 512 (8 at
+// least, 4 for rows of four accesses), beyond that whole wavefronts: bf16 rows of 5000 columns on 10 wavefronts, on 16 (RMS norms, forward 3.5 and
+// 2.7 TB/s, backward with layer norms 4.1 and 3.5), but of 2500 on 5, on 8 (5.0 and 5.1, 3.3 and 3.5).
+// fp32 rows above 8192 columns take all 16: fewer elements a lane count more there (9000 columns, 9 wavefronts, 16: 3.4 and 3.9, 1.7 and 2.3).
 struct Shape {
     int lanes, accesses; // per row, per lane
     Shape(int32_t width, int v)
     {
         const int all = (width + v - 1) / v, most = v == 1 ? 1 : (width <= WIDE ? ELEMS : 2 * ELEMS) / v;
         lanes = all <= 4 ? 4 : 8;
-        while (lanes * most < all) lanes *= 2;
+        while (lanes < 512 && lanes * most < all) lanes *= 2;
+        if (lanes * most < all) lanes = width > WIDE && v == 4 ? 1024 : (all + 64 * most - 1) / (64 * most) * 64;
         accesses = (all + lanes - 1) / lanes;
     }
     int threads() const { return lanes > 256 ? lanes : 256; }

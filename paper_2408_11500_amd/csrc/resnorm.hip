@@ -59,7 +59,7 @@ int64_t bwd_blocks(int64_t n, int32_t width, int32_t type, bool matrix)
     const int v = access_elems(width, type);
     const Shape s(width, v);
     const int64_t rows = s.threads() / s.lanes, want = (n + rows - 1) / rows, ahead = (int64_t)s.threads() * s.accesses * v * type_bytes(type) * 4;
-    const int64_t most = s.threads() <= 256 && (matrix || ahead < AHEAD) ? 2 * CUS : CUS;
+    const int64_t most = (s.threads() <= 256 && matrix) || ahead < AHEAD ? 2 * CUS : CUS;
     return want < most ? want : most;
 }
 

@@ -45,8 +45,8 @@ template <class T, int V, int K, bool MULTI, bool FULL, bool COUNTS> struct Row 
 
     __device__ Row(const Args &args, float *sh) : a(args), shared(sh)
     {
-        lane = threadIdx.x & (a.lanes - 1);
         slot = threadIdx.x / a.lanes;
+        lane = threadIdx.x - slot * a.lanes;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int32_t c = (lane + k * a.lanes) * V;
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_fwd_kernel(const Args a)
     Row<T, V, K, MULTI, FULL, LOOP && !MULTI> r(a, shared);
     Held<V, K> p;
     if (HOLD) p.template load<MATRIX, EXTRA, true>(r, a);
-    const int rows = THREADS / a.lanes;
+    const int rows = blockDim.x / a.lanes;
     const int64_t stride = (int64_t)gridDim.x * rows;
     Raw<T, V, K> next_x, next_y, next_g;
     auto request = [&](int64_t row) {
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
     constexpr bool HOLD = THREADS < 1024 || (K * V == ELEMS && !MATRIX && (sizeof(T) == 2 || !EXTRA));
     Held<V, K> p;
     if (HOLD) p.template load<MATRIX, EXTRA, false>(r, a);
-    const int rows = THREADS / a.lanes;
+    const int rows = blockDim.x / a.lanes;
     const int64_t stride = (int64_t)gridDim.x * rows;
     // the sums over rows: in registers, or, where 1024 threads have none to spare, in LDS (a lane's own places, so that nothing has to wait)
     constexpr int HELD_PLANES = EXTRA ? PLANES : PLANES / 2;
@@ -451,7 +451,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
         __syncthreads();
         for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2) {
             if (!(a.planes >> q & 1)) continue;
-            for (int c = threadIdx.x; c < a.width; c += THREADS) {
+            for (int c = threadIdx.x; c < a.width; c += blockDim.x) {
                 const float *from = sums + (EXTRA ? q : q / 2) * plane + c;
                 float sum = 0.f;
 #pragma unroll 8
@@ -462,30 +462,32 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
     }
 }
 
-template <bool BWD, class T, int V, int K, bool MULTI, bool FULL, int THREADS> void launch_kernel(const Args &a, int64_t blocks, hipStream_t s)
+template <bool BWD, class T, int V, int K, bool MULTI, bool FULL, int THREADS> void launch_kernel(const Args &a, int64_t blocks, int threads, hipStream_t s)
 {
     with_flag(a.gate.data != nullptr, [&](auto matrix) {
         with_flag(a.post == LAYER || a.pre == LAYER || a.post_b || a.pre_b, [&](auto extra) {
             constexpr bool MATRIX = decltype(matrix)::value, EXTRA = decltype(extra)::value;
-            if constexpr (BWD) resnorm_bwd_kernel<T, V, K, MULTI, FULL, THREADS, MATRIX, EXTRA><<<(unsigned)blocks, THREADS, 0, s>>>(a);
-            else resnorm_fwd_kernel<T, V, K, MULTI, FULL, THREADS, MATRIX, EXTRA><<<(unsigned)blocks, THREADS, 0, s>>>(a);
+            if constexpr (BWD) resnorm_bwd_kernel<T, V, K, MULTI, FULL, THREADS, MATRIX, EXTRA><<<(unsigned)blocks, threads, 0, s>>>(a);
+            else resnorm_fwd_kernel<T, V, K, MULTI, FULL, THREADS, MATRIX, EXTRA><<<(unsigned)blocks, threads, 0, s>>>(a);
         });
     });
 }
 
+// THREADS of the kernels: as many as a workgroup has, at most
 template <bool BWD, class T, int V, int K> void launch_lanes(const Args &a, const Shape &s, int64_t blocks, hipStream_t stream)
 {
+    const int threads = s.threads();
     if constexpr (V == 1) { // rows narrower than an access
-        launch_kernel<BWD, T, V, K, false, false, 256>(a, blocks, stream);
+        launch_kernel<BWD, T, V, K, false, false, 256>(a, blocks, threads, stream);
     } else if constexpr (K * V > ELEMS) { // the widest rows
-        launch_kernel<BWD, T, V, K, true, false, 1024>(a, blocks, stream);
+        launch_kernel<BWD, T, V, K, true, false, 1024>(a, blocks, threads, stream);
     } else if (s.lanes <= 64) {
-        if (s.full(a.width, V)) launch_kernel<BWD, T, V, K, false, true, 256>(a, blocks, stream);
-        else launch_kernel<BWD, T, V, K, false, false, 256>(a, blocks, stream);
-    } else if constexpr (2 * K * V > ELEMS) { // rows of fewer elements per lane take fewer lanes
-        if (s.lanes <= 256) launch_kernel<BWD, T, V, K, true, false, 256>(a, blocks, stream);
-        else if (s.lanes == 512) launch_kernel<BWD, T, V, K, true, false, 512>(a, blocks, stream);
-        else launch_kernel<BWD, T, V, K, true, false, 1024>(a, blocks, stream);
+        if (s.full(a.width, V)) launch_kernel<BWD, T, V, K, false, true, 256>(a, blocks, threads, stream);
+        else launch_kernel<BWD, T, V, K, false, false, 256>(a, blocks, threads, stream);
+    } else if constexpr (K * V == ELEMS) { // rows with fewer elements a lane take fewer lanes
+        if (s.lanes <= 256) launch_kernel<BWD, T, V, K, true, false, 256>(a, blocks, threads, stream);
+        else if (s.lanes <= 512) launch_kernel<BWD, T, V, K, true, false, 512>(a, blocks, threads, stream);
+        else launch_kernel<BWD, T, V, K, true, false, 1024>(a, blocks, threads, stream);
     }
 }
 
