@@ -13,8 +13,8 @@
 // being read (it would have to be kept, and rounded): bound by bytes.  Lanes hold 8 elements of a row each, so that the backward pass has room for
 // the parameters of its columns, the sums over its rows and the operands of the row after, which is what keeps the memory busy while
 // a row's sums go round its lanes.  Counters: every kernel moves its operands once (2 % more where rows are no whole lines).
-// Measured (a 4 GiB copy moves 6.2 TB/s): forward 169 343 rows of 256 fp32 columns 120 us, 5.8 TB/s; 16 384 of 4096 bf16 84 us, 6.4 TB/s.
-// Backward 16 384 of 4096 bf16 150 us, 5.4 TB/s; 232 965 of 602 fp32 with layer norms and a sigmoid gate per element 855 us, 5.3 TB/s; above 4096
+// Measured (a 4 GiB copy moves 6.2 TB/s): forward 169 343 rows of 256 fp32 columns 121 us, 5.7 TB/s; 16 384 of 4096 bf16 84 us, 6.4 TB/s.
+// Backward 16 384 of 4096 bf16 150 us, 5.4 TB/s; 232 965 of 602 fp32 with layer norms and a sigmoid gate per element 870 us, 5.2 TB/s; above 4096
 // columns 4.6 to 4.8 TB/s with RMS norms and 3.4 to 4.1 with layer norms or a gate per element (1024 threads have 128 registers each; their sums over rows lie in
 // LDS, in registers they spilled: 1.4 to 2.4); above 8192 0.5 to 2.6 TB/s, where twice the elements do not fit the registers.
 #pragma once
@@ -294,7 +294,6 @@ template <class T, int V, int K, bool MULTI, bool FULL, int THREADS, bool MATRIX
 __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
 {
     __shared__ float shared[MULTI ? 64 : 1];
-    __shared__ float sums[THREADS <= 256 ? (EXTRA ? PLANES : PLANES / 2) * THREADS * ELEMS : 1];
     // with a gate per element fp32 rows have no registers for the factors too: 232 965 rows of 602 with both 927 us, without the factors 855 (with a gate
     // per column 824 and 884)
     Row<T, V, K, MULTI, FULL, !FULL && THREADS < 1024 && !(MATRIX && sizeof(T) == 4)> r(a, shared);
@@ -306,18 +305,36 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
     if (HOLD) p.template load<MATRIX, EXTRA, false>(r, a);
     const int rows = blockDim.x / a.lanes;
     const int64_t stride = (int64_t)gridDim.x * rows;
-    // the sums over rows: in registers, or, where 1024 threads have none to spare, in LDS (a lane's own places, so that nothing has to wait)
-    constexpr int HELD_PLANES = EXTRA ? PLANES : PLANES / 2;
-    constexpr bool IN_LDS = THREADS == 1024 && HELD_PLANES * K * V <= PLANES * ELEMS;
-    __shared__ float own[IN_LDS ? HELD_PLANES * K * THREADS * V : 1];
+    // The sums over rows: in registers, added to places of the lane's own in LDS every FLUSH rows, so that long sums lose little (232 965 rows of 602
+    // on 512 workgroups: off by 1.3e-7 of their size for 2.9e-7, in 2 % more time); where 1024 threads have no registers to spare, in LDS throughout.
+    constexpr int FLUSH = 16, HELD_PLANES = EXTRA ? PLANES : PLANES / 2;
+    constexpr bool IN_LDS = THREADS == 1024 && HELD_PLANES * K * V <= PLANES * ELEMS, FLUSHES = THREADS < 1024;
+    __shared__ float own[IN_LDS || FLUSHES ? HELD_PLANES * K * THREADS * V : 1];
     float acc[IN_LDS ? 1 : PLANES][IN_LDS ? 1 : K][IN_LDS ? 1 : V] = {};
     const auto place = [&](int q, int k) { return own + (((EXTRA ? q : q / 2) * K + k) * THREADS + threadIdx.x) * V; };
-    if constexpr (IN_LDS) {
+    if constexpr (IN_LDS || FLUSHES) {
         const float zero[V] = {};
         for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2)
 #pragma unroll
             for (int k = 0; k < K; ++k) store_vec<float, V>(place(q, k), zero);
     }
+    const auto flush = [&]() {
+        if constexpr (FLUSHES) {
+#pragma unroll
+            for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2)
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const auto old = load_vec<float, V>(place(q, k));
+                    float sum[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        sum[j] = old[j] + acc[q][k][j];
+                        acc[q][k][j] = 0.f;
+                    }
+                    store_vec<float, V>(place(q, k), sum);
+                }
+        }
+    };
     // plane q += f(k, j) * g(k, j)
     const auto add = [&](int q, auto f, auto g) {
 #pragma unroll
@@ -337,9 +354,14 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
     const auto one = [](int, int) { return 1.f; };
     Operands<T, V, K> next;
     if (HOLD && (int64_t)blockIdx.x * rows < a.n) next.template request<MATRIX>(r, a, (int64_t)blockIdx.x * rows + r.slot, (int64_t)blockIdx.x * rows + r.slot < a.n);
+    int since = 0;
     for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < a.n; r0 += stride) {
         const int64_t row = r0 + r.slot;
         const bool there = row < a.n;
+        if (FLUSHES && ++since == FLUSH) {
+            flush();
+            since = 0;
+        }
         if (!HOLD) {
             next.template request<MATRIX>(r, a, row, there);
             p.template load<MATRIX, EXTRA, false>(r, a);
@@ -423,6 +445,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
         if (there) r.store(a.dy, row, dH);
     }
     if (!a.planes) return;
+    flush();
     // the workgroup's sums: over the rows it holds beside each other, in order
     float *out = a.partial + (int64_t)blockIdx.x * PLANES * a.width;
     if (rows == 1) {
@@ -433,29 +456,24 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
             for (int k = 0; k < K; ++k) {
                 if (!r.at[k].on) continue;
                 float *to = out + q * a.width + r.at[k].col;
-                if constexpr (IN_LDS) *reinterpret_cast<typename VecOf<float, V>::packed *>(to) = load_vec<float, V>(place(q, k));
+                if constexpr (IN_LDS || FLUSHES) *reinterpret_cast<typename VecOf<float, V>::packed *>(to) = load_vec<float, V>(place(q, k));
                 else store_vec<float, V>(to, acc[q][k]);
             }
         }
         return;
     }
     if constexpr (THREADS <= 256) {
-        const int plane = rows * a.width; // THREADS * ELEMS at most
-#pragma unroll
-        for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2) {
-            if (!(a.planes >> q & 1)) continue;
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                if (r.at[k].on) store_vec<float, V>(sums + (EXTRA ? q : q / 2) * plane + r.slot * a.width + r.at[k].col, acc[q][k]);
-        }
         __syncthreads();
         for (int q = 0; q < PLANES; q += EXTRA ? 1 : 2) {
             if (!(a.planes >> q & 1)) continue;
+            // column c lies in access c / V of its row, that is in access k of lane l (where the last access was moved left, in its first columns too)
             for (int c = threadIdx.x; c < a.width; c += blockDim.x) {
-                const float *from = sums + (EXTRA ? q : q / 2) * plane + c;
+                const int last = (a.width + V - 1) / V - 1, access = min(c / V, last), k = access / a.lanes, l = access - k * a.lanes;
+                const int j = access == last ? c - (a.width - V) : c - access * V;
+                const float *from = own + (((EXTRA ? q : q / 2) * K + k) * THREADS + l) * V + j;
                 float sum = 0.f;
 #pragma unroll 8
-                for (int i = 0; i < rows; ++i) sum += from[i * a.width];
+                for (int i = 0; i < rows; ++i) sum += from[i * a.lanes * V];
                 out[q * a.width + c] = sum;
             }
         }
