@@ -811,16 +811,23 @@ extern "C" int slicegcn_embed_sort(const slicegcn_embed_desc *d, const void *ids
                 constexpr int ITEMS = decltype(items)::value;
                 digit_count_kernel<ITEMS><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, shift, plan.bits, hist);
                 SG_LAUNCH_CHECK();
-                if (plan.tiles <= FEW_TILES) {
-                    digit_scatter_kernel<true, ITEMS><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, nullptr,
-                                                                                                   (int)plan.tiles, out_keys, out_from);
-                } else {
+                // one item a thread only ever means few tiles, SORT_ITEMS never
+                static_assert(FEW_ITEMS[0] <= (int64_t)FEW_TILES * SORT_THREADS && FEW_ITEMS[1] >= (int64_t)FEW_TILES * SORT_THREADS * SORT_ITEMS, "tiles");
+                if constexpr (ITEMS < SORT_ITEMS) {
+                    if (plan.tiles <= FEW_TILES) {
+                        digit_scatter_kernel<true, ITEMS><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, nullptr,
+                                                                                                       (int)plan.tiles, out_keys, out_from);
+                        SG_LAUNCH_CHECK();
+                        return (int)SLICEGCN_OK;
+                    }
+                }
+                if constexpr (ITEMS > 1) {
                     digit_scan_kernel<<<(unsigned)(((1 << plan.bits) + 63) / 64), 1024, 0, s>>>(hist, plan.tiles, plan.bits, total);
                     SG_LAUNCH_CHECK();
                     digit_scatter_kernel<false, ITEMS><<<(unsigned)plan.tiles, SORT_THREADS, 0, s>>>(t, in_keys, in_from, shift, plan.bits, hist, total, 0,
                                                                                                     out_keys, out_from);
+                    SG_LAUNCH_CHECK();
                 }
-                SG_LAUNCH_CHECK();
                 return (int)SLICEGCN_OK;
             }))
             return rc;
@@ -871,7 +878,7 @@ extern "C" int slicegcn_embed_bwd(const slicegcn_embed_desc *d, const int32_t *o
             // through the caches 180; 128 000 rows of 2048 bf16 columns 183 and 219
             const int64_t row_bytes = (int64_t)d->width * type_bytes(d->table_type);
             const bool whole_lines = row_bytes % 128 == 0 && ldt * type_bytes(d->table_type) % 128 == 0 && (reinterpret_cast<uintptr_t>(dTable) & 127u) == 0;
-            return with_flag(whole_lines && past_cache(d->vocab, ldt, d->table_type), [&](auto past) {
+            auto go = [&](auto past) {
                 constexpr bool PAST = decltype(past)::value;
                 if (int rc = launch_parts(chunk_blocks, [&](unsigned first, unsigned count) {
                         embed_grad_kernel<TR, TT, V, PAST><<<count, THREADS, 0, as_stream(stream)>>>(a, static_cast<const TR *>(dOut), static_cast<TT *>(dTable), first);
@@ -880,7 +887,10 @@ extern "C" int slicegcn_embed_bwd(const slicegcn_embed_desc *d, const int32_t *o
                 return launch_parts(join_blocks + zero_blocks, [&](unsigned first, unsigned count) {
                     embed_join_kernel<TT, V, PAST><<<count, THREADS, 0, as_stream(stream)>>>(a, static_cast<TT *>(dTable), first, (uint32_t)join_blocks);
                 });
-            });
+            };
+            if constexpr (V > 1)
+                if (whole_lines && past_cache(d->vocab, ldt, d->table_type)) return go(std::true_type());
+            return go(std::false_type());
         };
         constexpr int V = 16 / (int)sizeof(TR);
         if (d->width >= V) return launch(std::integral_constant<int, V>());

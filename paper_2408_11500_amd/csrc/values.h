@@ -18,9 +18,9 @@ inline bool known_type(int32_t type) { return type == SLICEGCN_F32 || type == SL
 // every element on a boundary of its size: accesses of 16 bytes start at any such boundary
 inline bool aligned_for(const void *p, int32_t type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
 
-// Whether rows are stored past the caches: where they exceed the last-level cache (256 MB).  A lookup of 128-wide fp32 rows alone / with a
-// pass that reads its output, through / past the caches: 64 MB 20.8 / 20.5 and 40.5 / 42.6 us, 192 MB 57.7 / 56.1 and 129.7 / 131.7, 256 MB
-// 74.8 / 73.6 and 176.7 / 170.6, 1 GB 304 / 288 and 665 / 648; 2.4 M rows of 100 columns that lie 128 apart (lines written in part) 397 / 292 alone.
+// Whether rows are stored past the caches: where they exceed the last-level cache (256 MB).  A lookup of 128-wide fp32 rows alone, and with a
+// pass that reads its output, through / past the caches: 64 MB 21.2 / 20.6 and 41.5 / 42.7 us, 128 MB 41.1 / 39.3 and 86.9 / 89.0, 256 MB 89.1 / 76.8 and
+// 185.8 / 180.2, 1 GB 334 / 294 and 686 / 680; 2.4 M rows of 100 columns that lie 128 apart (lines written in part) 412 / 263 alone.
 inline bool past_cache(int64_t rows, int64_t ld, int32_t type) { return rows * ld * type_bytes(type) >= (int64_t)256 << 20; }
 
 // V elements that one access moves (16 bytes at most), at any element boundary

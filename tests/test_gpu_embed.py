@@ -117,6 +117,21 @@ def test_sort(n, vocab):
         assert torch.equal(order.cpu().long()[:valid], want.indices[:valid]), (kind, "order")
 
 
+@pytest.mark.parametrize("n", [65_536, 65_537, 98_305, 196_608, 196_609, 524_288, 524_289, 1_100_003])
+@pytest.mark.parametrize("vocab", [7, 40_000, 2_000_000])
+def test_sort_of_many_tokens(n, vocab):
+    """Both sides of every number of tokens at which the sort takes other tiles or another way to their prefix sums."""
+    gen = torch.Generator().manual_seed(n + vocab)
+    for kind, dtype, pad in (("skewed", torch.int64, None), ("hot", torch.int32, vocab // 2)):
+        ids = tokens(gen, n, vocab, kind)
+        order, starts = sort(ids.to(dtype).cuda(), vocab, pad)
+        key = ids if pad is None else torch.where(ids == pad, vocab, ids)
+        want = torch.sort(key, stable=True)
+        valid = int((key < vocab).sum())
+        assert torch.equal(starts.cpu().long(), torch.searchsorted(want.values, torch.arange(vocab + 1))), (kind, "starts")
+        assert torch.equal(order.cpu().long()[:valid], want.indices[:valid]), (kind, "order")
+
+
 # ---- gradient -------------------------------------------------------------------------------------------------------------
 
 def check_grad(gen, ids, vocab, width, table, row, ldo, ldt, offset, scale, pad, accumulate, dtype=torch.int64):

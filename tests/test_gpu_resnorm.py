@@ -167,6 +167,18 @@ def test_many_rows_and_none(n):
         assert all((c.g[k] == 0).all() for k in ("dpost_w", "dpost_b", "dpre_w", "dpre_b", "dgate"))
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [602, 2049, 4097, 5120, 8192])
+@pytest.mark.parametrize("norm,gate", [(RMS, "column"), (LAYER, "column"), (LAYER, "matrix")])
+def test_wide_rows_in_turn(width, kind, norm, gate):
+    """More rows than workgroups, so that each takes several in turn: the row requested ahead, sums kept over rows."""
+    n = {602: 12_000, 2049: 2100, 4097: 1100, 5120: 600, 8192: 600}[width]
+    c = Call(n, width, kind, norm, norm, gate, sigmoid=gate == "matrix", residual=0.75)
+    c.forward()
+    c.check_forward()
+    c.backward()
+
+
 @pytest.mark.parametrize("kind,width", [("f32", 64), ("f32", 301), ("bf16", 1001), ("f32", 1333), ("f16", 5001)])
 def test_rows_in_place(kind, width):
     """Outputs in the rows of inputs give the same bits; nothing beside the rows is written."""
