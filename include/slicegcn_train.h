@@ -62,8 +62,10 @@ size_t slicegcn_embed_sort_workspace_bytes(int64_t n, int64_t vocab); /* 0 on ba
 int slicegcn_embed_sort(const slicegcn_embed_desc *desc, const void *ids, int32_t *order, int32_t *starts, void *ws, size_t ws_bytes,
                         void *stream);
 
-/* dTable[t, :] = scale * sum of dOut[i, :] over the positions i of token t, in fp32 over at most 64 positions at a time and in fp64 over those sums, in a fixed order; every row of dTable is written (zeros without positions), or with ACCUMULATE added to (rows without positions are
- * not touched).  order, starts: from slicegcn_embed_sort with the same n and vocab.  An entry outside [0, n) is skipped. */
+/* dTable[t, :] = scale * sum of dOut[i, :] over the positions i of token t, in fp32 over at most 64 positions at a time and in fp64
+ * over those sums, in a fixed order; every row of dTable is written (zeros without positions), or with ACCUMULATE added to (rows
+ * without positions are not touched).  order, starts: from slicegcn_embed_sort with the same n and vocab.  An entry outside [0, n)
+ * is skipped.  EINVAL, ERANGE as above; EWORKSPACE. */
 size_t slicegcn_embed_bwd_workspace_bytes(int64_t n, int32_t width); /* 0 on bad input, and where none is needed */
 int slicegcn_embed_bwd(const slicegcn_embed_desc *desc, const int32_t *order, const int32_t *starts, const void *dOut, int64_t ldo,
                        void *dTable, int64_t ldt, void *ws, size_t ws_bytes, void *stream);
@@ -133,8 +135,8 @@ int slicegcn_resnorm_fwd(const slicegcn_resnorm_desc *desc, const slicegcn_resno
                          void *stream);
 
 /* Backward: from dh, du and what the forward pass read (x, y, gate, parameters, stats).  Column sums (gradients of the parameters)
- * run in fp32 over the rows a workgroup takes and in fp64 over workgroups.  EINVAL as for the forward, and for a gradient of something absent,
- * stats absent; EWORKSPACE when a parameter's gradient is wanted and ws is NULL or too small. */
+ * run in fp32 over the rows a workgroup takes and in fp64 over workgroups.  EINVAL as for the forward, and for a gradient of
+ * something absent, stats absent; EWORKSPACE when a parameter's gradient is wanted and ws is NULL or too small. */
 size_t slicegcn_resnorm_bwd_workspace_bytes(int64_t n, int32_t width); /* 0 on bad input */
 int slicegcn_resnorm_bwd(const slicegcn_resnorm_desc *desc, const slicegcn_resnorm_params *params, const slicegcn_resnorm_io *io,
                          const slicegcn_resnorm_grads *grads, void *ws, size_t ws_bytes, void *stream);
@@ -161,8 +163,8 @@ size_t slicegcn_global_norm_workspace_bytes(const slicegcn_tensor *tensors, int3
 int slicegcn_global_norm(const slicegcn_tensor *tensors, int32_t count, int32_t kind, double max_norm, float *norm, float *factor,
                          void *ws, size_t ws_bytes, void *stream);
 
-/* The same (norm and factor may each be NULL), and to[i] = factor * from[i].  `to` has the counts and types of `from`; NULL, or a tensor at the same
- * address: in place (then nothing is written where factor is 1).  Tensors overlap in no other way. */
+/* The same (norm and factor may each be NULL), and to[i] = factor * from[i].  `to` has the counts and types of `from`; NULL, or a
+ * tensor at the same address: in place (then nothing is written where factor is 1).  Tensors overlap in no other way. */
 int slicegcn_clip(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_t count, int32_t kind, double max_norm, float *norm,
                   float *factor, void *ws, size_t ws_bytes, void *stream);
 
