@@ -25,7 +25,8 @@ from .stack import Classifier, FeatureFusion, GraphedStep, Optimizer, SliceStack
 
 class Embedding:
     """Rows of a learned table, looked up by the nodes' tokens.  The tokens stay the same in every epoch, so they are sorted once;
-    call ``set_tokens`` for new ones."""
+    call ``set_tokens`` for new ones.  The embedding keeps its own copy of them, in memory that stays where it is: a captured pass
+    finds new tokens there, as it finds their order."""
 
     def __init__(self, ids: torch.Tensor, vocab: int, width: int, scale: float | None = None, pad: int | None = None):
         self.vocab, self.pad = vocab, pad
@@ -34,6 +35,7 @@ class Embedding:
         n = ids.numel()
         self.table, self.dtable = (torch.zeros((vocab, width), **f32) for _ in range(2))
         self.X = torch.empty((n, width), **f32)
+        self.ids = torch.empty(n, dtype=torch.int64, device=ids.device)  # 64 bits hold any token of either type
         self.order = torch.empty(n, dtype=torch.int32, device=ids.device)
         self.starts = torch.empty(vocab + 1, dtype=torch.int32, device=ids.device)
         self.ws = torch.empty(max(B.slicegcn_embed_sort_workspace_bytes(n, vocab), B.slicegcn_embed_bwd_workspace_bytes(n, width)),
@@ -41,7 +43,12 @@ class Embedding:
         self.set_tokens(ids)
 
     def set_tokens(self, ids: torch.Tensor):
-        self.ids = ids.contiguous()
+        """As many tokens as before, int32 or int64."""
+        if ids.dtype not in (torch.int32, torch.int64) or ids.device != self.ids.device:
+            raise TypeError(f"ids: expected int32 or int64 on {self.ids.device}, not {ids.dtype} on {ids.device}")
+        if ids.numel() != self.ids.numel():
+            raise ValueError(f"expected {self.ids.numel()} tokens, not {ids.numel()}")
+        self.ids.copy_(ids.reshape(-1))
         B.slicegcn_embed_sort(self.ids, self.vocab, self.order, self.starts, self.ws, pad=self.pad)
 
     def forward(self) -> torch.Tensor:

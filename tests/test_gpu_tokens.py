@@ -151,3 +151,24 @@ def test_new_tokens_take_effect():
     want, _ = embed_grad(new, dX.cpu().to(F64), 40, tr.emb.scale, None)
     assert_close(tr.emb.dtable.cpu().numpy(), want.numpy(), "table", tol=1e-6)
     g.destroy()
+
+
+@pytest.mark.parametrize("dtype", [torch.int64, torch.int32])
+def test_new_tokens_reach_a_replayed_graph(dtype):
+    """set_tokens between replayed epochs, from a tensor that is overwritten afterwards: the same bits as eager epochs on those tokens."""
+    w, vocab = synth.WORKLOADS["cfg1"], 300
+    (g1, eager), (g2, replay) = seeded_trainer(w, vocab, 2), seeded_trainer(w, vocab, 2, graph_replay=True)
+    for tr in (eager, replay):
+        tr.start(1e-2, 1e-4, 60, max_norm=0.5)
+    for t in range(5):
+        if t:
+            ids = torch.randint(0, vocab, (w.n_nodes,), generator=torch.Generator().manual_seed(t)).to(dtype).cuda()
+            eager.emb.set_tokens(ids.clone())
+            replay.emb.set_tokens(ids)
+            ids.fill_(-5)
+        a, b = eager.epoch(t), replay.epoch(t)
+        torch.cuda.synchronize()
+        assert a.isfinite().all() and torch.equal(a, b), t
+        assert torch.equal(eager.emb.X, replay.emb.X) and torch.equal(eager.emb.dtable, replay.emb.dtable) and torch.equal(eager.opt.P, replay.opt.P), t
+    g1.destroy()
+    g2.destroy()

@@ -159,3 +159,31 @@ def test_binding_refuses_what_is_no_device_tensor(L):  # noqa: F811
         B.slicegcn_resnorm_fwd(None, None, t, None)
     with pytest.raises(TypeError):
         B.TensorList([t])
+
+
+def test_new_tokens_go_into_the_embeddings_own_memory(L, monkeypatch):  # noqa: F811
+    """A captured pass reads the tokens through their address, and a caller may use its own tensor again: set_tokens copies, and a refused
+    call changes nothing."""
+    from paper_2408_11500_amd import tokens
+    sorted_ids = []
+    monkeypatch.setattr(tokens.B, "slicegcn_embed_sort", lambda ids, *a, **k: sorted_ids.append((ids.data_ptr(), ids.tolist())))
+    given = torch.tensor([3, 1, 2, 1])
+    emb = tokens.Embedding(given, 5, 8)
+    at = emb.ids.data_ptr()
+    given.fill_(4)
+    assert emb.ids.tolist() == [3, 1, 2, 1] and sorted_ids == [(at, [3, 1, 2, 1])]
+    for dtype in (torch.int32, torch.int64):
+        emb.set_tokens(torch.tensor([0, 4, -1, 9], dtype=dtype))
+        assert emb.ids.data_ptr() == at and emb.ids.tolist() == [0, 4, -1, 9]
+        emb.set_tokens(torch.tensor([[5, 0], [2, 0]], dtype=dtype)[:, 0].repeat(2))
+        assert emb.ids.data_ptr() == at and emb.ids.tolist() == [5, 2, 5, 2]
+    emb.set_tokens(torch.tensor([2**40, -2**40, 2**32 + 1, 0]))
+    assert emb.ids.tolist() == [2**40, -2**40, 2**32 + 1, 0]
+    calls = len(sorted_ids)
+    for bad, error in ((torch.tensor([1, 2, 3]), ValueError), (torch.zeros(5, dtype=torch.int64), ValueError), (torch.zeros(4), TypeError),
+                       (torch.zeros(4, dtype=torch.int16), TypeError), (torch.zeros(4, dtype=torch.int64, device="meta"), TypeError)):
+        with pytest.raises(error):
+            emb.set_tokens(bad)
+    assert emb.ids.data_ptr() == at and emb.ids.tolist() == [2**40, -2**40, 2**32 + 1, 0] and len(sorted_ids) == calls
+    with pytest.raises(TypeError):
+        tokens.Embedding(torch.zeros(4), 5, 8)
