@@ -504,7 +504,8 @@ __global__ __launch_bounds__(THREADS) void embed_grad_kernel(const GradArgs a, c
         }
         list[group][i] = e;
     }
-    const bool starts_before = place(a, head) < p0, goes_on = (int64_t)place(a, (int64_t)tail + 1) > (int64_t)p0 + count;
+    // one chunk holds whatever there is, and has no workspace for pieces: only starts that do not ascend could say that its last token goes on
+    const bool starts_before = place(a, head) < p0, goes_on = a.chunks > 1 && (int64_t)place(a, (int64_t)tail + 1) > (int64_t)p0 + count;
     wave_fence();
     int32_t now = (int32_t)head;
     bool first = starts_before; // the token `now` started before the chunk

@@ -294,3 +294,21 @@ def test_orders_that_do_not_belong_touch_nothing_outside():
     B.slicegcn_embed_bwd(order, starts, dout, d, grad_ws(n, width))
     kept = ((order >= 0) & (order < n)).cpu()
     assert d[:, 0].cpu().tolist() == [int(kept[a:b].sum()) for a, b in ((0, 50), (50, 120), (120, 200))]
+
+
+@pytest.mark.parametrize("n", [1, 5, 8, 9, 64, 200, 3000])
+@pytest.mark.parametrize("kind", ["drop", "descend", "far", "end early"])
+def test_starts_that_do_not_ascend_touch_nothing_outside(n, kind):
+    """Also without a workspace, where few positions need none."""
+    vocab, width = 4, 16
+    starts = {"drop": [0, n, n // 2, n, n // 2], "descend": [n, n - 1, n // 2, 1, 0], "far": [-2**31, 2**31 - 1, -5, n + 7, 2**31 - 1],
+              "end early": [0, 0, n + 1, 2**31 - 1, (n + 1) // 2]}[kind]
+    order = torch.arange(n, dtype=torch.int32, device="cuda")
+    need = B.slicegcn_embed_bwd_workspace_bytes(n, width)
+    assert (need == 0) == (n <= 8)
+    guarded = torch.full((vocab + 8, width), 7.0, device="cuda")
+    ws = torch.full((need + 512,), 7, dtype=torch.uint8, device="cuda")
+    B.slicegcn_embed_bwd(order, torch.tensor(starts, dtype=torch.int32, device="cuda"), torch.ones(n, width, device="cuda"), guarded[4:4 + vocab],
+                         ws[:need] if need else None)
+    torch.cuda.synchronize()
+    assert (guarded[:4] == 7.0).all() and (guarded[4 + vocab:] == 7.0).all() and (ws[need:] == 7).all()
