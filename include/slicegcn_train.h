@@ -27,7 +27,7 @@ extern "C" {
  * slice models.
  *   n            number of tokens, at most 2^31 - 1
  *   vocab        rows of the table, at most 2^31 - 2
- *   width        columns of the table and of the looked-up rows
+ *   width        columns of the table and of the looked-up rows, at most 2^31 - 1024 (in a lookup 2^26 - 1024)
  *   table_type   type of the table, or of its gradient;  row_type: type of the looked-up rows, or of their gradient
  *                (equal, or one of them SLICEGCN_F32)
  *   scale        factor of every looked-up row
@@ -50,7 +50,7 @@ typedef struct {
 
 /* out[i, 0:width] = scale * table[ids[i], 0:width].  out: n x width (ldo), table: vocab x width (ldt).
  * EINVAL: NULL pointer, sizes < 1 (n < 0), ld < width, unknown type or pair of types, unknown flag, scale not finite, misaligned
- * base; ERANGE: n or vocab too large. */
+ * base; ERANGE: n, vocab or width too large. */
 int slicegcn_embed_fwd(const slicegcn_embed_desc *desc, const void *ids, const void *table, int64_t ldt, void *out, int64_t ldo,
                        void *stream);
 

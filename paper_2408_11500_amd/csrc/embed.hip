@@ -20,6 +20,7 @@ namespace slicegcn {
 namespace {
 
 constexpr int THREADS = 256;
+constexpr int32_t MAX_WIDTH = INT32_MAX - 1023; // lanes count columns in 32 bits, up to 64 accesses of 8 past the end of a row
 
 // ---- lookup ---------------------------------------------------------------------------------------------------------------
 
@@ -657,6 +658,7 @@ int check_desc(const char *what, const slicegcn_embed_desc *d, bool rows)
     SG_REQUIRE((d->flags & ~(SLICEGCN_EMBED_IDS64 | SLICEGCN_EMBED_PAD | SLICEGCN_EMBED_ACCUMULATE)) == 0, SLICEGCN_EINVAL, "%s: unknown flag", what);
     if (!rows) return SLICEGCN_OK;
     SG_REQUIRE(d->width >= 1, SLICEGCN_EINVAL, "%s: width < 1", what);
+    SG_REQUIRE(d->width <= MAX_WIDTH, SLICEGCN_ERANGE, "%s: width = %d too large", what, d->width);
     SG_REQUIRE(known_type(d->table_type) && known_type(d->row_type), SLICEGCN_EINVAL, "%s: unknown type", what);
     SG_REQUIRE(d->table_type == d->row_type || d->table_type == SLICEGCN_F32 || d->row_type == SLICEGCN_F32, SLICEGCN_EINVAL,
                "%s: a table and rows in two different 16-bit types", what);
@@ -843,7 +845,7 @@ extern "C" int slicegcn_embed_sort(const slicegcn_embed_desc *d, const void *ids
 
 extern "C" size_t slicegcn_embed_bwd_workspace_bytes(int64_t n, int32_t width)
 {
-    if (n < 1 || n > INT32_MAX || width < 1) return 0;
+    if (n < 1 || n > INT32_MAX || width < 1 || width > MAX_WIDTH) return 0;
     const size_t a = GradPlan(n, width, grad_access(width, SLICEGCN_F32)).bytes(width), b = GradPlan(n, width, grad_access(width, SLICEGCN_BF16)).bytes(width);
     return a > b ? a : b;
 }

@@ -187,3 +187,13 @@ def test_new_tokens_go_into_the_embeddings_own_memory(L, monkeypatch):  # noqa: 
     assert emb.ids.data_ptr() == at and emb.ids.tolist() == [2**40, -2**40, 2**32 + 1, 0] and len(sorted_ids) == calls
     with pytest.raises(TypeError):
         tokens.Embedding(torch.zeros(4), 5, 8)
+
+
+@pytest.mark.parametrize("width", [2**31 - 1023, 2**31 - 512, 2**31 - 8, 2**31 - 1])
+def test_rows_whose_columns_pass_32_bits_are_refused(L, width):  # noqa: F811
+    """Lanes count columns in 32 bits, some of them past the end of a row."""
+    d = embed(width=width)
+    assert L.slicegcn_embed_bwd(d, ONE, ONE, ONE, width, ONE, width, None, 0, None) == B.ERANGE
+    assert L.slicegcn_embed_fwd(d, ONE, ONE, width, ONE, width, None) == B.ERANGE
+    assert L.slicegcn_embed_bwd_workspace_bytes(4, width) == 0
+    assert L.slicegcn_embed_bwd_workspace_bytes(100_000, width) == 0
