@@ -77,6 +77,24 @@ template <class T, int V, int K, bool MULTI, bool FULL, bool COUNTS> struct Row 
         return s;
     }
 
+    // Sum of squares.  A column that another lane counts is left out, not multiplied by 0: where it holds an infinity, that would be NaN.
+    template <class F> __device__ float lane_squares(F f) const
+    {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (!COUNTS && !at[k].on) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float v = f(k, j);
+                if constexpr (COUNTS) v = counts[k][j] != 0.f ? v : 0.f;
+                else if constexpr (!FULL) v = j >= at[k].skip ? v : 0.f;
+                s = fmaf(v, v, s);
+            }
+        }
+        return s;
+    }
+
     template <class F> __device__ float lane_sum(F f) const
     {
         float s = 0.f;
@@ -181,8 +199,7 @@ template <class T, int V, int K, bool MULTI, bool FULL, bool COUNTS> struct Row 
             *mean = s[0] * a.inv_width;
         }
         const float m = *mean;
-        const auto apart = [&](int k, int j) { return v[k][j] - m; };
-        s[0] = lane_dot(apart, apart);
+        s[0] = lane_squares([&](int k, int j) { return v[k][j] - m; });
         over_lanes(s);
         *factor = rsqrtf(s[0] * a.inv_width + a.eps); // one operation, off by a unit in the last place at most
     }

@@ -259,3 +259,26 @@ def test_same_bits_on_any_stream_and_in_graphs():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, outs)), i
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("width", [3, 9, 66, 100, 257, 602, 1001, 4097, 5001, 8193])
+def test_one_infinity_in_a_row(width, kind):
+    """A root mean square of infinity leaves zeros and, in the infinity's own column, NaN, wherever in the row it stands: also in columns that two
+    lanes hold, where a row does not fill its lanes."""
+    places = sorted({0, 1, width // 2, *range(max(width - 17, 0), width)})
+    v = torch.randn((len(places), width), generator=torch.Generator().manual_seed(width)).to(TYPES[kind])
+    for row, place in enumerate(places):
+        v[row, place] = float("inf") if row % 2 else float("-inf")
+    want = torch.zeros(v.shape)
+    want[v.isinf()] = float("nan")
+    u = torch.full_like(v, 5.0, device="cuda")
+    same = lambda got: torch.equal(got.cpu().float().nan_to_num(9.0, 8.0, 7.0), want.nan_to_num(9.0))
+    B.slicegcn_resnorm_fwd(v.cuda(), None, None, u, pre=RMS)
+    assert same(u), "before a block"
+    B.slicegcn_resnorm_fwd(None, v.cuda(), u, None, post=RMS)
+    assert same(u), "after a block"
+    B.slicegcn_resnorm_fwd(None, v.cuda(), u, None, post=RMS, post_b=torch.zeros(width, device="cuda"), post_w=torch.ones(width, device="cuda"))
+    assert same(u), "with a bias"
+    B.slicegcn_resnorm_fwd(v.cuda(), None, None, u, pre=LAYER)
+    assert u.isnan().all(), "layer norm"
