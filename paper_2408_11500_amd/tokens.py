@@ -63,20 +63,24 @@ class Embedding:
 
 class BlockNorm:
     """What lies between two blocks: the norm after one, its gate (a learned value per column) and residual, the norm before the
-    next.  ``post`` = NORM_NONE and no block output: the norm before the first block."""
+    next.  ``block`` = False with ``post`` = NORM_NONE and no gate: the norm before the first block, which takes no block output."""
 
-    def __init__(self, n: int, width: int, post: int = B.NORM_RMS, pre: int = B.NORM_RMS, gated: bool = True, device="cuda"):
+    def __init__(self, n: int, width: int, post: int = B.NORM_RMS, pre: int = B.NORM_RMS, gated: bool = True, device="cuda",
+                 block: bool = True):
         f32 = dict(dtype=torch.float32, device=device)
         self.post, self.pre = post, pre
         names = (["post_w"] if post != B.NORM_NONE else []) + (["pre_w"] if pre != B.NORM_NONE else []) + (["gate"] if gated else [])
         self.params = {name: torch.ones(width, **f32) for name in names}
         self.grads = {"d" + name: torch.zeros(width, **f32) for name in names}
         self.h = torch.empty((n, width), **f32) if post != B.NORM_NONE or gated else None
-        self.u, self.dx, self.dy = (torch.empty((n, width), **f32) for _ in range(3))
+        self.u, self.dx = (torch.empty((n, width), **f32) for _ in range(2))
+        self.dy = torch.empty((n, width), **f32) if block else None
         self.stats = torch.empty((n, 4), **f32)
         self.ws = torch.empty(B.slicegcn_resnorm_bwd_workspace_bytes(n, width), dtype=torch.uint8, device=device)
 
     def forward(self, x: torch.Tensor, y: torch.Tensor | None):
+        if y is not None and self.dy is None:
+            raise ValueError("a norm before the first block takes no block output")
         B.slicegcn_resnorm_fwd(x, y, self.h, self.u, post=self.post, pre=self.pre, stats=self.stats, **self.params)
         return self.h, self.u
 
@@ -98,7 +102,8 @@ class TokenTrainer:
         dev = ids.device
         self.labels = labels.to(torch.int32)
         self.emb = Embedding(ids, vocab, width, pad=pad)
-        self.norms = [BlockNorm(n, width, post=B.NORM_NONE, gated=False, device=dev)] + [BlockNorm(n, width, device=dev) for _ in range(blocks)]
+        self.norms = [BlockNorm(n, width, post=B.NORM_NONE, gated=False, device=dev, block=False)]
+        self.norms += [BlockNorm(n, width, device=dev) for _ in range(blocks)]
         self.ffs = [FeatureFusion(n, width, slice_hidden, device=dev) for _ in range(blocks)]
         self.stacks = [SliceStack(graph, n, k, slice_hidden, slice_hidden, layers, device=dev, shared_input=ff.Xff) for ff in self.ffs]
         self.cls = Classifier(n, width, hidden, classes, device=dev)

@@ -197,3 +197,13 @@ def test_rows_whose_columns_pass_32_bits_are_refused(L, width):  # noqa: F811
     assert L.slicegcn_embed_fwd(d, ONE, ONE, width, ONE, width, None) == B.ERANGE
     assert L.slicegcn_embed_bwd_workspace_bytes(4, width) == 0
     assert L.slicegcn_embed_bwd_workspace_bytes(100_000, width) == 0
+
+
+def test_a_norm_without_a_block_keeps_no_gradient_of_one(L):  # noqa: F811
+    from paper_2408_11500_amd.tokens import BlockNorm
+    first = BlockNorm(10, 8, post=B.NORM_NONE, gated=False, device="cpu", block=False)
+    assert first.dy is None
+    with pytest.raises(ValueError):
+        first.forward(torch.zeros(10, 8), torch.zeros(10, 8))
+    for kw in (dict(), dict(post=B.NORM_NONE, gated=False)):
+        assert BlockNorm(10, 8, device="cpu", **kw).dy.shape == (10, 8)
