@@ -72,17 +72,17 @@ class BlockNorm:
         names = (["post_w"] if post != B.NORM_NONE else []) + (["pre_w"] if pre != B.NORM_NONE else []) + (["gate"] if gated else [])
         self.params = {name: torch.ones(width, **f32) for name in names}
         self.grads = {"d" + name: torch.zeros(width, **f32) for name in names}
-        self.h = torch.empty((n, width), **f32) if post != B.NORM_NONE or gated else None
         self.u, self.dx = (torch.empty((n, width), **f32) for _ in range(2))
-        self.dy = torch.empty((n, width), **f32) if block else None
+        self.h, self.dy = (torch.empty((n, width), **f32) if block else None for _ in range(2))
         self.stats = torch.empty((n, 4), **f32)
         self.ws = torch.empty(B.slicegcn_resnorm_bwd_workspace_bytes(n, width), dtype=torch.uint8, device=device)
 
     def forward(self, x: torch.Tensor, y: torch.Tensor | None):
         if y is not None and self.dy is None:
             raise ValueError("a norm before the first block takes no block output")
-        B.slicegcn_resnorm_fwd(x, y, self.h, self.u, post=self.post, pre=self.pre, stats=self.stats, **self.params)
-        return self.h, self.u
+        h = self.h if y is not None else None  # without a block h is x itself
+        B.slicegcn_resnorm_fwd(x, y, h, self.u, post=self.post, pre=self.pre, stats=self.stats, **self.params)
+        return h, self.u
 
     def backward(self, x: torch.Tensor, y: torch.Tensor | None, dh: torch.Tensor | None, du: torch.Tensor):
         B.slicegcn_resnorm_bwd(x, y, self.stats, dh, du, self.dx, self.dy if y is not None else None, self.ws, post=self.post,

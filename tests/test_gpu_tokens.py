@@ -172,3 +172,19 @@ def test_new_tokens_reach_a_replayed_graph(dtype):
         assert torch.equal(eager.emb.X, replay.emb.X) and torch.equal(eager.emb.dtable, replay.emb.dtable) and torch.equal(eager.opt.P, replay.opt.P), t
     g1.destroy()
     g2.destroy()
+
+
+def test_a_plain_residual_between_blocks():
+    """Neither norm nor gate after the block: h = x + y, and its gradient reaches both."""
+    from paper_2408_11500_amd.tokens import BlockNorm
+    n, width = 50, 24
+    norm = BlockNorm(n, width, post=B.NORM_NONE, gated=False)
+    x, y, dh, du = (torch.randn(n, width, device="cuda") for _ in range(4))
+    h, u = norm.forward(x, y)
+    assert torch.equal(h, x + y)
+    dx, dy = norm.backward(x, y, dh, du)
+    want = Resnorm(x.cpu().to(F64), y.cpu().to(F64), pre=B.NORM_RMS)
+    g, size = want.backward(dh.cpu().to(F64), du.cpu().to(F64))
+    assert_close(u.cpu().numpy(), want.u.numpy(), "u", tol=1e-5)
+    for got, name in ((dx, "dx"), (dy, "dy")):
+        assert_close(got.cpu().numpy(), g[name].numpy(), name, tol=1e-5)

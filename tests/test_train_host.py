@@ -207,3 +207,19 @@ def test_a_norm_without_a_block_keeps_no_gradient_of_one(L):  # noqa: F811
         first.forward(torch.zeros(10, 8), torch.zeros(10, 8))
     for kw in (dict(), dict(post=B.NORM_NONE, gated=False)):
         assert BlockNorm(10, 8, device="cpu", **kw).dy.shape == (10, 8)
+
+
+def test_a_residual_without_norm_and_gate_is_handed_on(L, monkeypatch):  # noqa: F811
+    """The next block's residual is x + y, whether or not a norm or a gate shapes y."""
+    from paper_2408_11500_amd import tokens
+    calls = []
+    monkeypatch.setattr(tokens.B, "slicegcn_resnorm_fwd", lambda x, y, h, u, **k: calls.append(h))
+    x, y = torch.zeros(10, 8), torch.zeros(10, 8)
+    for post in (B.NORM_NONE, B.NORM_RMS):
+        for gated in (False, True):
+            h, u = tokens.BlockNorm(10, 8, post=post, gated=gated, device="cpu").forward(x, y)
+            assert h is not None and h.shape == x.shape and calls[-1] is h, (post, gated)
+    h, u = tokens.BlockNorm(10, 8, post=B.NORM_NONE, gated=False, device="cpu", block=False).forward(x, None)
+    assert h is None and calls[-1] is None
+    h, u = tokens.BlockNorm(10, 8, post=B.NORM_NONE, gated=False, device="cpu").forward(x, None)
+    assert h is None and calls[-1] is None
