@@ -149,3 +149,83 @@ def test_scaled_adam_step(wd):
         B.slicegcn_adam_step(b[0], (0.25 * g).cuda(), b[1], b[2], 1e-2, step, weight_decay=wd)  # a power of two: the same product
     for s, t in zip(a, b):
         assert torch.equal(s, t)
+
+
+def mixed(tiles, gen, empty=True):
+    """Tensors of all types, sizes on, just below and just above whole tiles of 16 KB, empty ones among them; `tiles` of them in all, about."""
+    types, out, k = ["f32", "bf16", "f16"], [], 0
+    while tiles > 0:
+        kind = types[k % 3]
+        size = {"f32": 4096, "bf16": 8192, "f16": 8192}[kind]
+        share = min(tiles, 1 + k * 37 % 211)
+        out.append((torch.randn(share * size + (0, -1, 1, 7)[k % 4], generator=gen, device="cuda") * 0.1).to(TYPES[kind]))
+        if empty and k % 5 == 2:
+            out.append(torch.empty(0, dtype=TYPES[kind], device="cuda"))
+        tiles -= share
+        k += 1
+    return out
+
+
+@pytest.mark.parametrize("tiles", [2049, 2500, 5120, 9001])
+@pytest.mark.parametrize("kind", [B.NORM_TWO, B.NORM_MAX])
+def test_workgroups_that_take_tiles_in_turn(tiles, kind):
+    """More tiles than a launch has workgroups: each goes over tensors of several types, forwards for the norm and back for the scaling."""
+    gen = torch.Generator(device="cuda").manual_seed(tiles)
+    tensors = mixed(tiles, gen)
+    assert len(tensors) <= 144  # one launch
+    lst = B.TensorList(tensors)
+    if kind == B.NORM_TWO:
+        want = math.sqrt(math.fsum(float((t.to(F64) ** 2).sum()) for t in tensors))
+    else:
+        want = max(float(t.to(F64).abs().max()) for t in tensors if t.numel())
+    f = min(1.0, 0.37 / want)
+    outs, copies = [torch.full_like(t, 5.0) for t in tensors], [t.clone() for t in tensors]
+    norm, factor = scalars()
+    B.slicegcn_clip(lst, B.TensorList(outs), 0.37, norm, ws_for(lst), factor=factor, kind=kind)
+    assert abs(float(norm) - want) <= (1 + 1e-6) * U * want
+    assert abs(float(factor) - f) <= (1 + 1e-6) * U * f
+    n2, f2 = scalars()
+    B.slicegcn_global_norm(lst, n2, ws_for(lst), max_norm=0.37, factor=f2, kind=kind)
+    assert torch.equal(n2, norm) and torch.equal(f2, factor)
+    B.slicegcn_clip(B.TensorList(copies), None, 0.37, None, ws_for(lst), kind=kind)
+    for i, (t, o, c) in enumerate(zip(tensors, outs, copies)):
+        assert torch.equal(o, (factor * t.float()).to(t.dtype)), i  # one fp32 product, rounded once
+        assert torch.equal(c, o), i
+
+
+def test_one_large_value_is_found_in_every_tile():
+    """The largest absolute value in turn in the first and the last element of tensors that lie in any workgroup's share."""
+    tensors = mixed(3000, torch.Generator(device="cuda").manual_seed(5))
+    lst = B.TensorList(tensors)
+    norm, _ = scalars()
+    ws = ws_for(lst)
+    for t in tensors:
+        for place in (0, t.numel() // 2, t.numel() - 1) if t.numel() else ():
+            was = t[place].clone()
+            t[place] = -100.0
+            B.slicegcn_global_norm(lst, norm, ws, kind=B.NORM_MAX)
+            assert float(norm) == 100.0
+            t[place] = was
+
+
+@pytest.mark.parametrize("launches", [1, 2])
+def test_lists_beyond_the_caches(launches):
+    """256 MB and more: stored past the caches, in one launch and in two."""
+    gen = torch.Generator(device="cuda").manual_seed(launches)
+    if launches == 1:
+        tensors = mixed(12_000, gen) + [torch.randn(20_000_003, generator=gen, device="cuda")]
+        assert len(tensors) <= 144
+    else:
+        tensors = [(torch.randn(420_001 + 64 * i, generator=gen, device="cuda") * 0.1).to(TYPES[("f32", "bf16", "f16")[i % 3]]) for i in range(250)]
+    assert sum(t.numel() * t.element_size() for t in tensors) > 256 << 20
+    lst = B.TensorList(tensors)
+    want = math.sqrt(math.fsum(float((t.to(F64) ** 2).sum()) for t in tensors))
+    outs = [torch.full_like(t, 5.0) for t in tensors]
+    norm, factor = scalars()
+    B.slicegcn_clip(lst, B.TensorList(outs), 1.0, norm, ws_for(lst), factor=factor)
+    assert abs(float(norm) - want) <= (1 + 1e-6) * U * want
+    assert abs(float(factor) - 1 / want) <= (1 + 1e-6) * U / want
+    scaled = [(factor * t.float()).to(t.dtype) for t in tensors]
+    B.slicegcn_clip(lst, None, 1.0, None, ws_for(lst))
+    for i, (w, o, t) in enumerate(zip(scaled, outs, tensors)):
+        assert torch.equal(o, w) and torch.equal(t, w), i
