@@ -312,3 +312,64 @@ def test_starts_that_do_not_ascend_touch_nothing_outside(n, kind):
                          ws[:need] if need else None)
     torch.cuda.synchronize()
     assert (guarded[:4] == 7.0).all() and (guarded[4 + vocab:] == 7.0).all() and (ws[need:] == 7).all()
+
+
+@pytest.mark.parametrize("table,row", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("f16", "f32")])
+@pytest.mark.parametrize("kind", ["skewed", "hot"])
+def test_gradient_beyond_the_caches(kind, table, row):
+    """A table of 256 MB and more in whole lines: rows without tokens, with few and with many positions, stored past the caches."""
+    vocab, width, n = (560_000, 128, 150_001) if table == "f32" else (560_000, 256, 150_001)
+    gen = torch.Generator().manual_seed(n)
+    ids = tokens(gen, n, vocab, kind)
+    ids[: 50_000 : 2] = 77  # cut by every chunk
+    ids = ids[torch.randperm(n, generator=gen)].cuda()
+    order, starts = sort(ids, vocab, pad=3)
+    dout = torch.randint(-2, 3, (n, width), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(TYPES[row])
+    d = torch.full((vocab, width), 5.0, dtype=TYPES[table], device="cuda")
+    assert d.numel() * d.element_size() >= 256 << 20 and d.data_ptr() % 128 == 0 and width * d.element_size() % 128 == 0
+    B.slicegcn_embed_bwd(order, starts, dout, d, grad_ws(n, width))
+    want = torch.zeros((vocab, width), dtype=F64, device="cuda")
+    want.index_add_(0, ids, dout.to(F64))
+    want[3] = 0
+    # whole numbers below 2^24: sums are exact, and rounded once
+    assert want.abs().max() < 2**24 and torch.equal(d, want.to(torch.float32).to(TYPES[table]))
+
+
+def test_gradient_with_rows_not_in_whole_lines_beyond_the_caches():
+    vocab, width, n = 700_000, 100, 20_000
+    ids = torch.randint(0, vocab, (n,), device="cuda")
+    order, starts = sort(ids, vocab)
+    dout = torch.randint(-2, 3, (n, width), device="cuda").float()
+    d = torch.full((vocab, width), 5.0, device="cuda")
+    B.slicegcn_embed_bwd(order, starts, dout, d, grad_ws(n, width))
+    want = torch.zeros((vocab, width), device="cuda")
+    want.index_add_(0, ids, dout)
+    assert torch.equal(d, want)
+
+
+@pytest.mark.parametrize("n,vocab,width,table,out", [(1_050_003, 900, 260, "f32", "f32"), (540_001, 3000, 520, "bf16", "bf16"), (8_500_000, 50, 16, "f32", "f32")])
+def test_lookups_of_more_rows_than_one_turn_of_the_workgroups(n, vocab, width, table, out):
+    """More than 65 536 workgroups' rows, results of 256 MB and more, and tokens and rows in the last turn."""
+    tab = torch.randn(vocab, width, device="cuda").to(TYPES[table])
+    ids = torch.randint(0, vocab, (n,), device="cuda")
+    ids[-1], ids[-2] = vocab - 1, -1
+    o = torch.full((n, width), 5.0, dtype=TYPES[out], device="cuda")
+    B.slicegcn_embed_fwd(ids, tab, o, scale=2.0, pad=-1)
+    step = 1 << 20
+    for r in range(0, n, step):
+        i = ids[r:r + step]
+        want = tab[i.clamp_min(0)] * 2
+        want[i < 0] = 0
+        assert torch.equal(o[r:r + step], want), r
+
+
+def test_starts_of_more_rows_than_one_turn_of_the_workgroups():
+    """A vocabulary of more than 65 536 workgroups' entries, behind a sort in tiles."""
+    vocab, n = 17_000_000, 40_003
+    gen = torch.Generator().manual_seed(4)
+    ids = torch.randint(0, vocab, (n,), generator=gen)
+    ids[:3] = torch.tensor([vocab - 1, 0, 65_536 * 256])
+    order, starts = sort(ids.cuda(), vocab)
+    want = torch.sort(ids, stable=True)
+    assert torch.equal(starts.cpu().long(), torch.searchsorted(want.values, torch.arange(vocab + 1)))
+    assert torch.equal(order.cpu().long(), want.indices)
