@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2408_11500_amd import binding as B
-from train_util import F64, LAYER, NONE, RMS, TYPES, U, Resnorm, assert_within, rows
+from train_util import F64, LAYER, NONE, RMS, TYPES, U, Resnorm, assert_within, half_step, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -282,3 +282,68 @@ def test_one_infinity_in_a_row(width, kind):
     assert same(u), "with a bias"
     B.slicegcn_resnorm_fwd(v.cuda(), None, None, u, pre=LAYER)
     assert u.isnan().all(), "layer norm"
+
+
+def large(n, width, kind, norm, gate, sigmoid, seed=0):
+    """Operands of a call made on the device: rows of x, y, dh, du, and the parameters."""
+    gen = torch.Generator(device="cuda").manual_seed(seed + n + width)
+    values = lambda *shape: torch.randn(shape, generator=gen, device="cuda")
+    t = {k: values(n, width).to(TYPES[kind]) for k in ("x", "y", "dh", "du")}
+    p = {"post_w": 1 + 0.3 * values(width), "pre_w": 1 + 0.3 * values(width)}
+    if norm == LAYER:
+        p.update(post_b=0.3 * values(width), pre_b=0.3 * values(width))
+    p["gate"] = values(n, width).to(TYPES[kind]) if gate == "matrix" else 0.5 + 0.5 * values(width)
+    return t, p, dict(post=norm, pre=norm, sigmoid=sigmoid, residual=0.75, eps=1e-3)
+
+
+def run_large(t, p, args, params=True):
+    """All results of the forward and the backward pass."""
+    n, width = t["x"].shape
+    out = {k: torch.full_like(t["x"], float("nan")) for k in ("h", "u", "dx", "dy")}
+    out.update({"d" + k: torch.full_like(v, float("nan")) for k, v in p.items() if params or v.dim() == 2})
+    stats = torch.full((n, 4), float("nan"), device="cuda")
+    ws = torch.empty(B.slicegcn_resnorm_bwd_workspace_bytes(n, width), dtype=torch.uint8, device="cuda")
+    B.slicegcn_resnorm_fwd(t["x"], t["y"], out["h"], out["u"], stats=stats, **p, **args)
+    B.slicegcn_resnorm_bwd(t["x"], t["y"], stats, t["dh"], t["du"], out["dx"], out["dy"], ws,
+                           **{k: v for k, v in out.items() if k not in ("h", "u", "dx", "dy")}, **p, **args)
+    return out
+
+
+# Rows so many that every lane group of the backward pass takes more than 32 of them, twice what it adds up before it sets a sum aside (on rows of up
+# to 4096 columns); above that, several for every workgroup.
+MANY = [("f32", 256, RMS, "column", 70_000), ("f32", 64, LAYER, "column", 280_001), ("bf16", 100, LAYER, "column", 280_001), ("bf16", 64, RMS, "matrix", 560_001),
+        ("f32", 602, LAYER, "matrix", 36_001), ("f32", 1500, RMS, "column", 8_800), ("f16", 2048, RMS, "column", 17_600), ("bf16", 2500, LAYER, "matrix", 8_801),
+        ("f32", 3, LAYER, "column", 1_120_001), ("f32", 5000, RMS, "column", 8_800), ("bf16", 5000, LAYER, "column", 8_800), ("bf16", 8192, LAYER, "matrix", 2_000)]
+MANY += [(kind, width, norm, "column", 801) for kind in ("f32", "bf16") for width in (8193, 16_384) for norm in (RMS, LAYER)]
+
+
+@pytest.mark.parametrize("kind,width,norm,gate,n", MANY)
+def test_sums_over_many_rows_in_turn(kind, width, norm, gate, n):
+    # A column's sum: 16 rows and 3 sums of those in a lane, up to 64 rows beside each other; the rest as above: within C
+    t, p, args = large(n, width, kind, norm, gate, gate == "matrix")
+    got = run_large(t, p, args)
+    with torch.device("cuda"):
+        f64 = {k: v.to(F64) for k, v in {**t, **p}.items()}
+        dh, du = f64.pop("dh"), f64.pop("du")
+        w = Resnorm(**f64, **args)
+        want, size = w.backward(dh, du)
+        want.update(h=w.h, u=w.u)
+        size.update(h=w.h_size, u=w.u_size)
+        for name, g in got.items():
+            tol = C * U * size[name].reshape(g.shape) + half_step(want[name].reshape(g.shape), g.dtype)
+            err = (g.to(F64) - want[name].reshape(g.shape)).abs()
+            assert bool((err <= tol).all()), f"{name}: {float((err / tol).max()):.2f} of the bound"
+
+
+@pytest.mark.parametrize("kind,width,norm,gate", [("f32", 256, RMS, "column"), ("bf16", 100, LAYER, "column"), ("f32", 602, LAYER, "matrix"), ("bf16", 64, RMS, "matrix"),
+                                                  ("f32", 3, RMS, "column"), ("bf16", 2500, RMS, "column"), ("f16", 5000, LAYER, "column"), ("f32", 9000, RMS, "column")])
+def test_rows_beyond_the_caches_have_the_bits_of_smaller_calls(kind, width, norm, gate):
+    """Results of 256 MB and more are stored past the caches; rows do not depend on each other."""
+    n = (256 << 20) // (2 * width * (4 if kind == "f32" else 2)) + 1001
+    t, p, args = large(n, width, kind, norm, gate, gate == "matrix")
+    whole = run_large(t, p, args, params=False)
+    for a in range(0, n, n // 3 + 1):
+        part = slice(a, a + n // 3 + 1)
+        got = run_large({k: v[part] for k, v in t.items()}, {k: v[part] if v.dim() == 2 else v for k, v in p.items()}, args, params=False)
+        for name, g in got.items():
+            assert torch.equal(g, whole[name][part]), (name, a)
