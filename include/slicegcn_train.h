@@ -153,7 +153,7 @@ typedef struct {
     void *data;
     int64_t count;
     int32_t type;
-    int32_t reserved; /* 0 */
+    int32_t reserved; /* set it to 0; not read */
 } slicegcn_tensor;
 
 size_t slicegcn_global_norm_workspace_bytes(const slicegcn_tensor *tensors, int32_t count); /* 0 on bad input */

@@ -8,8 +8,8 @@
 //
 // The lookup is bound by the bytes it stores (2.4 M rows of 100 fp32 columns from a bf16 table 262 us, 4.3 TB/s of what has to be moved; the rows lie 128
 // apart, so that their last lines are written in part), the gradient by the bytes of dOut and dTable where those are many (65 536 rows of
-// 2048 bf16 columns into 128 000: 61 us for the sums, 85 for their join and 105 000 rows of zeros) and by the launches of the sort
-// where they are few (169 343 rows of 128 fp32 columns into 50 000: 35 of 63 us).
+// 2048 bf16 columns into 128 000: 61 us for the sums, 84 for their join and 105 000 rows of zeros) and by the launches of the sort
+// where they are few (169 343 rows of 128 fp32 columns into 50 000: 37 of 70 us).
 #include "common.h"
 #include "values.h"
 
@@ -149,7 +149,7 @@ __device__ inline void rank_items(const uint32_t (&key)[ITEMS], const bool (&the
     __syncthreads();
 }
 
-// counts[wave][digit] -> number of the digit in the wavefronts before; returns the digit's total for thread = digit (two digits per thread)
+// counts[wave][digit] -> number of the digit in the wavefronts before; returns the total of the thread's digit
 __device__ inline void counts_before(uint16_t (*counts)[DIGITS], int bits, uint32_t (&total)[DIGITS / SORT_THREADS])
 {
 #pragma unroll
@@ -183,7 +183,7 @@ __device__ inline uint32_t lower_bound(const uint32_t *keys, uint32_t count, uin
     return lo;
 }
 
-// Up to SORT_TILE tokens: every workgroup sorts all of them in LDS and writes its part of starts, the first one also the order: one launch
+// Up to SMALL_SORT tokens: every workgroup sorts all of them in LDS and writes its part of starts, the first one also the order: one launch
 constexpr int STARTS_PER_BLOCK = 4 * SORT_THREADS;
 template <int ITEMS>
 __global__ __launch_bounds__(SORT_THREADS) void sort_small_kernel(const Tokens t, int bits, int passes, int32_t *__restrict__ order, int32_t *__restrict__ starts)
@@ -568,7 +568,8 @@ __global__ __launch_bounds__(THREADS) void embed_grad_kernel(const GradArgs a, c
 }
 
 // Tokens that several chunks share: the pieces are added where the token starts.  A wavefront takes a chunk; what has many pieces is
-// added by the whole workgroup.
+// added by the whole workgroup.  One workgroup adds all pieces of a token, for its tile of columns: 2 M rows of 64 fp32 columns into 30 tokens, the
+// most frequent of which holds a fifth, 104 us for the sums and 32 for their join.
 constexpr int JOIN_CHUNKS = THREADS / 64, JOIN_MANY = 64;
 template <class TT, int V, bool PAST>
 __global__ __launch_bounds__(THREADS) void embed_join_kernel(const GradArgs a, TT *__restrict__ dTable, uint32_t first_block, uint32_t join_blocks)

@@ -14,9 +14,12 @@
 // the parameters of its columns, the sums over its rows and the operands of the row after, which is what keeps the memory busy while
 // a row's sums go round its lanes.  Counters: every kernel moves its operands once (2 % more where rows are no whole lines).
 // Measured (a 4 GiB copy moves 6.2 TB/s): forward 169 343 rows of 256 fp32 columns 121 us, 5.7 TB/s; 16 384 of 4096 bf16 84 us, 6.4 TB/s.
-// Backward 16 384 of 4096 bf16 150 us, 5.4 TB/s; 232 965 of 602 fp32 with layer norms and a sigmoid gate per element 870 us, 5.2 TB/s; above 4096
-// columns 4.6 to 4.8 TB/s with RMS norms and 3.4 to 4.1 with layer norms or a gate per element (1024 threads have 128 registers each; their sums over rows lie in
-// LDS, in registers they spilled: 1.4 to 2.4); above 8192 0.5 to 2.6 TB/s, where twice the elements do not fit the registers.
+// Backward 16 384 of 4096 bf16 150 us, 5.4 TB/s; 232 965 of 602 fp32 with layer norms and a sigmoid gate per element 865 us, 5.2 TB/s.
+// Above 4096 columns a row takes 1024 threads of 128 registers each.  Forward: parameters are read again for every row and no row is requested ahead, fp32 rows
+// 5.1 to 5.4 TB/s with RMS norms and 3.3 to 4.6 with layer norms or a gate per element, 16-bit rows 3.4 to 3.7 and 2.0 to 3.2.  Backward: 5.0 to 5.4
+// TB/s with RMS norms and 3.0 to 4.6 with layer norms or a gate per element (sums over rows lie in LDS, in registers they spilled: 1.4 to 2.4).  Above 8192
+// columns, where twice the elements do not fit the registers: forward 4.3 to 5.6 TB/s in fp32 and 3.8 to 4.4 in 16 bits with RMS norms, else 1.5 to 2.8; backward
+// 1.5 to 2.9 with RMS norms, else 0.7 to 1.4.
 #pragma once
 
 #include "resnorm.h"
@@ -312,7 +315,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
 {
     __shared__ float shared[MULTI ? 64 : 1];
     // with a gate per element fp32 rows have no registers for the factors too: 232 965 rows of 602 with both 927 us, without the factors 855 (with a gate
-    // per column 824 and 884)
+    // per column 824 and 884; all before the sums over rows had their second level)
     Row<T, V, K, MULTI, FULL, !FULL && THREADS < 1024 && !(MATRIX && sizeof(T) == 4)> r(a, shared);
     // A workgroup of 1024 threads has registers for the parameters and a row ahead only without a gate per element, and in fp32 without layer norms and
     // biases.  TB/s at 8192 columns with / without: bf16 layer norms 4.1 / 2.9, with a gate per element 3.4 / 3.6; fp32 RMS norms 4.6 / 4.5, layer
