@@ -1,6 +1,7 @@
 // Norms before and after a block, fused with the block's gate and the residual: the calls, and the gradients of the parameters.
 #include "resnorm.h"
 
+#include <cfloat>
 #include <cmath>
 #include <initializer_list>
 
@@ -39,8 +40,9 @@ __global__ __launch_bounds__(FINAL_THREADS) void resnorm_params_kernel(const Arg
     if (a.gate_col) {
         s = a.gate_col[col];
         if (a.sigmoid) {
-            s = 1.0 / (1.0 + exp(-s));
-            slope = s * (1.0 - s);
+            const double e = exp(-s);
+            s = 1.0 / (1.0 + e);
+            slope = fmin(e, DBL_MAX) * s * s; // s (1 - s), in full where s is near 1
         }
     }
     if (d.post_w) d.post_w[col] = (float)(s * total[2][c]);

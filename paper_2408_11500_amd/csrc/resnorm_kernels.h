@@ -24,6 +24,8 @@
 
 #include "resnorm.h"
 
+#include <cfloat>
+
 namespace slicegcn {
 namespace resnorm {
 
@@ -209,6 +211,15 @@ template <class T, int V, int K, bool MULTI, bool FULL, bool COUNTS> struct Row 
 
     // s, the factor of p, from a gate
     __device__ float opened(float g) const { return a.sigmoid ? 1.f / (1.f + expf(-g)) : g; }
+
+    // The same, and q times the slope s (1 - s) of a sigmoid.  With e = exp(-g), 1 - s is e s: formed as 1 - s, it would keep nothing of an s near 1.
+    __device__ float opened(float g, float *q) const
+    {
+        if (!a.sigmoid) return g;
+        const float e = expf(-g), s = 1.f / (1.f + e);
+        *q *= fminf(e, FLT_MAX) * s * s; // an e of infinity has an s of 0
+        return s;
+    }
 };
 
 // Parameters of the lane's columns, held over all rows.  With a gate per column (or none) s * p is one product: yn * (s * post_w) + s * post_b.
@@ -395,9 +406,10 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
             r.each([&](int k, int j) {
                 yn[k][j] = EXTRA ? ((float)o.y.v[k][j] - o.st.x) * o.st.y : (float)o.y.v[k][j] * o.st.y;
                 if (MATRIX) {
-                    s[k][j] = r.opened((float)o.g.v[k][j]);
-                    q[k][j] = EXTRA ? fmaf(yn[k][j], p.w[k][j], p.b[k][j]) : yn[k][j] * p.w[k][j];
-                    h[k][j] = fmaf(s[k][j], q[k][j], h[k][j]);
+                    const float v = EXTRA ? fmaf(yn[k][j], p.w[k][j], p.b[k][j]) : yn[k][j] * p.w[k][j];
+                    q[k][j] = v;
+                    s[k][j] = r.opened((float)o.g.v[k][j], &q[k][j]);
+                    h[k][j] = fmaf(s[k][j], v, h[k][j]);
                 } else {
                     if (EXTRA) h[k][j] += p.b[k][j];
                     h[k][j] = fmaf(yn[k][j], p.w[k][j], h[k][j]);
@@ -438,7 +450,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(const Args a)
         if (!a.y.data) continue;
         if (MATRIX) {
             if (a.dgate.data && there) {
-                r.each([&](int k, int j) { q[k][j] *= a.sigmoid ? dH[k][j] * (s[k][j] * (1.f - s[k][j])) : dH[k][j]; });
+                r.each([&](int k, int j) { q[k][j] *= dH[k][j]; });
                 r.store(a.dgate, row, q);
             }
             r.each([&](int k, int j) { dH[k][j] *= s[k][j]; });

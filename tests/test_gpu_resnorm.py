@@ -347,3 +347,41 @@ def test_rows_beyond_the_caches_have_the_bits_of_smaller_calls(kind, width, norm
         got = run_large({k: v[part] for k, v in t.items()}, {k: v[part] if v.dim() == 2 else v for k, v in p.items()}, args, params=False)
         for name, g in got.items():
             assert torch.equal(g, whole[name][part]), (name, a)
+
+
+@pytest.mark.parametrize("width", [3, 64, 101, 602, 5000, 9000])
+@pytest.mark.parametrize("post", [NONE, LAYER])
+def test_gradients_of_gates_that_are_wide_open_or_shut(width, post):
+    """s (1 - s) of a gate near 1 keeps its relative precision, as that of one near 0 does."""
+    n = 40
+    gate = torch.linspace(-80, 80, n)[:, None] + torch.linspace(0, 4, width)[None]
+    gen = torch.Generator().manual_seed(width)
+    y, dh = (torch.randn((n, width), generator=gen) for _ in range(2))
+    h, dgate = (torch.empty((n, width), device="cuda") for _ in range(2))
+    stats = torch.empty((n, 4), device="cuda")
+    args = dict(post=post, gate=gate.cuda(), sigmoid=True, eps=1e-3)
+    B.slicegcn_resnorm_fwd(None, y.cuda(), h, None, stats=stats, **args)
+    B.slicegcn_resnorm_bwd(None, y.cuda(), stats, dh.cuda(), None, None, None, None, dgate=dgate, **args)
+    g = gate.to(F64)
+    small = torch.exp(-g.abs()) / (1 + torch.exp(-g.abs()))
+    p = y.to(F64) if post == NONE else (y.to(F64) - stats.cpu().to(F64)[:, :1]) * stats.cpu().to(F64)[:, 1:2]
+    size = p.abs() if post == NONE else (y.to(F64).abs() + stats.cpu().to(F64)[:, :1].abs()) * stats.cpu().to(F64)[:, 1:2]
+    # exp within a unit in the last place (2), its sum, quotient and products (4 roundings of it, each twice in the slope), three products more
+    bound = 16 * U * dh.to(F64).abs() * size * small * (1 - small)
+    assert_within(dgate, dh.to(F64) * p * small * (1 - small), bound, "dgate")
+
+
+def test_gradients_of_column_gates_that_are_wide_open_or_shut():
+    n, width = 40, 161
+    gate = torch.linspace(-80, 80, width)
+    gen = torch.Generator().manual_seed(width)
+    y, dh = (torch.randn((n, width), generator=gen) for _ in range(2))
+    h, dgate = torch.empty((n, width), device="cuda"), torch.full((width,), float("nan"), device="cuda")
+    stats = torch.empty((n, 4), device="cuda")
+    ws = torch.empty(B.slicegcn_resnorm_bwd_workspace_bytes(n, width), dtype=torch.uint8, device="cuda")
+    args = dict(gate=gate.cuda(), sigmoid=True)
+    B.slicegcn_resnorm_fwd(None, y.cuda(), h, None, stats=stats, **args)
+    B.slicegcn_resnorm_bwd(None, y.cuda(), stats, dh.cuda(), None, None, None, ws, dgate=dgate, **args)
+    small = torch.exp(-gate.to(F64).abs()) / (1 + torch.exp(-gate.to(F64).abs()))
+    terms = dh.to(F64) * y.to(F64) * small * (1 - small)
+    assert_within(dgate, terms.sum(0), C * U * terms.abs().sum(0), "dgate")
