@@ -14,7 +14,7 @@
 // the parameters of its columns, the sums over its rows and the operands of the row after, which is what keeps the memory busy while
 // a row's sums go round its lanes.  Counters: every kernel moves its operands once (2 % more where rows are no whole lines).
 // Measured (a 4 GiB copy moves 6.2 TB/s): forward 169 343 rows of 256 fp32 columns 121 us, 5.7 TB/s; 16 384 of 4096 bf16 84 us, 6.4 TB/s.
-// Backward 16 384 of 4096 bf16 150 us, 5.4 TB/s; 232 965 of 602 fp32 with layer norms and a sigmoid gate per element 865 us, 5.2 TB/s.
+// Backward 16 384 of 4096 bf16 150 us, 5.4 TB/s; 232 965 of 602 fp32 with layer norms and a sigmoid gate per element 870 us, 5.2 TB/s.
 // Above 4096 columns a row takes 1024 threads of 128 registers each.  Forward: parameters are read again for every row and no row is requested ahead, fp32 rows
 // 5.1 to 5.4 TB/s with RMS norms and 3.3 to 4.6 with layer norms or a gate per element, 16-bit rows 3.4 to 3.7 and 2.0 to 3.2.  Backward: 5.0 to 5.4
 // TB/s with RMS norms and 3.0 to 4.6 with layer norms or a gate per element (sums over rows lie in LDS, in registers they spilled: 1.4 to 2.4).  Above 8192
