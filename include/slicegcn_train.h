@@ -1,7 +1,7 @@
 /*
  * slicegcn_train.h -- operators for models that learn their inputs and are built from blocks, beside slicegcn.h (same
- * conventions): token embeddings with their gradient, norms before and after a block fused with its gate and residual, the norm
- * over all gradients with clipping, and the optimiser step that takes the clipping along.
+ * conventions): token embeddings with their gradient, norms before and after a block fused with its gate and residual, the products of a
+ * feed-forward block, the norm over all gradients with clipping, and optimiser steps that take the clipping along.
  *
  * Rows of tokens and of blocks are fp32, bf16 or fp16; parameters of norms, their gradients and all sums are fp32 or fp64, and a
  * result is rounded once, when it is stored.  An empty batch (n = 0) is a valid one.
@@ -173,10 +173,106 @@ int slicegcn_clip(const slicegcn_tensor *from, const slicegcn_tensor *to, int32_
 int slicegcn_adam_step_scaled(float *param, const float *grad, const float *factor, float *m, float *v, int64_t count, double lr,
                               double beta1, double beta2, double eps, double weight_decay, int32_t step, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Products of rows with a weight matrix, and feed-forward blocks.  Rows, weights and the weights' gradients are of one type (fp32, bf16 or
+ * fp16); biases and their gradients are fp32.  Sums are fp32 on the matrix cores, and a result is rounded once; fp32 operands go
+ * through them as three 16-bit terms each (a relative error of 2^-22 of a product at most; an operand that is infinite, or above 2^128 (1 - 2^-9), makes its
+ * sums NaN).
+ *   X: n x w_in;  W, Wg, Wu: w_in x w_out, contiguous;  all other matrices have n rows, of w_out columns (dX: of w_in)
+ *   act: SLICEGCN_ACT_NONE v;  _RELU max(v, 0);  _SILU v / (1 + exp(-v));  _GELU v Phi(v), Phi the normal distribution
+ * n = 0 is a valid batch (gradients of weights and biases are zeros then).  Outputs overlap nothing else of the call, with one exception: Y may
+ * lie in the rows of R (same address and leading dimension).
+ * ws: the size that the query for the same sizes and type returns; as everywhere, calls that may overlap have a workspace each (two captured
+ * graphs that may run at the same time too). */
+#define SLICEGCN_ACT_SILU 2
+#define SLICEGCN_ACT_GELU 3
+typedef struct {
+    int64_t n;    /* at most 2^31 - 1 */
+    int32_t w_in; /* both widths: at most 2^24 */
+    int32_t w_out;
+    int32_t type;
+    int32_t act;
+    double residual; /* factor of R; products alone */
+} slicegcn_product_desc;
+
+typedef struct {
+    void *data; /* NULL: absent */
+    int64_t ld;
+} slicegcn_matrix;
+
+/* P = X W + b;  Y = residual * R + act(P).  b, R, P may be NULL; P is kept for the backward pass, which needs it where there is an activation.
+ * EINVAL: NULL descriptor, X, W or Y; n < 0, widths < 1, ld < width, unknown type or activation, misaligned base, residual not finite, Y in
+ * the rows of X; ERANGE: n or a width too large; EWORKSPACE. */
+size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type); /* 0 on bad input, and where none is needed */
+int slicegcn_product_fwd(const slicegcn_product_desc *desc, const slicegcn_matrix *X, const void *W, const float *b, const slicegcn_matrix *R,
+                         const slicegcn_matrix *P, const slicegcn_matrix *Y, void *ws, size_t ws_bytes, void *stream);
+
+/* dP = dY * act'(P);  dX = dP W^T;  dW = X^T dP;  db = column sums of dP;  dR = residual * dY.  NULL outputs are not formed (the inputs that only they
+ * need may be NULL too).  dP is rounded to the rows' type before the products; db is formed from it unrounded.
+ * EINVAL, ERANGE, EWORKSPACE as above. */
+size_t slicegcn_product_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
+int slicegcn_product_bwd(const slicegcn_product_desc *desc, const slicegcn_matrix *X, const void *W, const slicegcn_matrix *P,
+                         const slicegcn_matrix *dY, const slicegcn_matrix *dX, void *dW, float *db, const slicegcn_matrix *dR, void *ws,
+                         size_t ws_bytes, void *stream);
+
+/* Gated projections, the first half of a feed-forward block (slicegcn_product_fwd is the second):
+ *   G = X Wg + bg;  U = X Wu + bu;  H = act(G) * U
+ * H is formed from G and U before they are rounded.  bg, bu may be NULL; G and U (both or neither) are kept for the backward pass. */
+size_t slicegcn_gated_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
+int slicegcn_gated_fwd(const slicegcn_product_desc *desc, const slicegcn_matrix *X, const void *Wg, const void *Wu, const float *bg,
+                       const float *bu, const slicegcn_matrix *G, const slicegcn_matrix *U, const slicegcn_matrix *H, void *ws,
+                       size_t ws_bytes, void *stream);
+
+/* dG = dH * U * act'(G);  dU = dH * act(G);  dX = dG Wg^T + dU Wu^T;  dWg = X^T dG;  dWu = X^T dU;  dbg, dbu: column sums.  NULL outputs are not
+ * formed.  dG and dU are rounded to the rows' type before the products; dbg and dbu are formed from them unrounded. */
+size_t slicegcn_gated_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
+int slicegcn_gated_bwd(const slicegcn_product_desc *desc, const slicegcn_matrix *X, const void *Wg, const void *Wu, const slicegcn_matrix *G,
+                       const slicegcn_matrix *U, const slicegcn_matrix *dH, const slicegcn_matrix *dX, void *dWg, void *dWu, float *dbg,
+                       float *dbu, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------
+ * One AdamW step (decoupled weight decay) over many tensors at once, step >= 1, in place:
+ *   g = factor * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p - lr * decay * p - lr * (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * p is `master` (fp32) where there is one, and param receives it rounded; else param itself, of any type.
+ * states: SLICEGCN_STATES_32: m and v are fp32.  SLICEGCN_STATES_8: m and v are e4m3 numbers (8 bits: sign, 4 exponent bits of bias 7, 3 bits), times a
+ * power of two that SLICEGCN_STATE_BLOCK consecutive elements share: scales[2 b] and scales[2 b + 1] are the biased exponents (byte - 127) of block b's m and
+ * v.  A block's byte is that of its largest finite |m| (or v) less 7, at least 1.  Values are rounded up or down by chance, so that the stored value is on average the one
+ * that was to be stored (a running mean that moves by a thousandth a step would stand still under rounding to nearest): with t = |value| / scale, plus
+ * 2^-6 where t < 2^-6, 16 r is added to the bits of t as an integer and the low 20 bits are cleared (and the 2^-6 taken off), where r is the
+ * upper (m) or lower (v) half of 32 bits that depend on the element's index i, the tensor's index k in the list and `seed` (s):
+ *   x = low(i) * 0x9E3779B9 + low(s) * 0x6A09E667 + high(s) * 0xBB67AE85 + k * 0x3C6EF373;  x ^= x >> 15;  x *= 0xA54FF53B;  x ^= x >> 16   (mod 2^32)
+ * v > 0 is never stored as 0 (but as 2^-9 times its scale).  All operations up to there are rounded one by one in fp32.  States that start as zeros:
+ * codes of 0, with scales of any value from 1 to 247.  A value that is not finite is stored as NaN.
+ * tensors: HOST array of contiguous DEVICE tensors; count = 0 and empty tensors are valid; no two of them overlap.  factor: DEVICE scalar (slicegcn_global_norm's), or
+ * NULL for 1; where it is not positive (0 or NaN: the norm was infinite or NaN) the step is left out: nothing is written.
+ * EINVAL: NULL pointer, count < 0, step < 1, bad tensor (negative or too large count, unknown type, a master of fp32 parameters, no scales with 8 bits, misaligned:
+ * every element on a boundary of its size, scales on one of 2 bytes), betas outside [0, 1), eps <= 0, lr or a decay not finite. */
+#define SLICEGCN_STATES_32 32
+#define SLICEGCN_STATES_8 8
+#define SLICEGCN_STATE_BLOCK 128
+typedef struct {
+    void *param;
+    const void *grad;
+    float *master;   /* NULL: param holds the parameters */
+    void *m;
+    void *v;
+    uint8_t *scales; /* [ceil(count / SLICEGCN_STATE_BLOCK)][2], with states in 8 bits */
+    int64_t count;   /* at most 2^40 */
+    float decay;
+    int16_t param_type;
+    int16_t grad_type;
+} slicegcn_adam_tensor;
+
+int slicegcn_adamw_step(const slicegcn_adam_tensor *tensors, int32_t count, int32_t states, double lr, double beta1, double beta2, double eps,
+                        int32_t step, const float *factor, uint64_t seed, void *stream);
+
 /* further kinds of slicegcn_profile_entry */
 #define SLICEGCN_PROF_EMBED 11   /* lookup, sort and gradient; width = columns (0: sort) */
 #define SLICEGCN_PROF_RESNORM 12 /* norms around a block, forward and backward; width = columns */
 #define SLICEGCN_PROF_CLIP 13    /* norm over all gradients, clipping; width = tensors */
+#define SLICEGCN_PROF_PRODUCT 14 /* products and gated projections, forward and backward; width = w_out */
+#define SLICEGCN_PROF_ADAMW 15   /* AdamW step; width = tensors */
 
 #ifdef __cplusplus
 }

@@ -28,6 +28,8 @@ SCHED_SHORT_ITEMS = 16
 SCHED_LONG_ITEMS = 32
 ACT_NONE = 0
 ACT_RELU = 1
+ACT_SILU = 2  # products and gated projections
+ACT_GELU = 3
 LAYER_Z_VALID = 1
 LAYER_TRANSFORM_FIRST = 2
 LAYER_ORDER_AUTO = 4
@@ -50,7 +52,7 @@ EXPORTS = [
 
 PROF_KINDS = {0: "spmm", 1: "dense_fwd", 2: "dense_bwd", 3: "grad_reduce", 4: "concat", 5: "spmm_add",
               6: "linear_fwd", 7: "linear_bwd", 8: "linear_grad", 9: "loss", 10: "accumulate",
-              11: "embed", 12: "resnorm", 13: "clip"}
+              11: "embed", 12: "resnorm", 13: "clip", 14: "product", 15: "adamw"}
 
 
 class SliceGCNError(RuntimeError):
@@ -118,6 +120,7 @@ NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 GATE_SIGMOID = 1
 RESNORM_MAX_WIDTH = 16384
 NORM_TWO, NORM_MAX = 0, 1
+STATE_BLOCK = 128
 
 
 # Descriptors of slicegcn_train.h as packed bytes (a third of what filling ctypes structures takes, which is what small calls cost)
@@ -127,8 +130,18 @@ _RESNORM_PARAMS = struct.Struct("@5P")          # post_w, post_b, pre_w, pre_b, 
 _RESNORM_IO = struct.Struct("@" + 5 * "Pq" + "P" + 5 * "Pq")  # x, y, gate, h, u; stats; dh, du, dx, dy, dgate
 
 
+_PRODUCT_DESC = struct.Struct("@qiiiid")        # n, w_in, w_out, type, act, residual
+_MATRIX = struct.Struct("@Pq")                  # data, ld
+
+
 class _Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_int64), ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class _AdamTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("master", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("count", ctypes.c_int64), ("decay", ctypes.c_float),
+                ("param_type", ctypes.c_int16), ("grad_type", ctypes.c_int16)]
 
 
 _lib = None
@@ -208,6 +221,14 @@ def lib() -> ctypes.CDLL:
         L.slicegcn_global_norm.argtypes = [vp, i32, i32, f64, vp, vp, vp, sz, vp]
         L.slicegcn_clip.argtypes = [vp, vp, i32, i32, f64, vp, vp, vp, sz, vp]
         L.slicegcn_adam_step_scaled.argtypes = [vp, vp, vp, vp, vp, i64, f64, f64, f64, f64, f64, i32, vp]
+        for fn in (L.slicegcn_product_fwd_workspace_bytes, L.slicegcn_product_bwd_workspace_bytes, L.slicegcn_gated_fwd_workspace_bytes,
+                   L.slicegcn_gated_bwd_workspace_bytes):
+            fn.argtypes, fn.restype = [i64, i32, i32, i32], sz
+        L.slicegcn_product_fwd.argtypes = 7 * [vp] + [vp, sz, vp]
+        L.slicegcn_product_bwd.argtypes = 9 * [vp] + [vp, sz, vp]
+        L.slicegcn_gated_fwd.argtypes = 9 * [vp] + [vp, sz, vp]
+        L.slicegcn_gated_bwd.argtypes = 12 * [vp] + [vp, sz, vp]
+        L.slicegcn_adamw_step.argtypes = [vp, i32, i32, f64, f64, f64, f64, i32, vp, ctypes.c_uint64, vp]
         L.slicegcn_strerror.argtypes = [ctypes.c_int]
         L.slicegcn_strerror.restype = ctypes.c_char_p
         L.slicegcn_last_error.restype = ctypes.c_char_p
@@ -855,6 +876,139 @@ def slicegcn_adam_step_scaled(param, grad, factor, m, v, lr: float, step: int, b
             raise ValueError(f"{name} differs in size from param")
     _check(lib().slicegcn_adam_step_scaled(_vec(param, "param"), _vec(grad, "grad"), _vec(factor, "factor"), _vec(m, "m"), _vec(v, "v"), n,
                                            lr, beta1, beta2, eps, weight_decay, step, _stream()))
+
+
+# ---- products and feed-forward blocks
+def _weights(t, name: str, shape, dtype):
+    """Address of a contiguous matrix that may be absent."""
+    if t is None:
+        return 0
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected {tuple(shape)}, not {tuple(t.shape)}")
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous {dtype} device tensor")
+    return t.data_ptr()
+
+
+def _matrix(t, name: str, shape, dtype):
+    """A packed slicegcn_matrix, or None."""
+    return None if t is None else _MATRIX.pack(*_rows(t, name, shape, dtype))
+
+
+def _product_sizes(X, W, other):
+    """(shape of X, of W, of the results, type) of a product's call: n from a matrix with a row each, widths from the weights."""
+    w_in, w_out = W.shape
+    n = (X if X is not None else other).shape[0]
+    return (n, w_in), (w_in, w_out), (n, w_out), W.dtype
+
+
+def _workspace_bytes(fn, n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
+    if dtype not in VALUE_TYPES:
+        raise TypeError(f"expected fp32, bf16 or fp16, not {dtype}")
+    return int(fn(n, w_in, w_out, VALUE_TYPES[dtype]))
+
+
+def slicegcn_product_fwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
+    return _workspace_bytes(lib().slicegcn_product_fwd_workspace_bytes, n, w_in, w_out, dtype)
+
+
+def slicegcn_product_fwd(X, W, Y, ws=None, b=None, R=None, P=None, act: int = ACT_NONE, residual: float = 1.0):
+    """P = X W + b;  Y = residual * R + act(P).  ``b`` (fp32), ``R``, ``P`` may be None; the others are of one type."""
+    xs, wsh, ys, dtype = _product_sizes(X, W, Y)
+    desc = _PRODUCT_DESC.pack(ys[0], *wsh, _value_type(W, "W"), act, residual)
+    _check(lib().slicegcn_product_fwd(desc, _matrix(X, "X", xs, dtype), _weights(W, "W", wsh, dtype), _columns(b, "b", wsh[1]),
+                                      _matrix(R, "R", ys, dtype), _matrix(P, "P", ys, dtype), _matrix(Y, "Y", ys, dtype), *_ws(ws), _stream()))
+    return Y
+
+
+def slicegcn_product_bwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
+    return _workspace_bytes(lib().slicegcn_product_bwd_workspace_bytes, n, w_in, w_out, dtype)
+
+
+def slicegcn_product_bwd(X, W, P, dY, ws=None, dX=None, dW=None, db=None, dR=None, act: int = ACT_NONE, residual: float = 1.0):
+    """dP = dY * act'(P);  dX = dP W^T;  dW = X^T dP;  db (fp32) = column sums of dP;  dR = residual * dY.  Gradients that are None are not
+    formed; ``P`` is needed where there is an activation, ``X`` for dW."""
+    xs, wsh, ys, dtype = _product_sizes(X, W, dY)
+    desc = _PRODUCT_DESC.pack(ys[0], *wsh, _value_type(W, "W"), act, residual)
+    _check(lib().slicegcn_product_bwd(desc, _matrix(X, "X", xs, dtype), _weights(W, "W", wsh, dtype), _matrix(P, "P", ys, dtype),
+                                      _matrix(dY, "dY", ys, dtype), _matrix(dX, "dX", xs, dtype), _weights(dW, "dW", wsh, dtype),
+                                      _columns(db, "db", wsh[1]), _matrix(dR, "dR", ys, dtype), *_ws(ws), _stream()))
+
+
+def slicegcn_gated_fwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
+    return _workspace_bytes(lib().slicegcn_gated_fwd_workspace_bytes, n, w_in, w_out, dtype)
+
+
+def slicegcn_gated_fwd(X, Wg, Wu, H, ws=None, bg=None, bu=None, G=None, U=None, act: int = ACT_SILU):
+    """G = X Wg + bg;  U = X Wu + bu;  H = act(G) * U.  ``bg``, ``bu`` (fp32) may be None; ``G`` and ``U`` (both or neither) are kept for the
+    backward pass."""
+    xs, wsh, ys, dtype = _product_sizes(X, Wg, H)
+    desc = _PRODUCT_DESC.pack(ys[0], *wsh, _value_type(Wg, "Wg"), act, 0.0)
+    _check(lib().slicegcn_gated_fwd(desc, _matrix(X, "X", xs, dtype), _weights(Wg, "Wg", wsh, dtype), _weights(Wu, "Wu", wsh, dtype),
+                                    _columns(bg, "bg", wsh[1]), _columns(bu, "bu", wsh[1]), _matrix(G, "G", ys, dtype),
+                                    _matrix(U, "U", ys, dtype), _matrix(H, "H", ys, dtype), *_ws(ws), _stream()))
+    return H
+
+
+def slicegcn_gated_bwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
+    return _workspace_bytes(lib().slicegcn_gated_bwd_workspace_bytes, n, w_in, w_out, dtype)
+
+
+def slicegcn_gated_bwd(X, Wg, Wu, G, U, dH, ws=None, dX=None, dWg=None, dWu=None, dbg=None, dbu=None, act: int = ACT_SILU):
+    """Gradients of slicegcn_gated_fwd from ``dH`` and the G and U that it kept; those that are None are not formed."""
+    xs, wsh, ys, dtype = _product_sizes(X, Wg, dH)
+    desc = _PRODUCT_DESC.pack(ys[0], *wsh, _value_type(Wg, "Wg"), act, 0.0)
+    _check(lib().slicegcn_gated_bwd(desc, _matrix(X, "X", xs, dtype), _weights(Wg, "Wg", wsh, dtype), _weights(Wu, "Wu", wsh, dtype),
+                                    _matrix(G, "G", ys, dtype), _matrix(U, "U", ys, dtype), _matrix(dH, "dH", ys, dtype),
+                                    _matrix(dX, "dX", xs, dtype), _weights(dWg, "dWg", wsh, dtype), _weights(dWu, "dWu", wsh, dtype),
+                                    _columns(dbg, "dbg", wsh[1]), _columns(dbu, "dbu", wsh[1]), *_ws(ws), _stream()))
+
+
+# ---- AdamW over many tensors
+class AdamList:
+    """Parameters, gradients and states of a model as the list slicegcn_adamw_step takes, laid out once for tensors that stay where they are.
+    ``ms``, ``vs``: fp32, or float8_e4m3fn with ``scales`` of shape [ceil(count / STATE_BLOCK), 2] (uint8 or float8_e8m0fnu); zeros to
+    start with (scales: ones).  ``masters``: fp32 or None for every tensor of 16 bits.  ``decays``: the weight decay of each, or of all."""
+
+    def __init__(self, params, grads, ms, vs, scales=None, masters=None, decays=0.0):
+        params = list(params)
+        n = len(params)
+        columns = [list(c) if c is not None else [None] * n for c in (grads, ms, vs, scales, masters)]
+        decays = [decays] * n if isinstance(decays, (int, float)) else list(decays)
+        if any(len(c) != n for c in (*columns, decays)):
+            raise ValueError("as many gradients, states, scales, masters and decays as parameters expected")
+        self.tensors = [params, *columns]
+        self.array = (_AdamTensor * max(n, 1))()
+        states = {t.dtype for c in columns[1:3] for t in c}
+        if len(states) > 1 or not states <= {torch.float32, torch.float8_e4m3fn}:
+            raise TypeError(f"states must all be fp32 or all float8_e4m3fn, not {sorted(map(str, states))}")
+        self.states = 8 if torch.float8_e4m3fn in states else 32
+        for i, (p, g, m, v, s, master) in enumerate(zip(params, *columns)):
+            e, count = self.array[i], p.numel()
+            for t, name in ((g, "gradient"), (m, "m"), (v, "v"), (master, "master")):
+                if t is not None and t.numel() != count:
+                    raise ValueError(f"{name} {i} differs in size from its parameter")
+            e.param, e.grad, e.master = _vec(p, f"parameter {i}", p.dtype), _vec(g, f"gradient {i}", g.dtype), _vec(master, f"master {i}")
+            e.m, e.v = _vec(m, f"m {i}", m.dtype), _vec(v, f"v {i}", v.dtype)
+            if self.states == 8:
+                if s is None or s.numel() != 2 * -(-count // STATE_BLOCK) or s.element_size() != 1:
+                    raise ValueError(f"scales {i}: expected {-(-count // STATE_BLOCK)} x 2 bytes")
+                e.scales = _vec(s, f"scales {i}", s.dtype)
+            elif s is not None:
+                raise ValueError(f"scales {i}: states in 32 bits have none")
+            e.count, e.decay = count, decays[i]
+            e.param_type, e.grad_type = _value_type(p, f"parameter {i}"), _value_type(g, f"gradient {i}")
+
+    def __len__(self):
+        return len(self.tensors[0])
+
+
+def slicegcn_adamw_step(tensors: AdamList, lr: float, step: int, beta1=0.9, beta2=0.999, eps=1e-8, factor: torch.Tensor | None = None,
+                        seed: int = 0):
+    """One AdamW step in place on gradients times ``factor`` (fp32 [1] on the device; not positive: nothing is done).  ``seed``: another one for each
+    step, where the states have 8 bits."""
+    _check(lib().slicegcn_adamw_step(tensors.array, len(tensors), tensors.states, lr, beta1, beta2, eps, step, _vec(factor, "factor"),
+                                     seed & 0xFFFFFFFFFFFFFFFF, _stream()))
 
 
 def slicegcn_profile_reserve(scopes: int):

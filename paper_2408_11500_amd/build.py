@@ -17,7 +17,8 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libslicegcn.so")
 SOURCES = ["build_csr.hip", "edge_sort.hip", "order.hip", "spmm.hip", "dense.hip", "misc.hip", "loss.hip", "embed.hip", "resnorm.hip",
-           "resnorm_f32.hip", "resnorm_bf16.hip", "resnorm_f16.hip", "clip.hip"]
+           "resnorm_f32.hip", "resnorm_bf16.hip", "resnorm_f16.hip", "clip.hip", "feedforward.hip", "product_f32.hip", "product_bf16.hip",
+           "product_f16.hip", "adamw.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 instructions stay off for every kernel in this library
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,109 @@
+// Products of rows and weights on the matrix cores: what the kernels take, shared by the host code and the kernels of each type.
+//
+// Every product is C[M, N] = sum over k of A[m, k] B[n, k], with either operand stored k first (its rows lie along k: KC) or outer index first
+// (OC):           M side           N side
+//   X W           X, KC            W, OC
+//   dP W^T        dP, KC           W, KC
+//   X^T dP        X, OC            dP, OC
+#pragma once
+
+#include "common.h"
+#include "values.h"
+
+namespace slicegcn {
+
+constexpr int LAYOUT_KC = 0, LAYOUT_OC = 1;
+
+struct Operand {
+    const char *p;
+    int64_t ld;
+};
+
+// What becomes of the sums
+//   FORWARD  Y = residual R + act(P), P = sum + b
+//   GATED    H = act(G) U of two products with the same rows, which take turns of 16 columns in a tile
+//   STORE    the sum itself
+constexpr int EPI_FORWARD = 0, EPI_GATED = 1, EPI_STORE = 2;
+
+struct ProductArgs {
+    Operand a[2], b[2];    // operands of each set of products that the grid's depth counts, or of each segment of a sum
+    int64_t M, K;          // K of one segment
+    int32_t N;
+    int32_t segments;      // products that add up to one result (with `sets` = 1)
+    int32_t sets;          // results formed by one launch; GATED: 1
+    char *out[2];          // STORE: a result per set;  FORWARD: Y;  GATED: H
+    int64_t ldo[2];
+    const float *bias[2];
+    Operand r;             // FORWARD: the residual rows
+    char *keep[2];         // FORWARD: P;  GATED: G and U
+    int64_t ldk[2];
+    float residual;
+    int32_t act;
+    float *partial;        // sums of parts of k: [set][split][M][N], where splits > 1
+    int32_t splits;
+    int32_t steps_per_split;
+    int64_t first;         // first workgroup of this launch
+};
+
+// Sizes of a product and how it is cut: everything that a launch depends on follows from these
+struct ProductShape {
+    int64_t M, K;
+    int32_t N;
+    int32_t segments, sets, type;
+    bool gated; // GATED
+};
+struct ProductPlan {
+    int32_t tile; // of the register path: index of a tile shape
+    int32_t splits, steps_per_split;
+    size_t partial_bytes() const { return bytes; }
+    size_t bytes;
+};
+ProductPlan plan_product(const ProductShape &s);
+
+// product_f32.hip, product_bf16.hip, product_f16.hip
+int launch_product_f32(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream);
+int launch_product_bf16(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream);
+int launch_product_f16(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream);
+
+// layouts: which operands a product has
+constexpr int PRODUCT_XW = 0, PRODUCT_GWT = 1, PRODUCT_XTG = 2;
+
+constexpr int TILES = 3;
+constexpr int TILE_M[TILES] = {128, 64, 32}, TILE_N[TILES] = {128, 64, 128};
+constexpr int STEP_K_F32 = 32, STEP_K_16 = 64;
+inline int step_k(int32_t type) { return type == SLICEGCN_F32 ? STEP_K_F32 : STEP_K_16; }
+
+__device__ inline float sigmoid(float v) { return 1.f / (1.f + expf(-v)); }
+
+__device__ inline float activated(int act, float v)
+{
+    switch (act) {
+    case SLICEGCN_ACT_RELU: return v < 0.f ? 0.f : v;
+    case SLICEGCN_ACT_SILU: return v * sigmoid(v);
+    case SLICEGCN_ACT_GELU: return v * (0.5f * erfcf(v * -0.70710678118654752f));
+    default: return v;
+    }
+}
+
+// act(v) and its derivative
+__device__ inline void activated_slope(int act, float v, float &y, float &slope)
+{
+    switch (act) {
+    case SLICEGCN_ACT_RELU: y = v < 0.f ? 0.f : v; slope = v > 0.f ? 1.f : 0.f; break;
+    case SLICEGCN_ACT_SILU: {
+        const float s = sigmoid(v);
+        y = v * s;
+        slope = s * (1.f + v * (1.f - s));
+        break;
+    }
+    case SLICEGCN_ACT_GELU: {
+        const float p = 0.5f * erfcf(v * -0.70710678118654752f);
+        y = v * p;
+        slope = p + v * (0.39894228040143268f * expf(-0.5f * v * v));
+        break;
+    }
+    default: y = v; slope = 1.f;
+    }
+}
+
+} // namespace slicegcn

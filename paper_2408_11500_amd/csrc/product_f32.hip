@@ -1,0 +1,11 @@
+// The kernels of product.h for f32 rows.
+#include "product_kernels.h"
+
+namespace slicegcn {
+
+int launch_product_f32(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream)
+{
+    return launch_product<float>(layouts, epilogue, plan, a, stream);
+}
+
+} // namespace slicegcn

@@ -1,0 +1,310 @@
+"""Products with their epilogue and gated projections, forward and backward, against 64-bit references."""
+import pytest
+import torch
+
+from paper_2408_11500_amd import binding as B
+from product_util import ACTS, gated_bwd, gated_fwd, product_bwd, product_fwd
+from train_util import F64, TYPES, assert_within, rows
+
+pytestmark = pytest.mark.gpu
+ACT = dict(none=B.ACT_NONE, relu=B.ACT_RELU, silu=B.ACT_SILU, gelu=B.ACT_GELU)
+
+# rows, widths: single elements, less than a tile, whole tiles, one more, long sums that are cut, many rows
+SIZES = [(1, 1, 1), (1, 64, 96), (1, 2000, 136), (2, 300, 1032), (3, 7, 5), (5, 1048, 40), (9, 520, 264), (17, 33, 31), (24, 1024, 200), (32, 128, 256),
+         (33, 65, 129), (70, 2304, 64), (128, 64, 64), (200, 130, 70), (257, 520, 384), (300, 264, 520), (1000, 72, 40), (5000, 24, 8), (1, 8, 8), (64, 32, 16)]
+
+
+def weights(gen, w_in, w_out, dtype):
+    w = (torch.randn((w_in, w_out), generator=gen) / w_in ** 0.5).to(dtype)
+    return w.cuda(), w.to(F64)
+
+
+def vector(gen, width, present):
+    if not present:
+        return None, None
+    v = torch.randn(width, generator=gen)
+    return v.cuda(), v.to(F64)
+
+
+def result(n, width, dtype, ld):
+    """Rows that lie ld apart in a buffer of a value that no result has, and the buffer."""
+    buf = torch.full((n, ld), 777.0, dtype=dtype, device="cuda")
+    return buf[:, :width], buf
+
+
+def assert_padding(buf, width):
+    assert (buf[:, width:] == 777.0).all(), "written behind the last column"
+
+
+def workspace(count):
+    return torch.full((count,), 0xFF, dtype=torch.uint8, device="cuda")  # NaN in every type
+
+
+def lds(n, w, kind):
+    return {"dense": w, "lines": -(-w // 64) * 64, "odd": w + 3}[kind]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("name", ACTS)
+def test_product(size, name, kind):
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    case = SIZES.index(size) + ACTS.index(name)
+    gen = torch.Generator().manual_seed(case)
+    ld = ("dense", "lines", "odd")[case % 3]
+    offset = (0, 8, 1)[case % 3]
+    residual, with_r, with_b, with_p = (1.0, 0.5, 0.0, -2.0)[case % 4], case % 2 == 0, case % 3 != 1, case % 2 == 1 or name != "none"
+    x, x64 = rows(gen, n, wi, dtype, lds(n, wi, ld), offset)
+    w, w64 = weights(gen, wi, wo, dtype)
+    b, b64 = vector(gen, wo, with_b)
+    r, r64 = rows(gen, n, wo, dtype, lds(n, wo, ld), offset) if with_r else (None, None)
+    y, ybuf = result(n, wo, dtype, lds(n, wo, ld))
+    p, pbuf = result(n, wo, dtype, lds(n, wo, "odd")) if with_p else (None, None)
+    ws = workspace(B.slicegcn_product_fwd_workspace_bytes(n, wi, wo, dtype))
+    B.slicegcn_product_fwd(x, w, y, ws, b=b, R=r, P=p, act=ACT[name], residual=residual)
+    want = product_fwd(x64, w64, b64, r64, residual, name, dtype)
+    assert_within(y, *want["Y"], "Y")
+    assert_padding(ybuf, wo)
+    if with_p:
+        assert_within(p, *want["P"], "P")
+        assert_padding(pbuf, wo)
+
+    kept, k64 = rows(gen, n, wo, dtype, lds(n, wo, ld), offset, std=1.5)
+    dy, d64 = rows(gen, n, wo, dtype, lds(n, wo, ld), offset)
+    dx, dxbuf = result(n, wi, dtype, lds(n, wi, ld))
+    dr, drbuf = result(n, wo, dtype, lds(n, wo, "odd"))
+    dw, db = torch.full_like(w, 777.0), torch.full((wo,), 777.0, device="cuda")
+    ws = workspace(B.slicegcn_product_bwd_workspace_bytes(n, wi, wo, dtype))
+    B.slicegcn_product_bwd(x, w, kept if name != "none" else None, dy, ws, dX=dx, dW=dw, db=db, dR=dr, act=ACT[name], residual=residual)
+    want = product_bwd(x64, w64, k64, d64, residual, name, dtype)
+    for got, key in ((dx, "dX"), (dw, "dW"), (db, "db"), (dr, "dR")):
+        assert_within(got, *want[key], key)
+    assert_padding(dxbuf, wi)
+    assert_padding(drbuf, wo)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("name", ACTS)
+def test_gated(size, name, kind):
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    case = SIZES.index(size) + 2 * ACTS.index(name)
+    gen = torch.Generator().manual_seed(100 + case)
+    ld = ("dense", "lines", "odd")[case % 3]
+    offset = (0, 8, 1)[case % 3]
+    x, x64 = rows(gen, n, wi, dtype, lds(n, wi, ld), offset)
+    (wg, wg64), (wu, wu64) = weights(gen, wi, wo, dtype), weights(gen, wi, wo, dtype)
+    bg, bg64 = vector(gen, wo, case % 2 == 0)
+    bu, bu64 = vector(gen, wo, case % 3 == 0)
+    h, hbuf = result(n, wo, dtype, lds(n, wo, ld))
+    (g, gbuf), (u, ubuf) = (result(n, wo, dtype, lds(n, wo, k)) if case % 4 else (None, None) for k in ("odd", ld))
+    ws = workspace(B.slicegcn_gated_fwd_workspace_bytes(n, wi, wo, dtype))
+    B.slicegcn_gated_fwd(x, wg, wu, h, ws, bg=bg, bu=bu, G=g, U=u, act=ACT[name])
+    want = gated_fwd(x64, wg64, wu64, bg64, bu64, name, dtype)
+    for got, buf, key in ((h, hbuf, "H"), (g, gbuf, "G"), (u, ubuf, "U")):
+        if got is not None:
+            assert_within(got, *want[key], key)
+            assert_padding(buf, wo)
+
+    g, g64 = rows(gen, n, wo, dtype, lds(n, wo, ld), offset, std=1.5)
+    u, u64 = rows(gen, n, wo, dtype, lds(n, wo, "odd"), offset)
+    dh, d64 = rows(gen, n, wo, dtype, lds(n, wo, ld), offset)
+    dx, dxbuf = result(n, wi, dtype, lds(n, wi, ld))
+    dwg, dwu = torch.full_like(wg, 777.0), torch.full_like(wu, 777.0)
+    dbg, dbu = (torch.full((wo,), 777.0, device="cuda") for _ in range(2))
+    ws = workspace(B.slicegcn_gated_bwd_workspace_bytes(n, wi, wo, dtype))
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, dh, ws, dX=dx, dWg=dwg, dWu=dwu, dbg=dbg, dbu=dbu, act=ACT[name])
+    want = gated_bwd(x64, wg64, wu64, g64, u64, d64, name, dtype)
+    for got, key in ((dx, "dX"), (dwg, "dWg"), (dwu, "dWu"), (dbg, "dbg"), (dbu, "dbu")):
+        assert_within(got, *want[key], key)
+    assert_padding(dxbuf, wi)
+
+
+@pytest.mark.parametrize("size", [(40, 24, 16), (3, 600, 48), (700, 40, 136)], ids=str)
+@pytest.mark.parametrize("kind", TYPES)
+def test_gradients_that_are_not_wanted(size, kind):
+    """Each gradient alone, in the bits that it has among all of them."""
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(7)
+    x, g, u, dh = (rows(gen, n, w, dtype)[0] for w in (wi, wo, wo, wo))
+    (wg, _), (wu, _) = weights(gen, wi, wo, dtype), weights(gen, wi, wo, dtype)
+    ws = workspace(B.slicegcn_gated_bwd_workspace_bytes(n, wi, wo, dtype))
+    empty = dict(dX=(n, wi), dWg=(wi, wo), dWu=(wi, wo), dbg=(wo,), dbu=(wo,))
+    make = lambda names: {k: torch.full(empty[k], 777.0, dtype=torch.float32 if k in ("dbg", "dbu") else dtype, device="cuda") for k in names}
+    every = make(empty)
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, dh, ws, **every)
+    for k in empty:
+        alone = make([k])
+        needed = dict(X=x if k in ("dWg", "dWu") else None)
+        B.slicegcn_gated_bwd(needed["X"], wg, wu, g, u, dh, ws, **alone)
+        assert torch.equal(alone[k], every[k]), k
+    ws = workspace(B.slicegcn_product_bwd_workspace_bytes(n, wi, wo, dtype))
+    every = {k: torch.full(s, 777.0, dtype=torch.float32 if k == "db" else dtype, device="cuda")
+             for k, s in dict(dX=(n, wi), dW=(wi, wo), db=(wo,), dR=(n, wo)).items()}
+    B.slicegcn_product_bwd(x, wg, g, dh, ws, act=B.ACT_GELU, residual=3.0, **every)
+    for k, t in every.items():
+        alone = torch.full_like(t, 777.0)
+        B.slicegcn_product_bwd(x if k == "dW" else None, wg, g if k != "dR" else None, dh, ws, act=B.ACT_GELU, residual=3.0, **{k: alone})
+        assert torch.equal(alone, t), k
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_no_rows(kind):
+    dtype = TYPES[kind]
+    e = lambda w: torch.empty((0, w), dtype=dtype, device="cuda")
+    w, w2 = torch.ones((5, 7), dtype=dtype, device="cuda"), torch.ones((5, 7), dtype=dtype, device="cuda")
+    assert B.slicegcn_product_fwd_workspace_bytes(0, 5, 7, dtype) == 0
+    B.slicegcn_product_fwd(e(5), w, e(7), R=e(7), P=e(7), act=B.ACT_GELU)
+    B.slicegcn_gated_fwd(e(5), w, w2, e(7))
+    for t in (w, w2):
+        t.fill_(777.0)
+    db, db2 = torch.full((7,), 777.0, device="cuda"), torch.full((7,), 777.0, device="cuda")
+    ws = workspace(B.slicegcn_gated_bwd_workspace_bytes(0, 5, 7, dtype))
+    weight = torch.ones((5, 7), dtype=dtype, device="cuda")
+    B.slicegcn_gated_bwd(e(5), weight, weight, e(7), e(7), e(7), ws, dX=e(5), dWg=w, dWu=w2, dbg=db, dbu=db2)
+    for t in (w, w2, db, db2):
+        assert (t == 0).all()
+        t.fill_(777.0)
+    ws = workspace(B.slicegcn_product_bwd_workspace_bytes(0, 5, 7, dtype))
+    B.slicegcn_product_bwd(e(5), weight, e(7), e(7), ws, dX=e(5), dW=w, db=db, dR=e(7), act=B.ACT_SILU)
+    assert (w == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("size", [(3, 900, 40), (150, 64, 200)], ids=str)
+def test_result_in_the_rows_of_the_residual(size, kind):
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(5)
+    x, _ = rows(gen, n, wi, dtype)
+    w, _ = weights(gen, wi, wo, dtype)
+    r, _ = rows(gen, n, wo, dtype, wo + 5)
+    ws = workspace(B.slicegcn_product_fwd_workspace_bytes(n, wi, wo, dtype))
+    y = torch.empty((n, wo), dtype=dtype, device="cuda")
+    B.slicegcn_product_fwd(x, w, y, ws, R=r, act=B.ACT_SILU, residual=0.5)
+    B.slicegcn_product_fwd(x, w, r, ws, R=r, act=B.ACT_SILU, residual=0.5)
+    assert torch.equal(r, y)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("size", [(5, 1024, 136), (200, 128, 128), (129, 65, 40)], ids=str)
+def test_values_that_are_not_finite_stay_in_their_rows_and_columns(size, kind):
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(6)
+    x, _ = rows(gen, n, wi, dtype)
+    (wg, _), (wu, _) = weights(gen, wi, wo, dtype), weights(gen, wi, wo, dtype)
+    ws = workspace(B.slicegcn_gated_fwd_workspace_bytes(n, wi, wo, dtype))
+    h, h2 = (torch.empty((n, wo), dtype=dtype, device="cuda") for _ in range(2))
+    B.slicegcn_gated_fwd(x, wg, wu, h, ws)
+    x[n // 2, wi - 1] = float("inf")
+    wg[wi // 2, wo - 1] = float("nan")
+    B.slicegcn_gated_fwd(x, wg, wu, h2, ws)
+    assert not torch.isfinite(h2[n // 2]).any() and torch.isnan(h2[:, wo - 1]).all()
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[n // 2] = False
+    assert torch.equal(h2[keep, :wo - 1], h[keep, :wo - 1])
+
+
+def test_large_and_small_fp32_operands():
+    """Values over the whole range of exponents: each product by itself (a sum of one)."""
+    gen = torch.Generator().manual_seed(8)
+    n = 64
+    x = (torch.randn((n, 1), generator=gen) * torch.exp2(torch.randint(-60, 60, (n, 1), generator=gen).float()))
+    w = (torch.randn((1, n), generator=gen) * torch.exp2(torch.randint(-60, 60, (1, n), generator=gen).float()))
+    y = torch.empty((n, n), device="cuda")
+    B.slicegcn_product_fwd(x.cuda(), w.cuda(), y, workspace(B.slicegcn_product_fwd_workspace_bytes(n, 1, n, torch.float32)))
+    want = x.double() * w.double()
+    assert_within(y, want, 16 * 2.0 ** -24 * want.abs(), "products")
+
+
+def test_same_bits_again_and_on_another_stream():
+    gen = torch.Generator().manual_seed(9)
+    n, wi, wo = 333, 264, 200
+    x, g, u, dh = (rows(gen, n, w, torch.bfloat16)[0] for w in (wi, wo, wo, wo))
+    (wg, _), (wu, _) = weights(gen, wi, wo, torch.bfloat16), weights(gen, wi, wo, torch.bfloat16)
+
+    def once():
+        ws = workspace(B.slicegcn_gated_bwd_workspace_bytes(n, wi, wo, torch.bfloat16))
+        out = [torch.empty_like(t) for t in (x, wg, wu)] + [torch.empty(wo, device="cuda")]
+        B.slicegcn_gated_bwd(x, wg, wu, g, u, dh, ws, dX=out[0], dWg=out[1], dWu=out[2], dbg=out[3])
+        return out
+    first = once()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        other = once()
+    torch.cuda.current_stream().wait_stream(s)
+    for a, b in zip(first, other):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_a_block_in_a_graph(kind):
+    """Forward and backward of a feed-forward block captured and replayed with new rows, beside eager calls."""
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(10)
+    n, w, f = 70, 96, 264
+    x, dy = rows(gen, n, w, dtype)[0], rows(gen, n, w, dtype)[0]
+    (wg, _), (wu, _), (wd, _) = weights(gen, w, f, dtype), weights(gen, w, f, dtype), weights(gen, f, w, dtype)
+
+    def block(x):
+        e = lambda *s: torch.empty(s, dtype=dtype, device="cuda")
+        t = dict(h=e(n, f), g=e(n, f), u=e(n, f), y=e(n, w), dh=e(n, f), dwd=e(f, w), dx=e(n, w), dwg=e(w, f), dwu=e(w, f))
+        sizes = [B.slicegcn_gated_fwd_workspace_bytes(n, w, f, dtype), B.slicegcn_gated_bwd_workspace_bytes(n, w, f, dtype),
+                 B.slicegcn_product_fwd_workspace_bytes(n, f, w, dtype), B.slicegcn_product_bwd_workspace_bytes(n, f, w, dtype)]
+        ws = torch.empty(max(sizes), dtype=torch.uint8, device="cuda")
+
+        def run():
+            B.slicegcn_gated_fwd(x, wg, wu, t["h"], ws, G=t["g"], U=t["u"])
+            B.slicegcn_product_fwd(t["h"], wd, t["y"], ws, R=x)
+            B.slicegcn_product_bwd(t["h"], wd, None, dy, ws, dX=t["dh"], dW=t["dwd"])
+            B.slicegcn_gated_bwd(x, wg, wu, t["g"], t["u"], t["dh"], ws, dX=t["dx"], dWg=t["dwg"], dWu=t["dwu"])
+        return run, t, ws
+    captured, t, _ = block(x)
+    captured()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured()
+    for seed in range(3):
+        x.copy_(torch.randn((n, w), generator=torch.Generator().manual_seed(seed)).to(dtype))
+        eager, e, _ = block(x)
+        eager()
+        for v in t.values():
+            v.fill_(777.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in t:
+            assert torch.equal(t[k], e[k]), k
+
+
+def test_gradients_against_differences():
+    """dX and dWg of a small block against central differences of the block in 64 bits."""
+    gen = torch.Generator().manual_seed(11)
+    n, w, f = 4, 6, 5
+    x, x64 = rows(gen, n, w, torch.float32)
+    (wg, wg64), (wu, wu64) = weights(gen, w, f, torch.float32), weights(gen, w, f, torch.float32)
+    dh, d64 = rows(gen, n, f, torch.float32)
+    h, g, u = (torch.empty((n, f), device="cuda") for _ in range(3))
+    B.slicegcn_gated_fwd(x, wg, wu, h, workspace(B.slicegcn_gated_fwd_workspace_bytes(n, w, f, torch.float32)), G=g, U=u, act=B.ACT_GELU)
+    dx, dwg = torch.empty_like(x), torch.empty_like(wg)
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, dh, workspace(B.slicegcn_gated_bwd_workspace_bytes(n, w, f, torch.float32)), dX=dx, dWg=dwg,
+                         act=B.ACT_GELU)
+
+    def loss():
+        return float((gated_fwd(x64, wg64, wu64, None, None, "gelu", torch.float32)["H"][0] * d64).sum())
+    step = 1e-5  # error of the differences: step^2 times third derivatives of order 1, 1e-10
+    for t64, grad in ((x64, dx.cpu()), (wg64, dwg.cpu())):
+        for i in range(t64.shape[0]):
+            for j in range(t64.shape[1]):
+                old = float(t64[i, j])
+                t64[i, j] = old + step
+                up = loss()
+                t64[i, j] = old - step
+                down = loss()
+                t64[i, j] = old
+                assert abs((up - down) / (2 * step) - float(grad[i, j])) < 1e-5  # sums of at most 30 products of order 1 in fp32: 30 * 2^-20
