@@ -26,15 +26,18 @@ int tile_for(const ProductShape &s)
 
 } // namespace
 
-ProductPlan plan_product(const ProductShape &s)
+ProductPlan plan_product(const ProductShape &s, bool aligned)
 {
     ProductPlan p{};
+    p.direct = aligned && s.type != SLICEGCN_F32 && s.M > 128 && s.N > 64;
     p.tile = tile_for(s);
-    const int bk = step_k(s.type), bn = s.gated ? TILE_N[p.tile] / 2 : TILE_N[p.tile];
-    const int64_t tiles = (s.M + TILE_M[p.tile] - 1) / TILE_M[p.tile] * ((s.N + bn - 1) / bn) * s.sets;
+    const int bk = p.direct ? DIRECT_K : step_k(s.type), bm = p.direct ? DIRECT_TILE : TILE_M[p.tile], all_cols = p.direct ? DIRECT_TILE : TILE_N[p.tile];
+    const int bn = s.gated ? all_cols / 2 : all_cols;
+    const int64_t tiles = (s.M + bm - 1) / bm * ((s.N + bn - 1) / bn) * s.sets;
     const int64_t steps = (s.K + bk - 1) / bk * s.segments, one = (int64_t)(s.gated ? 2 : s.sets) * s.M * s.N * 4;
-    int64_t splits = tiles >= CUS ? 1 : 2 * CUS / (tiles > 0 ? tiles : 1);
-    if (splits > steps / 4) splits = steps / 4;
+    const int64_t want = p.direct ? CUS : 2 * CUS, least = p.direct ? 16 : 4;
+    int64_t splits = 2 * tiles > want ? 1 : want / (tiles > 0 ? tiles : 1);
+    if (splits > steps / least) splits = steps / least;
     if (splits * one > MOST_PARTIAL) splits = MOST_PARTIAL / one;
     if (splits < (steps + CHAIN - 1) / CHAIN) splits = (steps + CHAIN - 1) / CHAIN;
     if (splits < 1) splits = 1;
@@ -47,8 +50,31 @@ ProductPlan plan_product(const ProductShape &s)
 
 namespace {
 
-int launch_product(int32_t type, int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream)
+// What a call may need, however its operands lie
+size_t partial_bytes(const ProductShape &s)
 {
+    const size_t x = plan_product(s, false).bytes, y = plan_product(s, true).bytes;
+    return x > y ? x : y;
+}
+
+// Whether both operands can go straight into LDS: rows and columns in whole units of 16 bytes, offsets within a tile in 32 bits
+bool on_units(const Operand &o) { return aligned16(o.p) && o.ld % 8 == 0 && o.ld <= 1 << 22; }
+bool aligned_product(int layouts, const ProductShape &s, const ProductArgs &a)
+{
+    for (int i = 0; i < (s.segments > s.sets ? s.segments : s.sets); ++i)
+        if (!on_units(a.a[i]) || !on_units(a.b[i])) return false;
+    if (s.gated && !on_units(a.b[1])) return false;
+    switch (layouts) {
+    case PRODUCT_XW: return s.K % 8 == 0 && s.N % 8 == 0;
+    case PRODUCT_GWT: return s.K % 8 == 0;
+    default: return s.M % 8 == 0 && s.N % 8 == 0;
+    }
+}
+
+int launch_product(const ProductShape &s, int layouts, int epilogue, ProductArgs &a, hipStream_t stream)
+{
+    const int32_t type = s.type;
+    const ProductPlan plan = plan_product(s, aligned_product(layouts, s, a));
     return type == SLICEGCN_F32    ? launch_product_f32(layouts, epilogue, plan, a, stream)
            : type == SLICEGCN_BF16 ? launch_product_bf16(layouts, epilogue, plan, a, stream)
                                    : launch_product_f16(layouts, epilogue, plan, a, stream);
@@ -203,7 +229,7 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     w.ld = round_up(w_out, 8);
     w.rows = (size_t)round_up(n * w.ld * type_bytes(type), 256);
     w.sums = (size_t)round_up(slope_parts(n, w_out) * q * (int64_t)w_out * 8, 256);
-    const size_t x = plan_product(dx_shape(n, w_in, w_out, type, q)).bytes, y = plan_product(dw_shape(n, w_in, w_out, type, q)).bytes;
+    const size_t x = partial_bytes(dx_shape(n, w_in, w_out, type, q)), y = partial_bytes(dw_shape(n, w_in, w_out, type, q));
     w.partial = x > y ? x : y;
     return w;
 }
@@ -321,7 +347,7 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         a.out[0] = static_cast<char *>(c.dx->data);
         a.ldo[0] = c.dx->ld;
         a.partial = partial;
-        if (int rc = launch_product(d.type, PRODUCT_GWT, EPI_STORE, plan_product(dx_shape(d.n, d.w_in, d.w_out, d.type, q)), a, stream)) return rc;
+        if (int rc = launch_product(dx_shape(d.n, d.w_in, d.w_out, d.type, q), PRODUCT_GWT, EPI_STORE, a, stream)) return rc;
     }
     if (want_w) {
         ProductArgs a{};
@@ -340,7 +366,7 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         a.sets = sets;
         a.partial = partial;
         // one of the two alone: cut like both, so that the workspace suffices and its bits are the same
-        if (int rc = launch_product(d.type, PRODUCT_XTG, EPI_STORE, plan_product(dw_shape(d.n, d.w_in, d.w_out, d.type, q)), a, stream)) return rc;
+        if (int rc = launch_product(dw_shape(d.n, d.w_in, d.w_out, d.type, q), PRODUCT_XTG, EPI_STORE, a, stream)) return rc;
     }
     return SLICEGCN_OK;
 }
@@ -353,7 +379,7 @@ using namespace slicegcn;
 extern "C" size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
 {
     if (!sizes_fit(n, w_in, w_out) || !known_type(type) || n == 0) return 0;
-    return plan_product(fwd_shape(n, w_in, w_out, type, false)).bytes;
+    return partial_bytes(fwd_shape(n, w_in, w_out, type, false));
 }
 
 extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const slicegcn_matrix *X, const void *W, const float *b, const slicegcn_matrix *R,
@@ -369,8 +395,8 @@ extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const sliceg
     if (int rc = check_params(what, d->type, {W}, {b})) return rc;
     if (d->n == 0) return SLICEGCN_OK;
     SG_REQUIRE(Y->data != X->data, SLICEGCN_EINVAL, "%s: Y in the rows of X", what);
-    const ProductPlan plan = plan_product(fwd_shape(d->n, d->w_in, d->w_out, d->type, false));
-    if (int rc = check_workspace(what, ws, ws_bytes, plan.bytes)) return rc;
+    const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, false);
+    if (int rc = check_workspace(what, ws, ws_bytes, partial_bytes(shape))) return rc;
     ProductArgs a{};
     a.a[0] = operand(X);
     a.b[0] = weights(W, d->w_out);
@@ -390,7 +416,7 @@ extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const sliceg
     a.act = d->act;
     a.partial = static_cast<float *>(ws);
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d->w_out, as_stream(stream));
-    return launch_product(d->type, PRODUCT_XW, EPI_FORWARD, plan, a, as_stream(stream));
+    return launch_product(shape, PRODUCT_XW, EPI_FORWARD, a, as_stream(stream));
 }
 
 extern "C" size_t slicegcn_product_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
@@ -429,7 +455,7 @@ extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *d, const sliceg
 extern "C" size_t slicegcn_gated_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
 {
     if (!sizes_fit(n, w_in, w_out) || !known_type(type) || n == 0) return 0;
-    return plan_product(fwd_shape(n, w_in, w_out, type, true)).bytes;
+    return partial_bytes(fwd_shape(n, w_in, w_out, type, true));
 }
 
 extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn_matrix *X, const void *Wg, const void *Wu, const float *bg,
@@ -447,8 +473,8 @@ extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn
     if (int rc = check_params(what, d->type, {Wg, Wu}, {bg, bu})) return rc;
     if (d->n == 0) return SLICEGCN_OK;
     SG_REQUIRE(H->data != X->data, SLICEGCN_EINVAL, "%s: H in the rows of X", what);
-    const ProductPlan plan = plan_product(fwd_shape(d->n, d->w_in, d->w_out, d->type, true));
-    if (int rc = check_workspace(what, ws, ws_bytes, plan.bytes)) return rc;
+    const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, true);
+    if (int rc = check_workspace(what, ws, ws_bytes, partial_bytes(shape))) return rc;
     ProductArgs a{};
     a.a[0] = operand(X);
     a.b[0] = weights(Wg, d->w_out);
@@ -470,7 +496,7 @@ extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn
     a.act = d->act;
     a.partial = static_cast<float *>(ws);
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d->w_out, as_stream(stream));
-    return launch_product(d->type, PRODUCT_XW, EPI_GATED, plan, a, as_stream(stream));
+    return launch_product(shape, PRODUCT_XW, EPI_GATED, a, as_stream(stream));
 }
 
 extern "C" size_t slicegcn_gated_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)

@@ -53,12 +53,12 @@ struct ProductShape {
     bool gated; // GATED
 };
 struct ProductPlan {
-    int32_t tile; // of the register path: index of a tile shape
+    bool direct;  // tiles of 256 x 256, operands straight into LDS (product_direct.h); else through registers
+    int32_t tile; // there: index of a tile shape
     int32_t splits, steps_per_split;
-    size_t partial_bytes() const { return bytes; }
-    size_t bytes;
+    size_t bytes; // of the sums of parts of k
 };
-ProductPlan plan_product(const ProductShape &s);
+ProductPlan plan_product(const ProductShape &s, bool aligned);
 
 // product_f32.hip, product_bf16.hip, product_f16.hip
 int launch_product_f32(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream);
@@ -70,6 +70,7 @@ constexpr int PRODUCT_XW = 0, PRODUCT_GWT = 1, PRODUCT_XTG = 2;
 
 constexpr int TILES = 3;
 constexpr int TILE_M[TILES] = {128, 64, 32}, TILE_N[TILES] = {128, 64, 128};
+constexpr int DIRECT_TILE = 256, DIRECT_K = 32;
 constexpr int STEP_K_F32 = 32, STEP_K_16 = 64;
 inline int step_k(int32_t type) { return type == SLICEGCN_F32 ? STEP_K_F32 : STEP_K_16; }
 

@@ -1,0 +1,210 @@
+// Products of 16-bit operands that lie on 16-byte boundaries, in tiles of 256 x 256.
+//
+// A workgroup of eight wavefronts, two of them a SIMD, each with 128 x 64 of the results.  Steps of 32 k go from memory straight into LDS (buffer loads with
+// the lds bit: no registers, and what lies outside of the operand arrives as zeros), DEPTH - 1 steps ahead in DEPTH buffers.  A load writes 64 units of 16 bytes
+// in the order of its lanes, so the order in LDS that lds_unit wants is made by the addresses that the lanes read from.  At the top of a
+// step a wavefront waits for its own loads of the step after this one and meets the others at a barrier: then that step is whole in LDS, and nobody reads the
+// buffer any more that the next loads are for.  During a step the operand registers for the next one are read: those of the N side into a second set, those of the M
+// side into the registers that the step is done with.
+// The waits are counted by hand, since the compiler does not know which reads of LDS a load in flight has to do with; the loads are therefore inline assembly,
+// which has no register results.
+#pragma once
+
+#include "product_kernels.h"
+
+namespace slicegcn {
+namespace {
+
+typedef int int4v __attribute__((ext_vector_type(4)));
+
+constexpr int DIRECT_THREADS = 512, DIRECT_DEPTH = 4;
+
+// 64 x 16 bytes from the buffer at rsrc, each lane's at its offset, to LDS at `lds` and behind it.  (m0, which holds that address, cannot be named as overwritten; the
+// compiler sets it itself right before instructions that use it, of which these kernels have no others.)
+__device__ inline void load_to_lds(int4v rsrc, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(rsrc) : "memory");
+}
+
+template <int COUNT> __device__ inline void wait_loads_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(COUNT) : "memory");
+}
+
+// The buffer of an operand from byte `at` on; `bytes` from its start to its end.  Nothing where at >= bytes.
+__device__ inline int4v buffer_of(const char *p, int64_t at, int64_t bytes)
+{
+    int64_t left = bytes > at ? bytes - at : 0;
+    if (left > 0xfffffff0ll) left = 0xfffffff0ll;
+    const uint64_t base = (uint64_t)(p + at);
+    return int4v{__builtin_amdgcn_readfirstlane((int)(uint32_t)base), __builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32) & 0xffff),
+                 __builtin_amdgcn_readfirstlane((int)(uint32_t)left), 0x00020000};
+}
+
+// How a lane's loads of a step reach an operand's piece of R outer indexes: offsets within a buffer that starts at the piece's first element (KC: of the
+// tile's first row, moved along k; OC: of the first k, moved from line to line)
+template <int LAYOUT, int R> struct DirectPiece {
+    static constexpr int UNITS = R * DIRECT_K / 8, LOADS = UNITS / DIRECT_THREADS;
+    static constexpr uint32_t NOWHERE = 0xfffffff8u; // beyond any buffer
+    uint32_t offset[LOADS];
+    const char *p;
+    int64_t ld, bytes, at; // in bytes
+
+    __device__ static int unit(int i) { return (int)threadIdx.x + i * DIRECT_THREADS; }
+    // k of a load's unit within the step (KC)
+    __device__ static int unit_k(int i) { return ((unit(i) % 4) ^ ((unit(i) / 4 >> 1) & 3)) * 8; }
+
+    // The piece from outer index o0 and k0 on, of `outer` and K
+    __device__ void aim(const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t K)
+    {
+        p = op.p;
+        ld = op.ld * 2;
+        bytes = (LAYOUT == LAYOUT_KC ? (outer - 1) * op.ld + K : (K - 1) * op.ld + outer) * 2;
+        at = (LAYOUT == LAYOUT_KC ? o0 * op.ld + k0 : k0 * op.ld + o0) * 2;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int u = unit(i);
+            if (LAYOUT == LAYOUT_KC) {
+                offset[i] = (uint32_t)(u / 4) * (uint32_t)ld + unit_k(i) * 2;
+            } else {
+                const int k = u / (R / 8), turn = (k & 3) | ((k >> 3) & 1) << 2;
+                offset[i] = (uint32_t)k * (uint32_t)ld + ((u % (R / 8)) ^ (turn << 1)) * 16;
+            }
+        }
+    }
+
+    // The step from k0 on, to LDS; nothing of it where it is not `there`
+    __device__ void load(uint32_t lds, int64_t k0, int64_t K, bool there, int wave)
+    {
+        const int4v rsrc = buffer_of(p, at, there ? bytes : 0);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            uint32_t off = offset[i];
+            if (LAYOUT == LAYOUT_KC && k0 + DIRECT_K > K && k0 + unit_k(i) >= K) off = NOWHERE; // the row's end
+            load_to_lds(rsrc, off, lds + (uint32_t)(wave * 64 + i * DIRECT_THREADS) * 16);
+        }
+        at += LAYOUT == LAYOUT_KC ? DIRECT_K * 2 : DIRECT_K * ld;
+    }
+};
+
+// GATED: the N side is a piece of 128 columns of each of the two products
+template <class T, int LM, int LN, int EPI, bool SPLIT>
+__global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const ProductArgs a)
+{
+    constexpr bool TURNS = EPI == EPI_GATED;
+    constexpr int BM = DIRECT_TILE, BN = DIRECT_TILE, BK = DIRECT_K, COLS = TURNS ? BN / 2 : BN, PIECES = BN / COLS;
+    constexpr int WN = 4, FM = 8, FN = 4, UNITS_M = BM * BK / 8, UNITS_N = COLS * BK / 8, STEP_UNITS = UNITS_M + PIECES * UNITS_N;
+    constexpr int LOADS = STEP_UNITS / DIRECT_THREADS; // of a wavefront and step
+    __shared__ short8 lds[DIRECT_DEPTH * STEP_UNITS];
+
+    const int64_t tile_rows = (a.M + BM - 1) / BM, tile_cols = (a.N + COLS - 1) / COLS, tiles = tile_rows * tile_cols;
+    int64_t id = tile_of(a.first + blockIdx.x, tiles * a.splits * a.sets), row_tile, col_tile;
+    const int set = a.sets > 1 ? (int)(id / (tiles * a.splits)) : 0;
+    id -= set * (tiles * a.splits);
+    const int split = SPLIT ? (int)(id / tiles) : 0;
+    tile_place(id - split * tiles, tile_rows, tile_cols, row_tile, col_tile);
+    const int64_t m0 = row_tile * BM, n0 = col_tile * COLS;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), lane = threadIdx.x % 64, wm = wave / WN * 128, wn = wave % WN * 64;
+
+    float4v acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
+
+    const int64_t steps_each = (a.K + BK - 1) / BK, all = steps_each * a.segments;
+    const int64_t begin = SPLIT ? (int64_t)split * a.steps_per_split : 0;
+    const int64_t end = SPLIT && begin + a.steps_per_split < all ? begin + a.steps_per_split : all;
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short8 *)lds;
+    DirectPiece<LM, BM> pm;
+    DirectPiece<LN, COLS> pn[PIECES];
+    int64_t next = begin; // step of the next loads
+    auto aim = [&](int64_t t) { // at the first step of a segment, or of this part
+        const int seg = t >= steps_each ? 1 : 0, which = seg + set;
+        const int64_t k0 = (t - seg * steps_each) * BK;
+        pm.aim(a.a[which], m0, a.M, k0, a.K);
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) pn[q].aim(a.b[TURNS ? q : which], n0, a.N, k0, a.K);
+    };
+    auto issue = [&]() {
+        if (a.segments > 1 && next == steps_each) aim(next);
+        const int64_t k0 = (a.segments > 1 && next >= steps_each ? next - steps_each : next) * BK;
+        uint32_t to = lds0 + (uint32_t)((next - begin) % DIRECT_DEPTH) * (STEP_UNITS * 16);
+        pm.load(to, k0, a.K, next < end, wave);
+        to += UNITS_M * 16;
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) pn[q].load(to + q * UNITS_N * 16, k0, a.K, next < end, wave);
+        ++next;
+    };
+    short8 fm[FM], fn[2][FN];
+    auto read_m = [&](int64_t t, int i) { return fragment<LM, BM, BK>(lds + t % DIRECT_DEPTH * STEP_UNITS, wm + 16 * i, 0, lane); };
+    auto read_n = [&](int64_t t, int j) {
+        const short8 *at = lds + t % DIRECT_DEPTH * STEP_UNITS + UNITS_M;
+        return TURNS ? fragment<LN, COLS, BK>(at + j % 2 * UNITS_N, wn / 2 + 8 * (j - j % 2), 0, lane) : fragment<LN, COLS, BK>(at, wn + 16 * j, 0, lane);
+    };
+
+    aim(begin);
+#pragma unroll
+    for (int i = 0; i < DIRECT_DEPTH - 1; ++i) issue();
+    wait_loads_and_meet<(DIRECT_DEPTH - 2) * LOADS>();
+#pragma unroll
+    for (int i = 0; i < FM; ++i) fm[i] = read_m(0, i);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fn[0][j] = read_n(0, j);
+    auto step = [&](int64_t t, auto parity) {
+        constexpr int Q = decltype(parity)::value;
+        wait_loads_and_meet<(DIRECT_DEPTH - 3) * LOADS>();
+        issue();
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fn[1 - Q][j] = read_n(t + 1, j);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = mfma<T>(fn[Q][j], fm[i], acc[i][j]);
+            fm[i] = read_m(t + 1, i);
+        }
+    };
+    for (int64_t t = 0; t < end - begin; t += 2) { // an odd number of steps ends with one of zeros
+        step(t, std::integral_constant<int, 0>());
+        step(t + 1, std::integral_constant<int, 1>());
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // no load into LDS outlives the workgroup
+
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int64_t row = m0 + wm + 16 * i + lane % 16;
+        if (row >= a.M) continue;
+#pragma unroll
+        for (int j = 0; j < FN; j += PIECES) {
+            const int64_t col = n0 + (TURNS ? wn / 2 + 8 * j : wn + 16 * j) + 4 * (lane / 16);
+            const int left = a.N - col < 4 ? (int)(a.N - col) : 4;
+            if (left <= 0) continue;
+            float s[4], s2[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[r] = acc[i][j][r];
+                s2[r] = acc[i][j + PIECES - 1][r];
+            }
+            if constexpr (SPLIT) {
+                char *to = reinterpret_cast<char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N);
+                store4<float>(to, row * a.N + col, left, s);
+            } else {
+                finish4<T, EPI>(a, set, row, col, left, s, s2);
+            }
+        }
+    }
+}
+
+template <class T, int LM, int LN, int EPI, bool SPLIT> int launch_direct(ProductArgs &a, hipStream_t stream)
+{
+    constexpr int COLS = EPI == EPI_GATED ? DIRECT_TILE / 2 : DIRECT_TILE;
+    const int64_t blocks = (a.M + DIRECT_TILE - 1) / DIRECT_TILE * ((a.N + COLS - 1) / COLS) * a.splits * a.sets;
+    return launch_parts(blocks, [&](unsigned first, unsigned count) {
+        a.first = first;
+        product_direct_kernel<T, LM, LN, EPI, SPLIT><<<count, DIRECT_THREADS, 0, stream>>>(a);
+    });
+}
+
+} // namespace
+} // namespace slicegcn

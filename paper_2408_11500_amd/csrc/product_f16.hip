@@ -1,5 +1,5 @@
 // The kernels of product.h for f16 rows.
-#include "product_kernels.h"
+#include "product_launch.h"
 
 namespace slicegcn {
 

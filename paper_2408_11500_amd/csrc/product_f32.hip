@@ -1,5 +1,5 @@
 // The kernels of product.h for f32 rows.
-#include "product_kernels.h"
+#include "product_launch.h"
 
 namespace slicegcn {
 
