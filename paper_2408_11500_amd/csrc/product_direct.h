@@ -19,11 +19,11 @@ typedef int int4v __attribute__((ext_vector_type(4)));
 
 constexpr int DIRECT_THREADS = 512, DIRECT_DEPTH = 4;
 
-// 64 x 16 bytes from the buffer at rsrc, each lane's at its offset, to LDS at `lds` and behind it.  (m0, which holds that address, cannot be named as overwritten; the
+// 64 x 16 bytes from the buffer at rsrc, each lane's at its offset and the scalar one, to LDS at `lds` and behind it.  (m0, which holds that address, cannot be named as overwritten; the
 // compiler sets it itself right before instructions that use it, of which these kernels have no others.)
-__device__ inline void load_to_lds(int4v rsrc, uint32_t offset, uint32_t lds)
+__device__ inline void load_to_lds(int4v rsrc, uint32_t offset, uint32_t scalar, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(rsrc) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(rsrc), "s"(scalar) : "memory");
 }
 
 template <int COUNT> __device__ inline void wait_loads_and_meet()
@@ -31,59 +31,80 @@ template <int COUNT> __device__ inline void wait_loads_and_meet()
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(COUNT) : "memory");
 }
 
-// The buffer of an operand from byte `at` on; `bytes` from its start to its end.  Nothing where at >= bytes.
-__device__ inline int4v buffer_of(const char *p, int64_t at, int64_t bytes)
-{
-    int64_t left = bytes > at ? bytes - at : 0;
-    if (left > 0xfffffff0ll) left = 0xfffffff0ll;
-    const uint64_t base = (uint64_t)(p + at);
-    return int4v{__builtin_amdgcn_readfirstlane((int)(uint32_t)base), __builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32) & 0xffff),
-                 __builtin_amdgcn_readfirstlane((int)(uint32_t)left), 0x00020000};
-}
-
-// How a lane's loads of a step reach an operand's piece of R outer indexes: offsets within a buffer that starts at the piece's first element (KC: of the
-// tile's first row, moved along k; OC: of the first k, moved from line to line)
+// How a lane's loads of a step reach an operand's piece of R outer indexes.  KC: a buffer from the tile's first row on, of which a step reads 32 k from its
+// scalar offset on.  OC: a buffer of the step's own lines.  All of a step's arithmetic is scalar, in 32 bits and without branches, so that the compiler can
+// put it between the matrix instructions of the step before.
 template <int LAYOUT, int R> struct DirectPiece {
     static constexpr int UNITS = R * DIRECT_K / 8, LOADS = UNITS / DIRECT_THREADS;
     static constexpr uint32_t NOWHERE = 0xfffffff8u; // beyond any buffer
     uint32_t offset[LOADS];
-    const char *p;
-    int64_t ld, bytes, at; // in bytes
+    uint64_t base;
+    uint32_t line, size, scalar; // bytes: of a line; KC: of the buffer, OC: of a line's part; KC: the step's offset
+    int4v rsrc;
 
     __device__ static int unit(int i) { return (int)threadIdx.x + i * DIRECT_THREADS; }
     // k of a load's unit within the step (KC)
     __device__ static int unit_k(int i) { return ((unit(i) % 4) ^ ((unit(i) / 4 >> 1) & 3)) * 8; }
 
     // The piece from outer index o0 and k0 on, of `outer` and K
-    __device__ void aim(const Operand &op, int64_t o0, int64_t outer, int64_t k0, int64_t K)
+    __device__ void aim(const Operand &op, int64_t o0, int64_t outer, int32_t k0, int32_t K)
     {
-        p = op.p;
-        ld = op.ld * 2;
-        bytes = (LAYOUT == LAYOUT_KC ? (outer - 1) * op.ld + K : (K - 1) * op.ld + outer) * 2;
-        at = (LAYOUT == LAYOUT_KC ? o0 * op.ld + k0 : k0 * op.ld + o0) * 2;
+        line = (uint32_t)op.ld * 2;
+        const int64_t here = outer - o0 < R ? outer - o0 : R;
+        if (LAYOUT == LAYOUT_KC) {
+            base = (uint64_t)op.p + (uint64_t)o0 * line;
+            size = (uint32_t)(here - 1) * line + (uint32_t)K * 2;
+            scalar = (uint32_t)k0 * 2;
+        } else {
+            base = (uint64_t)op.p + (uint64_t)k0 * line + (uint64_t)o0 * 2;
+            size = (uint32_t)here * 2;
+            scalar = 0;
+        }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int u = unit(i);
             if (LAYOUT == LAYOUT_KC) {
-                offset[i] = (uint32_t)(u / 4) * (uint32_t)ld + unit_k(i) * 2;
+                offset[i] = (uint32_t)(u / 4) * line + unit_k(i) * 2;
             } else {
                 const int k = u / (R / 8), turn = (k & 3) | ((k >> 3) & 1) << 2;
-                offset[i] = (uint32_t)k * (uint32_t)ld + ((u % (R / 8)) ^ (turn << 1)) * 16;
+                offset[i] = (uint32_t)k * line + ((u % (R / 8)) ^ (turn << 1)) * 16;
             }
         }
     }
 
-    // The step from k0 on, to LDS; nothing of it where it is not `there`
-    __device__ void load(uint32_t lds, int64_t k0, int64_t K, bool there, int wave)
+    // The step whose operand has `left` more k (none: nothing is read, and zeros arrive)
+    __device__ void prepare(int32_t left)
     {
-        const int4v rsrc = buffer_of(p, at, there ? bytes : 0);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            uint32_t off = offset[i];
-            if (LAYOUT == LAYOUT_KC && k0 + DIRECT_K > K && k0 + unit_k(i) >= K) off = NOWHERE; // the row's end
-            load_to_lds(rsrc, off, lds + (uint32_t)(wave * 64 + i * DIRECT_THREADS) * 16);
+        uint32_t bytes;
+        if (LAYOUT == LAYOUT_KC) {
+            bytes = left > 0 ? size : 0;
+        } else {
+            const int32_t lines = left < DIRECT_K ? left : DIRECT_K;
+            bytes = left > 0 ? (uint32_t)(lines - 1) * line + size : 0;
         }
-        at += LAYOUT == LAYOUT_KC ? DIRECT_K * 2 : DIRECT_K * ld;
+        rsrc = int4v{__builtin_amdgcn_readfirstlane((int)(uint32_t)base), __builtin_amdgcn_readfirstlane((int)(uint32_t)(base >> 32) & 0xffff),
+                     __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+    }
+
+    // Load i of that step, to LDS
+    __device__ void load(int i, uint32_t lds, int32_t left, int wave) const
+    {
+        const uint32_t off = LAYOUT == LAYOUT_KC && unit_k(i) >= left ? NOWHERE : offset[i]; // the row's end
+        load_to_lds(rsrc, off, scalar, lds + (uint32_t)(wave * 64 + i * DIRECT_THREADS) * 16);
+    }
+
+    __device__ void advance()
+    {
+        if (LAYOUT == LAYOUT_KC) scalar += DIRECT_K * 2;
+        else base += (uint64_t)DIRECT_K * line;
+    }
+
+    // On to the same lines' continuation in another operand of the same ld
+    __device__ void turn_to(const char *p, int64_t o0, bool now)
+    {
+        const uint64_t there = (uint64_t)p + (LAYOUT == LAYOUT_KC ? (uint64_t)o0 * line : (uint64_t)o0 * 2);
+        base = now ? there : base;
+        if (LAYOUT == LAYOUT_KC) scalar = now ? 0 : scalar;
     }
 };
 
@@ -91,10 +112,10 @@ template <int LAYOUT, int R> struct DirectPiece {
 template <class T, int LM, int LN, int EPI, bool SPLIT>
 __global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const ProductArgs a)
 {
-    constexpr bool TURNS = EPI == EPI_GATED;
+    constexpr bool TURNS = EPI == EPI_GATED, SEGMENTS = LM == LAYOUT_KC && LN == LAYOUT_KC;
     constexpr int BM = DIRECT_TILE, BN = DIRECT_TILE, BK = DIRECT_K, COLS = TURNS ? BN / 2 : BN, PIECES = BN / COLS;
     constexpr int WN = 4, FM = 8, FN = 4, UNITS_M = BM * BK / 8, UNITS_N = COLS * BK / 8, STEP_UNITS = UNITS_M + PIECES * UNITS_N;
-    constexpr int LOADS = STEP_UNITS / DIRECT_THREADS; // of a wavefront and step
+    constexpr int LOADS_M = UNITS_M / DIRECT_THREADS, LOADS_N = UNITS_N / DIRECT_THREADS, LOADS = LOADS_M + PIECES * LOADS_N; // of a wavefront and step
     __shared__ short8 lds[DIRECT_DEPTH * STEP_UNITS];
 
     const int64_t tile_rows = (a.M + BM - 1) / BM, tile_cols = (a.N + COLS - 1) / COLS, tiles = tile_rows * tile_cols;
@@ -112,60 +133,90 @@ __global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
 
-    const int64_t steps_each = (a.K + BK - 1) / BK, all = steps_each * a.segments;
-    const int64_t begin = SPLIT ? (int64_t)split * a.steps_per_split : 0;
-    const int64_t end = SPLIT && begin + a.steps_per_split < all ? begin + a.steps_per_split : all;
+    const int32_t K = (int32_t)a.K, steps_each = (K + BK - 1) / BK, all = SEGMENTS ? steps_each * a.segments : steps_each;
+    const int32_t begin = SPLIT ? split * a.steps_per_split : 0;
+    const int32_t end = SPLIT && begin + a.steps_per_split < all ? begin + a.steps_per_split : all;
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short8 *)lds;
     DirectPiece<LM, BM> pm;
     DirectPiece<LN, COLS> pn[PIECES];
-    int64_t next = begin; // step of the next loads
-    auto aim = [&](int64_t t) { // at the first step of a segment, or of this part
-        const int seg = t >= steps_each ? 1 : 0, which = seg + set;
-        const int64_t k0 = (t - seg * steps_each) * BK;
-        pm.aim(a.a[which], m0, a.M, k0, a.K);
+    int32_t next = begin, left, segment = SEGMENTS && begin >= steps_each ? 1 : 0; // step of the next loads, k that are left from there on, its segment
+    uint32_t to;
+    {
+        const int which = set + segment; // one of them is 0
+        const int32_t k0 = (begin - segment * steps_each) * BK;
+        pm.aim(a.a[which], m0, a.M, k0, K);
 #pragma unroll
-        for (int q = 0; q < PIECES; ++q) pn[q].aim(a.b[TURNS ? q : which], n0, a.N, k0, a.K);
+        for (int q = 0; q < PIECES; ++q) pn[q].aim(a.b[TURNS ? q : which], n0, a.N, k0, K);
+    }
+    const char *second_m = a.a[1].p, *second_n = a.b[1].p;
+    auto prepare = [&]() { // the loads of step `next`
+        if (SEGMENTS) {
+            const bool now = next == steps_each && segment == 0 && a.segments > 1;
+            pm.turn_to(second_m, m0, now);
+            pn[0].turn_to(second_n, n0, now);
+            segment = now ? 1 : segment;
+        }
+        left = K - (next - segment * steps_each) * BK;
+        left = next < end ? left : 0;
+        to = lds0 + (uint32_t)((next - begin) % DIRECT_DEPTH) * (STEP_UNITS * 16);
+        pm.prepare(left);
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) pn[q].prepare(left);
     };
-    auto issue = [&]() {
-        if (a.segments > 1 && next == steps_each) aim(next);
-        const int64_t k0 = (a.segments > 1 && next >= steps_each ? next - steps_each : next) * BK;
-        uint32_t to = lds0 + (uint32_t)((next - begin) % DIRECT_DEPTH) * (STEP_UNITS * 16);
-        pm.load(to, k0, a.K, next < end, wave);
-        to += UNITS_M * 16;
+    auto load = [&](int i) { // one of LOADS
+        if (i < LOADS_M) pm.load(i, to, left, wave);
+        else pn[(i - LOADS_M) / LOADS_N].load((i - LOADS_M) % LOADS_N, to + (UNITS_M + (i - LOADS_M) / LOADS_N * UNITS_N) * 16, left, wave);
+    };
+    auto advance = [&]() {
+        pm.advance();
 #pragma unroll
-        for (int q = 0; q < PIECES; ++q) pn[q].load(to + q * UNITS_N * 16, k0, a.K, next < end, wave);
+        for (int q = 0; q < PIECES; ++q) pn[q].advance();
         ++next;
     };
     short8 fm[FM], fn[2][FN];
-    auto read_m = [&](int64_t t, int i) { return fragment<LM, BM, BK>(lds + t % DIRECT_DEPTH * STEP_UNITS, wm + 16 * i, 0, lane); };
-    auto read_n = [&](int64_t t, int j) {
+    auto read_m = [&](int t, int i) { return fragment<LM, BM, BK>(lds + t % DIRECT_DEPTH * STEP_UNITS, wm + 16 * i, 0, lane); };
+    auto read_n = [&](int t, int j) {
         const short8 *at = lds + t % DIRECT_DEPTH * STEP_UNITS + UNITS_M;
         return TURNS ? fragment<LN, COLS, BK>(at + j % 2 * UNITS_N, wn / 2 + 8 * (j - j % 2), 0, lane) : fragment<LN, COLS, BK>(at, wn + 16 * j, 0, lane);
     };
 
-    aim(begin);
 #pragma unroll
-    for (int i = 0; i < DIRECT_DEPTH - 1; ++i) issue();
+    for (int d = 0; d < DIRECT_DEPTH - 1; ++d) {
+        prepare();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(i);
+        advance();
+    }
+    prepare();
     wait_loads_and_meet<(DIRECT_DEPTH - 2) * LOADS>();
 #pragma unroll
     for (int i = 0; i < FM; ++i) fm[i] = read_m(0, i);
 #pragma unroll
     for (int j = 0; j < FN; ++j) fn[0][j] = read_n(0, j);
-    auto step = [&](int64_t t, auto parity) {
+    // Matrix instructions in groups of one fragment of the M side, with a load and a fragment of the N side beside each of the first four and the scalar
+    // arithmetic of the next loads in the last four; the barriers keep the compiler from moving reads that the next step begins with to its end.
+    static_assert(LOADS == 4 && FN == 4 && FM == 8, "the groups of a step");
+    auto step = [&](int t, auto parity) {
         constexpr int Q = decltype(parity)::value;
         wait_loads_and_meet<(DIRECT_DEPTH - 3) * LOADS>();
-        issue();
-#pragma unroll
-        for (int j = 0; j < FN; ++j) fn[1 - Q][j] = read_n(t + 1, j);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
+            if (i < LOADS) load(i);
+            if (i < FN) fn[1 - Q][i] = read_n(t + 1, i);
+            if (i == LOADS) {
+                advance();
+                prepare();
+            }
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = mfma<T>(fn[Q][j], fm[i], acc[i][j]);
             fm[i] = read_m(t + 1, i);
+            if (i < LOADS) __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    for (int64_t t = 0; t < end - begin; t += 2) { // an odd number of steps ends with one of zeros
+    for (int32_t t = 0; t < end - begin; t += 2) { // an odd number of steps ends with one of zeros
         step(t, std::integral_constant<int, 0>());
         step(t + 1, std::integral_constant<int, 1>());
     }
