@@ -29,13 +29,16 @@ int tile_for(const ProductShape &s)
 ProductPlan plan_product(const ProductShape &s, bool aligned)
 {
     ProductPlan p{};
-    p.direct = aligned && s.type != SLICEGCN_F32 && s.M > 128 && s.N > 64;
+    aligned = aligned && s.type != SLICEGCN_F32;
+    p.kernel = aligned && s.by_rows && s.M <= ROWS_MOST ? BY_ROWS : aligned && s.M > ROWS_MOST && s.N > 64 ? BY_TILES : BY_REGISTERS;
     p.tile = tile_for(s);
-    const int bk = p.direct ? DIRECT_K : step_k(s.type), bm = p.direct ? DIRECT_TILE : TILE_M[p.tile], all_cols = p.direct ? DIRECT_TILE : TILE_N[p.tile];
-    const int bn = s.gated ? all_cols / 2 : all_cols;
+    const int bk = p.kernel == BY_REGISTERS ? step_k(s.type) : DIRECT_K;
+    const int bm = p.kernel == BY_ROWS ? ROWS_MOST : p.kernel == BY_TILES ? DIRECT_TILE : TILE_M[p.tile];
+    const int both = p.kernel == BY_ROWS ? 64 : p.kernel == BY_TILES ? DIRECT_TILE : TILE_N[p.tile], bn = s.gated ? both / 2 : both;
     const int64_t tiles = (s.M + bm - 1) / bm * ((s.N + bn - 1) / bn) * s.sets;
     const int64_t steps = (s.K + bk - 1) / bk * s.segments, one = (int64_t)(s.gated ? 2 : s.sets) * s.M * s.N * 4;
-    const int64_t want = p.direct ? CUS : 2 * CUS, least = p.direct ? 16 : 4;
+    const int64_t want = p.kernel == BY_REGISTERS ? 2 * CUS : CUS;
+    const int64_t least = p.kernel == BY_REGISTERS ? 4 : p.kernel == BY_TILES ? 16 : 64; // steps of a part
     int64_t splits = 2 * tiles > want ? 1 : want / (tiles > 0 ? tiles : 1);
     if (splits > steps / least) splits = steps / least;
     if (splits * one > MOST_PARTIAL) splits = MOST_PARTIAL / one;
@@ -220,8 +223,8 @@ struct BwdWorkspace {
     size_t bytes(int q) const { return q * rows + sums + partial; }
 };
 
-ProductShape dx_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q) { return ProductShape{n, w_out, w_in, q, 1, type, false}; }
-ProductShape dw_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q) { return ProductShape{w_in, n, w_out, 1, q, type, false}; }
+ProductShape dx_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q) { return ProductShape{n, w_out, w_in, q, 1, type, false, true}; }
+ProductShape dw_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q) { return ProductShape{w_in, n, w_out, 1, q, type, false, false}; }
 
 BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q)
 {
@@ -274,7 +277,7 @@ int check_workspace(const char *what, const void *ws, size_t ws_bytes, size_t ne
 Operand operand(const slicegcn_matrix *m) { return present(m) ? Operand{static_cast<const char *>(m->data), m->ld} : Operand{nullptr, 0}; }
 Operand weights(const void *w, int32_t w_out) { return Operand{static_cast<const char *>(w), w_out}; }
 
-ProductShape fwd_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, bool gated) { return ProductShape{n, w_in, w_out, 1, 1, type, gated}; }
+ProductShape fwd_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, bool gated) { return ProductShape{n, w_in, w_out, 1, 1, type, gated, true}; }
 
 // Both backward passes.  q = 2: gated
 struct BwdCall {

@@ -50,11 +50,13 @@ struct ProductShape {
     int64_t M, K;
     int32_t N;
     int32_t segments, sets, type;
-    bool gated; // GATED
+    bool gated;   // GATED
+    bool by_rows; // rows of the M side lie along k
 };
+constexpr int BY_REGISTERS = 0, BY_TILES = 1, BY_ROWS = 2; // product_kernels.h, product_direct.h, product_rows.h
 struct ProductPlan {
-    bool direct;  // tiles of 256 x 256, operands straight into LDS (product_direct.h); else through registers
-    int32_t tile; // there: index of a tile shape
+    int32_t kernel;
+    int32_t tile; // BY_REGISTERS: index of a tile shape
     int32_t splits, steps_per_split;
     size_t bytes; // of the sums of parts of k
 };
@@ -71,6 +73,8 @@ constexpr int PRODUCT_XW = 0, PRODUCT_GWT = 1, PRODUCT_XTG = 2;
 constexpr int TILES = 3;
 constexpr int TILE_M[TILES] = {128, 64, 32}, TILE_N[TILES] = {128, 64, 128};
 constexpr int DIRECT_TILE = 256, DIRECT_K = 32;
+constexpr int ROWS_MOST = 128;
+constexpr int rows_waves(int f) { return f <= 2 ? 8 : 4; } // wavefronts of product_rows_kernel for 16 f rows
 constexpr int STEP_K_F32 = 32, STEP_K_16 = 64;
 inline int step_k(int32_t type) { return type == SLICEGCN_F32 ? STEP_K_F32 : STEP_K_16; }
 

@@ -34,15 +34,17 @@ template <int COUNT> __device__ inline void wait_loads_and_meet()
 // How a lane's loads of a step reach an operand's piece of R outer indexes.  KC: a buffer from the tile's first row on, of which a step reads 32 k from its
 // scalar offset on.  OC: a buffer of the step's own lines.  All of a step's arithmetic is scalar, in 32 bits and without branches, so that the compiler can
 // put it between the matrix instructions of the step before.
-template <int LAYOUT, int R> struct DirectPiece {
-    static constexpr int UNITS = R * DIRECT_K / 8, LOADS = UNITS / DIRECT_THREADS;
+// THREADS: those that share the loads out: the workgroup's, or a wavefront's
+template <int LAYOUT, int R, int THREADS> struct DirectPiece {
+    static constexpr int UNITS = R * DIRECT_K / 8, LOADS = UNITS / THREADS;
+    static_assert(UNITS % THREADS == 0, "units are dealt evenly");
     static constexpr uint32_t NOWHERE = 0xfffffff8u; // beyond any buffer
     uint32_t offset[LOADS];
     uint64_t base;
     uint32_t line, size, scalar; // bytes: of a line; KC: of the buffer, OC: of a line's part; KC: the step's offset
     int4v rsrc;
 
-    __device__ static int unit(int i) { return (int)threadIdx.x + i * DIRECT_THREADS; }
+    __device__ static int unit(int i) { return (int)threadIdx.x % THREADS + i * THREADS; }
     // k of a load's unit within the step (KC)
     __device__ static int unit_k(int i) { return ((unit(i) % 4) ^ ((unit(i) / 4 >> 1) & 3)) * 8; }
 
@@ -66,7 +68,7 @@ template <int LAYOUT, int R> struct DirectPiece {
             if (LAYOUT == LAYOUT_KC) {
                 offset[i] = (uint32_t)(u / 4) * line + unit_k(i) * 2;
             } else {
-                const int k = u / (R / 8), turn = (k & 3) | ((k >> 3) & 1) << 2;
+                const int k = u / (R / 8), turn = line_turn<R>(k);
                 offset[i] = (uint32_t)k * line + ((u % (R / 8)) ^ (turn << 1)) * 16;
             }
         }
@@ -90,7 +92,7 @@ template <int LAYOUT, int R> struct DirectPiece {
     __device__ void load(int i, uint32_t lds, int32_t left, int wave) const
     {
         const uint32_t off = LAYOUT == LAYOUT_KC && unit_k(i) >= left ? NOWHERE : offset[i]; // the row's end
-        load_to_lds(rsrc, off, scalar, lds + (uint32_t)(wave * 64 + i * DIRECT_THREADS) * 16);
+        load_to_lds(rsrc, off, scalar, lds + (uint32_t)(wave * 64 + i * THREADS) * 16);
     }
 
     __device__ void advance()
@@ -138,8 +140,8 @@ __global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const
     const int32_t end = SPLIT && begin + a.steps_per_split < all ? begin + a.steps_per_split : all;
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short8 *)lds;
-    DirectPiece<LM, BM> pm;
-    DirectPiece<LN, COLS> pn[PIECES];
+    DirectPiece<LM, BM, DIRECT_THREADS> pm;
+    DirectPiece<LN, COLS, DIRECT_THREADS> pn[PIECES];
     int32_t next = begin, left, segment = SEGMENTS && begin >= steps_each ? 1 : 0; // step of the next loads, k that are left from there on, its segment
     uint32_t to;
     {

@@ -74,6 +74,7 @@ template <class T> __device__ inline void split8(const T (&v)[8], short8 (&out)[
 
 // Where a tile's piece of an operand lies in LDS (in 16-byte units; R outer indexes by BK of k), so that the lanes of a read meet in different banks:
 // KC: a row's units are permuted by its index; OC: 32-byte pairs of units of a line of k are permuted by its index, as the transposing read takes pairs.
+template <int R> __device__ inline int line_turn(int k) { return ((k & 3) | ((k >> 3) & 1) << 2) & (R / 16 - 1); }
 template <int LAYOUT, int R, int BK> __device__ inline int lds_unit(int outer_or_unit, int k_or_unit)
 {
     if constexpr (LAYOUT == LAYOUT_KC) {
@@ -81,8 +82,7 @@ template <int LAYOUT, int R, int BK> __device__ inline int lds_unit(int outer_or
         return row * (BK / 8) + (unit ^ (BK == 64 ? row & 7 : (row >> 1) & 3));
     } else {
         const int unit = outer_or_unit, k = k_or_unit;
-        const int turn = ((k & 3) | ((k >> 3) & 1) << 2) & (R / 16 - 1);
-        return k * (R / 8) + (unit ^ (turn << 1));
+        return k * (R / 8) + (unit ^ (line_turn<R>(k) << 1));
     }
 }
 

@@ -1,15 +1,18 @@
 // Which kernel a product of one element type takes.
 #pragma once
 
-#include "product_direct.h"
+#include "product_rows.h"
 
 namespace slicegcn {
 namespace {
 
 template <class T, int LM, int LN, int EPI, bool SPLIT> int launch_sums(const ProductPlan &plan, ProductArgs &a, hipStream_t stream)
 {
-    if constexpr (sizeof(T) == 2)
-        if (plan.direct) return launch_direct<T, LM, LN, EPI, SPLIT>(a, stream);
+    if constexpr (sizeof(T) == 2) {
+        if (plan.kernel == BY_TILES) return launch_direct<T, LM, LN, EPI, SPLIT>(a, stream);
+        if constexpr (LM == LAYOUT_KC)
+            if (plan.kernel == BY_ROWS) return launch_rows<T, LN, EPI, SPLIT>(a, stream);
+    }
     switch (plan.tile) {
     case 0: return launch_tile<T, LM, LN, EPI, 0, SPLIT>(a, stream);
     case 1: return launch_tile<T, LM, LN, EPI, 1, SPLIT>(a, stream);

@@ -13,7 +13,9 @@ ACT = dict(none=B.ACT_NONE, relu=B.ACT_RELU, silu=B.ACT_SILU, gelu=B.ACT_GELU)
 SIZES = [(1, 1, 1), (1, 64, 96), (1, 2000, 136), (2, 300, 1032), (3, 7, 5), (5, 1048, 40), (9, 520, 264), (17, 33, 31), (24, 1024, 200), (32, 128, 256),
          (33, 65, 129), (70, 2304, 64), (128, 64, 64), (200, 130, 70), (257, 520, 384), (300, 264, 520), (1000, 72, 40), (5000, 24, 8), (1, 8, 8), (64, 32, 16),
          # rows and columns in whole units of 16 bytes, tiles of 256: less than one, sums of one step, of an odd number, cut sums, ends within a step
-         (129, 8, 72), (256, 64, 256), (300, 40, 72), (513, 1000, 776), (130, 2056, 136), (1040, 96, 264)]
+         (129, 8, 72), (256, 64, 256), (300, 40, 72), (513, 1000, 776), (130, 2056, 136), (1040, 96, 264),
+         # few rows of such operands: strips of 64 columns, k shared out among wavefronts and cut, more wavefronts than steps
+         (1, 4104, 136), (16, 40, 64), (17, 2304, 72), (31, 5000, 24), (40, 264, 96), (64, 4096, 64), (65, 72, 200), (100, 2600, 136), (128, 1000, 40)]
 
 
 def weights(gen, w_in, w_out, dtype):
