@@ -200,35 +200,59 @@ typedef struct {
     int64_t ld;
 } slicegcn_matrix;
 
-/* P = X W + b;  Y = residual * R + act(P).  b, R, P may be NULL; P is kept for the backward pass, which needs it where there is an activation.
- * EINVAL: NULL descriptor, X, W or Y; n < 0, widths < 1, ld < width, unknown type or activation, misaligned base, residual not finite, Y in
- * the rows of X; ERANGE: n or a width too large; EWORKSPACE. */
-size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type); /* 0 on bad input, and where none is needed */
-int slicegcn_product_fwd(const slicegcn_product_desc *desc, const slicegcn_matrix *X, const void *W, const float *b, const slicegcn_matrix *R,
-                         const slicegcn_matrix *P, const slicegcn_matrix *Y, void *ws, size_t ws_bytes, void *stream);
+/* What a call works on; a backward pass reads what the forward pass read and kept, and writes the gradients.  Absent matrices and vectors: NULL. */
+typedef struct {
+    slicegcn_matrix X;
+    const void *W;
+    const float *b;
+    slicegcn_matrix R;
+    slicegcn_matrix P;
+    slicegcn_matrix Y;  /* forward */
+    slicegcn_matrix dY; /* from here on: backward */
+    slicegcn_matrix dX;
+    void *dW;
+    float *db;
+    slicegcn_matrix dR;
+} slicegcn_product_io;
+typedef struct {
+    slicegcn_matrix X;
+    const void *Wg;
+    const void *Wu;
+    const float *bg;
+    const float *bu;
+    slicegcn_matrix G;
+    slicegcn_matrix U;
+    slicegcn_matrix H;  /* forward */
+    slicegcn_matrix dH; /* from here on: backward */
+    slicegcn_matrix dX;
+    void *dWg;
+    void *dWu;
+    float *dbg;
+    float *dbu;
+} slicegcn_gated_io;
 
-/* dP = dY * act'(P);  dX = dP W^T;  dW = X^T dP;  db = column sums of dP;  dR = residual * dY.  NULL outputs are not formed (the inputs that only they
- * need may be NULL too).  dP is rounded to the rows' type before the products; db is formed from it unrounded.
+/* P = X W + b;  Y = residual * R + act(P).  b, R, P may be absent; P is kept for the backward pass, which needs it where there is an activation.
+ * EINVAL: NULL descriptor, io, X, W or Y; n < 0, widths < 1, ld < width or beyond 2^31, unknown type or activation, misaligned base, residual not
+ * finite, Y in the rows of X; ERANGE: n or a width too large; EWORKSPACE. */
+size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type); /* 0 on bad input, and where none is needed */
+int slicegcn_product_fwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream);
+
+/* dP = dY * act'(P);  dX = dP W^T;  dW = X^T dP;  db = column sums of dP;  dR = residual * dY.  Absent outputs are not formed (the inputs that only they
+ * need may be absent too).  dP is rounded to the rows' type before the products; db is formed from it unrounded.
  * EINVAL, ERANGE, EWORKSPACE as above. */
 size_t slicegcn_product_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
-int slicegcn_product_bwd(const slicegcn_product_desc *desc, const slicegcn_matrix *X, const void *W, const slicegcn_matrix *P,
-                         const slicegcn_matrix *dY, const slicegcn_matrix *dX, void *dW, float *db, const slicegcn_matrix *dR, void *ws,
-                         size_t ws_bytes, void *stream);
+int slicegcn_product_bwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream);
 
 /* Gated projections, the first half of a feed-forward block (slicegcn_product_fwd is the second):
  *   G = X Wg + bg;  U = X Wu + bu;  H = act(G) * U
- * H is formed from G and U before they are rounded.  bg, bu may be NULL; G and U (both or neither) are kept for the backward pass. */
+ * H is formed from G and U before they are rounded.  bg, bu may be absent; G and U (both or neither) are kept for the backward pass. */
 size_t slicegcn_gated_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
-int slicegcn_gated_fwd(const slicegcn_product_desc *desc, const slicegcn_matrix *X, const void *Wg, const void *Wu, const float *bg,
-                       const float *bu, const slicegcn_matrix *G, const slicegcn_matrix *U, const slicegcn_matrix *H, void *ws,
-                       size_t ws_bytes, void *stream);
+int slicegcn_gated_fwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream);
 
-/* dG = dH * U * act'(G);  dU = dH * act(G);  dX = dG Wg^T + dU Wu^T;  dWg = X^T dG;  dWu = X^T dU;  dbg, dbu: column sums.  NULL outputs are not
+/* dG = dH * U * act'(G);  dU = dH * act(G);  dX = dG Wg^T + dU Wu^T;  dWg = X^T dG;  dWu = X^T dU;  dbg, dbu: column sums.  Absent outputs are not
  * formed.  dG and dU are rounded to the rows' type before the products; dbg and dbu are formed from them unrounded. */
 size_t slicegcn_gated_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
-int slicegcn_gated_bwd(const slicegcn_product_desc *desc, const slicegcn_matrix *X, const void *Wg, const void *Wu, const slicegcn_matrix *G,
-                       const slicegcn_matrix *U, const slicegcn_matrix *dH, const slicegcn_matrix *dX, void *dWg, void *dWu, float *dbg,
-                       float *dbu, void *ws, size_t ws_bytes, void *stream);
+int slicegcn_gated_bwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------
  * One AdamW step (decoupled weight decay) over many tensors at once, step >= 1, in place:

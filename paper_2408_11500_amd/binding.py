@@ -131,7 +131,8 @@ _RESNORM_IO = struct.Struct("@" + 5 * "Pq" + "P" + 5 * "Pq")  # x, y, gate, h, u
 
 
 _PRODUCT_DESC = struct.Struct("@qiiiid")        # n, w_in, w_out, type, act, residual
-_MATRIX = struct.Struct("@Pq")                  # data, ld
+_PRODUCT_IO = struct.Struct("@" + "Pq" + "2P" + 5 * "Pq" + "2P" + "Pq")  # X; W, b; R, P, Y, dY, dX; dW, db; dR
+_GATED_IO = struct.Struct("@" + "Pq" + "4P" + 5 * "Pq" + "4P")  # X; Wg, Wu, bg, bu; G, U, H, dH, dX; dWg, dWu, dbg, dbu
 
 
 class _Tensor(ctypes.Structure):
@@ -224,10 +225,8 @@ def lib() -> ctypes.CDLL:
         for fn in (L.slicegcn_product_fwd_workspace_bytes, L.slicegcn_product_bwd_workspace_bytes, L.slicegcn_gated_fwd_workspace_bytes,
                    L.slicegcn_gated_bwd_workspace_bytes):
             fn.argtypes, fn.restype = [i64, i32, i32, i32], sz
-        L.slicegcn_product_fwd.argtypes = 7 * [vp] + [vp, sz, vp]
-        L.slicegcn_product_bwd.argtypes = 9 * [vp] + [vp, sz, vp]
-        L.slicegcn_gated_fwd.argtypes = 9 * [vp] + [vp, sz, vp]
-        L.slicegcn_gated_bwd.argtypes = 12 * [vp] + [vp, sz, vp]
+        for fn in (L.slicegcn_product_fwd, L.slicegcn_product_bwd, L.slicegcn_gated_fwd, L.slicegcn_gated_bwd):
+            fn.argtypes = [vp, vp, vp, sz, vp]
         L.slicegcn_adamw_step.argtypes = [vp, i32, i32, f64, f64, f64, f64, i32, vp, ctypes.c_uint64, vp]
         L.slicegcn_strerror.argtypes = [ctypes.c_int]
         L.slicegcn_strerror.restype = ctypes.c_char_p
@@ -890,18 +889,6 @@ def _weights(t, name: str, shape, dtype):
     return t.data_ptr()
 
 
-def _matrix(t, name: str, shape, dtype):
-    """A packed slicegcn_matrix, or None."""
-    return None if t is None else _MATRIX.pack(*_rows(t, name, shape, dtype))
-
-
-def _product_sizes(X, W, other):
-    """(shape of X, of W, of the results, type) of a product's call: n from a matrix with a row each, widths from the weights."""
-    w_in, w_out = W.shape
-    n = (X if X is not None else other).shape[0]
-    return (n, w_in), (w_in, w_out), (n, w_out), W.dtype
-
-
 def _workspace_bytes(fn, n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
     if dtype not in VALUE_TYPES:
         raise TypeError(f"expected fp32, bf16 or fp16, not {dtype}")
@@ -914,10 +901,12 @@ def slicegcn_product_fwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: t
 
 def slicegcn_product_fwd(X, W, Y, ws=None, b=None, R=None, P=None, act: int = ACT_NONE, residual: float = 1.0):
     """P = X W + b;  Y = residual * R + act(P).  ``b`` (fp32), ``R``, ``P`` may be None; the others are of one type."""
-    xs, wsh, ys, dtype = _product_sizes(X, W, Y)
-    desc = _PRODUCT_DESC.pack(ys[0], *wsh, _value_type(W, "W"), act, residual)
-    _check(lib().slicegcn_product_fwd(desc, _matrix(X, "X", xs, dtype), _weights(W, "W", wsh, dtype), _columns(b, "b", wsh[1]),
-                                      _matrix(R, "R", ys, dtype), _matrix(P, "P", ys, dtype), _matrix(Y, "Y", ys, dtype), *_ws(ws), _stream()))
+    (w_in, w_out), wsh, dtype, ys = W.shape, W.shape, W.dtype, Y.shape
+    xs = (ys[0], w_in)
+    desc = _PRODUCT_DESC.pack(ys[0], w_in, w_out, _value_type(W, "W"), act, residual)
+    io = _PRODUCT_IO.pack(*_rows(X, "X", xs, dtype), _weights(W, "W", wsh, dtype), _columns(b, "b", w_out), *_rows(R, "R", ys, dtype),
+                          *_rows(P, "P", ys, dtype), *_rows(Y, "Y", (ys[0], w_out), dtype), 0, 0, 0, 0, 0, 0, 0, 0)
+    _check(lib().slicegcn_product_fwd(desc, io, *_ws(ws), _stream()))
     return Y
 
 
@@ -928,11 +917,13 @@ def slicegcn_product_bwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: t
 def slicegcn_product_bwd(X, W, P, dY, ws=None, dX=None, dW=None, db=None, dR=None, act: int = ACT_NONE, residual: float = 1.0):
     """dP = dY * act'(P);  dX = dP W^T;  dW = X^T dP;  db (fp32) = column sums of dP;  dR = residual * dY.  Gradients that are None are not
     formed; ``P`` is needed where there is an activation, ``X`` for dW."""
-    xs, wsh, ys, dtype = _product_sizes(X, W, dY)
-    desc = _PRODUCT_DESC.pack(ys[0], *wsh, _value_type(W, "W"), act, residual)
-    _check(lib().slicegcn_product_bwd(desc, _matrix(X, "X", xs, dtype), _weights(W, "W", wsh, dtype), _matrix(P, "P", ys, dtype),
-                                      _matrix(dY, "dY", ys, dtype), _matrix(dX, "dX", xs, dtype), _weights(dW, "dW", wsh, dtype),
-                                      _columns(db, "db", wsh[1]), _matrix(dR, "dR", ys, dtype), *_ws(ws), _stream()))
+    (w_in, w_out), wsh, dtype, ys = W.shape, W.shape, W.dtype, dY.shape
+    xs = (ys[0], w_in)
+    desc = _PRODUCT_DESC.pack(ys[0], w_in, w_out, _value_type(W, "W"), act, residual)
+    io = _PRODUCT_IO.pack(*_rows(X, "X", xs, dtype), _weights(W, "W", wsh, dtype), 0, 0, 0, *_rows(P, "P", ys, dtype), 0, 0,
+                          *_rows(dY, "dY", (ys[0], w_out), dtype), *_rows(dX, "dX", xs, dtype), _weights(dW, "dW", wsh, dtype),
+                          _columns(db, "db", w_out), *_rows(dR, "dR", ys, dtype))
+    _check(lib().slicegcn_product_bwd(desc, io, *_ws(ws), _stream()))
 
 
 def slicegcn_gated_fwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
@@ -942,11 +933,12 @@ def slicegcn_gated_fwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: tor
 def slicegcn_gated_fwd(X, Wg, Wu, H, ws=None, bg=None, bu=None, G=None, U=None, act: int = ACT_SILU):
     """G = X Wg + bg;  U = X Wu + bu;  H = act(G) * U.  ``bg``, ``bu`` (fp32) may be None; ``G`` and ``U`` (both or neither) are kept for the
     backward pass."""
-    xs, wsh, ys, dtype = _product_sizes(X, Wg, H)
-    desc = _PRODUCT_DESC.pack(ys[0], *wsh, _value_type(Wg, "Wg"), act, 0.0)
-    _check(lib().slicegcn_gated_fwd(desc, _matrix(X, "X", xs, dtype), _weights(Wg, "Wg", wsh, dtype), _weights(Wu, "Wu", wsh, dtype),
-                                    _columns(bg, "bg", wsh[1]), _columns(bu, "bu", wsh[1]), _matrix(G, "G", ys, dtype),
-                                    _matrix(U, "U", ys, dtype), _matrix(H, "H", ys, dtype), *_ws(ws), _stream()))
+    (w_in, w_out), wsh, dtype, ys = Wg.shape, Wg.shape, Wg.dtype, H.shape
+    desc = _PRODUCT_DESC.pack(ys[0], w_in, w_out, _value_type(Wg, "Wg"), act, 0.0)
+    io = _GATED_IO.pack(*_rows(X, "X", (ys[0], w_in), dtype), _weights(Wg, "Wg", wsh, dtype), _weights(Wu, "Wu", wsh, dtype),
+                        _columns(bg, "bg", w_out), _columns(bu, "bu", w_out), *_rows(G, "G", ys, dtype), *_rows(U, "U", ys, dtype),
+                        *_rows(H, "H", (ys[0], w_out), dtype), 0, 0, 0, 0, 0, 0, 0, 0)
+    _check(lib().slicegcn_gated_fwd(desc, io, *_ws(ws), _stream()))
     return H
 
 
@@ -956,12 +948,14 @@ def slicegcn_gated_bwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: tor
 
 def slicegcn_gated_bwd(X, Wg, Wu, G, U, dH, ws=None, dX=None, dWg=None, dWu=None, dbg=None, dbu=None, act: int = ACT_SILU):
     """Gradients of slicegcn_gated_fwd from ``dH`` and the G and U that it kept; those that are None are not formed."""
-    xs, wsh, ys, dtype = _product_sizes(X, Wg, dH)
-    desc = _PRODUCT_DESC.pack(ys[0], *wsh, _value_type(Wg, "Wg"), act, 0.0)
-    _check(lib().slicegcn_gated_bwd(desc, _matrix(X, "X", xs, dtype), _weights(Wg, "Wg", wsh, dtype), _weights(Wu, "Wu", wsh, dtype),
-                                    _matrix(G, "G", ys, dtype), _matrix(U, "U", ys, dtype), _matrix(dH, "dH", ys, dtype),
-                                    _matrix(dX, "dX", xs, dtype), _weights(dWg, "dWg", wsh, dtype), _weights(dWu, "dWu", wsh, dtype),
-                                    _columns(dbg, "dbg", wsh[1]), _columns(dbu, "dbu", wsh[1]), *_ws(ws), _stream()))
+    (w_in, w_out), wsh, dtype, ys = Wg.shape, Wg.shape, Wg.dtype, dH.shape
+    xs = (ys[0], w_in)
+    desc = _PRODUCT_DESC.pack(ys[0], w_in, w_out, _value_type(Wg, "Wg"), act, 0.0)
+    io = _GATED_IO.pack(*_rows(X, "X", xs, dtype), _weights(Wg, "Wg", wsh, dtype), _weights(Wu, "Wu", wsh, dtype), 0, 0,
+                        *_rows(G, "G", ys, dtype), *_rows(U, "U", ys, dtype), 0, 0, *_rows(dH, "dH", (ys[0], w_out), dtype),
+                        *_rows(dX, "dX", xs, dtype), _weights(dWg, "dWg", wsh, dtype), _weights(dWu, "dWu", wsh, dtype),
+                        _columns(dbg, "dbg", w_out), _columns(dbu, "dbu", w_out))
+    _check(lib().slicegcn_gated_bwd(desc, io, *_ws(ws), _stream()))
 
 
 # ---- AdamW over many tensors

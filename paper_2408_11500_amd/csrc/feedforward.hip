@@ -90,22 +90,23 @@ struct SlopeArgs {
     Operand g, u, d;
     char *dg, *du, *dr;
     int64_t ldg, ldu, ldr, n;
-    int32_t w, act;
+    int32_t w, lanes; // columns; threads that share a row out
     float residual;
     double *partial; // column sums of parts of the rows: [part][1 or 2][w], where biases have gradients
-    int32_t parts;
     int64_t rows_per_part;
 };
 
-constexpr int SLOPE_V = 4, SLOPE_RUN = 32; // columns a thread owns; rows that are added in fp32 before they are added in fp64
+constexpr int SLOPE_RUN = 32; // rows that are added in fp32 before they are added in fp64
 
-// Workgroup (x, y): 64 x 4 columns, rows of part y; the four wavefronts take rows in turn
-template <class T, bool GATED> __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a)
+// Workgroup (x, y): `lanes` accesses of 16 bytes of the rows of part y, 256 / lanes rows at a time and ROWS such turns in flight.  Bound by bytes:
+// 2.4 M rows of 256 bf16 columns through a gelu
+template <class T, bool GATED, int ACT> __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a)
 {
-    constexpr int V = SLOPE_V, Q = GATED ? 2 : 1;
-    __shared__ double sums[3][Q * V][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t col = ((int64_t)blockIdx.x * 64 + lane) * V;
+    constexpr int V = 16 / sizeof(T), Q = GATED ? 2 : 1, ROWS = GATED ? 2 : 4;
+    constexpr bool SLOPES = GATED || ACT != SLICEGCN_ACT_NONE;
+    __shared__ double sums[256][Q * V];
+    const int groups = 256 / a.lanes, lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
+    const int64_t col = ((int64_t)blockIdx.x * a.lanes + lane) * V;
     const int left = a.w - col < V ? (int)(a.w - col) : V;
     const int64_t first = blockIdx.y * a.rows_per_part, last = first + a.rows_per_part < a.n ? first + a.rows_per_part : a.n;
     double total[Q][V] = {};
@@ -133,40 +134,48 @@ template <class T, bool GATED> __global__ __launch_bounds__(256) void slope_kern
         }
     };
     if (left > 0) {
-        for (int64_t row = first + wave; row < last; row += 4) {
-            float d[V], g[V], u[V], o[Q][V];
-            read(a.d, row, d);
-            if (a.g.p) read(a.g, row, g);
-            if (GATED) read(a.u, row, u);
+        for (int64_t row0 = first + group; row0 < last; row0 += (int64_t)groups * ROWS) {
+            float d[ROWS][V], g[ROWS][V], u[ROWS][V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float y = 0.f, slope = 1.f;
-                if (a.g.p) activated_slope(a.act, g[i], y, slope);
-                o[0][i] = GATED ? d[i] * u[i] * slope : d[i] * slope;
-                if (GATED) o[Q - 1][i] = d[i] * y;
+            for (int r = 0; r < ROWS; ++r) {
+                const int64_t row = row0 + r * groups < last ? row0 + r * groups : row0; // the last turn reads a row again rather than branch
+                read(a.d, row, d[r]);
+                if (SLOPES) read(a.g, row, g[r]);
+                if (GATED) read(a.u, row, u[r]);
             }
-            if (a.dg) write(a.dg, a.ldg, row, o[0]);
-            if (GATED && a.du) write(a.du, a.ldu, row, o[Q - 1]);
-            if (a.dr) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) d[i] *= a.residual;
-                write(a.dr, a.ldr, row, d);
-            }
-            if (a.partial) {
+            for (int r = 0; r < ROWS; ++r) {
+                const int64_t row = row0 + r * groups;
+                if (row >= last) break;
+                float o[Q][V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float y = 0.f, slope = 1.f;
+                    if (SLOPES) activated_slope<ACT>(g[r][i], y, slope);
+                    o[0][i] = GATED ? d[r][i] * u[r][i] * slope : d[r][i] * slope;
+                    if (GATED) o[Q - 1][i] = d[r][i] * y;
+                }
+                if (a.dg) write(a.dg, a.ldg, row, o[0]);
+                if (GATED && a.du) write(a.du, a.ldu, row, o[Q - 1]);
+                if (a.dr) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) d[r][i] *= a.residual;
+                    write(a.dr, a.ldr, row, d[r]);
+                }
 #pragma unroll
                 for (int q = 0; q < Q; ++q)
 #pragma unroll
                     for (int i = 0; i < V; ++i) run[q][i] += o[q][i];
-                if (++in_run == SLOPE_RUN) {
-                    in_run = 0;
+            }
+            if (a.partial && (in_run += ROWS) >= SLOPE_RUN) {
+                in_run = 0;
 #pragma unroll
-                    for (int q = 0; q < Q; ++q)
+                for (int q = 0; q < Q; ++q)
 #pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            total[q][i] += (double)run[q][i];
-                            run[q][i] = 0.f;
-                        }
-                }
+                    for (int i = 0; i < V; ++i) {
+                        total[q][i] += (double)run[q][i];
+                        run[q][i] = 0.f;
+                    }
             }
         }
     }
@@ -174,46 +183,57 @@ template <class T, bool GATED> __global__ __launch_bounds__(256) void slope_kern
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            total[q][i] += (double)run[q][i];
-            if (wave > 0) sums[wave - 1][q * V + i][lane] = total[q][i];
-        }
+        for (int i = 0; i < V; ++i) sums[threadIdx.x][q * V + i] = total[q][i] + (double)run[q][i];
     __syncthreads();
-    if (wave > 0 || left <= 0) return;
+    if (group > 0 || left <= 0) return;
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if (i >= left) continue;
-            double t = total[q][i];
-#pragma unroll
-            for (int w = 0; w < 3; ++w) t += sums[w][q * V + i][lane];
+            double t = 0.0;
+            for (int w = 0; w < groups; ++w) t += sums[w * a.lanes + lane][q * V + i];
             a.partial[((int64_t)blockIdx.y * Q + q) * a.w + col + i] = t;
         }
 }
 
-// db[q][j] = sum over the parts, in order; 64 columns and 4 shares of the parts a workgroup
-__global__ __launch_bounds__(256) void bias_kernel(const double *__restrict__ partial, int32_t parts, int32_t q_count, int32_t w, float *__restrict__ db0,
-                                                   float *__restrict__ db1)
+// db[q][j] = sum over the parts: 16 columns and 64 shares of the parts a workgroup, the shares added in order
+__global__ __launch_bounds__(1024) void bias_kernel(const double *__restrict__ partial, int32_t parts, int32_t q_count, int32_t w, float *__restrict__ db0,
+                                                    float *__restrict__ db1)
 {
-    __shared__ double sums[4][64];
-    const int lane = threadIdx.x % 64, share = threadIdx.x / 64, q = blockIdx.y;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ double sums[64][17];
+    const int lane = threadIdx.x % 16, share = threadIdx.x / 16, q = blockIdx.y;
+    const int64_t col = (int64_t)blockIdx.x * 16 + lane;
     double t = 0.0;
-    if (col < w)
-        for (int32_t p = share; p < parts; p += 4) t += partial[((int64_t)p * q_count + q) * w + col];
+    if (col < w) {
+#pragma unroll 4
+        for (int32_t p = share; p < parts; p += 64) t += partial[((int64_t)p * q_count + q) * w + col];
+    }
     sums[share][lane] = t;
     __syncthreads();
     float *db = q ? db1 : db0;
-    if (share == 0 && col < w && db) db[col] = (float)(((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane]);
+    if (share != 0 || col >= w || !db) return;
+    for (int s = 1; s < 64; ++s) t += sums[s][lane];
+    db[col] = (float)t;
 }
 
-int64_t slope_parts(int64_t n, int32_t w)
+struct SlopeGrid {
+    int32_t lanes;
+    int64_t cols, parts; // workgroups
+};
+
+SlopeGrid slope_grid(int64_t n, int32_t w, int32_t type)
 {
-    const int64_t cols = ((int64_t)w + 64 * SLOPE_V - 1) / (64 * SLOPE_V);
-    int64_t parts = (8 * CUS + cols - 1) / cols;
-    if (parts > (n + 15) / 16) parts = (n + 15) / 16;
-    return parts > 0 ? parts : 1;
+    const int64_t accesses = ((int64_t)w * type_bytes(type) + 15) / 16;
+    SlopeGrid g;
+    g.lanes = 1;
+    while (g.lanes < 64 && g.lanes < accesses) g.lanes *= 2;
+    g.cols = (accesses + g.lanes - 1) / g.lanes;
+    const int64_t rows = 256 / g.lanes;
+    g.parts = (8 * CUS + g.cols - 1) / g.cols;
+    if (g.parts > (n + rows - 1) / rows) g.parts = (n + rows - 1) / rows;
+    if (g.parts < 1) g.parts = 1;
+    return g;
 }
 
 // Workspace of a backward pass: gradients before the activation, their column sums, sums of parts of k
@@ -231,7 +251,7 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     BwdWorkspace w;
     w.ld = round_up(w_out, 8);
     w.rows = (size_t)round_up(n * w.ld * type_bytes(type), 256);
-    w.sums = (size_t)round_up(slope_parts(n, w_out) * q * (int64_t)w_out * 8, 256);
+    w.sums = (size_t)round_up(slope_grid(n, w_out, type).parts * q * (int64_t)w_out * 8, 256);
     const size_t x = partial_bytes(dx_shape(n, w_in, w_out, type, q)), y = partial_bytes(dw_shape(n, w_in, w_out, type, q));
     w.partial = x > y ? x : y;
     return w;
@@ -239,9 +259,9 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
 
 bool sizes_fit(int64_t n, int32_t w_in, int32_t w_out) { return n >= 0 && n <= INT32_MAX && w_in >= 1 && w_out >= 1 && w_in <= 1 << 24 && w_out <= 1 << 24; }
 
-int check(const char *what, const slicegcn_product_desc *d)
+int check(const char *what, const slicegcn_product_desc *d, const void *io)
 {
-    SG_REQUIRE(d, SLICEGCN_EINVAL, "%s: NULL descriptor", what);
+    SG_REQUIRE(d && io, SLICEGCN_EINVAL, "%s: NULL descriptor or io", what);
     SG_REQUIRE(d->n >= 0 && d->w_in >= 1 && d->w_out >= 1, SLICEGCN_EINVAL, "%s: need n >= 0 and widths >= 1", what);
     SG_REQUIRE(known_type(d->type), SLICEGCN_EINVAL, "%s: unknown type", what);
     SG_REQUIRE(d->act >= SLICEGCN_ACT_NONE && d->act <= SLICEGCN_ACT_GELU, SLICEGCN_EINVAL, "%s: unknown activation", what);
@@ -250,12 +270,10 @@ int check(const char *what, const slicegcn_product_desc *d)
     return SLICEGCN_OK;
 }
 
-bool present(const slicegcn_matrix *m) { return m && m->data; }
-
-int check_rows(const char *what, const char *name, const slicegcn_matrix *m, int32_t width, int32_t type, bool needed)
+int check_rows(const char *what, const char *name, const slicegcn_matrix &m, int32_t width, int32_t type, bool needed)
 {
-    SG_REQUIRE(!needed || present(m), SLICEGCN_EINVAL, "%s: NULL %s", what, name);
-    SG_REQUIRE(!present(m) || (m->ld >= width && m->ld <= (int64_t)1 << 31 && aligned_for(m->data, type)), SLICEGCN_EINVAL,
+    SG_REQUIRE(!needed || m.data, SLICEGCN_EINVAL, "%s: NULL %s", what, name);
+    SG_REQUIRE(!m.data || (m.ld >= width && m.ld <= (int64_t)1 << 31 && aligned_for(m.data, type)), SLICEGCN_EINVAL,
                "%s: %s has an ld smaller than its width (or beyond 2^31), or a misaligned base", what, name);
     return SLICEGCN_OK;
 }
@@ -274,7 +292,7 @@ int check_workspace(const char *what, const void *ws, size_t ws_bytes, size_t ne
     return SLICEGCN_OK;
 }
 
-Operand operand(const slicegcn_matrix *m) { return present(m) ? Operand{static_cast<const char *>(m->data), m->ld} : Operand{nullptr, 0}; }
+Operand operand(const slicegcn_matrix &m) { return Operand{static_cast<const char *>(m.data), m.ld}; }
 Operand weights(const void *w, int32_t w_out) { return Operand{static_cast<const char *>(w), w_out}; }
 
 ProductShape fwd_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, bool gated) { return ProductShape{n, w_in, w_out, 1, 1, type, gated, true}; }
@@ -283,7 +301,7 @@ ProductShape fwd_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, boo
 struct BwdCall {
     const slicegcn_product_desc *d;
     Operand x, w[2], g, u, dy;
-    const slicegcn_matrix *dx, *dr;
+    slicegcn_matrix dx, dr;
     void *dw[2];
     float *db[2];
 };
@@ -293,7 +311,7 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
     const slicegcn_product_desc &d = *c.d;
     const BwdWorkspace w = bwd_workspace(d.n, d.w_in, d.w_out, d.type, q);
     if (int rc = check_workspace(what, ws, ws_bytes, w.bytes(q))) return rc;
-    const bool want_x = present(c.dx) && d.n > 0, want_w = c.dw[0] || c.dw[1], want_b = c.db[0] || c.db[1], want_r = present(c.dr) && d.n > 0;
+    const bool want_x = c.dx.data && d.n > 0, want_w = c.dw[0] || c.dw[1], want_b = c.db[0] || c.db[1], want_r = c.dr.data && d.n > 0;
     char *at = static_cast<char *>(ws);
     const bool plain = q == 1 && d.act == SLICEGCN_ACT_NONE; // dP is dY itself
     Operand dg[2] = {c.dy, c.dy};
@@ -303,7 +321,6 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
     s.d = c.dy;
     s.n = d.n;
     s.w = d.w_out;
-    s.act = d.act;
     s.residual = (float)d.residual;
     if (!plain && (want_x || want_w)) {
         s.dg = at;
@@ -313,8 +330,8 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         dg[1] = Operand{s.du, w.ld};
     }
     if (want_r) {
-        s.dr = static_cast<char *>(c.dr->data);
-        s.ldr = c.dr->ld;
+        s.dr = static_cast<char *>(c.dr.data);
+        s.ldr = c.dr.ld;
     }
     at += q * w.rows;
     if (want_b) s.partial = reinterpret_cast<double *>(at);
@@ -323,16 +340,19 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
 
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d.w_out, stream);
     if (s.dg || s.dr || s.partial) {
-        s.parts = (int32_t)slope_parts(d.n, d.w_out);
-        s.rows_per_part = (d.n + s.parts - 1) / s.parts;
-        const dim3 grid((d.w_out + 64 * SLOPE_V - 1) / (64 * SLOPE_V), (unsigned)s.parts);
+        const SlopeGrid g = slope_grid(d.n, d.w_out, d.type);
+        s.lanes = g.lanes;
+        s.rows_per_part = (d.n + g.parts - 1) / g.parts;
+        const dim3 grid((unsigned)g.cols, (unsigned)g.parts);
         with_type(d.type, [&](auto t) {
-            if (q == 2) slope_kernel<decltype(t), true><<<grid, 256, 0, stream>>>(s);
-            else slope_kernel<decltype(t), false><<<grid, 256, 0, stream>>>(s);
+            with_act(s.g.p ? d.act : SLICEGCN_ACT_NONE, [&](auto act) {
+                if (q == 2) slope_kernel<decltype(t), true, decltype(act)::value><<<grid, 256, 0, stream>>>(s);
+                else slope_kernel<decltype(t), false, decltype(act)::value><<<grid, 256, 0, stream>>>(s);
+            });
         });
         SG_LAUNCH_CHECK();
         if (want_b) {
-            bias_kernel<<<dim3((d.w_out + 63) / 64, q), 256, 0, stream>>>(s.partial, s.parts, q, d.w_out, c.db[0], c.db[1]);
+            bias_kernel<<<dim3((d.w_out + 15) / 16, q), 1024, 0, stream>>>(s.partial, (int32_t)g.parts, q, d.w_out, c.db[0], c.db[1]);
             SG_LAUNCH_CHECK();
         }
     }
@@ -347,8 +367,8 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         a.N = d.w_in;
         a.segments = q;
         a.sets = 1;
-        a.out[0] = static_cast<char *>(c.dx->data);
-        a.ldo[0] = c.dx->ld;
+        a.out[0] = static_cast<char *>(c.dx.data);
+        a.ldo[0] = c.dx.ld;
         a.partial = partial;
         if (int rc = launch_product(dx_shape(d.n, d.w_in, d.w_out, d.type, q), PRODUCT_GWT, EPI_STORE, a, stream)) return rc;
     }
@@ -385,36 +405,33 @@ extern "C" size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, 
     return partial_bytes(fwd_shape(n, w_in, w_out, type, false));
 }
 
-extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const slicegcn_matrix *X, const void *W, const float *b, const slicegcn_matrix *R,
-                                    const slicegcn_matrix *P, const slicegcn_matrix *Y, void *ws, size_t ws_bytes, void *stream)
+extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream)
 {
     const char *what = "product_fwd";
-    if (int rc = check(what, d)) return rc;
-    SG_REQUIRE(W, SLICEGCN_EINVAL, "%s: NULL W", what);
-    if (int rc = check_rows(what, "X", X, d->w_in, d->type, true)) return rc;
-    if (int rc = check_rows(what, "Y", Y, d->w_out, d->type, true)) return rc;
-    if (int rc = check_rows(what, "R", R, d->w_out, d->type, false)) return rc;
-    if (int rc = check_rows(what, "P", P, d->w_out, d->type, false)) return rc;
-    if (int rc = check_params(what, d->type, {W}, {b})) return rc;
+    if (int rc = check(what, d, io)) return rc;
+    SG_REQUIRE(io->W, SLICEGCN_EINVAL, "%s: NULL W", what);
+    if (int rc = check_rows(what, "X", io->X, d->w_in, d->type, true)) return rc;
+    if (int rc = check_rows(what, "Y", io->Y, d->w_out, d->type, true)) return rc;
+    if (int rc = check_rows(what, "R", io->R, d->w_out, d->type, false)) return rc;
+    if (int rc = check_rows(what, "P", io->P, d->w_out, d->type, false)) return rc;
+    if (int rc = check_params(what, d->type, {io->W}, {io->b})) return rc;
     if (d->n == 0) return SLICEGCN_OK;
-    SG_REQUIRE(Y->data != X->data, SLICEGCN_EINVAL, "%s: Y in the rows of X", what);
+    SG_REQUIRE(io->Y.data != io->X.data, SLICEGCN_EINVAL, "%s: Y in the rows of X", what);
     const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, false);
     if (int rc = check_workspace(what, ws, ws_bytes, partial_bytes(shape))) return rc;
     ProductArgs a{};
-    a.a[0] = operand(X);
-    a.b[0] = weights(W, d->w_out);
+    a.a[0] = operand(io->X);
+    a.b[0] = weights(io->W, d->w_out);
     a.M = d->n;
     a.K = d->w_in;
     a.N = d->w_out;
     a.segments = a.sets = 1;
-    a.out[0] = static_cast<char *>(Y->data);
-    a.ldo[0] = Y->ld;
-    a.bias[0] = b;
-    a.r = operand(R);
-    if (present(P)) {
-        a.keep[0] = static_cast<char *>(P->data);
-        a.ldk[0] = P->ld;
-    }
+    a.out[0] = static_cast<char *>(io->Y.data);
+    a.ldo[0] = io->Y.ld;
+    a.bias[0] = io->b;
+    a.r = operand(io->R);
+    a.keep[0] = static_cast<char *>(io->P.data);
+    a.ldk[0] = io->P.ld;
     a.residual = (float)d->residual;
     a.act = d->act;
     a.partial = static_cast<float *>(ws);
@@ -428,30 +445,28 @@ extern "C" size_t slicegcn_product_bwd_workspace_bytes(int64_t n, int32_t w_in, 
     return bwd_workspace(n, w_in, w_out, type, 1).bytes(1);
 }
 
-extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *d, const slicegcn_matrix *X, const void *W, const slicegcn_matrix *P,
-                                    const slicegcn_matrix *dY, const slicegcn_matrix *dX, void *dW, float *db, const slicegcn_matrix *dR, void *ws,
-                                    size_t ws_bytes, void *stream)
+extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *d, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream)
 {
     const char *what = "product_bwd";
-    if (int rc = check(what, d)) return rc;
-    const bool rows = d->n > 0, slope = d->act != SLICEGCN_ACT_NONE && (present(dX) || dW || db);
-    if (int rc = check_rows(what, "X", X, d->w_in, d->type, rows && dW)) return rc;
-    if (int rc = check_rows(what, "P", P, d->w_out, d->type, rows && slope)) return rc;
-    if (int rc = check_rows(what, "dY", dY, d->w_out, d->type, rows)) return rc;
-    if (int rc = check_rows(what, "dX", dX, d->w_in, d->type, false)) return rc;
-    if (int rc = check_rows(what, "dR", dR, d->w_out, d->type, false)) return rc;
-    SG_REQUIRE(W || !present(dX) || !rows, SLICEGCN_EINVAL, "%s: NULL W", what);
-    if (int rc = check_params(what, d->type, {W, dW}, {db})) return rc;
+    if (int rc = check(what, d, io)) return rc;
+    const bool rows = d->n > 0, slope = d->act != SLICEGCN_ACT_NONE && (io->dX.data || io->dW || io->db);
+    if (int rc = check_rows(what, "X", io->X, d->w_in, d->type, rows && io->dW)) return rc;
+    if (int rc = check_rows(what, "P", io->P, d->w_out, d->type, rows && slope)) return rc;
+    if (int rc = check_rows(what, "dY", io->dY, d->w_out, d->type, rows)) return rc;
+    if (int rc = check_rows(what, "dX", io->dX, d->w_in, d->type, false)) return rc;
+    if (int rc = check_rows(what, "dR", io->dR, d->w_out, d->type, false)) return rc;
+    SG_REQUIRE(io->W || !io->dX.data || !rows, SLICEGCN_EINVAL, "%s: NULL W", what);
+    if (int rc = check_params(what, d->type, {io->W, io->dW}, {io->db})) return rc;
     BwdCall c{};
     c.d = d;
-    c.x = operand(X);
-    c.w[0] = weights(W, d->w_out);
-    c.g = operand(P);
-    c.dy = operand(dY);
-    c.dx = dX;
-    c.dr = dR;
-    c.dw[0] = dW;
-    c.db[0] = db;
+    c.x = operand(io->X);
+    c.w[0] = weights(io->W, d->w_out);
+    c.g = operand(io->P);
+    c.dy = operand(io->dY);
+    c.dx = io->dX;
+    c.dr = io->dR;
+    c.dw[0] = io->dW;
+    c.db[0] = io->db;
     return backward(what, c, 1, ws, ws_bytes, as_stream(stream));
 }
 
@@ -461,41 +476,37 @@ extern "C" size_t slicegcn_gated_fwd_workspace_bytes(int64_t n, int32_t w_in, in
     return partial_bytes(fwd_shape(n, w_in, w_out, type, true));
 }
 
-extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn_matrix *X, const void *Wg, const void *Wu, const float *bg,
-                                  const float *bu, const slicegcn_matrix *G, const slicegcn_matrix *U, const slicegcn_matrix *H, void *ws,
-                                  size_t ws_bytes, void *stream)
+extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream)
 {
     const char *what = "gated_fwd";
-    if (int rc = check(what, d)) return rc;
-    SG_REQUIRE(Wg && Wu, SLICEGCN_EINVAL, "%s: NULL Wg or Wu", what);
-    if (int rc = check_rows(what, "X", X, d->w_in, d->type, true)) return rc;
-    if (int rc = check_rows(what, "H", H, d->w_out, d->type, true)) return rc;
-    if (int rc = check_rows(what, "G", G, d->w_out, d->type, false)) return rc;
-    if (int rc = check_rows(what, "U", U, d->w_out, d->type, false)) return rc;
-    SG_REQUIRE(present(G) == present(U), SLICEGCN_EINVAL, "%s: G without U, or U without G", what);
-    if (int rc = check_params(what, d->type, {Wg, Wu}, {bg, bu})) return rc;
+    if (int rc = check(what, d, io)) return rc;
+    SG_REQUIRE(io->Wg && io->Wu, SLICEGCN_EINVAL, "%s: NULL Wg or Wu", what);
+    if (int rc = check_rows(what, "X", io->X, d->w_in, d->type, true)) return rc;
+    if (int rc = check_rows(what, "H", io->H, d->w_out, d->type, true)) return rc;
+    if (int rc = check_rows(what, "G", io->G, d->w_out, d->type, false)) return rc;
+    if (int rc = check_rows(what, "U", io->U, d->w_out, d->type, false)) return rc;
+    SG_REQUIRE(!io->G.data == !io->U.data, SLICEGCN_EINVAL, "%s: G without U, or U without G", what);
+    if (int rc = check_params(what, d->type, {io->Wg, io->Wu}, {io->bg, io->bu})) return rc;
     if (d->n == 0) return SLICEGCN_OK;
-    SG_REQUIRE(H->data != X->data, SLICEGCN_EINVAL, "%s: H in the rows of X", what);
+    SG_REQUIRE(io->H.data != io->X.data, SLICEGCN_EINVAL, "%s: H in the rows of X", what);
     const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, true);
     if (int rc = check_workspace(what, ws, ws_bytes, partial_bytes(shape))) return rc;
     ProductArgs a{};
-    a.a[0] = operand(X);
-    a.b[0] = weights(Wg, d->w_out);
-    a.b[1] = weights(Wu, d->w_out);
+    a.a[0] = operand(io->X);
+    a.b[0] = weights(io->Wg, d->w_out);
+    a.b[1] = weights(io->Wu, d->w_out);
     a.M = d->n;
     a.K = d->w_in;
     a.N = d->w_out;
     a.segments = a.sets = 1;
-    a.out[0] = static_cast<char *>(H->data);
-    a.ldo[0] = H->ld;
-    a.bias[0] = bg;
-    a.bias[1] = bu;
-    if (present(G)) {
-        a.keep[0] = static_cast<char *>(G->data);
-        a.ldk[0] = G->ld;
-        a.keep[1] = static_cast<char *>(U->data);
-        a.ldk[1] = U->ld;
-    }
+    a.out[0] = static_cast<char *>(io->H.data);
+    a.ldo[0] = io->H.ld;
+    a.bias[0] = io->bg;
+    a.bias[1] = io->bu;
+    a.keep[0] = static_cast<char *>(io->G.data);
+    a.ldk[0] = io->G.ld;
+    a.keep[1] = static_cast<char *>(io->U.data);
+    a.ldk[1] = io->U.ld;
     a.act = d->act;
     a.partial = static_cast<float *>(ws);
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d->w_out, as_stream(stream));
@@ -508,32 +519,30 @@ extern "C" size_t slicegcn_gated_bwd_workspace_bytes(int64_t n, int32_t w_in, in
     return bwd_workspace(n, w_in, w_out, type, 2).bytes(2);
 }
 
-extern "C" int slicegcn_gated_bwd(const slicegcn_product_desc *d, const slicegcn_matrix *X, const void *Wg, const void *Wu, const slicegcn_matrix *G,
-                                  const slicegcn_matrix *U, const slicegcn_matrix *dH, const slicegcn_matrix *dX, void *dWg, void *dWu, float *dbg,
-                                  float *dbu, void *ws, size_t ws_bytes, void *stream)
+extern "C" int slicegcn_gated_bwd(const slicegcn_product_desc *d, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream)
 {
     const char *what = "gated_bwd";
-    if (int rc = check(what, d)) return rc;
+    if (int rc = check(what, d, io)) return rc;
     const bool rows = d->n > 0;
-    if (int rc = check_rows(what, "X", X, d->w_in, d->type, rows && (dWg || dWu))) return rc;
-    if (int rc = check_rows(what, "G", G, d->w_out, d->type, rows)) return rc;
-    if (int rc = check_rows(what, "U", U, d->w_out, d->type, rows)) return rc;
-    if (int rc = check_rows(what, "dH", dH, d->w_out, d->type, rows)) return rc;
-    if (int rc = check_rows(what, "dX", dX, d->w_in, d->type, false)) return rc;
-    SG_REQUIRE((Wg && Wu) || !present(dX) || !rows, SLICEGCN_EINVAL, "%s: NULL Wg or Wu", what);
-    if (int rc = check_params(what, d->type, {Wg, Wu, dWg, dWu}, {dbg, dbu})) return rc;
+    if (int rc = check_rows(what, "X", io->X, d->w_in, d->type, rows && (io->dWg || io->dWu))) return rc;
+    if (int rc = check_rows(what, "G", io->G, d->w_out, d->type, rows)) return rc;
+    if (int rc = check_rows(what, "U", io->U, d->w_out, d->type, rows)) return rc;
+    if (int rc = check_rows(what, "dH", io->dH, d->w_out, d->type, rows)) return rc;
+    if (int rc = check_rows(what, "dX", io->dX, d->w_in, d->type, false)) return rc;
+    SG_REQUIRE((io->Wg && io->Wu) || !io->dX.data || !rows, SLICEGCN_EINVAL, "%s: NULL Wg or Wu", what);
+    if (int rc = check_params(what, d->type, {io->Wg, io->Wu, io->dWg, io->dWu}, {io->dbg, io->dbu})) return rc;
     BwdCall c{};
     c.d = d;
-    c.x = operand(X);
-    c.w[0] = weights(Wg, d->w_out);
-    c.w[1] = weights(Wu, d->w_out);
-    c.g = operand(G);
-    c.u = operand(U);
-    c.dy = operand(dH);
-    c.dx = dX;
-    c.dw[0] = dWg;
-    c.dw[1] = dWu;
-    c.db[0] = dbg;
-    c.db[1] = dbu;
+    c.x = operand(io->X);
+    c.w[0] = weights(io->Wg, d->w_out);
+    c.w[1] = weights(io->Wu, d->w_out);
+    c.g = operand(io->G);
+    c.u = operand(io->U);
+    c.dy = operand(io->dH);
+    c.dx = io->dX;
+    c.dw[0] = io->dWg;
+    c.dw[1] = io->dWu;
+    c.db[0] = io->dbg;
+    c.db[1] = io->dbu;
     return backward(what, c, 2, ws, ws_bytes, as_stream(stream));
 }

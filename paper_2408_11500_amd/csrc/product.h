@@ -78,36 +78,76 @@ constexpr int rows_waves(int f) { return f <= 2 ? 8 : 4; } // wavefronts of prod
 constexpr int STEP_K_F32 = 32, STEP_K_16 = 64;
 inline int step_k(int32_t type) { return type == SLICEGCN_F32 ? STEP_K_F32 : STEP_K_16; }
 
-__device__ inline float sigmoid(float v) { return 1.f / (1.f + expf(-v)); }
+// Activations of v and their derivatives in some 5 (silu) and 20 (gelu) instructions, within a few 2^-24 of |v| and of 1 + |v|.
+__device__ inline float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.4426950408889634f)); }
 
+// The normal distribution Phi(v), and e = exp(-v^2 / 2).  The tail Phi(-|v|) is e times half of erfcx(|v| / sqrt 2), which is a polynomial of t = 1 / (1 + 0.265 |v|)
+// without constant term: degree 9, fitted for the least relative error over |v| <= 14 (1.2e-8).  With erfcf and expf, some 100 instructions, the gradients before a gelu
+// were bound by them: 2.4 M rows of 256 bf16 columns 1.22 ms.
+__device__ inline float normal_distribution(float v, float &e)
+{
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.265f, fabsf(v), 1.f));
+    e = __builtin_amdgcn_exp2f(v * v * -0.72134752044448170f);
+    float q = 0.030821435153484344f;
+    q = fmaf(q, t, -0.1442311853170395f);
+    q = fmaf(q, t, 0.21781975030899048f);
+    q = fmaf(q, t, -0.11636755615472794f);
+    q = fmaf(q, t, 0.1379561871290207f);
+    q = fmaf(q, t, 0.060311924666166306f);
+    q = fmaf(q, t, 0.10270125418901443f);
+    q = fmaf(q, t, 0.10524662584066391f);
+    q = fmaf(q, t, 0.10574156790971756f);
+    const float tail = q * t * e;
+    return v < 0.f ? tail : 1.f - tail;
+}
+
+template <int ACT> __device__ inline float activated(float v)
+{
+    float e;
+    if (ACT == SLICEGCN_ACT_RELU) return v < 0.f ? 0.f : v;
+    if (ACT == SLICEGCN_ACT_SILU) return v * sigmoid(v);
+    if (ACT == SLICEGCN_ACT_GELU) return v * normal_distribution(v, e);
+    return v;
+}
 __device__ inline float activated(int act, float v)
 {
     switch (act) {
-    case SLICEGCN_ACT_RELU: return v < 0.f ? 0.f : v;
-    case SLICEGCN_ACT_SILU: return v * sigmoid(v);
-    case SLICEGCN_ACT_GELU: return v * (0.5f * erfcf(v * -0.70710678118654752f));
+    case SLICEGCN_ACT_RELU: return activated<SLICEGCN_ACT_RELU>(v);
+    case SLICEGCN_ACT_SILU: return activated<SLICEGCN_ACT_SILU>(v);
+    case SLICEGCN_ACT_GELU: return activated<SLICEGCN_ACT_GELU>(v);
     default: return v;
     }
 }
 
 // act(v) and its derivative
-__device__ inline void activated_slope(int act, float v, float &y, float &slope)
+template <int ACT> __device__ inline void activated_slope(float v, float &y, float &slope)
 {
-    switch (act) {
-    case SLICEGCN_ACT_RELU: y = v < 0.f ? 0.f : v; slope = v > 0.f ? 1.f : 0.f; break;
-    case SLICEGCN_ACT_SILU: {
+    if (ACT == SLICEGCN_ACT_RELU) {
+        y = v < 0.f ? 0.f : v;
+        slope = v > 0.f ? 1.f : 0.f;
+    } else if (ACT == SLICEGCN_ACT_SILU) {
         const float s = sigmoid(v);
         y = v * s;
-        slope = s * (1.f + v * (1.f - s));
-        break;
-    }
-    case SLICEGCN_ACT_GELU: {
-        const float p = 0.5f * erfcf(v * -0.70710678118654752f);
+        slope = s * fmaf(v, 1.f - s, 1.f);
+    } else if (ACT == SLICEGCN_ACT_GELU) {
+        float e;
+        const float p = normal_distribution(v, e);
         y = v * p;
-        slope = p + v * (0.39894228040143268f * expf(-0.5f * v * v));
-        break;
+        slope = fmaf(v * 0.39894228040143268f, e, p);
+    } else {
+        y = v;
+        slope = 1.f;
     }
-    default: y = v; slope = 1.f;
+}
+
+// f(std::integral_constant) with the activation as a constant
+template <class F> inline auto with_act(int act, F f)
+{
+    switch (act) {
+    case SLICEGCN_ACT_RELU: return f(std::integral_constant<int, SLICEGCN_ACT_RELU>());
+    case SLICEGCN_ACT_SILU: return f(std::integral_constant<int, SLICEGCN_ACT_SILU>());
+    case SLICEGCN_ACT_GELU: return f(std::integral_constant<int, SLICEGCN_ACT_GELU>());
+    default: return f(std::integral_constant<int, SLICEGCN_ACT_NONE>());
     }
 }
 
