@@ -236,6 +236,17 @@ SlopeGrid slope_grid(int64_t n, int32_t w, int32_t type)
     return g;
 }
 
+// Whether a backward pass may go in one sweep over the rows, by its sizes, and with how many workgroups (0: it may not).  Many rows, since every workgroup leaves a
+// dW of its own:
+constexpr int64_t NARROW_LEAST = 16384;
+unsigned narrow_blocks(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q)
+{
+    if (type == SLICEGCN_F32 || w_in > NARROW_WIDTH_IN || w_out * q > NARROW_WIDTH_OUT || w_in % 2 || w_out % 2 || n < NARROW_LEAST) return 0;
+    return CUS;
+}
+// ... and by how its rows lie: on boundaries of 4 bytes, 32 rows within 2^31 bytes
+bool narrow_rows_fit(const Operand &o) { return !o.p || ((reinterpret_cast<uintptr_t>(o.p) & 3u) == 0 && o.ld % 2 == 0 && o.ld <= 1 << 24); }
+
 // Workspace of a backward pass: gradients before the activation, their column sums, sums of parts of k
 struct BwdWorkspace {
     int64_t ld; // of the gradients before the activation: rows on 16-byte boundaries
@@ -251,9 +262,12 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     BwdWorkspace w;
     w.ld = round_up(w_out, 8);
     w.rows = (size_t)round_up(n * w.ld * type_bytes(type), 256);
-    w.sums = (size_t)round_up(slope_grid(n, w_out, type).parts * q * (int64_t)w_out * 8, 256);
+    const int64_t parts = slope_grid(n, w_out, type).parts, blocks = narrow_blocks(n, w_in, w_out, type, q);
+    w.sums = (size_t)round_up((parts > blocks ? parts : blocks) * q * (int64_t)w_out * 8, 256);
     const size_t x = partial_bytes(dx_shape(n, w_in, w_out, type, q)), y = partial_bytes(dw_shape(n, w_in, w_out, type, q));
+    const size_t z = (size_t)round_up(blocks * q * w_in * (int64_t)w_out * 4, 256);
     w.partial = x > y ? x : y;
+    w.partial = w.partial > z ? w.partial : z;
     return w;
 }
 
@@ -339,6 +353,43 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
     float *partial = reinterpret_cast<float *>(at);
 
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d.w_out, stream);
+    const Operand dx{static_cast<const char *>(c.dx.data), c.dx.ld};
+    const unsigned narrow = narrow_blocks(d.n, d.w_in, d.w_out, d.type, q);
+    if (narrow && (want_x || want_w) && !want_r && narrow_rows_fit(c.x) && narrow_rows_fit(c.g) && narrow_rows_fit(c.u) && narrow_rows_fit(c.dy) &&
+        narrow_rows_fit(dx) && (q == 1 || !want_w || (c.dw[0] && c.dw[1]))) {
+        NarrowArgs a{};
+        a.x = c.x;
+        a.w[0] = c.w[0];
+        a.w[1] = c.w[1];
+        a.g = c.g;
+        a.u = c.u;
+        a.d = c.dy;
+        a.dx = want_x ? static_cast<char *>(c.dx.data) : nullptr;
+        a.lddx = c.dx.ld;
+        a.n = d.n;
+        a.w_in = d.w_in;
+        a.w_out = d.w_out;
+        a.want_w = want_w;
+        a.partial = partial;
+        a.columns = s.partial;
+        ProductArgs join{};
+        for (int i = 0; i < q; ++i) {
+            join.out[i] = static_cast<char *>(c.dw[i]);
+            join.ldo[i] = d.w_out;
+        }
+        join.M = d.w_in;
+        join.N = d.w_out;
+        join.sets = q;
+        join.splits = (int32_t)narrow;
+        join.partial = partial;
+        const auto launch = d.type == SLICEGCN_BF16 ? launch_narrow_bf16 : launch_narrow_f16;
+        if (int rc = launch(a, join, d.act, q == 2, narrow, stream)) return rc;
+        if (want_b) {
+            bias_kernel<<<dim3((d.w_out + 15) / 16, q), 1024, 0, stream>>>(s.partial, (int32_t)narrow, q, d.w_out, c.db[0], c.db[1]);
+            SG_LAUNCH_CHECK();
+        }
+        return SLICEGCN_OK;
+    }
     if (s.dg || s.dr || s.partial) {
         const SlopeGrid g = slope_grid(d.n, d.w_out, d.type);
         s.lanes = g.lanes;

@@ -67,6 +67,20 @@ int launch_product_f32(int layouts, int epilogue, const ProductPlan &plan, Produ
 int launch_product_bf16(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream);
 int launch_product_f16(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream);
 
+// product_narrow.h: a backward pass in one sweep over the rows
+constexpr int NARROW_WIDTH_IN = 128, NARROW_WIDTH_OUT = 256; // at most; of all products together
+constexpr int NARROW_RUN = 32;                               // blocks of rows whose column sums a thread adds in fp32
+struct NarrowArgs {
+    Operand x, w[2], g, u, d; // as in a backward pass
+    char *dx;                 // NULL: not wanted
+    int64_t lddx, n;
+    int32_t w_in, w_out, want_w;
+    float *partial;  // sums of dW: [set][workgroup][w_in][w_out]
+    double *columns; // NULL, or column sums [workgroup][1 or 2][w_out]
+};
+int launch_narrow_bf16(const NarrowArgs &a, ProductArgs &join, int act, bool gated, unsigned blocks, hipStream_t stream);
+int launch_narrow_f16(const NarrowArgs &a, ProductArgs &join, int act, bool gated, unsigned blocks, hipStream_t stream);
+
 // layouts: which operands a product has
 constexpr int PRODUCT_XW = 0, PRODUCT_GWT = 1, PRODUCT_XTG = 2;
 

@@ -1,11 +1,18 @@
 // The kernels of product.h for f16 rows.
 #include "product_launch.h"
+#include "product_narrow.h"
 
 namespace slicegcn {
 
 int launch_product_f16(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream)
 {
     return launch_product<f16>(layouts, epilogue, plan, a, stream);
+}
+
+int launch_narrow_f16(const NarrowArgs &a, ProductArgs &join, int act, bool gated, unsigned blocks, hipStream_t stream)
+{
+    if (int rc = launch_narrow<f16>(a, act, gated, blocks, stream)) return rc;
+    return a.want_w ? launch_join<f16>(join, stream) : SLICEGCN_OK;
 }
 
 } // namespace slicegcn

@@ -312,3 +312,55 @@ def test_gradients_against_differences():
                 down = loss()
                 t64[i, j] = old
                 assert abs((up - down) / (2 * step) - float(grad[i, j])) < 1e-5  # sums of at most 30 products of order 1 in fp32: 30 * 2^-20
+
+
+NARROW = [(16384, 100, 256), (20_011, 128, 126), (17_000, 6, 2), (16_500, 64, 64), (16_390, 34, 250), (33_333, 72, 40)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("size", NARROW, ids=str)
+@pytest.mark.parametrize("gated", [False, True])
+def test_narrow_backward_passes_of_many_rows(size, kind, gated):
+    """In one sweep over the rows where they lie on boundaries of 4 bytes, and in the general form where they do not."""
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    case = NARROW.index(size)
+    if gated:
+        wo = min(wo, 128)
+    gen = torch.Generator().manual_seed(200 + case)
+    name = ACTS[(case + gated) % 4]
+    x, x64 = rows(gen, n, wi, dtype, wi + (0, 2, 30)[case % 3], (0, 2, 8)[case % 3])
+    w = [weights(gen, wi, wo, dtype) for _ in range(2)]
+    g, g64 = rows(gen, n, wo, dtype, wo + (2, 0, 6)[case % 3], std=1.5)
+    u, u64 = rows(gen, n, wo, dtype, wo, 2)
+    d, d64 = rows(gen, n, wo, dtype, wo + (0, 4, 2)[case % 3])
+    if gated:
+        want = gated_bwd(x64, w[0][1], w[1][1], g64, u64, d64, name, dtype)
+        call, keys = (lambda ws, x=x, **out: B.slicegcn_gated_bwd(x, w[0][0], w[1][0], g, u, d, ws, act=ACT[name], **out)), ("dX", "dWg", "dWu", "dbg", "dbu")
+        ws = workspace(B.slicegcn_gated_bwd_workspace_bytes(n, wi, wo, dtype))
+    else:
+        want = product_bwd(x64, w[0][1], g64, d64, 1.0, name, dtype)
+        call, keys = (lambda ws, x=x, **out: B.slicegcn_product_bwd(x, w[0][0], g if name != "none" else None, d, ws, act=ACT[name], **out)), ("dX", "dW", "db")
+        ws = workspace(B.slicegcn_product_bwd_workspace_bytes(n, wi, wo, dtype))
+
+    def outputs(ld):
+        dx, buf = result(n, wi, dtype, ld)
+        return {k: dx if k == "dX" else torch.full((wi, wo) if k[1] == "W" else (wo,), 777.0, dtype=dtype if k[1] == "W" else torch.float32, device="cuda")
+                for k in keys}, buf
+    first, buf = outputs(wi + 2)
+    call(ws, **first)
+    for k in keys:
+        assert_within(first[k], *want[k], k)
+    assert_padding(buf, wi)
+    again, _ = outputs(wi)
+    call(ws, **again)
+    assert all(torch.equal(first[k], again[k]) for k in keys)
+    for some in (("dX",), tuple(k for k in keys if k[1] == "W"), ("dX", keys[-1])):  # without the others, and without X where dW is not wanted
+        few = {k: v for k, v in outputs(wi)[0].items() if k in some}
+        call(ws, x=x if any(k[1] == "W" for k in some) else None, **few)
+        assert all(torch.equal(few[k], first[k]) for k in some if k != "X"), some
+    general, buf = outputs(wi + 3)  # rows of dX on odd elements
+    call(ws, **general)
+    for k in keys:
+        assert_within(general[k], *want[k], k)
+    assert_padding(buf, wi)
