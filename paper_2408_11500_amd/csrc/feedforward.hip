@@ -60,8 +60,8 @@ size_t partial_bytes(const ProductShape &s)
     return x > y ? x : y;
 }
 
-// Whether both operands can go straight into LDS: rows and columns in whole units of 16 bytes, offsets within a tile in 32 bits
-bool on_units(const Operand &o) { return aligned16(o.p) && o.ld % 8 == 0 && o.ld <= 1 << 22; }
+// Whether both operands can go straight into LDS: rows and columns in whole units of 16 bytes
+bool on_units(const Operand &o) { return aligned16(o.p) && o.ld % 8 == 0; }
 bool aligned_product(int layouts, const ProductShape &s, const ProductArgs &a)
 {
     for (int i = 0; i < (s.segments > s.sets ? s.segments : s.sets); ++i)
@@ -74,10 +74,29 @@ bool aligned_product(int layouts, const ProductShape &s, const ProductArgs &a)
     }
 }
 
+// Whether buffers can read both operands: their range checks go by words, so no word may hold an element that exists and one that does not
+bool on_words(const Operand &o, int32_t type)
+{
+    return type == SLICEGCN_F32 || ((reinterpret_cast<uintptr_t>(o.p) & 3u) == 0 && o.ld % 2 == 0);
+}
+bool product_on_words(int layouts, const ProductShape &s, const ProductArgs &a)
+{
+    for (int i = 0; i < (s.segments > s.sets ? s.segments : s.sets); ++i)
+        if (!on_words(a.a[i], s.type) || !on_words(a.b[i], s.type)) return false;
+    if (s.gated && !on_words(a.b[1], s.type)) return false;
+    if (s.type == SLICEGCN_F32) return true;
+    switch (layouts) {
+    case PRODUCT_XW: return s.K % 2 == 0 && s.N % 2 == 0;
+    case PRODUCT_GWT: return s.K % 2 == 0;
+    default: return s.M % 2 == 0 && s.N % 2 == 0;
+    }
+}
+
 int launch_product(const ProductShape &s, int layouts, int epilogue, ProductArgs &a, hipStream_t stream)
 {
     const int32_t type = s.type;
     const ProductPlan plan = plan_product(s, aligned_product(layouts, s, a));
+    a.on_words = product_on_words(layouts, s, a);
     return type == SLICEGCN_F32    ? launch_product_f32(layouts, epilogue, plan, a, stream)
            : type == SLICEGCN_BF16 ? launch_product_bf16(layouts, epilogue, plan, a, stream)
                                    : launch_product_f16(layouts, epilogue, plan, a, stream);
@@ -244,8 +263,8 @@ unsigned narrow_blocks(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int
     if (type == SLICEGCN_F32 || w_in > NARROW_WIDTH_IN || w_out * q > NARROW_WIDTH_OUT || w_in % 2 || w_out % 2 || n < NARROW_LEAST) return 0;
     return CUS;
 }
-// ... and by how its rows lie: on boundaries of 4 bytes, 32 rows within 2^31 bytes
-bool narrow_rows_fit(const Operand &o) { return !o.p || ((reinterpret_cast<uintptr_t>(o.p) & 3u) == 0 && o.ld % 2 == 0 && o.ld <= 1 << 24); }
+// ... and by how its rows lie: on boundaries of 4 bytes
+bool narrow_rows_fit(const Operand &o) { return !o.p || ((reinterpret_cast<uintptr_t>(o.p) & 3u) == 0 && o.ld % 2 == 0); }
 
 // Workspace of a backward pass: gradients before the activation, their column sums, sums of parts of k
 struct BwdWorkspace {
@@ -271,7 +290,7 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     return w;
 }
 
-bool sizes_fit(int64_t n, int32_t w_in, int32_t w_out) { return n >= 0 && n <= INT32_MAX && w_in >= 1 && w_out >= 1 && w_in <= 1 << 24 && w_out <= 1 << 24; }
+bool sizes_fit(int64_t n, int32_t w_in, int32_t w_out) { return n >= 0 && n <= INT32_MAX && w_in >= 1 && w_out >= 1 && w_in <= 1 << 20 && w_out <= 1 << 20; }
 
 int check(const char *what, const slicegcn_product_desc *d, const void *io)
 {
@@ -287,8 +306,8 @@ int check(const char *what, const slicegcn_product_desc *d, const void *io)
 int check_rows(const char *what, const char *name, const slicegcn_matrix &m, int32_t width, int32_t type, bool needed)
 {
     SG_REQUIRE(!needed || m.data, SLICEGCN_EINVAL, "%s: NULL %s", what, name);
-    SG_REQUIRE(!m.data || (m.ld >= width && m.ld <= (int64_t)1 << 31 && aligned_for(m.data, type)), SLICEGCN_EINVAL,
-               "%s: %s has an ld smaller than its width (or beyond 2^31), or a misaligned base", what, name);
+    SG_REQUIRE(!m.data || (m.ld >= width && aligned_for(m.data, type)), SLICEGCN_EINVAL, "%s: %s has an ld smaller than its width, or a misaligned base", what, name);
+    SG_REQUIRE(!m.data || m.ld <= 1 << 21, SLICEGCN_ERANGE, "%s: %s has an ld beyond 2^21", what, name); // offsets within a tile fit 31 bits
     return SLICEGCN_OK;
 }
 

@@ -43,6 +43,8 @@ struct ProductArgs {
     int32_t splits;
     int32_t steps_per_split;
     int64_t first;         // first workgroup of this launch
+    int32_t shares;        // threads that share the parts of a result out where they are joined
+    int32_t on_words;      // whether buffers can read the operands: product_kernels.h
 };
 
 // Sizes of a product and how it is cut: everything that a launch depends on follows from these

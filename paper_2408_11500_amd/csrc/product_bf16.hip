@@ -12,7 +12,7 @@ int launch_product_bf16(int layouts, int epilogue, const ProductPlan &plan, Prod
 int launch_narrow_bf16(const NarrowArgs &a, ProductArgs &join, int act, bool gated, unsigned blocks, hipStream_t stream)
 {
     if (int rc = launch_narrow<bf16>(a, act, gated, blocks, stream)) return rc;
-    return a.want_w ? launch_join<bf16>(join, stream) : SLICEGCN_OK;
+    return a.want_w ? launch_join<bf16, EPI_STORE>(join, stream) : SLICEGCN_OK;
 }
 
 } // namespace slicegcn

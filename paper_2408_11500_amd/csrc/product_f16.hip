@@ -12,7 +12,7 @@ int launch_product_f16(int layouts, int epilogue, const ProductPlan &plan, Produ
 int launch_narrow_f16(const NarrowArgs &a, ProductArgs &join, int act, bool gated, unsigned blocks, hipStream_t stream)
 {
     if (int rc = launch_narrow<f16>(a, act, gated, blocks, stream)) return rc;
-    return a.want_w ? launch_join<f16>(join, stream) : SLICEGCN_OK;
+    return a.want_w ? launch_join<f16, EPI_STORE>(join, stream) : SLICEGCN_OK;
 }
 
 } // namespace slicegcn

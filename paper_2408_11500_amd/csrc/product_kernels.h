@@ -338,33 +338,263 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     }
 }
 
-// The sums of all parts of k, added in order in fp64; four columns a thread.  GATED: the parts of the second product are those of set 1.
+// The sums of all parts of k, in fp64: four columns a thread, and a.shares threads of a workgroup share the parts out (part s, s + shares, ... each), whose sums
+// are added in order.  GATED: the parts of the second product are those of set 1.  256 parts of 100 x 256 with one share 84 us.
 template <class T, int EPI> __global__ __launch_bounds__(256) void product_join_kernel(const ProductArgs a)
 {
-    const int64_t per_row = (a.N + 3) / 4, at = (a.first + blockIdx.x) * 256 + threadIdx.x;
-    const int64_t each = per_row * a.M;
-    const int sets = EPI == EPI_STORE ? a.sets : 1;
-    if (at >= each * sets) return;
-    const int set = (int)(at / each);
-    const int64_t row = (at - set * each) / per_row, col = (at - set * each) % per_row * 4;
+    constexpr int Q = EPI == EPI_GATED ? 2 : 1;
+    __shared__ double sums[256][Q * 4 + 1];
+    const int here = 256 / a.shares, share = threadIdx.x / here;
+    const int64_t per_row = (a.N + 3) / 4, each = per_row * a.M, at = (a.first + blockIdx.x) * here + threadIdx.x % here;
+    const bool there = at < each * (EPI == EPI_STORE ? a.sets : 1);
+    const int set = there ? (int)(at / each) : 0;
+    const int64_t row = there ? (at - set * each) / per_row : 0, col = there ? (at - set * each) % per_row * 4 : 0;
     const int left = a.N - col < 4 ? (int)(a.N - col) : 4;
-    double sum[2][4] = {};
-    for (int q = 0; q < (EPI == EPI_GATED ? 2 : 1); ++q) {
-        const char *part = reinterpret_cast<const char *>(a.partial + (int64_t)(set + q) * a.splits * a.M * a.N);
-        for (int i = 0; i < a.splits; ++i) {
-            float v[4];
-            load4<float>(part, ((int64_t)i * a.M + row) * a.N + col, left, v);
+    double sum[Q][4] = {};
+    if (there)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum[q][r] += (double)v[r];
+        for (int q = 0; q < Q; ++q) {
+            const char *part = reinterpret_cast<const char *>(a.partial + (int64_t)(set + q) * a.splits * a.M * a.N);
+#pragma unroll 4
+            for (int i = share; i < a.splits; i += a.shares) {
+                float v[4];
+                load4<float>(part, ((int64_t)i * a.M + row) * a.N + col, left, v);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[q][r] += (double)v[r];
+            }
         }
+    if (a.shares > 1) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sums[threadIdx.x][q * 4 + r] = sum[q][r];
+        __syncthreads();
+        if (share > 0) return;
+        for (int i = 1; i < a.shares; ++i)
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[q][r] += sums[i * here + threadIdx.x][q * 4 + r];
     }
+    if (!there) return;
     float s[2][4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         s[0][r] = (float)sum[0][r];
-        s[1][r] = (float)sum[1][r];
+        s[1][r] = (float)sum[Q - 1][r];
     }
     finish4<T, EPI>(a, set, row, col, left, s[0], s[1]);
+}
+
+template <class T, int EPI> int launch_join(ProductArgs &a, hipStream_t stream)
+{
+    a.shares = 1;
+    while (a.shares < 32 && a.shares * 4 <= a.splits) a.shares *= 2;
+    const int64_t here = 256 / a.shares, threads = (a.N + 3) / 4 * a.M * (EPI == EPI_STORE ? a.sets : 1);
+    return launch_parts((threads + here - 1) / here, [&](unsigned first, unsigned count) {
+        a.first = first;
+        product_join_kernel<T, EPI><<<count, 256, 0, stream>>>(a);
+    });
+}
+
+// ---- operands on boundaries of 4 bytes: through buffers -----------------------------------------------------------------
+
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+
+// A piece of an operand (R outer indexes, BK of k) on its way from memory to LDS, 8 elements a unit.  It is read through a buffer whose range check takes care of rows, lines
+// and columns behind the last one, so that the loads of a step depend on no lane's branch and two steps can be in flight.  KC: the buffer of the tile's rows, of which a step
+// reads from its scalar offset on; OC: the buffer of the step's lines.
+template <class T, int LAYOUT, int R, int BK, int THREADS> struct BufferPiece {
+    static constexpr int UNITS = R * BK / 8, EACH = (UNITS + THREADS - 1) / THREADS, V = sizeof(T) / 2; // accesses of 16 bytes a unit
+    static constexpr uint32_t NOWHERE = 0xffffff00u;
+    uint32_t offset[EACH];
+    uint64_t base;
+    uint32_t line, size; // bytes: of a line; KC: of the buffer, OC: of a line's part
+    struct Regs {
+        uint4v v[EACH][V];
+    };
+
+    __device__ static int unit(int i) { return (int)threadIdx.x + i * THREADS; }
+    __device__ static int unit_k(int i) { return unit(i) % (BK / 8) * 8; } // KC
+
+    __device__ void aim(const Operand &op, int64_t o0, int64_t outer, int32_t K)
+    {
+        line = (uint32_t)op.ld * sizeof(T);
+        const int64_t here = outer - o0 < R ? outer - o0 : R;
+        base = (uint64_t)op.p + (LAYOUT == LAYOUT_KC ? (uint64_t)o0 * line : (uint64_t)o0 * sizeof(T));
+        size = LAYOUT == LAYOUT_KC ? (uint32_t)(here - 1) * line + (uint32_t)K * sizeof(T) : (uint32_t)here * sizeof(T);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int q = unit(i);
+            offset[i] = LAYOUT == LAYOUT_KC ? (uint32_t)(q / (BK / 8)) * line + unit_k(i) * sizeof(T)
+                                            : (uint32_t)(q / (R / 8)) * line + (uint32_t)(q % (R / 8)) * 8 * sizeof(T);
+            if (UNITS % THREADS != 0 && q >= UNITS) offset[i] = NOWHERE;
+            // OC: a unit that begins behind the last column would read the next line's first ones
+            if (LAYOUT == LAYOUT_OC && (q % (R / 8)) * 8 >= here) offset[i] = NOWHERE;
+        }
+    }
+
+    // The step from k0 on; zeros where it is not there
+    __device__ void load(Regs &r, int32_t k0, int32_t K, bool there) const
+    {
+        uint32_t bytes = size, scalar = 0;
+        uint64_t from = base;
+        if (LAYOUT == LAYOUT_KC) {
+            scalar = (uint32_t)k0 * sizeof(T);
+        } else {
+            const int32_t lines = K - k0 < BK ? K - k0 : BK;
+            from += (uint64_t)(uint32_t)k0 * line;
+            bytes += (uint32_t)(lines - 1) * line;
+        }
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(from), 0, there ? (int)bytes : 0, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) r.v[i][v] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(offset[i] + 16 * v), (int)scalar, 0);
+    }
+
+    // left: k that exist from the step's first one on (KC: what follows in the buffer is the next row)
+    __device__ static void store(const Regs &r, short8 *lds, int32_t left)
+    {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int q = unit(i);
+            if (UNITS % THREADS != 0 && q >= UNITS) break;
+            T v[8];
+            __builtin_memcpy(v, r.v[i], sizeof(v));
+            if (LAYOUT == LAYOUT_KC && left < BK) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = unit_k(i) + j < left ? v[j] : (T)0.f;
+            }
+            const int at = LAYOUT == LAYOUT_KC ? lds_unit<LAYOUT, R, BK>(q / (BK / 8), q % (BK / 8)) : lds_unit<LAYOUT, R, BK>(q % (R / 8), q / (R / 8));
+            short8 t[Planes<T>::count];
+            split8(v, t);
+#pragma unroll
+            for (int p = 0; p < Planes<T>::count; ++p) lds[p * UNITS + at] = t[p];
+        }
+    }
+};
+
+// product_kernel for such operands: two steps on their way in registers, one in LDS
+template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const ProductArgs a)
+{
+    constexpr int P = Planes<T>::count, BK = P == 3 ? STEP_K_F32 : STEP_K_16, THREADS = 64 * WM * WN;
+    constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr bool TURNS = EPI == EPI_GATED, SEGMENTS = LM == LAYOUT_KC && LN == LAYOUT_KC;
+    constexpr int PIECES = TURNS ? 2 : 1, COLS = BN / PIECES; // columns of results; GATED: a piece of each product
+    static_assert(!TURNS || FN % 2 == 0, "a wavefront holds both products of its columns");
+    typedef BufferPiece<T, LM, BM, BK, THREADS> PieceM;
+    typedef BufferPiece<T, LN, COLS, BK, THREADS> PieceN;
+    __shared__ short8 lds[P * (PieceM::UNITS + PIECES * PieceN::UNITS)];
+    short8 *lds_m = lds, *lds_n = lds + P * PieceM::UNITS;
+
+    const int64_t tile_rows = (a.M + BM - 1) / BM, tile_cols = (a.N + COLS - 1) / COLS, tiles = tile_rows * tile_cols;
+    int64_t id = tile_of(a.first + blockIdx.x, tiles * a.splits * a.sets), row_tile, col_tile;
+    const int set = a.sets > 1 ? (int)(id / (tiles * a.splits)) : 0;
+    id -= set * (tiles * a.splits);
+    const int split = SPLIT ? (int)(id / tiles) : 0;
+    tile_place(id - split * tiles, tile_rows, tile_cols, row_tile, col_tile);
+    const int64_t m0 = row_tile * BM, n0 = col_tile * COLS;
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+
+    float4v acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
+
+    const int32_t K = (int32_t)a.K, steps_each = (K + BK - 1) / BK, all = SEGMENTS ? steps_each * a.segments : steps_each;
+    const int32_t begin = SPLIT ? split * a.steps_per_split : 0, end = SPLIT && begin + a.steps_per_split < all ? begin + a.steps_per_split : all;
+    PieceM pm;
+    PieceN pn[PIECES];
+    pm.aim(a.a[set], m0, a.M, K);
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) pn[q].aim(a.b[TURNS ? q : set], n0, a.N, K);
+    // the second segment's operands have the leading dimensions of the first one's
+    const uint64_t base_m = pm.base, base_n = pn[0].base, second_m = base_m + (uint64_t)(a.a[1].p - a.a[0].p), second_n = base_n + (uint64_t)(a.b[1].p - a.b[0].p);
+    struct Step {
+        typename PieceM::Regs m;
+        typename PieceN::Regs n[PIECES];
+    } regs[2];
+    auto load = [&](Step &s, int32_t t) {
+        int32_t k0 = t * BK;
+        if (SEGMENTS) {
+            const bool second = t >= steps_each;
+            k0 -= second ? steps_each * BK : 0;
+            pm.base = second ? second_m : base_m;
+            pn[0].base = second ? second_n : base_n;
+        }
+        pm.load(s.m, k0, K, t < end);
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) pn[q].load(s.n[q], k0, K, t < end);
+    };
+    auto step = [&](Step &s, int32_t t) {
+        const int32_t left = K - (SEGMENTS && t >= steps_each ? t - steps_each : t) * BK;
+        __syncthreads();
+        PieceM::store(s.m, lds_m, left);
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) PieceN::store(s.n[q], lds_n + q * P * PieceN::UNITS, left);
+        __syncthreads();
+        load(s, t + 2);
+#pragma unroll
+        for (int kk = 0; kk < BK / 32; ++kk) {
+            short8 fm[FM][P];
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int p = 0; p < P; ++p) fm[i][p] = fragment<LM, BM, BK>(lds_m + p * PieceM::UNITS, wm + 16 * i, kk, lane);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                short8 fn[P];
+                const int q = TURNS ? j % 2 : 0, base = TURNS ? wn / 2 + 8 * (j - j % 2) : wn + 16 * j;
+#pragma unroll
+                for (int p = 0; p < P; ++p) fn[p] = fragment<LN, COLS, BK>(lds_n + (q * P + p) * PieceN::UNITS, base, kk, lane);
+                if constexpr (P == 3) {
+#pragma unroll
+                    for (int order = 2; order >= 0; --order) // terms of order 2, 1, 0: the sum of the two planes' numbers
+#pragma unroll
+                        for (int p = 0; p <= order; ++p)
+#pragma unroll
+                            for (int i = 0; i < FM; ++i) acc[i][j] = mfma<T>(fn[p], fm[i][order - p], acc[i][j]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < FM; ++i) acc[i][j] = mfma<T>(fn[0], fm[i][0], acc[i][j]);
+                }
+            }
+        }
+    };
+    load(regs[0], begin);
+    load(regs[1], begin + 1);
+    for (int32_t t = begin; t < end; t += 2) { // an odd number of steps ends with one of zeros
+        step(regs[0], t);
+        step(regs[1], t + 1);
+    }
+
+    // lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of every 16 x 16 results
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int64_t row = m0 + wm + 16 * i + lane % 16;
+        if (row >= a.M) continue;
+#pragma unroll
+        for (int j = 0; j < FN; j += PIECES) {
+            const int64_t col = n0 + (TURNS ? wn / 2 + 8 * j : wn + 16 * j) + 4 * (lane / 16);
+            const int left = a.N - col < 4 ? (int)(a.N - col) : 4;
+            if (left <= 0) continue;
+            float s[4], s2[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[r] = acc[i][j][r];
+                s2[r] = acc[i][j + PIECES - 1][r];
+            }
+            if constexpr (SPLIT) {
+                char *to = reinterpret_cast<char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N);
+                store4<float>(to, row * a.N + col, left, s);
+            } else {
+                finish4<T, EPI>(a, set, row, col, left, s, s2);
+            }
+        }
+    }
 }
 
 template <class T, int LM, int LN, int EPI, int TILE, bool SPLIT> int launch_tile(ProductArgs &a, hipStream_t stream)
@@ -374,7 +604,12 @@ template <class T, int LM, int LN, int EPI, int TILE, bool SPLIT> int launch_til
     const int64_t blocks = (a.M + BM - 1) / BM * ((a.N + COLS - 1) / COLS) * a.splits * a.sets;
     return launch_parts(blocks, [&](unsigned first, unsigned count) {
         a.first = first;
-        product_kernel<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT><<<count, 64 * WM * WN, 0, stream>>>(a);
+        if constexpr (sizeof(T) == 2)
+            if (!a.on_words) {
+                product_kernel<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT><<<count, 64 * WM * WN, 0, stream>>>(a);
+                return;
+            }
+        product_buffer_kernel<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT><<<count, 64 * WM * WN, 0, stream>>>(a);
     });
 }
 

@@ -33,11 +33,7 @@ template <class T, int LM, int LN, int EPI> int launch_layouts(const ProductPlan
     const int rc = launch_sums<T, LM, LN, EPI_STORE, true>(plan, a, stream);
     a.sets = sets;
     if (rc) return rc;
-    const int64_t threads = (a.N + 3) / 4 * a.M * (EPI == EPI_STORE ? a.sets : 1);
-    return launch_parts((threads + 255) / 256, [&](unsigned first, unsigned count) {
-        a.first = first;
-        product_join_kernel<T, EPI><<<count, 256, 0, stream>>>(a);
-    });
+    return launch_join<T, EPI>(a, stream);
 }
 
 template <class T> int launch_product(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream)

@@ -19,7 +19,6 @@ namespace {
 
 constexpr int NARROW_THREADS = 512, NARROW_ROWS = 32, NARROW_X = NARROW_WIDTH_IN / 8, NARROW_G = NARROW_WIDTH_OUT / 8; // units of 8 columns
 
-typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 
 // A block's rows of a matrix as a buffer
@@ -263,16 +262,6 @@ template <class T> int launch_narrow(const NarrowArgs &a, int act, bool gated, u
     });
     SG_LAUNCH_CHECK();
     return SLICEGCN_OK;
-}
-
-// dW of the workgroups' sums
-template <class T> int launch_join(ProductArgs &a, hipStream_t stream)
-{
-    const int64_t threads = (a.N + 3) / 4 * a.M * a.sets;
-    return launch_parts((threads + 255) / 256, [&](unsigned first, unsigned count) {
-        a.first = first;
-        product_join_kernel<T, EPI_STORE><<<count, 256, 0, stream>>>(a);
-    });
 }
 
 } // namespace
