@@ -74,7 +74,11 @@ template <class T> __device__ inline void split8(const T (&v)[8], short8 (&out)[
 
 // Where a tile's piece of an operand lies in LDS (in 16-byte units; R outer indexes by BK of k), so that the lanes of a read meet in different banks:
 // KC: a row's units are permuted by its index; OC: 32-byte pairs of units of a line of k are permuted by its index, as the transposing read takes pairs.
-template <int R> __device__ inline int line_turn(int k) { return ((k & 3) | ((k >> 3) & 1) << 2) & (R / 16 - 1); }
+template <int R> __device__ inline int line_turn(int k)
+{
+    if constexpr (R >= 128) return (k & 3) | ((k >> 3) & 1) << 2;
+    return ((k & 3) ^ ((k >> 3) & 1)) & (R / 16 - 1); // lines shorter than the banks: two or four of them side by side
+}
 template <int LAYOUT, int R, int BK> __device__ inline int lds_unit(int outer_or_unit, int k_or_unit)
 {
     if constexpr (LAYOUT == LAYOUT_KC) {
@@ -477,8 +481,9 @@ template <class T, int LAYOUT, int R, int BK, int THREADS> struct BufferPiece {
 
 // product_kernel for such operands: two steps on their way in registers, one in LDS
 template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT>
-__global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const ProductArgs a)
+__global__ __launch_bounds__(64 * WM * WN, sizeof(T) == 4 ? 3 : 2) void product_buffer_kernel(const ProductArgs a)
 {
+    constexpr int SETS = sizeof(T) == 4 ? 1 : 2;
     constexpr int P = Planes<T>::count, BK = P == 3 ? STEP_K_F32 : STEP_K_16, THREADS = 64 * WM * WN;
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
     constexpr bool TURNS = EPI == EPI_GATED, SEGMENTS = LM == LAYOUT_KC && LN == LAYOUT_KC;
@@ -516,7 +521,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const P
     struct Step {
         typename PieceM::Regs m;
         typename PieceN::Regs n[PIECES];
-    } regs[2];
+    } regs[SETS];
     auto load = [&](Step &s, int32_t t) {
         int32_t k0 = t * BK;
         if (SEGMENTS) {
@@ -536,7 +541,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const P
 #pragma unroll
         for (int q = 0; q < PIECES; ++q) PieceN::store(s.n[q], lds_n + q * P * PieceN::UNITS, left);
         __syncthreads();
-        load(s, t + 2);
+        load(s, t + SETS);
 #pragma unroll
         for (int kk = 0; kk < BK / 32; ++kk) {
             short8 fm[FM][P];
@@ -564,11 +569,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const P
             }
         }
     };
-    load(regs[0], begin);
-    load(regs[1], begin + 1);
-    for (int32_t t = begin; t < end; t += 2) { // an odd number of steps ends with one of zeros
-        step(regs[0], t);
-        step(regs[1], t + 1);
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) load(regs[i], begin + i);
+    for (int32_t t = begin; t < end; t += SETS) { // with two sets an odd number of steps ends with one of zeros
+#pragma unroll
+        for (int i = 0; i < SETS; ++i) step(regs[i], t + i);
     }
 
     // lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of every 16 x 16 results
