@@ -525,6 +525,48 @@ class Optimizer:
         return lr
 
 
+class AdamW:
+    """AdamW (decoupled weight decay, on matrices alone) with a cosine-annealed learning rate over all learnable tensors of the given
+    models, which stay where they are: one library call updates them all.  ``state_bits`` = 8: the means are kept as e4m3 numbers with a
+    scale per 128 elements, 2 bytes a parameter instead of 8.  Tensors of 16 bits get fp32 masters.  ``max_norm`` as in ``Optimizer``;
+    where the gradients' norm is not finite, an update is left out."""
+
+    def __init__(self, models, lr_max: float, lr_min: float = 0.0, t_max: int = 1, beta1: float = 0.9, beta2: float = 0.999,
+                 eps: float = 1e-8, weight_decay: float = 0.01, max_norm: float | None = None, state_bits: int = 32, seed: int = 0):
+        if state_bits not in (8, 32):
+            raise ValueError(f"states of {state_bits} bits")
+        get = lambda o, k: o[k] if isinstance(o, dict) else getattr(o, k)
+        slots = [s for m in models for s in m.parameter_slots()]
+        self.params, self.grads = [get(po, pk) for po, pk, _, _ in slots], [get(go, gk) for _, _, go, gk in slots]
+        dev = self.params[0].device
+        state = dict(dtype=torch.float32 if state_bits == 32 else torch.float8_e4m3fn, device=dev)
+        self.m, self.v = ([torch.zeros(p.numel(), **state) for p in self.params] for _ in range(2))
+        self.scales = None
+        if state_bits == 8:
+            self.scales = [torch.ones((-(-p.numel() // B.STATE_BLOCK), 2), dtype=torch.uint8, device=dev) for p in self.params]
+        self.masters = [p.float() if p.dtype != torch.float32 else None for p in self.params]
+        self.tensors = B.AdamList(self.params, self.grads, self.m, self.v, scales=self.scales, masters=self.masters,
+                                  decays=[weight_decay if p.dim() > 1 else 0.0 for p in self.params])
+        self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps)
+        self.lr_max, self.lr_min, self.t_max, self.seed = lr_max, lr_min, t_max, seed
+        self.t = 0
+        self.max_norm = max_norm
+        self.factor = None
+        if max_norm is not None:
+            self.norm, self.factor = (torch.zeros(1, dtype=torch.float32, device=dev) for _ in range(2))
+            self.gradients = B.TensorList(self.grads)
+            self.norm_ws = torch.empty(B.slicegcn_global_norm_workspace_bytes(self.gradients), dtype=torch.uint8, device=dev)
+
+    def step(self, epoch: int) -> float:
+        """One update with the learning rate of ``epoch`` (0-based); returns that rate."""
+        self.t += 1
+        lr = B.slicegcn_cosine_lr(self.lr_max, self.lr_min, epoch, self.t_max)
+        if self.max_norm is not None:
+            B.slicegcn_global_norm(self.gradients, self.norm, self.norm_ws, max_norm=self.max_norm, factor=self.factor)
+        B.slicegcn_adamw_step(self.tensors, lr, self.t, factor=self.factor, seed=self.seed + self.t, **self.hyper)
+        return lr
+
+
 class GraphedStep:
     """A sequence of library calls captured once into a HIP graph and replayed with one launch.
 

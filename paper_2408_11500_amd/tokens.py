@@ -5,6 +5,8 @@ stacks put one after another, with a norm before and after each, a gated residua
     y_b = stack_b(MLP_FF_b(u_b));  x_{b+1} = x_b + gate_b * post_b(y_b);  u_{b+1} = pre_{b+1}(x_{b+1})
     loss = cross-entropy(MLP_CLS(u_blocks))
 
+and with a feed-forward block behind each stack, x_{b+1} += (silu(u_{b+1} Wg) * (u_{b+1} Wu)) Wd before the next block, normed again.
+
 This module orders library calls and owns buffers; every arithmetic step of an epoch is a kernel of the library.  Run
 ``python -m paper_2408_11500_amd.tokens --workload cfg1 --epochs 60`` for a seeded synthetic run (a node's label is a function of its
 token, so that there is something to learn).
@@ -20,7 +22,7 @@ import time
 import torch
 
 from . import binding as B
-from .stack import Classifier, FeatureFusion, GraphedStep, Optimizer, SliceStack
+from .stack import AdamW, Classifier, FeatureFusion, GraphedStep, Optimizer, SliceStack
 
 
 class Embedding:
@@ -93,10 +95,45 @@ class BlockNorm:
         return [(self.params, name, self.grads, "d" + name) for name in self.params]
 
 
+class GatedFeedForward:
+    """x' = x + (act(u Wg) * (u Wu)) Wd on rows of fp32, bf16 or fp16: gated projections to ``inner`` columns and the way back with the
+    residual in its epilogue.  ``u``: x behind the norm before the block."""
+
+    def __init__(self, n: int, width: int, inner: int, act: int = B.ACT_SILU, dtype: torch.dtype = torch.float32, device="cuda"):
+        self.act = act
+        like = dict(dtype=dtype, device=device)
+        self.Wg, self.Wu, self.dWg, self.dWu = (torch.zeros((width, inner), **like) for _ in range(4))
+        self.Wd, self.dWd = (torch.zeros((inner, width), **like) for _ in range(2))
+        self.G, self.U, self.H, self.dH = (torch.empty((n, inner), **like) for _ in range(4))
+        self.x, self.du = (torch.empty((n, width), **like) for _ in range(2))
+        self.ws = torch.empty(max(B.slicegcn_gated_fwd_workspace_bytes(n, width, inner, dtype), B.slicegcn_gated_bwd_workspace_bytes(n, width, inner, dtype),
+                                  B.slicegcn_product_fwd_workspace_bytes(n, inner, width, dtype),
+                                  B.slicegcn_product_bwd_workspace_bytes(n, inner, width, dtype)), dtype=torch.uint8, device=device)
+
+    def set_params(self, Wg, Wu, Wd):
+        for dst, src in ((self.Wg, Wg), (self.Wu, Wu), (self.Wd, Wd)):
+            dst.copy_(src)
+
+    def forward(self, x: torch.Tensor, u: torch.Tensor) -> torch.Tensor:
+        B.slicegcn_gated_fwd(u, self.Wg, self.Wu, self.H, self.ws, G=self.G, U=self.U, act=self.act)
+        return B.slicegcn_product_fwd(self.H, self.Wd, self.x, self.ws, R=x)
+
+    def backward(self, u: torch.Tensor, dx: torch.Tensor) -> torch.Tensor:
+        """Gradient of u from that of x'; the gradient of x is that of x' (and what reaches it through u)."""
+        B.slicegcn_product_bwd(self.H, self.Wd, None, dx, self.ws, dX=self.dH, dW=self.dWd)
+        B.slicegcn_gated_bwd(u, self.Wg, self.Wu, self.G, self.U, self.dH, self.ws, dX=self.du, dWg=self.dWg, dWu=self.dWu, act=self.act)
+        return self.du
+
+    def parameter_slots(self):
+        return [(self, w, self, "d" + w) for w in ("Wg", "Wu", "Wd")]
+
+
 class TokenTrainer:
     def __init__(self, graph: B.Graph, ids: torch.Tensor, vocab: int, labels: torch.Tensor, k: int, slice_hidden: int, layers: int,
-                 hidden: int, classes: int, blocks: int = 1, pad: int | None = None, graph_replay: bool = False):
-        """``blocks`` slice stacks of k slice models with ``layers`` layers each.  ``graph_replay``: forward, loss and backward of an
+                 hidden: int, classes: int, blocks: int = 1, pad: int | None = None, graph_replay: bool = False,
+                 feed_forward: int = 0):
+        """``blocks`` slice stacks of k slice models with ``layers`` layers each.  ``feed_forward``: columns inside the gated feed-forward
+        block behind each stack (0: none).  ``graph_replay``: forward, loss and backward of an
         epoch are captured into a HIP graph at the first epoch and replayed afterwards."""
         n, width = ids.numel(), k * slice_hidden
         dev = ids.device
@@ -106,33 +143,46 @@ class TokenTrainer:
         self.norms += [BlockNorm(n, width, device=dev) for _ in range(blocks)]
         self.ffs = [FeatureFusion(n, width, slice_hidden, device=dev) for _ in range(blocks)]
         self.stacks = [SliceStack(graph, n, k, slice_hidden, slice_hidden, layers, device=dev, shared_input=ff.Xff) for ff in self.ffs]
+        self.gated = [GatedFeedForward(n, width, feed_forward, device=dev) for _ in range(blocks if feed_forward else 0)]
+        self.gated_norms = [BlockNorm(n, width, post=B.NORM_NONE, gated=False, device=dev, block=False) for _ in self.gated]
         self.cls = Classifier(n, width, hidden, classes, device=dev)
         self.du = torch.empty((n, width), dtype=torch.float32, device=dev)
         self.opt = None
         self.graph_replay, self._graph = graph_replay, None
 
     def models(self):
-        return [self.emb, *self.norms, *self.ffs, *self.stacks, self.cls]
+        return [self.emb, *self.norms, *self.ffs, *self.stacks, *self.gated, *self.gated_norms, self.cls]
 
-    def start(self, lr_max: float, lr_min: float, epochs: int, weight_decay: float = 0.0, max_norm: float | None = 1.0):
-        """Call once after the parameters of all models are set."""
-        self.opt = Optimizer(self.models(), lr_max=lr_max, lr_min=lr_min, t_max=epochs, weight_decay=weight_decay, max_norm=max_norm)
+    def start(self, lr_max: float, lr_min: float, epochs: int, weight_decay: float = 0.0, max_norm: float | None = 1.0,
+              state_bits: int | None = None):
+        """Call once after the parameters of all models are set.  ``state_bits`` (8 or 32): AdamW with such states instead of Adam."""
+        args = dict(lr_max=lr_max, lr_min=lr_min, t_max=epochs, weight_decay=weight_decay, max_norm=max_norm)
+        self.opt = Optimizer(self.models(), **args) if state_bits is None else AdamW(self.models(), state_bits=state_bits, **args)
 
     def forward_backward(self):
         """Forward, loss and backward of one epoch (no update)."""
         xs = [self.emb.forward()]
         _, u = self.norms[0].forward(xs[0], None)
         us, ys = [u], []
-        for ff, stack, norm in zip(self.ffs, self.stacks, self.norms[1:]):
+        inner = []  # what enters the feed-forward blocks
+        for b, (ff, stack, norm) in enumerate(zip(self.ffs, self.stacks, self.norms[1:])):
             ff.forward(us[-1])
             ys.append(stack.forward())
             x, u = norm.forward(xs[-1], ys[-1])
+            if self.gated:
+                inner.append(u)
+                x = self.gated[b].forward(x, u)
+                _, u = self.gated_norms[b].forward(x, None)
             xs.append(x)
             us.append(u)
         self.cls.forward_backward(us[-1], self.labels, self.du)
         dx = None
         for b in reversed(range(len(self.stacks))):
-            dx, dy = self.norms[b + 1].backward(xs[b], ys[b], dx, self.du)
+            du = self.du
+            if self.gated:
+                dx, _ = self.gated_norms[b].backward(xs[b + 1], None, dx, du)
+                du = self.gated[b].backward(inner[b], dx)
+            dx, dy = self.norms[b + 1].backward(xs[b], ys[b], dx, du)
             self.stacks[b].backward(dy)
             self.ffs[b].backward(us[b], self.stacks[b].dXin[:, :self.ffs[b].s], self.du)
         dx, _ = self.norms[0].backward(xs[0], None, dx, self.du)
@@ -150,7 +200,7 @@ class TokenTrainer:
         return self.cls.loss
 
 
-def seeded_trainer(w, vocab: int, blocks: int = 1, graph_replay: bool = False, device="cuda:0"):
+def seeded_trainer(w, vocab: int, blocks: int = 1, graph_replay: bool = False, device="cuda:0", feed_forward: int = 0):
     """(graph, trainer) for a workload of ``synth.configs`` with seeded tokens, labels and parameters."""
     from synth import configs, model, rng
     src, dst = configs.edges(w, device=device)
@@ -158,7 +208,7 @@ def seeded_trainer(w, vocab: int, blocks: int = 1, graph_replay: bool = False, d
     u = rng.uniform(w.seed, STREAM_TOKENS, rng.arange64(w.n_nodes, device))
     ids = (float(vocab) ** u).long().clamp_(1, vocab) - 1  # a token's frequency falls with its rank
     tr = TokenTrainer(g, ids, vocab, ids % w.classes, w.k, w.slice_hidden, w.layers, w.hidden, w.classes, blocks=blocks,
-                      graph_replay=graph_replay)
+                      graph_replay=graph_replay, feed_forward=feed_forward)
     width = w.k * w.slice_hidden
     tr.emb.table.copy_(configs.normal_matrix(w.seed, STREAM_TABLE, vocab, width, device=device, std=1 / tr.emb.scale))
     for b, (ff, stack) in enumerate(zip(tr.ffs, tr.stacks)):
@@ -168,11 +218,15 @@ def seeded_trainer(w, vocab: int, blocks: int = 1, graph_replay: bool = False, d
         for i in range(w.k):
             for layer, (wi, wo) in enumerate(stack.widths):
                 stack.set_params(i, layer, *model.slice_layer_params(w, i, layer, wi, wo, device=device))
+    for b, ff in enumerate(tr.gated):
+        tag = TAG_GATED + 10 * b
+        ff.set_params(*(configs.glorot(w.seed, tag + i, *shape, device) for i, shape in enumerate(2 * [(width, feed_forward)] + [(feed_forward, width)])))
     tr.cls.set_params(*model.classifier_params(w, width, device=device))
     return g, tr
 
 
 STREAM_TOKENS, STREAM_TABLE = 20, 21  # of the seeded generator
+TAG_GATED = (1 << 20) + 1000  # behind those of the classifier
 
 
 def main(argv=None):
@@ -183,12 +237,15 @@ def main(argv=None):
     ap.add_argument("--epochs", type=int, default=60)
     ap.add_argument("--lr", type=float, default=1e-2)
     ap.add_argument("--max-norm", type=float, default=1.0, help="gradients are clipped to this norm")
+    ap.add_argument("--feed-forward", type=int, default=0, help="columns inside a gated feed-forward block behind each stack (0: none)")
+    ap.add_argument("--state-bits", type=int, choices=(8, 32), default=None, help="AdamW with states of so many bits instead of Adam")
+    ap.add_argument("--weight-decay", type=float, default=0.0)
     ap.add_argument("--graph", action="store_true", help="replay forward + loss + backward as one HIP graph")
     args = ap.parse_args(argv)
     sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     import synth
-    g, tr = seeded_trainer(synth.WORKLOADS[args.workload], args.vocab, args.blocks, args.graph)
-    tr.start(args.lr, args.lr * 1e-2, args.epochs, max_norm=args.max_norm)
+    g, tr = seeded_trainer(synth.WORKLOADS[args.workload], args.vocab, args.blocks, args.graph, feed_forward=args.feed_forward)
+    tr.start(args.lr, args.lr * 1e-2, args.epochs, weight_decay=args.weight_decay, max_norm=args.max_norm, state_bits=args.state_bits)
     torch.cuda.synchronize()
     t0 = time.perf_counter()
     for t in range(args.epochs):
