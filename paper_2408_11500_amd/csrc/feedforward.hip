@@ -92,11 +92,19 @@ bool product_on_words(int layouts, const ProductShape &s, const ProductArgs &a)
     }
 }
 
+bool results_on_words(const ProductShape &s, const ProductArgs &a)
+{
+    for (int i = 0; i < 2; ++i)
+        if (!on_words(Operand{a.out[i], a.ldo[i]}, s.type) || !on_words(Operand{a.keep[i], a.ldk[i]}, s.type)) return false;
+    return on_words(a.r, s.type);
+}
+
 int launch_product(const ProductShape &s, int layouts, int epilogue, ProductArgs &a, hipStream_t stream)
 {
     const int32_t type = s.type;
     const ProductPlan plan = plan_product(s, aligned_product(layouts, s, a));
     a.on_words = product_on_words(layouts, s, a);
+    a.whole = s.N % 4 == 0 && (plan.splits > 1 || results_on_words(s, a));
     return type == SLICEGCN_F32    ? launch_product_f32(layouts, epilogue, plan, a, stream)
            : type == SLICEGCN_BF16 ? launch_product_bf16(layouts, epilogue, plan, a, stream)
                                    : launch_product_f16(layouts, epilogue, plan, a, stream);

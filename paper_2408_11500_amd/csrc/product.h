@@ -44,6 +44,7 @@ struct ProductArgs {
     int32_t steps_per_split;
     int64_t first;         // first workgroup of this launch
     int32_t shares;        // threads that share the parts of a result out where they are joined
+    int32_t whole;         // whether results come in whole groups of four columns, on words
     int32_t on_words;      // whether buffers can read the operands: product_kernels.h
 };
 

@@ -224,29 +224,7 @@ __global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // no load into LDS outlives the workgroup
 
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int64_t row = m0 + wm + 16 * i + lane % 16;
-        if (row >= a.M) continue;
-#pragma unroll
-        for (int j = 0; j < FN; j += PIECES) {
-            const int64_t col = n0 + (TURNS ? wn / 2 + 8 * j : wn + 16 * j) + 4 * (lane / 16);
-            const int left = a.N - col < 4 ? (int)(a.N - col) : 4;
-            if (left <= 0) continue;
-            float s[4], s2[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s[r] = acc[i][j][r];
-                s2[r] = acc[i][j + PIECES - 1][r];
-            }
-            if constexpr (SPLIT) {
-                char *to = reinterpret_cast<char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N);
-                store4<float>(to, row * a.N + col, left, s);
-            } else {
-                finish4<T, EPI>(a, set, row, col, left, s, s2);
-            }
-        }
-    }
+    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, acc);
 }
 
 template <class T, int LM, int LN, int EPI, bool SPLIT> int launch_direct(ProductArgs &a, hipStream_t stream)

@@ -19,6 +19,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short short8 __attribute__((ext_vector_type(8)));
 typedef short short4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 
 template <class T> struct Planes { static constexpr int count = 1; };
 template <> struct Planes<float> { static constexpr int count = 3; };
@@ -244,6 +246,150 @@ __device__ inline void finish4(const ProductArgs &a, int set, int64_t row, int64
     }
 }
 
+// A tile's rows of a matrix as a buffer: what a lane reads or writes of them is four columns at its own offset plus a scalar one per 16 x 16 results, and rows behind the
+// last one are neither read nor written.
+constexpr uint32_t NOT_THERE = 0xffffff00u; // beyond any buffer
+template <class T> struct TileRows {
+    __amdgpu_buffer_rsrc_t rsrc;
+    uint32_t offset, line; // bytes
+
+    __device__ TileRows(const char *p, int64_t ld, int64_t m0, int64_t n0, int64_t rows, int32_t cols, int row, int col)
+    {
+        line = (uint32_t)ld * sizeof(T);
+        const uint32_t bytes = (uint32_t)(rows - 1) * line + (uint32_t)cols * sizeof(T);
+        rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p + (m0 * ld + n0) * (int64_t)sizeof(T)), 0, (int)bytes, 0x00020000);
+        offset = (uint32_t)row * line + (uint32_t)col * sizeof(T);
+    }
+    // `on`: whether the lane has such columns
+    __device__ void load(int i, int col, bool on, float (&v)[4]) const
+    {
+        const int at = (int)(on ? offset : NOT_THERE), scalar = (int)(16 * i * line + col * sizeof(T));
+        if constexpr (sizeof(T) == 4) {
+            const uint4v x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, scalar, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = __uint_as_float(x[r]);
+        } else {
+            typedef T T4 __attribute__((ext_vector_type(4)));
+            const T4 x = __builtin_bit_cast(T4, __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, scalar, 0));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = (float)x[r];
+        }
+    }
+    __device__ void store(int i, int col, bool on, const float (&v)[4]) const
+    {
+        const int at = (int)(on ? offset : NOT_THERE), scalar = (int)(16 * i * line + col * sizeof(T));
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        T4 x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = (T)v[r];
+        if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, x), rsrc, at, scalar, 0);
+        else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(uint2v, x), rsrc, at, scalar, 0);
+    }
+};
+
+// A wavefront's sums into results, as finish4 forms them.  Lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of every 16 x 16 results, which begin at row wm and column wn of
+// the tile; GATED: acc[.][j] and acc[.][j + 1] are both products of the same columns.  Where N is a multiple of 4 and rows lie on words (a.whole), a lane has all of its four
+// columns or none, and stores have a scalar address each.
+template <class T, int EPI, bool SPLIT, int BM, int FM, int FN>
+__device__ inline void finish_tile(const ProductArgs &a, int set, int split, int64_t m0, int64_t n0, int wm, int wn, const float4v (&acc)[FM][FN])
+{
+    constexpr bool TURNS = EPI == EPI_GATED;
+    constexpr int J = TURNS ? 2 : 1, W = TURNS ? 8 : 16;
+    const int lane = threadIdx.x % 64, row = wm + lane % 16, col = (TURNS ? wn / 2 : wn) + 4 * (lane / 16);
+    const int64_t rows = a.M - m0 < BM ? a.M - m0 : BM;
+    const int32_t cols = a.N - (int32_t)n0;
+    auto sums = [&](int i, int j, float (&s)[4]) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = acc[i][j][r];
+    };
+    if (!a.whole) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int64_t at = m0 + row + 16 * i;
+            if (at >= a.M) continue;
+#pragma unroll
+            for (int j = 0; j < FN; j += J) {
+                const int left = cols - (col + W * j) < 4 ? cols - (col + W * j) : 4;
+                if (left <= 0) continue;
+                float s[4], s2[4];
+                sums(i, j, s);
+                sums(i, j + J - 1, s2);
+                if constexpr (SPLIT) store4<float>(reinterpret_cast<char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N), at * a.N + n0 + col + W * j, left, s);
+                else finish4<T, EPI>(a, set, at, n0 + col + W * j, left, s, s2);
+            }
+        }
+        return;
+    }
+    if constexpr (SPLIT) {
+        const TileRows<float> to(reinterpret_cast<const char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N), a.N, m0, n0, rows, cols, row, col);
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                float s[4];
+                sums(i, j, s);
+                to.store(i, W * j, col + W * j < cols, s);
+            }
+    } else if constexpr (EPI == EPI_STORE) {
+        const TileRows<T> to(a.out[set], a.ldo[set], m0, n0, rows, cols, row, col);
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                float s[4];
+                sums(i, j, s);
+                to.store(i, W * j, col + W * j < cols, s);
+            }
+    } else {
+        auto with = [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+            const TileRows<T> to(a.out[0], a.ldo[0], m0, n0, rows, cols, row, col), k0(a.keep[0], a.ldk[0], m0, n0, rows, cols, row, col);
+            const TileRows<T> other(TURNS ? a.keep[1] : a.r.p, TURNS ? a.ldk[1] : a.r.ld, m0, n0, rows, cols, row, col);
+#pragma unroll
+            for (int j = 0; j < FN; j += J) {
+                const bool on = col + W * j < cols;
+                float b[4], b2[4];
+                load_bias(a.bias[0], n0 + col + W * j, on ? 4 : 0, b);
+                if (TURNS) load_bias(a.bias[1], n0 + col + W * j, on ? 4 : 0, b2);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    float s[4], y[4];
+                    sums(i, j, s);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[r] += b[r];
+                    if (a.keep[0]) k0.store(i, W * j, on, s);
+                    if constexpr (TURNS) {
+                        float u[4];
+                        sums(i, j + 1, u);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            u[r] += b2[r];
+                            y[r] = activated<ACT>(s[r]) * u[r];
+                        }
+                        if (a.keep[0]) other.store(i, W * j, on, u);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) y[r] = activated<ACT>(s[r]);
+                        if (a.r.p) {
+                            float v[4];
+                            other.load(i, W * j, on, v);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) y[r] = fmaf(a.residual, v[r], y[r]);
+                        }
+                    }
+                    to.store(i, W * j, on, y);
+                }
+            }
+        };
+        switch (a.act) {
+        case SLICEGCN_ACT_RELU: with(std::integral_constant<int, SLICEGCN_ACT_RELU>()); break;
+        case SLICEGCN_ACT_SILU: with(std::integral_constant<int, SLICEGCN_ACT_SILU>()); break;
+        case SLICEGCN_ACT_GELU: with(std::integral_constant<int, SLICEGCN_ACT_GELU>()); break;
+        default: with(std::integral_constant<int, SLICEGCN_ACT_NONE>());
+        }
+    }
+}
+
 // WM x WN wavefronts.  SPLIT: sums of a part of k go to a.partial.
 template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs a)
@@ -316,30 +462,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
         }
     }
 
-    // lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of every 16 x 16 results
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int64_t row = m0 + wm + 16 * i + lane % 16;
-        if (row >= a.M) continue;
-#pragma unroll
-        for (int j = 0; j < FN; j += TURNS ? 2 : 1) {
-            const int64_t col = n0 + (TURNS ? wn / 2 + 8 * j : wn + 16 * j) + 4 * (lane / 16);
-            const int left = a.N - col < 4 ? (int)(a.N - col) : 4;
-            if (left <= 0) continue;
-            float s[4], s2[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s[r] = acc[i][j][r];
-                s2[r] = acc[i][TURNS ? j + 1 : j][r];
-            }
-            if constexpr (SPLIT) {
-                char *to = reinterpret_cast<char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N);
-                store4<float>(to, row * a.N + col, left, s);
-            } else {
-                finish4<T, EPI>(a, set, row, col, left, s, s2);
-            }
-        }
-    }
+    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, acc);
 }
 
 // The sums of all parts of k, in fp64: four columns a thread, and a.shares threads of a workgroup share the parts out (part s, s + shares, ... each), whose sums
@@ -403,7 +526,6 @@ template <class T, int EPI> int launch_join(ProductArgs &a, hipStream_t stream)
 
 // ---- operands on boundaries of 4 bytes: through buffers -----------------------------------------------------------------
 
-typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 // A piece of an operand (R outer indexes, BK of k) on its way from memory to LDS, 8 elements a unit.  It is read through a buffer whose range check takes care of rows, lines
 // and columns behind the last one, so that the loads of a step depend on no lane's branch and two steps can be in flight.  KC: the buffer of the tile's rows, of which a step
@@ -576,30 +698,7 @@ __global__ __launch_bounds__(64 * WM * WN, sizeof(T) == 4 ? 3 : 2) void product_
         for (int i = 0; i < SETS; ++i) step(regs[i], t + i);
     }
 
-    // lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of every 16 x 16 results
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int64_t row = m0 + wm + 16 * i + lane % 16;
-        if (row >= a.M) continue;
-#pragma unroll
-        for (int j = 0; j < FN; j += PIECES) {
-            const int64_t col = n0 + (TURNS ? wn / 2 + 8 * j : wn + 16 * j) + 4 * (lane / 16);
-            const int left = a.N - col < 4 ? (int)(a.N - col) : 4;
-            if (left <= 0) continue;
-            float s[4], s2[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s[r] = acc[i][j][r];
-                s2[r] = acc[i][j + PIECES - 1][r];
-            }
-            if constexpr (SPLIT) {
-                char *to = reinterpret_cast<char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N);
-                store4<float>(to, row * a.N + col, left, s);
-            } else {
-                finish4<T, EPI>(a, set, row, col, left, s, s2);
-            }
-        }
-    }
+    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, acc);
 }
 
 template <class T, int LM, int LN, int EPI, int TILE, bool SPLIT> int launch_tile(ProductArgs &a, hipStream_t stream)

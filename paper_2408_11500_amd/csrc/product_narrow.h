@@ -19,8 +19,6 @@ namespace {
 
 constexpr int NARROW_THREADS = 512, NARROW_ROWS = 32, NARROW_X = NARROW_WIDTH_IN / 8, NARROW_G = NARROW_WIDTH_OUT / 8; // units of 8 columns
 
-typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
-
 // A block's rows of a matrix as a buffer
 __device__ inline __amdgpu_buffer_rsrc_t rows_buffer(const char *p, int64_t ld, int64_t row0, int64_t n, int32_t w)
 {
