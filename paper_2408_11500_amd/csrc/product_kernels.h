@@ -289,7 +289,7 @@ template <class T> struct TileRows {
 
 // A wavefront's sums into results, as finish4 forms them.  Lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of every 16 x 16 results, which begin at row wm and column wn of
 // the tile; GATED: acc[.][j] and acc[.][j + 1] are both products of the same columns.  Where N is a multiple of 4 and rows lie on words (a.whole), a lane has all of its four
-// columns or none, and stores have a scalar address each.
+// columns or none, and stores have a scalar address each.  The parts of a row follow one another, so that lines are whole when they leave the L2.
 template <class T, int EPI, bool SPLIT, int BM, int FM, int FN>
 __device__ inline void finish_tile(const ProductArgs &a, int set, int split, int64_t m0, int64_t n0, int wm, int wn, const float4v (&acc)[FM][FN])
 {
@@ -323,9 +323,9 @@ __device__ inline void finish_tile(const ProductArgs &a, int set, int split, int
     if constexpr (SPLIT) {
         const TileRows<float> to(reinterpret_cast<const char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N), a.N, m0, n0, rows, cols, row, col);
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
+            for (int j = 0; j < FN; ++j) {
                 float s[4];
                 sums(i, j, s);
                 to.store(i, W * j, col + W * j < cols, s);
@@ -333,9 +333,9 @@ __device__ inline void finish_tile(const ProductArgs &a, int set, int split, int
     } else if constexpr (EPI == EPI_STORE) {
         const TileRows<T> to(a.out[set], a.ldo[set], m0, n0, rows, cols, row, col);
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
+            for (int j = 0; j < FN; ++j) {
                 float s[4];
                 sums(i, j, s);
                 to.store(i, W * j, col + W * j < cols, s);
@@ -345,25 +345,25 @@ __device__ inline void finish_tile(const ProductArgs &a, int set, int split, int
             constexpr int ACT = decltype(act)::value;
             const TileRows<T> to(a.out[0], a.ldo[0], m0, n0, rows, cols, row, col), k0(a.keep[0], a.ldk[0], m0, n0, rows, cols, row, col);
             const TileRows<T> other(TURNS ? a.keep[1] : a.r.p, TURNS ? a.ldk[1] : a.r.ld, m0, n0, rows, cols, row, col);
+            float bias[FN][4];
 #pragma unroll
-            for (int j = 0; j < FN; j += J) {
-                const bool on = col + W * j < cols;
-                float b[4], b2[4];
-                load_bias(a.bias[0], n0 + col + W * j, on ? 4 : 0, b);
-                if (TURNS) load_bias(a.bias[1], n0 + col + W * j, on ? 4 : 0, b2);
+            for (int j = 0; j < FN; ++j) load_bias(a.bias[TURNS ? j % 2 : 0], n0 + col + W * (j - (TURNS ? j % 2 : 0)), col + W * (j - (TURNS ? j % 2 : 0)) < cols ? 4 : 0, bias[j]);
 #pragma unroll
-                for (int i = 0; i < FM; ++i) {
+            for (int i = 0; i < FM; ++i) {
+#pragma unroll
+                for (int j = 0; j < FN; j += J) {
+                    const bool on = col + W * j < cols;
                     float s[4], y[4];
                     sums(i, j, s);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[r] += b[r];
+                    for (int r = 0; r < 4; ++r) s[r] += bias[j][r];
                     if (a.keep[0]) k0.store(i, W * j, on, s);
                     if constexpr (TURNS) {
                         float u[4];
                         sums(i, j + 1, u);
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            u[r] += b2[r];
+                            u[r] += bias[j + 1][r];
                             y[r] = activated<ACT>(s[r]) * u[r];
                         }
                         if (a.keep[0]) other.store(i, W * j, on, u);
@@ -603,7 +603,7 @@ template <class T, int LAYOUT, int R, int BK, int THREADS> struct BufferPiece {
 
 // product_kernel for such operands: two steps on their way in registers, one in LDS
 template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT>
-__global__ __launch_bounds__(64 * WM * WN, sizeof(T) == 4 ? 3 : 2) void product_buffer_kernel(const ProductArgs a)
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const ProductArgs a)
 {
     constexpr int SETS = sizeof(T) == 4 ? 1 : 2;
     constexpr int P = Planes<T>::count, BK = P == 3 ? STEP_K_F32 : STEP_K_16, THREADS = 64 * WM * WN;
