@@ -60,18 +60,91 @@ size_t partial_bytes(const ProductShape &s)
     return x > y ? x : y;
 }
 
-// Whether both operands can go straight into LDS: rows and columns in whole units of 16 bytes
-bool on_units(const Operand &o) { return aligned16(o.p) && o.ld % 8 == 0; }
+// Whether an operand can go straight into LDS: rows in whole units of 16 bytes
+bool on_units(const Operand &o, int64_t width) { return aligned16(o.p) && o.ld % 8 == 0 && (width % 8 == 0 || o.padded); }
+int operands(const ProductArgs &a) { return a.segments > a.sets ? a.segments : a.sets; } // on either side; GATED: one, and two on the N side
+int64_t width_a(int layouts, const ProductShape &s) { return layouts == PRODUCT_XTG ? s.M : s.K; } // of a row as stored
+int64_t width_b(int layouts, const ProductShape &s) { return layouts == PRODUCT_GWT ? s.K : s.N; }
+
 bool aligned_product(int layouts, const ProductShape &s, const ProductArgs &a)
 {
-    for (int i = 0; i < (s.segments > s.sets ? s.segments : s.sets); ++i)
-        if (!on_units(a.a[i]) || !on_units(a.b[i])) return false;
-    if (s.gated && !on_units(a.b[1])) return false;
-    switch (layouts) {
-    case PRODUCT_XW: return s.K % 8 == 0 && s.N % 8 == 0;
-    case PRODUCT_GWT: return s.K % 8 == 0;
-    default: return s.M % 8 == 0 && s.N % 8 == 0;
+    for (int i = 0; i < operands(a); ++i)
+        if (!on_units(a.a[i], width_a(layouts, s)) || !on_units(a.b[i], width_b(layouts, s))) return false;
+    return !s.gated || on_units(a.b[1], width_b(layouts, s));
+}
+
+// ---- 16-bit operands whose rows are no whole units of 16 bytes: copied so that they are, where the product is long against a copy of its operands.
+
+// 6263 rows 9079 -> 557 bf16:
+constexpr double PACK_LEAST = 2e9; // multiplications
+bool worth_packing(const ProductShape &s)
+{
+    return s.type != SLICEGCN_F32 && s.M > ROWS_MOST && s.N > 64 && (double)s.M * (double)s.N * (double)s.K * (s.gated ? 2 : s.segments * s.sets) >= PACK_LEAST;
+}
+int64_t packed_bytes(int64_t rows, int64_t width) { return width % 8 == 0 ? 0 : round_up(rows * round_up(width, 8) * 2, 256); }
+int64_t rows_a(int layouts, const ProductShape &s) { return layouts == PRODUCT_XTG ? s.K : s.M; }
+int64_t rows_b(int layouts, const ProductShape &s) { return layouts == PRODUCT_GWT ? s.N : s.K; }
+// Room for copies of the operands whose width asks for one (`both`: of the M side too, which a backward pass has formed itself for dX)
+size_t pack_bytes(int layouts, const ProductShape &s, bool a, bool b)
+{
+    if (!worth_packing(s)) return 0;
+    return (size_t)((a ? packed_bytes(rows_a(layouts, s), width_a(layouts, s)) : 0) +
+                    (b ? packed_bytes(rows_b(layouts, s), width_b(layouts, s)) * (s.gated ? 2 : s.segments * s.sets) : 0));
+}
+
+typedef unsigned short ushort8 __attribute__((ext_vector_type(8)));
+typedef unsigned short ushort8_packed __attribute__((ext_vector_type(8), aligned(2)));
+
+// 8 elements a thread; zeros behind a row's last one
+__global__ __launch_bounds__(256) void pack_kernel(const unsigned short *__restrict__ from, int64_t ld, int64_t rows, int32_t width, unsigned short *__restrict__ to,
+                                                   int64_t first)
+{
+    const int64_t units = (width + 7) / 8, at = (first + blockIdx.x) * 256 + threadIdx.x;
+    if (at >= units * rows) return;
+    const int64_t row = at / units;
+    const int32_t col = (int32_t)(at % units) * 8;
+    const unsigned short *p = from + row * ld + col;
+    ushort8 v;
+    if (width - col >= 8) {
+        v = *reinterpret_cast<const ushort8_packed *>(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = col + i < width ? p[i] : (unsigned short)0;
     }
+    *reinterpret_cast<ushort8 *>(to + at * 8) = v;
+}
+
+int pack(Operand &o, int64_t rows, int64_t width, char *&to, hipStream_t stream)
+{
+    const int64_t units = (width + 7) / 8 * rows;
+    unsigned short *out = reinterpret_cast<unsigned short *>(to);
+    const int rc = launch_parts((units + 255) / 256, [&](unsigned first, unsigned count) {
+        pack_kernel<<<count, 256, 0, stream>>>(reinterpret_cast<const unsigned short *>(o.p), o.ld, rows, (int32_t)width, out, first);
+    });
+    o = Operand{to, round_up(width, 8), 1};
+    to += packed_bytes(rows, width);
+    return rc;
+}
+
+// Copies of the operands that need one into `room`.  Not where one that has no room kept (rows that lie oddly though their width is a multiple of 8) needs it too.
+int pack_operands(int layouts, const ProductShape &s, ProductArgs &a, char *room, hipStream_t stream)
+{
+    const int64_t wa = width_a(layouts, s), wb = width_b(layouts, s);
+    const int count = s.gated ? 2 : operands(a);
+    bool fit = worth_packing(s);
+    for (int i = 0; i < operands(a); ++i) fit = fit && (on_units(a.a[i], wa) || wa % 8);
+    for (int i = 0; i < count; ++i) fit = fit && (on_units(a.b[i], wb) || wb % 8);
+    if (!fit || aligned_product(layouts, s, a)) return SLICEGCN_OK;
+    const Operand first = a.a[0];
+    for (int i = 0; i < operands(a); ++i) {
+        if (on_units(a.a[i], wa)) continue;
+        if (i > 0 && a.a[i].p == first.p) a.a[i] = a.a[0]; // both products of one X
+        else if (int rc = pack(a.a[i], rows_a(layouts, s), wa, room, stream)) return rc;
+    }
+    for (int i = 0; i < count; ++i)
+        if (!on_units(a.b[i], wb))
+            if (int rc = pack(a.b[i], rows_b(layouts, s), wb, room, stream)) return rc;
+    return SLICEGCN_OK;
 }
 
 // Whether buffers can read both operands: their range checks go by words, so no word may hold an element that exists and one that does not
@@ -81,7 +154,7 @@ bool on_words(const Operand &o, int32_t type)
 }
 bool product_on_words(int layouts, const ProductShape &s, const ProductArgs &a)
 {
-    for (int i = 0; i < (s.segments > s.sets ? s.segments : s.sets); ++i)
+    for (int i = 0; i < operands(a); ++i)
         if (!on_words(a.a[i], s.type) || !on_words(a.b[i], s.type)) return false;
     if (s.gated && !on_words(a.b[1], s.type)) return false;
     if (s.type == SLICEGCN_F32) return true;
@@ -92,19 +165,14 @@ bool product_on_words(int layouts, const ProductShape &s, const ProductArgs &a)
     }
 }
 
-bool results_on_words(const ProductShape &s, const ProductArgs &a)
-{
-    for (int i = 0; i < 2; ++i)
-        if (!on_words(Operand{a.out[i], a.ldo[i]}, s.type) || !on_words(Operand{a.keep[i], a.ldk[i]}, s.type)) return false;
-    return on_words(a.r, s.type);
-}
-
-int launch_product(const ProductShape &s, int layouts, int epilogue, ProductArgs &a, hipStream_t stream)
+// partial, room: parts of the workspace, for sums of parts of k and for copies of operands
+int launch_product(const ProductShape &s, int layouts, int epilogue, ProductArgs &a, void *partial, char *room, hipStream_t stream)
 {
     const int32_t type = s.type;
+    a.partial = static_cast<float *>(partial);
+    if (int rc = pack_operands(layouts, s, a, room, stream)) return rc;
     const ProductPlan plan = plan_product(s, aligned_product(layouts, s, a));
     a.on_words = product_on_words(layouts, s, a);
-    a.whole = s.N % 4 == 0 && (plan.splits > 1 || results_on_words(s, a));
     return type == SLICEGCN_F32    ? launch_product_f32(layouts, epilogue, plan, a, stream)
            : type == SLICEGCN_BF16 ? launch_product_bf16(layouts, epilogue, plan, a, stream)
                                    : launch_product_f16(layouts, epilogue, plan, a, stream);
@@ -150,9 +218,10 @@ template <class T, bool GATED, int ACT> __global__ __launch_bounds__(256) void s
             for (int i = 0; i < V; ++i) v[i] = i < left ? (float)p[i] : 0.f;
         }
     };
-    auto write = [&](char *base, int64_t ld, int64_t row, const float (&v)[V]) {
+    // whole: rows have room for the access, and what is behind the last column (zeros: it was read as zeros) belongs to them
+    auto write = [&](char *base, int64_t ld, int64_t row, const float (&v)[V], bool whole) {
         T *p = reinterpret_cast<T *>(base) + row * ld + col;
-        if (left >= V) {
+        if (left >= V || whole) {
             store_vec<T, V>(p, v);
         } else {
 #pragma unroll
@@ -182,12 +251,12 @@ template <class T, bool GATED, int ACT> __global__ __launch_bounds__(256) void s
                     o[0][i] = GATED ? d[r][i] * u[r][i] * slope : d[r][i] * slope;
                     if (GATED) o[Q - 1][i] = d[r][i] * y;
                 }
-                if (a.dg) write(a.dg, a.ldg, row, o[0]);
-                if (GATED && a.du) write(a.du, a.ldu, row, o[Q - 1]);
+                if (a.dg) write(a.dg, a.ldg, row, o[0], true);
+                if (GATED && a.du) write(a.du, a.ldu, row, o[Q - 1], true);
                 if (a.dr) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) d[r][i] *= a.residual;
-                    write(a.dr, a.ldr, row, d[r]);
+                    write(a.dr, a.ldr, row, d[r], false);
                 }
 #pragma unroll
                 for (int q = 0; q < Q; ++q)
@@ -277,8 +346,8 @@ bool narrow_rows_fit(const Operand &o) { return !o.p || ((reinterpret_cast<uintp
 // Workspace of a backward pass: gradients before the activation, their column sums, sums of parts of k
 struct BwdWorkspace {
     int64_t ld; // of the gradients before the activation: rows on 16-byte boundaries
-    size_t rows, sums, partial;
-    size_t bytes(int q) const { return q * rows + sums + partial; }
+    size_t rows, sums, partial, room;
+    size_t bytes(int q) const { return q * rows + sums + partial + room; }
 };
 
 ProductShape dx_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q) { return ProductShape{n, w_out, w_in, q, 1, type, false, true}; }
@@ -295,6 +364,8 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     const size_t z = (size_t)round_up(blocks * q * w_in * (int64_t)w_out * 4, 256);
     w.partial = x > y ? x : y;
     w.partial = w.partial > z ? w.partial : z;
+    const size_t u = pack_bytes(PRODUCT_GWT, dx_shape(n, w_in, w_out, type, q), false, true), v = pack_bytes(PRODUCT_XTG, dw_shape(n, w_in, w_out, type, q), true, false);
+    w.room = u > v ? u : v;
     return w;
 }
 
@@ -333,10 +404,12 @@ int check_workspace(const char *what, const void *ws, size_t ws_bytes, size_t ne
     return SLICEGCN_OK;
 }
 
-Operand operand(const slicegcn_matrix &m) { return Operand{static_cast<const char *>(m.data), m.ld}; }
-Operand weights(const void *w, int32_t w_out) { return Operand{static_cast<const char *>(w), w_out}; }
+Operand operand(const slicegcn_matrix &m) { return Operand{static_cast<const char *>(m.data), m.ld, 0}; }
+Operand weights(const void *w, int32_t w_out) { return Operand{static_cast<const char *>(w), w_out, 0}; }
 
 ProductShape fwd_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, bool gated) { return ProductShape{n, w_in, w_out, 1, 1, type, gated, true}; }
+
+size_t fwd_bytes(const ProductShape &s) { return partial_bytes(s) + pack_bytes(PRODUCT_XW, s, true, true); }
 
 // Both backward passes.  q = 2: gated
 struct BwdCall {
@@ -354,10 +427,12 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
     if (int rc = check_workspace(what, ws, ws_bytes, w.bytes(q))) return rc;
     const bool want_x = c.dx.data && d.n > 0, want_w = c.dw[0] || c.dw[1], want_b = c.db[0] || c.db[1], want_r = c.dr.data && d.n > 0;
     char *at = static_cast<char *>(ws);
-    const bool plain = q == 1 && d.act == SLICEGCN_ACT_NONE; // dP is dY itself
+    // without an activation dP is dY itself, or a copy of it where its rows are no whole units and the products gain from that
+    const bool plain = q == 1 && d.act == SLICEGCN_ACT_NONE &&
+                       (on_units(c.dy, d.w_out) || !(worth_packing(dx_shape(d.n, d.w_in, d.w_out, d.type, q)) || worth_packing(dw_shape(d.n, d.w_in, d.w_out, d.type, q))));
     Operand dg[2] = {c.dy, c.dy};
     SlopeArgs s{};
-    s.g = plain ? Operand{nullptr, 0} : c.g;
+    s.g = q == 1 && d.act == SLICEGCN_ACT_NONE ? Operand{nullptr, 0, 0} : c.g;
     s.u = c.u;
     s.d = c.dy;
     s.n = d.n;
@@ -367,8 +442,8 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         s.dg = at;
         s.ldg = s.ldu = w.ld;
         if (q == 2) s.du = at + w.rows;
-        dg[0] = Operand{s.dg, w.ld};
-        dg[1] = Operand{s.du, w.ld};
+        dg[0] = Operand{s.dg, w.ld, 1};
+        dg[1] = Operand{s.du, w.ld, 1};
     }
     if (want_r) {
         s.dr = static_cast<char *>(c.dr.data);
@@ -378,9 +453,10 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
     if (want_b) s.partial = reinterpret_cast<double *>(at);
     at += w.sums;
     float *partial = reinterpret_cast<float *>(at);
+    char *room = at + w.partial;
 
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d.w_out, stream);
-    const Operand dx{static_cast<const char *>(c.dx.data), c.dx.ld};
+    const Operand dx{static_cast<const char *>(c.dx.data), c.dx.ld, 0};
     const unsigned narrow = narrow_blocks(d.n, d.w_in, d.w_out, d.type, q);
     if (narrow && (want_x || want_w) && !want_r && narrow_rows_fit(c.x) && narrow_rows_fit(c.g) && narrow_rows_fit(c.u) && narrow_rows_fit(c.dy) &&
         narrow_rows_fit(dx) && (q == 1 || !want_w || (c.dw[0] && c.dw[1]))) {
@@ -447,8 +523,7 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         a.sets = 1;
         a.out[0] = static_cast<char *>(c.dx.data);
         a.ldo[0] = c.dx.ld;
-        a.partial = partial;
-        if (int rc = launch_product(dx_shape(d.n, d.w_in, d.w_out, d.type, q), PRODUCT_GWT, EPI_STORE, a, stream)) return rc;
+        if (int rc = launch_product(dx_shape(d.n, d.w_in, d.w_out, d.type, q), PRODUCT_GWT, EPI_STORE, a, partial, room, stream)) return rc;
     }
     if (want_w) {
         ProductArgs a{};
@@ -465,9 +540,8 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         a.N = d.w_out;
         a.segments = 1;
         a.sets = sets;
-        a.partial = partial;
         // one of the two alone: cut like both, so that the workspace suffices and its bits are the same
-        if (int rc = launch_product(dw_shape(d.n, d.w_in, d.w_out, d.type, q), PRODUCT_XTG, EPI_STORE, a, stream)) return rc;
+        if (int rc = launch_product(dw_shape(d.n, d.w_in, d.w_out, d.type, q), PRODUCT_XTG, EPI_STORE, a, partial, room, stream)) return rc;
     }
     return SLICEGCN_OK;
 }
@@ -480,7 +554,7 @@ using namespace slicegcn;
 extern "C" size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
 {
     if (!sizes_fit(n, w_in, w_out) || !known_type(type) || n == 0) return 0;
-    return partial_bytes(fwd_shape(n, w_in, w_out, type, false));
+    return fwd_bytes(fwd_shape(n, w_in, w_out, type, false));
 }
 
 extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream)
@@ -496,7 +570,7 @@ extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const sliceg
     if (d->n == 0) return SLICEGCN_OK;
     SG_REQUIRE(io->Y.data != io->X.data, SLICEGCN_EINVAL, "%s: Y in the rows of X", what);
     const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, false);
-    if (int rc = check_workspace(what, ws, ws_bytes, partial_bytes(shape))) return rc;
+    if (int rc = check_workspace(what, ws, ws_bytes, fwd_bytes(shape))) return rc;
     ProductArgs a{};
     a.a[0] = operand(io->X);
     a.b[0] = weights(io->W, d->w_out);
@@ -512,9 +586,8 @@ extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const sliceg
     a.ldk[0] = io->P.ld;
     a.residual = (float)d->residual;
     a.act = d->act;
-    a.partial = static_cast<float *>(ws);
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d->w_out, as_stream(stream));
-    return launch_product(shape, PRODUCT_XW, EPI_FORWARD, a, as_stream(stream));
+    return launch_product(shape, PRODUCT_XW, EPI_FORWARD, a, ws, static_cast<char *>(ws) + partial_bytes(shape), as_stream(stream));
 }
 
 extern "C" size_t slicegcn_product_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
@@ -551,7 +624,7 @@ extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *d, const sliceg
 extern "C" size_t slicegcn_gated_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
 {
     if (!sizes_fit(n, w_in, w_out) || !known_type(type) || n == 0) return 0;
-    return partial_bytes(fwd_shape(n, w_in, w_out, type, true));
+    return fwd_bytes(fwd_shape(n, w_in, w_out, type, true));
 }
 
 extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream)
@@ -568,7 +641,7 @@ extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn
     if (d->n == 0) return SLICEGCN_OK;
     SG_REQUIRE(io->H.data != io->X.data, SLICEGCN_EINVAL, "%s: H in the rows of X", what);
     const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, true);
-    if (int rc = check_workspace(what, ws, ws_bytes, partial_bytes(shape))) return rc;
+    if (int rc = check_workspace(what, ws, ws_bytes, fwd_bytes(shape))) return rc;
     ProductArgs a{};
     a.a[0] = operand(io->X);
     a.b[0] = weights(io->Wg, d->w_out);
@@ -586,9 +659,8 @@ extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn
     a.keep[1] = static_cast<char *>(io->U.data);
     a.ldk[1] = io->U.ld;
     a.act = d->act;
-    a.partial = static_cast<float *>(ws);
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d->w_out, as_stream(stream));
-    return launch_product(shape, PRODUCT_XW, EPI_GATED, a, as_stream(stream));
+    return launch_product(shape, PRODUCT_XW, EPI_GATED, a, ws, static_cast<char *>(ws) + partial_bytes(shape), as_stream(stream));
 }
 
 extern "C" size_t slicegcn_gated_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)

@@ -17,6 +17,7 @@ constexpr int LAYOUT_KC = 0, LAYOUT_OC = 1;
 struct Operand {
     const char *p;
     int64_t ld;
+    int32_t padded; // host: rows end with zeros up to whole units of 8 elements, which ld has room for
 };
 
 // What becomes of the sums
@@ -44,7 +45,6 @@ struct ProductArgs {
     int32_t steps_per_split;
     int64_t first;         // first workgroup of this launch
     int32_t shares;        // threads that share the parts of a result out where they are joined
-    int32_t whole;         // whether results come in whole groups of four columns, on words
     int32_t on_words;      // whether buffers can read the operands: product_kernels.h
 };
 

@@ -20,10 +20,11 @@ typedef int int4v __attribute__((ext_vector_type(4)));
 constexpr int DIRECT_THREADS = 512, DIRECT_DEPTH = 4;
 
 // 64 x 16 bytes from the buffer at rsrc, each lane's at its offset and the scalar one, to LDS at `lds` and behind it.  (m0, which holds that address, cannot be named as overwritten; the
-// compiler sets it itself right before instructions that use it, of which these kernels have no others.)
+// compiler sets it itself right before instructions that use it, of which these kernels have no others.  Nor does it look into the block for hazards: m0 is to be written one
+// wait state ahead of the load, and a scalar register that a vector instruction wrote five.)
 __device__ inline void load_to_lds(int4v rsrc, uint32_t offset, uint32_t scalar, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(rsrc), "s"(scalar) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(rsrc), "s"(scalar) : "memory");
 }
 
 template <int COUNT> __device__ inline void wait_loads_and_meet()
@@ -55,11 +56,11 @@ template <int LAYOUT, int R, int THREADS> struct DirectPiece {
         const int64_t here = outer - o0 < R ? outer - o0 : R;
         if (LAYOUT == LAYOUT_KC) {
             base = (uint64_t)op.p + (uint64_t)o0 * line;
-            size = (uint32_t)(here - 1) * line + (uint32_t)K * 2;
+            size = (uint32_t)(here - 1) * line + (uint32_t)(K + 7) / 8 * 16; // whole units: what is behind the last k are zeros
             scalar = (uint32_t)k0 * 2;
         } else {
             base = (uint64_t)op.p + (uint64_t)k0 * line + (uint64_t)o0 * 2;
-            size = (uint32_t)here * 2;
+            size = (uint32_t)(here + 7) / 8 * 16;
             scalar = 0;
         }
 #pragma unroll
@@ -224,7 +225,7 @@ __global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // no load into LDS outlives the workgroup
 
-    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, acc);
+    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, COLS, acc);
 }
 
 template <class T, int LM, int LN, int EPI, bool SPLIT> int launch_direct(ProductArgs &a, hipStream_t stream)

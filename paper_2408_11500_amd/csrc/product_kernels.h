@@ -260,10 +260,10 @@ template <class T> struct TileRows {
         rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p + (m0 * ld + n0) * (int64_t)sizeof(T)), 0, (int)bytes, 0x00020000);
         offset = (uint32_t)row * line + (uint32_t)col * sizeof(T);
     }
-    // `on`: whether the lane has such columns
-    __device__ void load(int i, int col, bool on, float (&v)[4]) const
+    // `there`: columns that the lane has there, of four.  TAIL: it may be one to three of them
+    template <bool TAIL> __device__ void load(int i, int col, int there, float (&v)[4]) const
     {
-        const int at = (int)(on ? offset : NOT_THERE), scalar = (int)(16 * i * line + col * sizeof(T));
+        const int at = (int)(there >= 4 ? offset : NOT_THERE), scalar = (int)(16 * i * line + col * sizeof(T));
         if constexpr (sizeof(T) == 4) {
             const uint4v x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, scalar, 0);
 #pragma unroll
@@ -274,24 +274,44 @@ template <class T> struct TileRows {
 #pragma unroll
             for (int r = 0; r < 4; ++r) v[r] = (float)x[r];
         }
+        if constexpr (TAIL) {
+#pragma unroll
+            for (int r = 0; r < 3; ++r) {
+                const int one = (int)(there < 4 && r < there ? offset + r * sizeof(T) : NOT_THERE);
+                float x;
+                if constexpr (sizeof(T) == 4) x = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, one, scalar, 0));
+                else x = (float)__builtin_bit_cast(T, (short)__builtin_amdgcn_raw_buffer_load_b16(rsrc, one, scalar, 0));
+                v[r] = there < 4 ? x : v[r];
+            }
+        }
     }
-    __device__ void store(int i, int col, bool on, const float (&v)[4]) const
+    template <bool TAIL> __device__ void store(int i, int col, int there, const float (&v)[4]) const
     {
-        const int at = (int)(on ? offset : NOT_THERE), scalar = (int)(16 * i * line + col * sizeof(T));
+        const int at = (int)(there >= 4 ? offset : NOT_THERE), scalar = (int)(16 * i * line + col * sizeof(T));
         typedef T T4 __attribute__((ext_vector_type(4)));
         T4 x;
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = (T)v[r];
-        if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, x), rsrc, at, scalar, 0);
+        // 16 bytes without a scalar offset: with one in a register the compiler lets the next instruction overwrite the stored registers, and the fourth of them has then
+        // been read too late in the last lanes of each row of 16 now and then
+        if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, x), rsrc, there >= 4 ? at + scalar : at, 0, 0);
         else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(uint2v, x), rsrc, at, scalar, 0);
+        if constexpr (TAIL) {
+#pragma unroll
+            for (int r = 0; r < 3; ++r) {
+                const int one = (int)(there < 4 && r < there ? offset + r * sizeof(T) : NOT_THERE);
+                if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v[r]), rsrc, one, scalar, 0);
+                else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, (T)v[r]), rsrc, one, scalar, 0);
+            }
+        }
     }
 };
 
 // A wavefront's sums into results, as finish4 forms them.  Lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of every 16 x 16 results, which begin at row wm and column wn of
-// the tile; GATED: acc[.][j] and acc[.][j + 1] are both products of the same columns.  Where N is a multiple of 4 and rows lie on words (a.whole), a lane has all of its four
-// columns or none, and stores have a scalar address each.  The parts of a row follow one another, so that lines are whole when they leave the L2.
-template <class T, int EPI, bool SPLIT, int BM, int FM, int FN>
-__device__ inline void finish_tile(const ProductArgs &a, int set, int split, int64_t m0, int64_t n0, int wm, int wn, const float4v (&acc)[FM][FN])
+// the tile; GATED: acc[.][j] and acc[.][j + 1] are both products of the same columns.  Stores have a scalar address each, and the parts of a row follow one another, so that
+// lines are whole when they leave the L2.  TAIL: the last tile of columns where N is no multiple of 4.
+template <class T, int EPI, bool SPLIT, bool TAIL, int ACT, int BM, int FM, int FN>
+__device__ inline void finish_with(const ProductArgs &a, int set, int split, int64_t m0, int64_t n0, int wm, int wn, const float4v (&acc)[FM][FN])
 {
     constexpr bool TURNS = EPI == EPI_GATED;
     constexpr int J = TURNS ? 2 : 1, W = TURNS ? 8 : 16;
@@ -302,24 +322,6 @@ __device__ inline void finish_tile(const ProductArgs &a, int set, int split, int
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[r] = acc[i][j][r];
     };
-    if (!a.whole) {
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int64_t at = m0 + row + 16 * i;
-            if (at >= a.M) continue;
-#pragma unroll
-            for (int j = 0; j < FN; j += J) {
-                const int left = cols - (col + W * j) < 4 ? cols - (col + W * j) : 4;
-                if (left <= 0) continue;
-                float s[4], s2[4];
-                sums(i, j, s);
-                sums(i, j + J - 1, s2);
-                if constexpr (SPLIT) store4<float>(reinterpret_cast<char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N), at * a.N + n0 + col + W * j, left, s);
-                else finish4<T, EPI>(a, set, at, n0 + col + W * j, left, s, s2);
-            }
-        }
-        return;
-    }
     if constexpr (SPLIT) {
         const TileRows<float> to(reinterpret_cast<const char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N), a.N, m0, n0, rows, cols, row, col);
 #pragma unroll
@@ -328,7 +330,7 @@ __device__ inline void finish_tile(const ProductArgs &a, int set, int split, int
             for (int j = 0; j < FN; ++j) {
                 float s[4];
                 sums(i, j, s);
-                to.store(i, W * j, col + W * j < cols, s);
+                to.template store<TAIL>(i, W * j, cols - (col + W * j), s);
             }
     } else if constexpr (EPI == EPI_STORE) {
         const TileRows<T> to(a.out[set], a.ldo[set], m0, n0, rows, cols, row, col);
@@ -338,55 +340,70 @@ __device__ inline void finish_tile(const ProductArgs &a, int set, int split, int
             for (int j = 0; j < FN; ++j) {
                 float s[4];
                 sums(i, j, s);
-                to.store(i, W * j, col + W * j < cols, s);
+                to.template store<TAIL>(i, W * j, cols - (col + W * j), s);
             }
     } else {
-        auto with = [&](auto act) {
-            constexpr int ACT = decltype(act)::value;
-            const TileRows<T> to(a.out[0], a.ldo[0], m0, n0, rows, cols, row, col), k0(a.keep[0], a.ldk[0], m0, n0, rows, cols, row, col);
-            const TileRows<T> other(TURNS ? a.keep[1] : a.r.p, TURNS ? a.ldk[1] : a.r.ld, m0, n0, rows, cols, row, col);
-            float bias[FN][4];
+        const TileRows<T> to(a.out[0], a.ldo[0], m0, n0, rows, cols, row, col), k0(a.keep[0], a.ldk[0], m0, n0, rows, cols, row, col);
+        const TileRows<T> other(TURNS ? a.keep[1] : a.r.p, TURNS ? a.ldk[1] : a.r.ld, m0, n0, rows, cols, row, col);
+        float bias[FN][4];
 #pragma unroll
-            for (int j = 0; j < FN; ++j) load_bias(a.bias[TURNS ? j % 2 : 0], n0 + col + W * (j - (TURNS ? j % 2 : 0)), col + W * (j - (TURNS ? j % 2 : 0)) < cols ? 4 : 0, bias[j]);
-#pragma unroll
-            for (int i = 0; i < FM; ++i) {
-#pragma unroll
-                for (int j = 0; j < FN; j += J) {
-                    const bool on = col + W * j < cols;
-                    float s[4], y[4];
-                    sums(i, j, s);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s[r] += bias[j][r];
-                    if (a.keep[0]) k0.store(i, W * j, on, s);
-                    if constexpr (TURNS) {
-                        float u[4];
-                        sums(i, j + 1, u);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            u[r] += bias[j + 1][r];
-                            y[r] = activated<ACT>(s[r]) * u[r];
-                        }
-                        if (a.keep[0]) other.store(i, W * j, on, u);
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) y[r] = activated<ACT>(s[r]);
-                        if (a.r.p) {
-                            float v[4];
-                            other.load(i, W * j, on, v);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) y[r] = fmaf(a.residual, v[r], y[r]);
-                        }
-                    }
-                    to.store(i, W * j, on, y);
-                }
-            }
-        };
-        switch (a.act) {
-        case SLICEGCN_ACT_RELU: with(std::integral_constant<int, SLICEGCN_ACT_RELU>()); break;
-        case SLICEGCN_ACT_SILU: with(std::integral_constant<int, SLICEGCN_ACT_SILU>()); break;
-        case SLICEGCN_ACT_GELU: with(std::integral_constant<int, SLICEGCN_ACT_GELU>()); break;
-        default: with(std::integral_constant<int, SLICEGCN_ACT_NONE>());
+        for (int j = 0; j < FN; ++j) {
+            const int at = col + W * (TURNS ? j - j % 2 : j);
+            load_bias(a.bias[TURNS ? j % 2 : 0], n0 + at, cols - at, bias[j]);
         }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+#pragma unroll
+            for (int j = 0; j < FN; j += J) {
+                const int there = cols - (col + W * j);
+                float s[4], y[4];
+                sums(i, j, s);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[r] += bias[j][r];
+                if (a.keep[0]) k0.template store<TAIL>(i, W * j, there, s);
+                if constexpr (TURNS) {
+                    float u[4];
+                    sums(i, j + 1, u);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        u[r] += bias[j + 1][r];
+                        y[r] = activated<ACT>(s[r]) * u[r];
+                    }
+                    if (a.keep[0]) other.template store<TAIL>(i, W * j, there, u);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[r] = activated<ACT>(s[r]);
+                    if (a.r.p) {
+                        float v[4];
+                        other.template load<TAIL>(i, W * j, there, v);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) y[r] = fmaf(a.residual, v[r], y[r]);
+                    }
+                }
+                to.template store<TAIL>(i, W * j, there, y);
+            }
+        }
+    }
+}
+
+template <class T, int EPI, bool SPLIT, int BM, int FM, int FN>
+__device__ inline void finish_tile(const ProductArgs &a, int set, int split, int64_t m0, int64_t n0, int wm, int wn, int tile_cols, const float4v (&acc)[FM][FN])
+{
+    const bool tail = a.N % 4 != 0 && n0 + tile_cols > a.N;
+    auto with = [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+        if (tail) finish_with<T, EPI, SPLIT, true, ACT, BM>(a, set, split, m0, n0, wm, wn, acc);
+        else finish_with<T, EPI, SPLIT, false, ACT, BM>(a, set, split, m0, n0, wm, wn, acc);
+    };
+    if (SPLIT || EPI == EPI_STORE) {
+        with(std::integral_constant<int, SLICEGCN_ACT_NONE>());
+        return;
+    }
+    switch (a.act) {
+    case SLICEGCN_ACT_RELU: with(std::integral_constant<int, SLICEGCN_ACT_RELU>()); break;
+    case SLICEGCN_ACT_SILU: with(std::integral_constant<int, SLICEGCN_ACT_SILU>()); break;
+    case SLICEGCN_ACT_GELU: with(std::integral_constant<int, SLICEGCN_ACT_GELU>()); break;
+    default: with(std::integral_constant<int, SLICEGCN_ACT_NONE>());
     }
 }
 
@@ -462,7 +479,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
         }
     }
 
-    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, acc);
+    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, COLS, acc);
 }
 
 // The sums of all parts of k, in fp64: four columns a thread, and a.shares threads of a workgroup share the parts out (part s, s + shares, ... each), whose sums
@@ -698,7 +715,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const P
         for (int i = 0; i < SETS; ++i) step(regs[i], t + i);
     }
 
-    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, acc);
+    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, COLS, acc);
 }
 
 template <class T, int LM, int LN, int EPI, int TILE, bool SPLIT> int launch_tile(ProductArgs &a, hipStream_t stream)

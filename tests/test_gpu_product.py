@@ -364,3 +364,48 @@ def test_narrow_backward_passes_of_many_rows(size, kind, gated):
     for k in keys:
         assert_within(general[k], *want[k], k)
     assert_padding(buf, wi)
+
+
+# rows that are no whole units of 16 bytes, where the operands are copied: odd widths, even ones, one of the two
+COPIED = [(2050, 1003, 1021), (1500, 1026, 1401), (2100, 1016, 1001), (3000, 701, 1024), (140, 4001, 4103)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("size", COPIED, ids=str)
+@pytest.mark.parametrize("ld", ["dense", "lines", "odd"])
+def test_large_products_of_rows_that_lie_oddly(size, ld, kind):
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(sum(size))
+    x, x64 = rows(gen, n, wi, dtype, lds(n, wi, ld))
+    (wg, wg64), (wu, wu64) = weights(gen, wi, wo, dtype), weights(gen, wi, wo, dtype)
+    g, g64 = rows(gen, n, wo, dtype, lds(n, wo, ld))
+    u, u64 = rows(gen, n, wo, dtype, lds(n, wo, ld))
+    d, d64 = rows(gen, n, wo, dtype, lds(n, wo, ld))
+    for name in ("none", "silu"):
+        y, ybuf = result(n, wo, dtype, lds(n, wo, ld))
+        B.slicegcn_product_fwd(x, wg, y, workspace(B.slicegcn_product_fwd_workspace_bytes(n, wi, wo, dtype)), R=u, act=ACT[name])
+        assert_within(y, *product_fwd(x64, wg64, None, u64, 1.0, name, dtype)["Y"], "Y")
+        assert_padding(ybuf, wo)
+        dx, dxbuf = result(n, wi, dtype, lds(n, wi, ld))
+        dw, db = torch.full_like(wg, 777.0), torch.full((wo,), 777.0, device="cuda")
+        B.slicegcn_product_bwd(x, wg, g, d, workspace(B.slicegcn_product_bwd_workspace_bytes(n, wi, wo, dtype)), dX=dx, dW=dw, db=db, act=ACT[name])
+        want = product_bwd(x64, wg64, g64, d64, 1.0, name, dtype)
+        for got, key in ((dx, "dX"), (dw, "dW"), (db, "db")):
+            assert_within(got, *want[key], key)
+        assert_padding(dxbuf, wi)
+    h, hbuf = result(n, wo, dtype, lds(n, wo, ld))
+    B.slicegcn_gated_fwd(x, wg, wu, h, workspace(B.slicegcn_gated_fwd_workspace_bytes(n, wi, wo, dtype)))
+    assert_within(h, *gated_fwd(x64, wg64, wu64, None, None, "silu", dtype)["H"], "H")
+    assert_padding(hbuf, wo)
+    dx, dxbuf = result(n, wi, dtype, lds(n, wi, ld))
+    dwg, dwu = torch.full_like(wg, 777.0), torch.full_like(wu, 777.0)
+    ws = workspace(B.slicegcn_gated_bwd_workspace_bytes(n, wi, wo, dtype))
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, d, ws, dX=dx, dWg=dwg, dWu=dwu)
+    want = gated_bwd(x64, wg64, wu64, g64, u64, d64, "silu", dtype)
+    for got, key in ((dx, "dX"), (dwg, "dWg"), (dwu, "dWu")):
+        assert_within(got, *want[key], key)
+    assert_padding(dxbuf, wi)
+    alone = torch.full_like(wu, 777.0)
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, d, ws, dWu=alone)
+    assert torch.equal(alone, dwu)
