@@ -53,6 +53,29 @@ ProductPlan plan_product(const ProductShape &s, bool aligned)
 
 namespace {
 
+// Whether the products of a backward pass of these sizes share a launch, by the multiplications in both; and how each is cut then.
+// 2048 rows 64 -> 170 gated fp32:
+constexpr int64_t PAIR_MOST = (int64_t)1 << 28;
+constexpr int64_t PAIR_RESULTS = (int64_t)1 << 20; // elements of dX and of dW, which all go through memory as sums of parts
+bool paired(int64_t n, int32_t w_in, int32_t w_out, int q)
+{
+    return n > 0 && (double)n * (double)w_in * (double)w_out * q <= (double)PAIR_MOST && n * w_in <= PAIR_RESULTS && (int64_t)w_in * w_out * q <= PAIR_RESULTS;
+}
+ProductPlan pair_plan(const ProductShape &s)
+{
+    ProductPlan p{};
+    const int64_t tiles = (s.M + PAIR_TILE - 1) / PAIR_TILE * ((s.N + PAIR_TILE - 1) / PAIR_TILE) * s.sets;
+    const int64_t bk = step_k(s.type), steps = (s.K + bk - 1) / bk * s.segments, one = s.sets * s.M * s.N * 4;
+    int64_t splits = CUS / tiles;
+    if (splits > steps / 2) splits = steps / 2;
+    if (splits < (steps + CHAIN - 1) / CHAIN) splits = (steps + CHAIN - 1) / CHAIN;
+    if (splits < 1) splits = 1;
+    p.steps_per_split = (int32_t)((steps + splits - 1) / splits);
+    p.splits = (int32_t)((steps + p.steps_per_split - 1) / p.steps_per_split);
+    p.bytes = (size_t)round_up(p.splits * one, 256);
+    return p;
+}
+
 // What a call may need, however its operands lie
 size_t partial_bytes(const ProductShape &s)
 {
@@ -293,24 +316,18 @@ template <class T, bool GATED, int ACT> __global__ __launch_bounds__(256) void s
         }
 }
 
-// db[q][j] = sum over the parts: 16 columns and 64 shares of the parts a workgroup, the shares added in order
-__global__ __launch_bounds__(1024) void bias_kernel(const double *__restrict__ partial, int32_t parts, int32_t q_count, int32_t w, float *__restrict__ db0,
-                                                    float *__restrict__ db1)
+__global__ __launch_bounds__(1024) void bias_kernel(const BiasSums b)
 {
-    __shared__ double sums[64][17];
-    const int lane = threadIdx.x % 16, share = threadIdx.x / 16, q = blockIdx.y;
-    const int64_t col = (int64_t)blockIdx.x * 16 + lane;
-    double t = 0.0;
-    if (col < w) {
-#pragma unroll 4
-        for (int32_t p = share; p < parts; p += 64) t += partial[((int64_t)p * q_count + q) * w + col];
-    }
-    sums[share][lane] = t;
-    __syncthreads();
-    float *db = q ? db1 : db0;
-    if (share != 0 || col >= w || !db) return;
-    for (int s = 1; s < 64; ++s) t += sums[s][lane];
-    db[col] = (float)t;
+    __shared__ double sums[1024 + 1024 / BIAS_COLS];
+    bias_sums<1024>(b, blockIdx.x, sums);
+}
+
+int launch_bias(const BiasSums &b, hipStream_t stream)
+{
+    if (!b.partial) return SLICEGCN_OK;
+    bias_kernel<<<(unsigned)bias_workgroups(b), 1024, 0, stream>>>(b);
+    SG_LAUNCH_CHECK();
+    return SLICEGCN_OK;
 }
 
 struct SlopeGrid {
@@ -364,6 +381,10 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     const size_t z = (size_t)round_up(blocks * q * w_in * (int64_t)w_out * 4, 256);
     w.partial = x > y ? x : y;
     w.partial = w.partial > z ? w.partial : z;
+    if (paired(n, w_in, w_out, q)) {
+        const size_t both = pair_plan(dx_shape(n, w_in, w_out, type, q)).bytes + pair_plan(dw_shape(n, w_in, w_out, type, q)).bytes;
+        w.partial = w.partial > both ? w.partial : both;
+    }
     const size_t u = pack_bytes(PRODUCT_GWT, dx_shape(n, w_in, w_out, type, q), false, true), v = pack_bytes(PRODUCT_XTG, dw_shape(n, w_in, w_out, type, q), true, false);
     w.room = u > v ? u : v;
     return w;
@@ -487,12 +508,9 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         join.partial = partial;
         const auto launch = d.type == SLICEGCN_BF16 ? launch_narrow_bf16 : launch_narrow_f16;
         if (int rc = launch(a, join, d.act, q == 2, narrow, stream)) return rc;
-        if (want_b) {
-            bias_kernel<<<dim3((d.w_out + 15) / 16, q), 1024, 0, stream>>>(s.partial, (int32_t)narrow, q, d.w_out, c.db[0], c.db[1]);
-            SG_LAUNCH_CHECK();
-        }
-        return SLICEGCN_OK;
+        return launch_bias(BiasSums{s.partial, (int32_t)narrow, q, d.w_out, {c.db[0], c.db[1]}}, stream);
     }
+    BiasSums bias{};
     if (s.dg || s.dr || s.partial) {
         const SlopeGrid g = slope_grid(d.n, d.w_out, d.type);
         s.lanes = g.lanes;
@@ -505,44 +523,53 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
             });
         });
         SG_LAUNCH_CHECK();
-        if (want_b) {
-            bias_kernel<<<dim3((d.w_out + 15) / 16, q), 1024, 0, stream>>>(s.partial, (int32_t)g.parts, q, d.w_out, c.db[0], c.db[1]);
-            SG_LAUNCH_CHECK();
-        }
+        bias = BiasSums{s.partial, (int32_t)g.parts, q, d.w_out, {c.db[0], c.db[1]}};
     }
+    const ProductShape shape_x = dx_shape(d.n, d.w_in, d.w_out, d.type, q), shape_w = dw_shape(d.n, d.w_in, d.w_out, d.type, q);
+    ProductArgs x{}, y{};
     if (want_x) {
-        ProductArgs a{};
         for (int i = 0; i < q; ++i) {
-            a.a[i] = dg[i];
-            a.b[i] = c.w[i];
+            x.a[i] = dg[i];
+            x.b[i] = c.w[i];
         }
-        a.M = d.n;
-        a.K = d.w_out;
-        a.N = d.w_in;
-        a.segments = q;
-        a.sets = 1;
-        a.out[0] = static_cast<char *>(c.dx.data);
-        a.ldo[0] = c.dx.ld;
-        if (int rc = launch_product(dx_shape(d.n, d.w_in, d.w_out, d.type, q), PRODUCT_GWT, EPI_STORE, a, partial, room, stream)) return rc;
+        x.M = d.n;
+        x.K = d.w_out;
+        x.N = d.w_in;
+        x.segments = q;
+        x.sets = 1;
+        x.out[0] = static_cast<char *>(c.dx.data);
+        x.ldo[0] = c.dx.ld;
     }
     if (want_w) {
-        ProductArgs a{};
-        int sets = 0;
         for (int i = 0; i < q; ++i) {
             if (!c.dw[i]) continue;
-            a.a[sets] = c.x;
-            a.b[sets] = dg[i];
-            a.out[sets] = static_cast<char *>(c.dw[i]);
-            a.ldo[sets++] = d.w_out;
+            y.a[y.sets] = c.x;
+            y.b[y.sets] = dg[i];
+            y.out[y.sets] = static_cast<char *>(c.dw[i]);
+            y.ldo[y.sets++] = d.w_out;
         }
-        a.M = d.w_in;
-        a.K = d.n;
-        a.N = d.w_out;
-        a.segments = 1;
-        a.sets = sets;
-        // one of the two alone: cut like both, so that the workspace suffices and its bits are the same
-        if (int rc = launch_product(dw_shape(d.n, d.w_in, d.w_out, d.type, q), PRODUCT_XTG, EPI_STORE, a, partial, room, stream)) return rc;
+        y.M = d.w_in;
+        y.K = d.n;
+        y.N = d.w_out;
+        y.segments = 1;
     }
+    // one of two dW alone is cut like both, so that the workspace suffices and its bits are the same
+    if (paired(d.n, d.w_in, d.w_out, q) && (!want_x || product_on_words(PRODUCT_GWT, shape_x, x)) && (!want_w || product_on_words(PRODUCT_XTG, shape_w, y))) {
+        const ProductPlan px = pair_plan(shape_x), pw = pair_plan(shape_w);
+        x.splits = px.splits;
+        x.steps_per_split = px.steps_per_split;
+        x.partial = partial;
+        y.splits = pw.splits;
+        y.steps_per_split = pw.steps_per_split;
+        y.partial = partial + px.bytes / 4;
+        const auto launch = d.type == SLICEGCN_F32 ? launch_pair_f32 : d.type == SLICEGCN_BF16 ? launch_pair_bf16 : launch_pair_f16;
+        return launch(want_x ? &x : nullptr, want_w ? &y : nullptr, bias, stream);
+    }
+    if (int rc = launch_bias(bias, stream)) return rc;
+    if (want_x)
+        if (int rc = launch_product(shape_x, PRODUCT_GWT, EPI_STORE, x, partial, room, stream)) return rc;
+    if (want_w)
+        if (int rc = launch_product(shape_w, PRODUCT_XTG, EPI_STORE, y, partial, room, stream)) return rc;
     return SLICEGCN_OK;
 }
 

@@ -70,6 +70,39 @@ int launch_product_f32(int layouts, int epilogue, const ProductPlan &plan, Produ
 int launch_product_bf16(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream);
 int launch_product_f16(int layouts, int epilogue, const ProductPlan &plan, ProductArgs &a, hipStream_t stream);
 
+// Column sums of parts of the rows, [part][q][w] in fp64, on their way into fp32 gradients of one or two biases
+struct BiasSums {
+    const double *partial; // NULL: none are wanted
+    int32_t parts, q, w;
+    float *db[2];
+};
+constexpr int BIAS_COLS = 16; // columns of a workgroup
+inline int64_t bias_workgroups(const BiasSums &b) { return b.partial ? (int64_t)((b.w + BIAS_COLS - 1) / BIAS_COLS) * b.q : 0; }
+
+// 16 columns of one bias; the threads of a column share the parts out, and their sums are added in order.  sums: THREADS + THREADS / 16 of them
+template <int THREADS> __device__ inline void bias_sums(const BiasSums &b, unsigned block, double *sums)
+{
+    constexpr int SHARES = THREADS / BIAS_COLS;
+    const int lane = threadIdx.x % BIAS_COLS, share = threadIdx.x / BIAS_COLS, q = (int)(block % b.q);
+    const int64_t col = (int64_t)(block / b.q) * BIAS_COLS + lane;
+    double t = 0.0;
+    if (col < b.w) {
+#pragma unroll 4
+        for (int32_t p = share; p < b.parts; p += SHARES) t += b.partial[((int64_t)p * b.q + q) * b.w + col];
+    }
+    sums[share * (BIAS_COLS + 1) + lane] = t;
+    __syncthreads();
+    if (share != 0 || col >= b.w || !b.db[q]) return;
+    for (int s = 1; s < SHARES; ++s) t += sums[s * (BIAS_COLS + 1) + lane];
+    b.db[q][col] = (float)t;
+}
+
+// Backward passes of which both products take one launch: tiles of 64 x 64 through registers
+constexpr int PAIR_TILE = 64;
+int launch_pair_f32(ProductArgs *x, ProductArgs *w, const BiasSums &bias, hipStream_t stream);
+int launch_pair_bf16(ProductArgs *x, ProductArgs *w, const BiasSums &bias, hipStream_t stream);
+int launch_pair_f16(ProductArgs *x, ProductArgs *w, const BiasSums &bias, hipStream_t stream);
+
 // product_narrow.h: a backward pass in one sweep over the rows
 constexpr int NARROW_WIDTH_IN = 128, NARROW_WIDTH_OUT = 256; // at most; of all products together
 constexpr int NARROW_RUN = 32;                               // blocks of rows whose column sums a thread adds in fp32

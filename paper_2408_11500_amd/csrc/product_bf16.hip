@@ -15,4 +15,6 @@ int launch_narrow_bf16(const NarrowArgs &a, ProductArgs &join, int act, bool gat
     return a.want_w ? launch_join<bf16, EPI_STORE>(join, stream) : SLICEGCN_OK;
 }
 
+int launch_pair_bf16(ProductArgs *x, ProductArgs *w, const BiasSums &bias, hipStream_t stream) { return launch_pair<bf16>(x, w, bias, stream); }
+
 } // namespace slicegcn

@@ -15,4 +15,6 @@ int launch_narrow_f16(const NarrowArgs &a, ProductArgs &join, int act, bool gate
     return a.want_w ? launch_join<f16, EPI_STORE>(join, stream) : SLICEGCN_OK;
 }
 
+int launch_pair_f16(ProductArgs *x, ProductArgs *w, const BiasSums &bias, hipStream_t stream) { return launch_pair<f16>(x, w, bias, stream); }
+
 } // namespace slicegcn

@@ -8,4 +8,6 @@ int launch_product_f32(int layouts, int epilogue, const ProductPlan &plan, Produ
     return launch_product<float>(layouts, epilogue, plan, a, stream);
 }
 
+int launch_pair_f32(ProductArgs *x, ProductArgs *w, const BiasSums &bias, hipStream_t stream) { return launch_pair<float>(x, w, bias, stream); }
+
 } // namespace slicegcn

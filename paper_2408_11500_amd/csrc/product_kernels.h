@@ -484,12 +484,12 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
 
 // The sums of all parts of k, in fp64: four columns a thread, and a.shares threads of a workgroup share the parts out (part s, s + shares, ... each), whose sums
 // are added in order.  GATED: the parts of the second product are those of set 1.  256 parts of 100 x 256 with one share 84 us.
-template <class T, int EPI> __global__ __launch_bounds__(256) void product_join_kernel(const ProductArgs a)
+template <int EPI> constexpr int JOIN_SUMS = (EPI == EPI_GATED ? 2 : 1) * 4 + 1;
+template <class T, int EPI> __device__ inline void join_parts(const ProductArgs &a, int64_t block, double *sums)
 {
-    constexpr int Q = EPI == EPI_GATED ? 2 : 1;
-    __shared__ double sums[256][Q * 4 + 1];
+    constexpr int Q = EPI == EPI_GATED ? 2 : 1, EACH = JOIN_SUMS<EPI>;
     const int here = 256 / a.shares, share = threadIdx.x / here;
-    const int64_t per_row = (a.N + 3) / 4, each = per_row * a.M, at = (a.first + blockIdx.x) * here + threadIdx.x % here;
+    const int64_t per_row = (a.N + 3) / 4, each = per_row * a.M, at = block * here + threadIdx.x % here;
     const bool there = at < each * (EPI == EPI_STORE ? a.sets : 1);
     const int set = there ? (int)(at / each) : 0;
     const int64_t row = there ? (at - set * each) / per_row : 0, col = there ? (at - set * each) % per_row * 4 : 0;
@@ -511,14 +511,14 @@ template <class T, int EPI> __global__ __launch_bounds__(256) void product_join_
 #pragma unroll
         for (int q = 0; q < Q; ++q)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sums[threadIdx.x][q * 4 + r] = sum[q][r];
+            for (int r = 0; r < 4; ++r) sums[threadIdx.x * EACH + q * 4 + r] = sum[q][r];
         __syncthreads();
         if (share > 0) return;
         for (int i = 1; i < a.shares; ++i)
 #pragma unroll
             for (int q = 0; q < Q; ++q)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum[q][r] += sums[i * here + threadIdx.x][q * 4 + r];
+                for (int r = 0; r < 4; ++r) sum[q][r] += sums[(i * here + threadIdx.x) * EACH + q * 4 + r];
     }
     if (!there) return;
     float s[2][4];
@@ -530,11 +530,23 @@ template <class T, int EPI> __global__ __launch_bounds__(256) void product_join_
     finish4<T, EPI>(a, set, row, col, left, s[0], s[1]);
 }
 
-template <class T, int EPI> int launch_join(ProductArgs &a, hipStream_t stream)
+template <class T, int EPI> __global__ __launch_bounds__(256) void product_join_kernel(const ProductArgs a)
+{
+    __shared__ double sums[256 * JOIN_SUMS<EPI>];
+    join_parts<T, EPI>(a, a.first + blockIdx.x, sums);
+}
+
+// How many threads share the parts out: about four parts each
+inline int join_shares(ProductArgs &a)
 {
     a.shares = 1;
     while (a.shares < 32 && a.shares * 4 <= a.splits) a.shares *= 2;
-    const int64_t here = 256 / a.shares, threads = (a.N + 3) / 4 * a.M * (EPI == EPI_STORE ? a.sets : 1);
+    return a.shares;
+}
+
+template <class T, int EPI> int launch_join(ProductArgs &a, hipStream_t stream)
+{
+    const int64_t here = 256 / join_shares(a), threads = (a.N + 3) / 4 * a.M * (EPI == EPI_STORE ? a.sets : 1);
     return launch_parts((threads + here - 1) / here, [&](unsigned first, unsigned count) {
         a.first = first;
         product_join_kernel<T, EPI><<<count, 256, 0, stream>>>(a);
@@ -618,9 +630,13 @@ template <class T, int LAYOUT, int R, int BK, int THREADS> struct BufferPiece {
     }
 };
 
-// product_kernel for such operands: two steps on their way in registers, one in LDS
+// LDS of product_buffer_tile, in units
+template <class T, int BM, int BN> constexpr int buffer_units = Planes<T>::count * (BM + BN) * (sizeof(T) == 4 ? STEP_K_F32 : STEP_K_16) / 8;
+
+// A tile of results of such operands, by workgroup `block` of a product: SETS steps on their way in registers, one in LDS.  (fp32: with two on their way 233 k rows 602 -> 256
+// take 500 us, with one 452; with three workgroups a CU instead of two 484.)
 template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT>
-__global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const ProductArgs a)
+__device__ inline void product_buffer_tile(const ProductArgs &a, int64_t block, short8 *lds)
 {
     constexpr int SETS = sizeof(T) == 4 ? 1 : 2;
     constexpr int P = Planes<T>::count, BK = P == 3 ? STEP_K_F32 : STEP_K_16, THREADS = 64 * WM * WN;
@@ -630,11 +646,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const P
     static_assert(!TURNS || FN % 2 == 0, "a wavefront holds both products of its columns");
     typedef BufferPiece<T, LM, BM, BK, THREADS> PieceM;
     typedef BufferPiece<T, LN, COLS, BK, THREADS> PieceN;
-    __shared__ short8 lds[P * (PieceM::UNITS + PIECES * PieceN::UNITS)];
+    static_assert(P * (PieceM::UNITS + PIECES * PieceN::UNITS) == buffer_units<T, BM, BN>, "LDS of a step");
     short8 *lds_m = lds, *lds_n = lds + P * PieceM::UNITS;
 
     const int64_t tile_rows = (a.M + BM - 1) / BM, tile_cols = (a.N + COLS - 1) / COLS, tiles = tile_rows * tile_cols;
-    int64_t id = tile_of(a.first + blockIdx.x, tiles * a.splits * a.sets), row_tile, col_tile;
+    int64_t id = tile_of(block, tiles * a.splits * a.sets), row_tile, col_tile;
     const int set = a.sets > 1 ? (int)(id / (tiles * a.splits)) : 0;
     id -= set * (tiles * a.splits);
     const int split = SPLIT ? (int)(id / tiles) : 0;
@@ -716,6 +732,57 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const P
     }
 
     finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, COLS, acc);
+}
+
+// product_kernel for such operands
+template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const ProductArgs a)
+{
+    __shared__ short8 lds[buffer_units<T, BM, BN>];
+    product_buffer_tile<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT>(a, a.first + blockIdx.x, lds);
+}
+
+// Both products of a backward pass in one launch, where they are short and launches would take longer than they: dX by the first workgroups, dW by the others, all as sums of
+// parts of k.
+template <class T> __global__ __launch_bounds__(256, 2) void product_pair_kernel(const ProductArgs x, const ProductArgs w, unsigned blocks_x)
+{
+    __shared__ short8 lds[buffer_units<T, PAIR_TILE, PAIR_TILE>];
+    if (blockIdx.x < blocks_x) product_buffer_tile<T, LAYOUT_KC, LAYOUT_KC, EPI_STORE, PAIR_TILE, PAIR_TILE, 2, 2, true>(x, blockIdx.x, lds);
+    else product_buffer_tile<T, LAYOUT_OC, LAYOUT_OC, EPI_STORE, PAIR_TILE, PAIR_TILE, 2, 2, true>(w, blockIdx.x - blocks_x, lds);
+}
+
+// What is left of it: the parts of dX and of dW joined, and the column sums' parts
+template <class T>
+__global__ __launch_bounds__(256) void product_pair_join_kernel(const ProductArgs x, const ProductArgs w, const BiasSums bias, unsigned blocks_x, unsigned blocks_w)
+{
+    __shared__ double sums[256 * JOIN_SUMS<EPI_STORE>];
+    if (blockIdx.x < blocks_x) join_parts<T, EPI_STORE>(x, blockIdx.x, sums);
+    else if (blockIdx.x < blocks_x + blocks_w) join_parts<T, EPI_STORE>(w, blockIdx.x - blocks_x, sums);
+    else bias_sums<256>(bias, blockIdx.x - blocks_x - blocks_w, sums);
+}
+
+template <class T> int launch_pair(ProductArgs *x, ProductArgs *w, const BiasSums &bias, hipStream_t stream)
+{
+    auto tiles = [](const ProductArgs *a) {
+        return a ? (a->M + PAIR_TILE - 1) / PAIR_TILE * ((a->N + PAIR_TILE - 1) / PAIR_TILE) * a->splits * a->sets : 0;
+    };
+    auto joins = [](ProductArgs *a) -> int64_t {
+        if (!a) return 0;
+        const int64_t here = 256 / join_shares(*a), threads = (a->N + 3) / 4 * a->M * a->sets;
+        return (threads + here - 1) / here;
+    };
+    const ProductArgs none{};
+    const int64_t x_tiles = tiles(x), w_tiles = tiles(w), x_joins = joins(x), w_joins = joins(w), bias_blocks = bias_workgroups(bias);
+    if (x_tiles + w_tiles > 0) {
+        product_pair_kernel<T><<<(unsigned)(x_tiles + w_tiles), 256, 0, stream>>>(x ? *x : none, w ? *w : none, (unsigned)x_tiles);
+        SG_LAUNCH_CHECK();
+    }
+    if (x_joins + w_joins + bias_blocks > 0) {
+        product_pair_join_kernel<T><<<(unsigned)(x_joins + w_joins + bias_blocks), 256, 0, stream>>>(x ? *x : none, w ? *w : none, bias, (unsigned)x_joins,
+                                                                                                     (unsigned)w_joins);
+        SG_LAUNCH_CHECK();
+    }
+    return SLICEGCN_OK;
 }
 
 template <class T, int LM, int LN, int EPI, int TILE, bool SPLIT> int launch_tile(ProductArgs &a, hipStream_t stream)
