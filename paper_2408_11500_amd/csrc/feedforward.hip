@@ -271,7 +271,7 @@ template <class T, bool GATED, int ACT> __global__ __launch_bounds__(256) void s
                 for (int i = 0; i < V; ++i) {
                     float y = 0.f, slope = 1.f;
                     if (SLOPES) activated_slope<ACT>(g[r][i], y, slope);
-                    o[0][i] = GATED ? d[r][i] * u[r][i] * slope : d[r][i] * slope;
+                    o[0][i] = through_slope<ACT>(GATED ? d[r][i] * u[r][i] : d[r][i], SLOPES ? g[r][i] : 0.f, slope);
                     if (GATED) o[Q - 1][i] = d[r][i] * y;
                 }
                 if (a.dg) write(a.dg, a.ldg, row, o[0], true);

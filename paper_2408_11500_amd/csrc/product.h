@@ -190,6 +190,12 @@ template <int ACT> __device__ inline void activated_slope(float v, float &y, flo
     }
 }
 
+// d act'(v).  Where a relu is flat, whatever d is
+template <int ACT> __device__ inline float through_slope(float d, float v, float slope)
+{
+    return ACT == SLICEGCN_ACT_RELU ? (v > 0.f ? d : 0.f) : d * slope;
+}
+
 // f(std::integral_constant) with the activation as a constant
 template <class F> inline auto with_act(int act, F f)
 {

@@ -39,7 +39,7 @@ template <int COUNT> __device__ inline void wait_loads_and_meet()
 template <int LAYOUT, int R, int THREADS> struct DirectPiece {
     static constexpr int UNITS = R * DIRECT_K / 8, LOADS = UNITS / THREADS;
     static_assert(UNITS % THREADS == 0, "units are dealt evenly");
-    static constexpr uint32_t NOWHERE = 0xfffffff8u; // beyond any buffer
+    static constexpr uint32_t NOWHERE = 0xffffff00u; // beyond any buffer, with all words of an access
     uint32_t offset[LOADS];
     uint64_t base;
     uint32_t line, size, scalar; // bytes: of a line; KC: of the buffer, OC: of a line's part; KC: the step's offset

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(NARROW_THREADS, 2) void product_narrow_kernel(const
     constexpr int Q = GATED ? 2 : 1, EACH = GATED ? 1 : 2; // pieces of the gradients; units of a piece and block that a thread forms
     constexpr int PIECE = NARROW_G / Q;                    // units
     constexpr bool SLOPES = GATED || ACT != SLICEGCN_ACT_NONE;
-    constexpr uint32_t NOWHERE = 0xfffffff0u;
+    constexpr uint32_t NOWHERE = 0xffffff00u; // beyond any buffer
     __shared__ short8 tile_g[2][NARROW_ROWS * NARROW_G], tile_x[2][NARROW_ROWS * NARROW_X];
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
 
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(NARROW_THREADS, 2) void product_narrow_kernel(const
             for (int j = 0; j < 8; ++j) {
                 float y = 0.f, slope = 1.f, v[Q];
                 if (SLOPES) activated_slope<ACT>((float)g[j], y, slope);
-                v[0] = GATED ? (float)d[j] * (float)u[j] * slope : (float)d[j] * slope;
+                v[0] = through_slope<ACT>(GATED ? (float)d[j] * (float)u[j] : (float)d[j], SLOPES ? (float)g[j] : 0.f, slope);
                 if (GATED) v[Q - 1] = (float)d[j] * y;
 #pragma unroll
                 for (int q = 0; q < Q; ++q) {

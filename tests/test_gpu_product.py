@@ -213,6 +213,31 @@ def test_values_that_are_not_finite_stay_in_their_rows_and_columns(size, kind):
     assert torch.equal(h2[keep, :wo - 1], h[keep, :wo - 1])
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("size", [(300, 40, 72), (2000, 1100, 136), (16_500, 64, 64)], ids=str)
+def test_what_lies_behind_the_flat_part_of_a_relu_is_not_looked_at(size, kind):
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(7)
+    x, g, d, u = (rows(gen, n, w, dtype)[0] for w in (wi, wo, wo, wo))
+    (wg, _), (wu, _) = weights(gen, wi, wo, dtype), weights(gen, wi, wo, dtype)
+
+    def grads(d, u):
+        dx, dx2 = (torch.empty((n, wi), dtype=dtype, device="cuda") for _ in range(2))
+        dw, dwg, dwu = (torch.empty_like(wg) for _ in range(3))
+        db, dbg = (torch.empty(wo, device="cuda") for _ in range(2))
+        B.slicegcn_product_bwd(x, wg, g, d, workspace(B.slicegcn_product_bwd_workspace_bytes(n, wi, wo, dtype)), dX=dx, dW=dw, db=db, act=B.ACT_RELU)
+        B.slicegcn_gated_bwd(x, wg, wu, g, u, d.nan_to_num(0.0, 0.0, 0.0), workspace(B.slicegcn_gated_bwd_workspace_bytes(n, wi, wo, dtype)), dX=dx2, dWg=dwg,
+                             dWu=dwu, dbg=dbg, act=B.ACT_RELU)
+        return dx, dw, db, dx2, dwg, dwu, dbg
+    flat = g <= 0
+    want = grads(d.masked_fill(flat, 0.0), u.masked_fill(flat, 0.0))
+    d[flat] = float("inf")
+    u[flat] = float("nan")
+    for a, b in zip(grads(d, u), want):
+        assert torch.isfinite(b).all() and torch.equal(a, b)
+
+
 def test_large_and_small_fp32_operands():
     """Values over the whole range of exponents: each product by itself (a sum of one)."""
     gen = torch.Generator().manual_seed(8)
