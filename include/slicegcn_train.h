@@ -187,7 +187,7 @@ int slicegcn_adam_step_scaled(float *param, const float *grad, const float *fact
 #define SLICEGCN_ACT_SILU 2
 #define SLICEGCN_ACT_GELU 3
 typedef struct {
-    int64_t n;    /* at most 2^31 - 1 */
+    int64_t n;    /* at most 2^31 - 2^16 */
     int32_t w_in; /* both widths: at most 2^20 */
     int32_t w_out;
     int32_t type;

@@ -390,7 +390,9 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     return w;
 }
 
-bool sizes_fit(int64_t n, int32_t w_in, int32_t w_out) { return n >= 0 && n <= INT32_MAX && w_in >= 1 && w_out >= 1 && w_in <= 1 << 20 && w_out <= 1 << 20; }
+// The kernels count k in 32 bits, up to some steps behind the last one: n is the k of dW
+constexpr int64_t MOST_ROWS = ((int64_t)1 << 31) - (1 << 16);
+bool sizes_fit(int64_t n, int32_t w_in, int32_t w_out) { return n >= 0 && n <= MOST_ROWS && w_in >= 1 && w_out >= 1 && w_in <= 1 << 20 && w_out <= 1 << 20; }
 
 int check(const char *what, const slicegcn_product_desc *d, const void *io)
 {
