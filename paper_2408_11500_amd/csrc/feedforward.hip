@@ -413,6 +413,17 @@ int check_rows(const char *what, const char *name, const slicegcn_matrix &m, int
     return SLICEGCN_OK;
 }
 
+// Outputs at the address of another operand (of any part of them an output may overlap nothing, but that is the caller's)
+int check_apart(const char *what, std::initializer_list<const void *> outputs, std::initializer_list<const void *> inputs)
+{
+    for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+        if (!*o) continue;
+        for (auto p = o + 1; p != outputs.end(); ++p) SG_REQUIRE(*o != *p, SLICEGCN_EINVAL, "%s: two outputs at one address", what);
+        for (const void *i : inputs) SG_REQUIRE(*o != i, SLICEGCN_EINVAL, "%s: an output at the address of an input", what);
+    }
+    return SLICEGCN_OK;
+}
+
 int check_params(const char *what, int32_t type, std::initializer_list<const void *> weights, std::initializer_list<const float *> biases)
 {
     for (const void *w : weights) SG_REQUIRE(!w || aligned_for(w, type), SLICEGCN_EINVAL, "%s: misaligned weights", what);
@@ -597,7 +608,9 @@ extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const sliceg
     if (int rc = check_rows(what, "P", io->P, d->w_out, d->type, false)) return rc;
     if (int rc = check_params(what, d->type, {io->W}, {io->b})) return rc;
     if (d->n == 0) return SLICEGCN_OK;
-    SG_REQUIRE(io->Y.data != io->X.data, SLICEGCN_EINVAL, "%s: Y in the rows of X", what);
+    if (int rc = check_apart(what, {io->Y.data, io->P.data}, {io->X.data, io->W, io->b})) return rc;
+    if (int rc = check_apart(what, {io->P.data}, {io->R.data})) return rc;
+    SG_REQUIRE(io->Y.data != io->R.data || io->Y.ld == io->R.ld, SLICEGCN_EINVAL, "%s: Y in the rows of R with another ld", what);
     const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, false);
     if (int rc = check_workspace(what, ws, ws_bytes, fwd_bytes(shape))) return rc;
     ProductArgs a{};
@@ -637,6 +650,8 @@ extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *d, const sliceg
     if (int rc = check_rows(what, "dR", io->dR, d->w_out, d->type, false)) return rc;
     SG_REQUIRE(io->W || !io->dX.data || !rows, SLICEGCN_EINVAL, "%s: NULL W", what);
     if (int rc = check_params(what, d->type, {io->W, io->dW}, {io->db})) return rc;
+    if (rows)
+        if (int rc = check_apart(what, {io->dX.data, io->dW, io->db, io->dR.data}, {io->X.data, io->W, io->P.data, io->dY.data})) return rc;
     BwdCall c{};
     c.d = d;
     c.x = operand(io->X);
@@ -668,7 +683,7 @@ extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn
     SG_REQUIRE(!io->G.data == !io->U.data, SLICEGCN_EINVAL, "%s: G without U, or U without G", what);
     if (int rc = check_params(what, d->type, {io->Wg, io->Wu}, {io->bg, io->bu})) return rc;
     if (d->n == 0) return SLICEGCN_OK;
-    SG_REQUIRE(io->H.data != io->X.data, SLICEGCN_EINVAL, "%s: H in the rows of X", what);
+    if (int rc = check_apart(what, {io->H.data, io->G.data, io->U.data}, {io->X.data, io->Wg, io->Wu, io->bg, io->bu})) return rc;
     const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, true);
     if (int rc = check_workspace(what, ws, ws_bytes, fwd_bytes(shape))) return rc;
     ProductArgs a{};
@@ -710,6 +725,8 @@ extern "C" int slicegcn_gated_bwd(const slicegcn_product_desc *d, const slicegcn
     if (int rc = check_rows(what, "dX", io->dX, d->w_in, d->type, false)) return rc;
     SG_REQUIRE((io->Wg && io->Wu) || !io->dX.data || !rows, SLICEGCN_EINVAL, "%s: NULL Wg or Wu", what);
     if (int rc = check_params(what, d->type, {io->Wg, io->Wu, io->dWg, io->dWu}, {io->dbg, io->dbu})) return rc;
+    if (rows)
+        if (int rc = check_apart(what, {io->dX.data, io->dWg, io->dWu, io->dbg, io->dbu}, {io->X.data, io->Wg, io->Wu, io->G.data, io->U.data, io->dH.data})) return rc;
     BwdCall c{};
     c.d = d;
     c.x = operand(io->X);

@@ -38,7 +38,7 @@ def io(op, ld=8, **given):
 
 GOOD = {("product", "fwd"): dict(X=ONE, W=ONE, Y=2 * ONE), ("product", "bwd"): dict(X=ONE, W=ONE, P=ONE, dY=ONE, dX=2 * ONE, dW=3 * ONE, db=4 * ONE),
         ("gated", "fwd"): dict(X=ONE, Wg=ONE, Wu=ONE, H=2 * ONE),
-        ("gated", "bwd"): dict(X=ONE, Wg=ONE, Wu=ONE, G=ONE, U=ONE, dH=ONE, dX=2 * ONE, dWg=3 * ONE, dWu=3 * ONE)}
+        ("gated", "bwd"): dict(X=ONE, Wg=ONE, Wu=ONE, G=ONE, U=ONE, dH=ONE, dX=2 * ONE, dWg=3 * ONE, dWu=4 * ONE)}
 
 
 def call(L, op, way, d=None, ws=ONE, ws_bytes=1 << 40, raw=None, **changes):  # noqa: F811
@@ -73,6 +73,24 @@ def test_refusals_of_combinations(L):  # noqa: F811
     assert call(L, "product", "fwd", Y=ONE) == B.EINVAL and call(L, "gated", "fwd", H=ONE) == B.EINVAL  # in the rows of X
     assert call(L, "product", "fwd", b=ONE + 2) == B.EINVAL and call(L, "product", "bwd", db=ONE + 1) == B.EINVAL
     assert call(L, "gated", "bwd", dbu=ONE + 1) == B.EINVAL and call(L, "gated", "bwd", dWg=ONE + 1) == B.EINVAL
+
+
+OUTPUTS = {("product", "fwd"): ("Y", "P"), ("product", "bwd"): ("dX", "dW", "db", "dR"), ("gated", "fwd"): ("H", "G", "U"),
+           ("gated", "bwd"): ("dX", "dWg", "dWu", "dbg", "dbu")}
+
+
+@pytest.mark.parametrize("op,way", GOOD)
+def test_refusals_of_outputs_at_the_address_of_another_operand(L, op, way):  # noqa: F811
+    apart = {f: (10 + i) * ONE for i, f in enumerate(FIELDS[op]) if way == "bwd" or f[0] != "d"}
+    if way == "bwd":
+        apart = {f: a for f, a in apart.items() if f not in ("Y", "H", "R", "b", "bg", "bu")}
+    for out in OUTPUTS[op, way]:
+        for other, at in apart.items():
+            if other != out and (out, other) != ("Y", "R"):
+                assert call(L, op, way, d=desc(act=B.ACT_GELU), **{**apart, out: at}) == B.EINVAL, (out, other)
+    if (op, way) == ("product", "fwd"):
+        assert call(L, op, way, d=desc(n=3, w_in=4096, w_out=512), ws_bytes=0, **{**apart, "ld": 4096, "Y": apart["R"]}) == B.EWORKSPACE  # allowed as such
+        assert call(L, op, way, **{**apart, "Y": (apart["R"], 9)}) == B.EINVAL
 
 
 @pytest.mark.parametrize("op,way", GOOD)
