@@ -434,3 +434,109 @@ def test_large_products_of_rows_that_lie_oddly(size, ld, kind):
     alone = torch.full_like(wu, 777.0)
     B.slicegcn_gated_bwd(x, wg, wu, g, u, d, ws, dWu=alone)
     assert torch.equal(alone, dwu)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_rows_of_more_than_4_gb_give_the_bits_of_close_rows(kind):
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(12)
+    n, wi, wo, ld = 70_000, 64, 136, (1 << 15) if dtype != torch.float32 else 1 << 14  # 4.6 GB
+    gaps = [torch.empty((n, ld), dtype=dtype, device="cuda") for _ in range(2)]
+    assert gaps[0].numel() * gaps[0].element_size() > 1 << 32
+    (wg, _), (wu, _) = weights(gen, wi, wo, dtype), weights(gen, wi, wo, dtype)
+    x, g, u, d = (rows(gen, n, w, dtype)[0] for w in (wi, wo, wo, wo))
+
+    def far(t, i, col):
+        v = gaps[i][:, col:col + t.shape[1]]
+        return v.copy_(t)
+    # 8 columns apart, so that rows lie on the boundaries that close ones lie on
+    fx, fg, fu, fd = far(x, 0, 0), far(g, 0, 72), far(u, 0, 216), far(d, 0, 360)
+    empty = lambda i, w, col: gaps[i][:, col:col + w]
+    close = lambda w: torch.empty((n, w), dtype=dtype, device="cuda")
+    h, ks, dx, y = close(wo), [close(wo), close(wo)], close(wi), close(wo)
+    fh, fks, fdx, fy = empty(1, wo, 0), [empty(1, wo, 144), empty(1, wo, 288)], empty(1, wi, 432), empty(1, wo, 504)
+    ws = workspace(max(f(n, wi, wo, dtype) for f in (B.slicegcn_gated_fwd_workspace_bytes, B.slicegcn_gated_bwd_workspace_bytes,
+                                                     B.slicegcn_product_fwd_workspace_bytes, B.slicegcn_product_bwd_workspace_bytes)))
+    dw = [torch.empty_like(wg) for _ in range(6)]
+    B.slicegcn_gated_fwd(x, wg, wu, h, ws, G=ks[0], U=ks[1])
+    B.slicegcn_gated_fwd(fx, wg, wu, fh, ws, G=fks[0], U=fks[1])
+    B.slicegcn_product_fwd(x, wg, y, ws, R=u, act=B.ACT_GELU)
+    B.slicegcn_product_fwd(fx, wg, fy, ws, R=fu, act=B.ACT_GELU)
+    assert torch.equal(h, fh) and torch.equal(ks[0], fks[0]) and torch.equal(ks[1], fks[1]) and torch.equal(y, fy)
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, d, ws, dX=dx, dWg=dw[0], dWu=dw[1])
+    B.slicegcn_gated_bwd(fx, wg, wu, fg, fu, fd, ws, dX=fdx, dWg=dw[2], dWu=dw[3])
+    assert torch.equal(dx, fdx) and torch.equal(dw[0], dw[2]) and torch.equal(dw[1], dw[3])
+    B.slicegcn_product_bwd(x, wg, None, d, ws, dX=dx, dW=dw[4])
+    B.slicegcn_product_bwd(fx, wg, None, fd, ws, dX=fdx, dW=dw[5])
+    assert torch.equal(dx, fdx) and torch.equal(dw[4], dw[5])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_calls_at_the_same_time(kind):
+    """Two streams with a workspace each; what either forms is what it forms alone."""
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(13)
+    n, w, f = 700, 264, 712
+    (wg, _), (wu, _), (wd, _) = weights(gen, w, f, dtype), weights(gen, w, f, dtype), weights(gen, f, w, dtype)
+    calls = []
+    for _ in range(2):
+        x, dy = rows(gen, n, w, dtype)[0], rows(gen, n, w, dtype)[0]
+        e = lambda *s: torch.empty(s, dtype=dtype, device="cuda")
+        ws = workspace(max(fn(n, a, b, dtype) for fn in (B.slicegcn_gated_fwd_workspace_bytes, B.slicegcn_gated_bwd_workspace_bytes,
+                                                         B.slicegcn_product_fwd_workspace_bytes, B.slicegcn_product_bwd_workspace_bytes)
+                           for a, b in ((w, f), (f, w))))
+        calls.append((x, dy, ws, dict(h=e(n, f), g=e(n, f), u=e(n, f), y=e(n, w), dh=e(n, f), dwd=e(f, w), dx=e(n, w), dwg=e(w, f), dwu=e(w, f))))
+
+    def block(x, dy, ws, t):
+        B.slicegcn_gated_fwd(x, wg, wu, t["h"], ws, G=t["g"], U=t["u"])
+        B.slicegcn_product_fwd(t["h"], wd, t["y"], ws, R=x)
+        B.slicegcn_product_bwd(t["h"], wd, None, dy, ws, dX=t["dh"], dW=t["dwd"])
+        B.slicegcn_gated_bwd(x, wg, wu, t["g"], t["u"], t["dh"], ws, dX=t["dx"], dWg=t["dwg"], dWu=t["dwu"])
+    alone = []
+    for c in calls:
+        block(*c)
+        alone.append({k: v.clone() for k, v in c[3].items()})
+    streams = [torch.cuda.Stream() for _ in calls]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for s, c in zip(streams, calls):
+            with torch.cuda.stream(s):
+                block(*c)
+    torch.cuda.synchronize()
+    for c, want in zip(calls, alone):
+        assert all(torch.equal(c[3][k], want[k]) for k in want)
+
+
+# on either side of where both products of a backward pass share a launch: by the multiplications in them, by the elements of dX, by those of dW
+SHORT = [(2048, 512, 128), (2049, 512, 128), (2048, 512, 130), (1030, 1018, 120), (40, 1400, 740), (40, 1400, 760), (1000, 2, 3), (1200, 301, 13)]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("size", SHORT, ids=str)
+@pytest.mark.parametrize("q", [1, 2])
+def test_short_backward_passes(size, q, kind):
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(14)
+    x, x64 = rows(gen, n, wi, dtype)
+    (wg, wg64), (wu, wu64) = weights(gen, wi, wo, dtype), weights(gen, wi, wo, dtype)
+    g, g64 = rows(gen, n, wo, dtype, std=1.5)
+    u, u64 = rows(gen, n, wo, dtype)
+    d, d64 = rows(gen, n, wo, dtype)
+    dx, dxbuf = result(n, wi, dtype, wi + 1)
+    dwg, dwu = torch.full_like(wg, 777.0), torch.full_like(wu, 777.0)
+    db = torch.full((wo,), 777.0, device="cuda")
+    if q == 2:
+        ws = workspace(B.slicegcn_gated_bwd_workspace_bytes(n, wi, wo, dtype))
+        B.slicegcn_gated_bwd(x, wg, wu, g, u, d, ws, dX=dx, dWg=dwg, dWu=dwu, dbu=db)
+        want = gated_bwd(x64, wg64, wu64, g64, u64, d64, "silu", dtype)
+        got = ((dx, "dX"), (dwg, "dWg"), (dwu, "dWu"), (db, "dbu"))
+    else:
+        ws = workspace(B.slicegcn_product_bwd_workspace_bytes(n, wi, wo, dtype))
+        B.slicegcn_product_bwd(x, wg, g, d, ws, dX=dx, dW=dwg, db=db, act=B.ACT_GELU)
+        want = product_bwd(x64, wg64, g64, d64, 1.0, "gelu", dtype)
+        got = ((dx, "dX"), (dwg, "dW"), (db, "db"))
+    for t, key in got:
+        assert_within(t, *want[key], key)
+    assert_padding(dxbuf, wi)
