@@ -16,21 +16,49 @@ constexpr int CUS = 256;
 constexpr int64_t MOST_PARTIAL = (int64_t)256 << 20; // bytes of sums of parts of k
 constexpr int64_t CHAIN = 1024;                      // steps of k that one sum runs over in fp32 at most
 
+// Tiles through registers.  Few rows: 32 x 128 (4 rows 535 -> 6038 fp32 11.7 us, in 64 x 64 12.3; 28 rows 3970 -> 1475 gated fp32 19.2 and 23.4).  fp32: 128 x 128 where that
+// gives every CU a tile (16000 rows 1000 -> 1000 180 us, in 64 x 64 218), 64 x 64 where it does not (1000 rows 512 -> 512 15.9 us, in 128 x 128 19.5).  16-bit operands:
+// 64 x 64 alone, since with 128 x 128 the epilogue of a forward pass does not fit the registers beside the sums (65536 rows 256 -> 64 bf16 gelu 68 us, in 64 x 64 13).
 int tile_for(const ProductShape &s)
 {
     if (s.M <= 32) return 2;
+    if (s.type != SLICEGCN_F32) return 1;
     const int64_t cols = s.gated ? TILE_N[0] / 2 : TILE_N[0];
     const int64_t large = (s.M + TILE_M[0] - 1) / TILE_M[0] * ((s.N + cols - 1) / cols) * s.sets;
     return large >= CUS ? 0 : 1;
 }
 
+// 16-bit products that are worth tiles of 256 x 256, straight into LDS, and copies of operands that lie oddly.  A wavefront's epilogue alone takes 13 us there, with a gelu
+// (4096 rows 1024 -> 1024 36 us, in 64 x 64 through registers 22; 4096 rows 1024 -> 4096 48 and 66; 8192 rows 1024 -> 1024 gated 34 and 61), and half-empty tiles do
+// not pay (200 k rows 1024 -> 128 190 us and 145), but for sums over the rows, whose operands are read once then (dX and dW of 200 k rows 1000 -> 104 331 us and 407).
+constexpr double TILES_LEAST = 1e10; // multiplications
+double multiplications(const ProductShape &s) { return (double)s.M * (double)s.N * (double)s.K * (s.gated ? 2 : s.segments * s.sets); }
+bool long_product(const ProductShape &s)
+{
+    return s.type != SLICEGCN_F32 && s.M > 128 && s.N * (s.gated ? 2 : 1) > (s.by_rows ? 128 : 64) && multiplications(s) >= TILES_LEAST;
+}
+
+// Few rows of 16 bits in strips of columns, where that is one launch for two: sums of up to 2048 (one row 2048 -> 2048 bf16 9.0 us, cut in parts through registers 12.7;
+// 32 rows 1024 -> 2816 gated 9.5 and 12.3; one row 4096 -> 4096 16.5 and 13.6), and fewer columns than keep all CUs busy in another way (32 rows 2048 -> 5632 gated 19.8 and
+// 18.5).  More rows go through registers (48 rows 2048 -> 2048 14.9 us in strips, 11.7).
+int kernel_for(const ProductShape &s, bool aligned)
+{
+    if (!aligned || s.type == SLICEGCN_F32) return BY_REGISTERS;
+    const int64_t steps = (s.K + DIRECT_K - 1) / DIRECT_K * s.segments, strips = (s.N * (s.gated ? 2 : 1) + 63) / 64;
+    if (s.by_rows && s.M <= ROWS_MOST && steps <= 64 && strips <= CUS / 2) return BY_ROWS;
+    return long_product(s) ? BY_TILES : BY_REGISTERS;
+}
+
 } // namespace
 
+// How k is cut: so that about `want` workgroups run, which are two a CU through registers (300 rows 4096 -> 512 bf16 14.6 us, with four 17.1; 300 rows 10240 -> 1024 31.5 and
+// with one 33.8), in parts of `least` steps or more (300 rows 4096 -> 1024 in tiles of 256: 16 steps 29 us, 4 33, 64 51; 300 rows 700 -> 500 fp32 through registers: 4 steps 12.2,
+// 1 14.4, 16 19.7).  Short sums are not cut, as the launch that joins the parts takes longer than they do (1000 rows 1024 -> 1024 bf16 11.7 us, in two parts 17.1; 2000 rows 256 ->
+// 256 fp32 10.7 and 12.2); 16-bit operands that no buffer reads are slower by the step and cut all the same (300 rows 1001 -> 1203 bf16 17.2 us, in one part 29.9).
 ProductPlan plan_product(const ProductShape &s, bool aligned)
 {
     ProductPlan p{};
-    aligned = aligned && s.type != SLICEGCN_F32;
-    p.kernel = aligned && s.by_rows && s.M <= ROWS_MOST ? BY_ROWS : aligned && s.M > ROWS_MOST && s.N > 64 ? BY_TILES : BY_REGISTERS;
+    p.kernel = kernel_for(s, aligned);
     p.tile = tile_for(s);
     const int bk = p.kernel == BY_REGISTERS ? step_k(s.type) : DIRECT_K;
     const int bm = p.kernel == BY_ROWS ? ROWS_MOST : p.kernel == BY_TILES ? DIRECT_TILE : TILE_M[p.tile];
@@ -38,12 +66,13 @@ ProductPlan plan_product(const ProductShape &s, bool aligned)
     const int64_t tiles = (s.M + bm - 1) / bm * ((s.N + bn - 1) / bn) * s.sets;
     const int64_t steps = (s.K + bk - 1) / bk * s.segments, one = (int64_t)(s.gated ? 2 : s.sets) * s.M * s.N * 4;
     const int64_t want = p.kernel == BY_REGISTERS ? 2 * CUS : CUS;
-    const int64_t least = p.kernel == BY_REGISTERS ? 4 : p.kernel == BY_TILES ? 16 : 64; // steps of a part
+    const int64_t least = p.kernel == BY_REGISTERS ? 4 : 16; // steps of a part
     int64_t splits = 2 * tiles > want ? 1 : want / (tiles > 0 ? tiles : 1);
     if (splits > steps / least) splits = steps / least;
+    if (p.kernel == BY_REGISTERS && (s.type == SLICEGCN_F32 ? steps < 16 : aligned && steps < 24)) splits = 1;
     if (splits * one > MOST_PARTIAL) splits = MOST_PARTIAL / one;
     if (splits < (steps + CHAIN - 1) / CHAIN) splits = (steps + CHAIN - 1) / CHAIN;
-    if (splits < 1) splits = 1;
+    if (splits < 1 || p.kernel == BY_ROWS) splits = 1;
     const int64_t each = (steps + splits - 1) / splits;
     p.steps_per_split = (int32_t)(each > 0 ? each : 1);
     p.splits = (int32_t)(steps > 0 ? (steps + p.steps_per_split - 1) / p.steps_per_split : 1);
@@ -53,13 +82,14 @@ ProductPlan plan_product(const ProductShape &s, bool aligned)
 
 namespace {
 
-// Whether the products of a backward pass of these sizes share a launch, by the multiplications in both; and how each is cut then.
-// 2048 rows 64 -> 170 gated fp32:
-constexpr int64_t PAIR_MOST = (int64_t)1 << 28;
-constexpr int64_t PAIR_RESULTS = (int64_t)1 << 20; // elements of dX and of dW, which all go through memory as sums of parts
-bool paired(int64_t n, int32_t w_in, int32_t w_out, int q)
+// Whether the products of a backward pass of these sizes share a launch, by the multiplications in both; and how each is cut then.  2048 rows 64 -> 170 gated fp32 17.7 us,
+// in launches of their own 27.1; 2048 rows 256 -> 688 gated bf16 28 and 40, fp32 48 and 52; beyond: 4096 rows 256 -> 688 gated fp32 82 and 75, 8192 rows 512 -> 1024 bf16 69
+// and 63.
+constexpr int64_t PAIR_MOST_F32 = (int64_t)1 << 30, PAIR_MOST_16 = (int64_t)1 << 31;
+constexpr int64_t PAIR_RESULTS = (int64_t)1 << 20; // elements of dX and of dW, which all go through memory as sums of parts: 1182 rows 2488 -> 13 gated fp32 31.5 us so, 26.2 apart
+bool paired(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q)
 {
-    return n > 0 && (double)n * (double)w_in * (double)w_out * q <= (double)PAIR_MOST && n * w_in <= PAIR_RESULTS && (int64_t)w_in * w_out * q <= PAIR_RESULTS;
+    return n > 0 && (double)n * (double)w_in * (double)w_out * q <= (double)(type == SLICEGCN_F32 ? PAIR_MOST_F32 : PAIR_MOST_16) && n * w_in <= PAIR_RESULTS && (int64_t)w_in * w_out * q <= PAIR_RESULTS;
 }
 ProductPlan pair_plan(const ProductShape &s)
 {
@@ -98,19 +128,13 @@ bool aligned_product(int layouts, const ProductShape &s, const ProductArgs &a)
 
 // ---- 16-bit operands whose rows are no whole units of 16 bytes: copied so that they are, where the product is long against a copy of its operands.
 
-// 6263 rows 9079 -> 557 bf16:
-constexpr double PACK_LEAST = 2e9; // multiplications
-bool worth_packing(const ProductShape &s)
-{
-    return s.type != SLICEGCN_F32 && s.M > ROWS_MOST && s.N > 64 && (double)s.M * (double)s.N * (double)s.K * (s.gated ? 2 : s.segments * s.sets) >= PACK_LEAST;
-}
 int64_t packed_bytes(int64_t rows, int64_t width) { return width % 8 == 0 ? 0 : round_up(rows * round_up(width, 8) * 2, 256); }
 int64_t rows_a(int layouts, const ProductShape &s) { return layouts == PRODUCT_XTG ? s.K : s.M; }
 int64_t rows_b(int layouts, const ProductShape &s) { return layouts == PRODUCT_GWT ? s.N : s.K; }
 // Room for copies of the operands whose width asks for one (`both`: of the M side too, which a backward pass has formed itself for dX)
 size_t pack_bytes(int layouts, const ProductShape &s, bool a, bool b)
 {
-    if (!worth_packing(s)) return 0;
+    if (!long_product(s)) return 0;
     return (size_t)((a ? packed_bytes(rows_a(layouts, s), width_a(layouts, s)) : 0) +
                     (b ? packed_bytes(rows_b(layouts, s), width_b(layouts, s)) * (s.gated ? 2 : s.segments * s.sets) : 0));
 }
@@ -154,7 +178,7 @@ int pack_operands(int layouts, const ProductShape &s, ProductArgs &a, char *room
 {
     const int64_t wa = width_a(layouts, s), wb = width_b(layouts, s);
     const int count = s.gated ? 2 : operands(a);
-    bool fit = worth_packing(s);
+    bool fit = long_product(s);
     for (int i = 0; i < operands(a); ++i) fit = fit && (on_units(a.a[i], wa) || wa % 8);
     for (int i = 0; i < count; ++i) fit = fit && (on_units(a.b[i], wb) || wb % 8);
     if (!fit || aligned_product(layouts, s, a)) return SLICEGCN_OK;
@@ -217,7 +241,7 @@ struct SlopeArgs {
 constexpr int SLOPE_RUN = 32; // rows that are added in fp32 before they are added in fp64
 
 // Workgroup (x, y): `lanes` accesses of 16 bytes of the rows of part y, 256 / lanes rows at a time and ROWS such turns in flight.  Bound by bytes:
-// 2.4 M rows of 256 bf16 columns through a gelu
+// 8192 rows of 10240 gated bf16 columns 178 us, 4.7 TB/s.
 template <class T, bool GATED, int ACT> __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a)
 {
     constexpr int V = 16 / sizeof(T), Q = GATED ? 2 : 1, ROWS = GATED ? 2 : 4;
@@ -350,7 +374,7 @@ SlopeGrid slope_grid(int64_t n, int32_t w, int32_t type)
 }
 
 // Whether a backward pass may go in one sweep over the rows, by its sizes, and with how many workgroups (0: it may not).  Many rows, since every workgroup leaves a
-// dW of its own:
+// dW of its own: 100 -> 256 columns bf16 gelu, 8192 rows 30 us, 22 in the general form; 16384 rows 28 and 37; 2.4 M rows 0.95 and 1.83 ms.
 constexpr int64_t NARROW_LEAST = 16384;
 unsigned narrow_blocks(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q)
 {
@@ -381,7 +405,7 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     const size_t z = (size_t)round_up(blocks * q * w_in * (int64_t)w_out * 4, 256);
     w.partial = x > y ? x : y;
     w.partial = w.partial > z ? w.partial : z;
-    if (paired(n, w_in, w_out, q)) {
+    if (paired(n, w_in, w_out, type, q)) {
         const size_t both = pair_plan(dx_shape(n, w_in, w_out, type, q)).bytes + pair_plan(dw_shape(n, w_in, w_out, type, q)).bytes;
         w.partial = w.partial > both ? w.partial : both;
     }
@@ -463,7 +487,7 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
     char *at = static_cast<char *>(ws);
     // without an activation dP is dY itself, or a copy of it where its rows are no whole units and the products gain from that
     const bool plain = q == 1 && d.act == SLICEGCN_ACT_NONE &&
-                       (on_units(c.dy, d.w_out) || !(worth_packing(dx_shape(d.n, d.w_in, d.w_out, d.type, q)) || worth_packing(dw_shape(d.n, d.w_in, d.w_out, d.type, q))));
+                       (on_units(c.dy, d.w_out) || !(long_product(dx_shape(d.n, d.w_in, d.w_out, d.type, q)) || long_product(dw_shape(d.n, d.w_in, d.w_out, d.type, q))));
     Operand dg[2] = {c.dy, c.dy};
     SlopeArgs s{};
     s.g = q == 1 && d.act == SLICEGCN_ACT_NONE ? Operand{nullptr, 0, 0} : c.g;
@@ -567,7 +591,7 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         y.segments = 1;
     }
     // one of two dW alone is cut like both, so that the workspace suffices and its bits are the same
-    if (paired(d.n, d.w_in, d.w_out, q) && (!want_x || product_on_words(PRODUCT_GWT, shape_x, x)) && (!want_w || product_on_words(PRODUCT_XTG, shape_w, y))) {
+    if (paired(d.n, d.w_in, d.w_out, d.type, q) && (!want_x || product_on_words(PRODUCT_GWT, shape_x, x)) && (!want_w || product_on_words(PRODUCT_XTG, shape_w, y))) {
         const ProductPlan px = pair_plan(shape_x), pw = pair_plan(shape_w);
         x.splits = px.splits;
         x.steps_per_split = px.steps_per_split;

@@ -123,8 +123,7 @@ constexpr int PRODUCT_XW = 0, PRODUCT_GWT = 1, PRODUCT_XTG = 2;
 constexpr int TILES = 3;
 constexpr int TILE_M[TILES] = {128, 64, 32}, TILE_N[TILES] = {128, 64, 128};
 constexpr int DIRECT_TILE = 256, DIRECT_K = 32;
-constexpr int ROWS_MOST = 128;
-constexpr int rows_waves(int f) { return f <= 2 ? 8 : 4; } // wavefronts of product_rows_kernel for 16 f rows
+constexpr int ROWS_MOST = 32;
 constexpr int STEP_K_F32 = 32, STEP_K_16 = 64;
 inline int step_k(int32_t type) { return type == SLICEGCN_F32 ? STEP_K_F32 : STEP_K_16; }
 

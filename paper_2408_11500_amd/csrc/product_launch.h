@@ -10,11 +10,12 @@ template <class T, int LM, int LN, int EPI, bool SPLIT> int launch_sums(const Pr
 {
     if constexpr (sizeof(T) == 2) {
         if (plan.kernel == BY_TILES) return launch_direct<T, LM, LN, EPI, SPLIT>(a, stream);
-        if constexpr (LM == LAYOUT_KC)
-            if (plan.kernel == BY_ROWS) return launch_rows<T, LN, EPI, SPLIT>(a, stream);
+        if constexpr (LM == LAYOUT_KC && !SPLIT)
+            if (plan.kernel == BY_ROWS) return launch_rows<T, LN, EPI>(a, stream);
     }
+    if constexpr (sizeof(T) == 4)
+        if (plan.tile == 0) return launch_tile<T, LM, LN, EPI, 0, SPLIT>(a, stream);
     switch (plan.tile) {
-    case 0: return launch_tile<T, LM, LN, EPI, 0, SPLIT>(a, stream);
     case 1: return launch_tile<T, LM, LN, EPI, 1, SPLIT>(a, stream);
     default: return launch_tile<T, LM, LN, EPI, 2, SPLIT>(a, stream);
     }

@@ -1,9 +1,10 @@
-// Products of few rows (up to 128) of 16-bit operands that lie on 16-byte boundaries: a request or some requests at a time, where the weights are all there is to
-// read.
+// Products of few rows (up to 32) of 16-bit operands that lie on 16-byte boundaries, sums of up to 2048: a request or some requests at a time, where the weights are all there is
+// to read, and a second launch would take as long as reading them.
 //
 // A workgroup forms all rows of a strip of 64 columns (GATED: 32 of each product).  Its wavefronts share out the strip's k, each with a ring of its own in LDS
-// that its loads go to straight from memory, ROWS_DEPTH - 1 steps of 32 k ahead: no barrier in the loop, and some 20 to 100 KB on their way per CU.  The
-// wavefronts' sums are added in order through LDS at the end.
+// that its loads go to straight from memory, ROWS_DEPTH - 1 steps of 32 k ahead: no barrier in the loop, and some 80 KB on their way per CU.  The
+// wavefronts' sums are added in order through LDS at the end.  One row 1024 -> 2816 gated bf16: 6.4 us, 1.8 TB/s; bound by the latency of the launch and of a wavefront's four
+// steps.
 #pragma once
 
 #include "product_direct.h"
@@ -11,24 +12,20 @@
 namespace slicegcn {
 namespace {
 
-constexpr int ROWS_DEPTH = 3;
+constexpr int ROWS_DEPTH = 3, ROWS_WAVES = 8;
 
-// F: 16 rows each.  WAVES: what LDS holds rings for
-template <class T, int LN, int EPI, int F, bool SPLIT>
-__global__ __launch_bounds__(64 * rows_waves(F)) void product_rows_kernel(const ProductArgs a)
+// F: 16 rows each
+template <class T, int LN, int EPI, int F> __global__ __launch_bounds__(64 * ROWS_WAVES) void product_rows_kernel(const ProductArgs a)
 {
     constexpr bool TURNS = EPI == EPI_GATED, SEGMENTS = LN == LAYOUT_KC;
-    constexpr int WAVES = rows_waves(F), BK = DIRECT_K, COLS = TURNS ? 32 : 64, PIECES = 64 / COLS, FN = 4;
+    constexpr int WAVES = ROWS_WAVES, BK = DIRECT_K, COLS = TURNS ? 32 : 64, PIECES = 64 / COLS, FN = 4;
     constexpr int UNITS_M = 16 * F * BK / 8, UNITS_N = COLS * BK / 8, STEP_UNITS = UNITS_M + PIECES * UNITS_N;
     constexpr int LOADS_M = UNITS_M / 64, LOADS_N = UNITS_N / 64, LOADS = LOADS_M + PIECES * LOADS_N;
     constexpr int RING = ROWS_DEPTH * STEP_UNITS, SUMS = 16 * F * 64; // floats of a wavefront's sums
     static_assert(SUMS * 4 <= RING * 16, "the sums take the place of the rings");
     __shared__ short8 lds[WAVES * RING];
 
-    const int64_t strips = (a.N + COLS - 1) / COLS, id = a.first + blockIdx.x;
-    const int set = a.sets > 1 ? (int)(id / (strips * a.splits)) : 0;
-    const int split = SPLIT ? (int)(id / strips % a.splits) : 0;
-    const int64_t n0 = id % strips * COLS;
+    const int64_t n0 = (a.first + blockIdx.x) * COLS;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), lane = threadIdx.x % 64;
 
     float4v acc[F][FN];
@@ -38,10 +35,7 @@ __global__ __launch_bounds__(64 * rows_waves(F)) void product_rows_kernel(const 
         for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
 
     const int32_t K = (int32_t)a.K, steps_each = (K + BK - 1) / BK, all = SEGMENTS ? steps_each * a.segments : steps_each;
-    const int32_t part_begin = SPLIT ? split * a.steps_per_split : 0;
-    const int32_t part_end = SPLIT && part_begin + a.steps_per_split < all ? part_begin + a.steps_per_split : all;
-    const int32_t share = (part_end - part_begin + WAVES - 1) / WAVES, begin = part_begin + wave * share;
-    const int32_t end = begin + share < part_end ? begin + share : part_end;
+    const int32_t share = (all + WAVES - 1) / WAVES, begin = wave * share, end = begin + share < all ? begin + share : all;
 
     const short8 *ring = lds + wave * RING;
     const uint32_t ring0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short8 *)lds + (uint32_t)wave * (RING * 16);
@@ -49,11 +43,10 @@ __global__ __launch_bounds__(64 * rows_waves(F)) void product_rows_kernel(const 
     DirectPiece<LN, COLS, 64> pn[PIECES];
     int32_t next = begin, segment = SEGMENTS && begin >= steps_each ? 1 : 0, slot = 0;
     {
-        const int which = set + segment; // one of them is 0
         const int32_t k0 = (begin - segment * steps_each) * BK;
-        pm.aim(a.a[which], 0, a.M, k0, K);
+        pm.aim(a.a[segment], 0, a.M, k0, K);
 #pragma unroll
-        for (int q = 0; q < PIECES; ++q) pn[q].aim(a.b[TURNS ? q : which], n0, a.N, k0, K);
+        for (int q = 0; q < PIECES; ++q) pn[q].aim(a.b[TURNS ? q : segment], n0, a.N, k0, K);
     }
     const char *second_m = a.a[1].p, *second_n = a.b[1].p;
     auto issue = [&]() { // the loads of step `next`; of one that is not there, zeros
@@ -130,25 +123,17 @@ __global__ __launch_bounds__(64 * rows_waves(F)) void product_rows_kernel(const 
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[p][r] += v[r];
             }
-        if constexpr (SPLIT) {
-            char *to = reinterpret_cast<char *>(a.partial + ((int64_t)set * a.splits + split) * a.M * a.N);
-            store4<float>(to, row * a.N + col, left, s[0]);
-        } else {
-            finish4<T, EPI>(a, set, row, col, left, s[0], s[PIECES - 1]);
-        }
+        finish4<T, EPI>(a, 0, row, col, left, s[0], s[PIECES - 1]);
     }
 }
 
-template <class T, int LN, int EPI, bool SPLIT> int launch_rows(ProductArgs &a, hipStream_t stream)
+template <class T, int LN, int EPI> int launch_rows(ProductArgs &a, hipStream_t stream)
 {
     constexpr int COLS = EPI == EPI_GATED ? 32 : 64;
-    const int64_t blocks = (a.N + COLS - 1) / COLS * a.splits * a.sets;
-    return launch_parts(blocks, [&](unsigned first, unsigned count) {
+    return launch_parts((a.N + COLS - 1) / COLS, [&](unsigned first, unsigned count) {
         a.first = first;
-        if (a.M <= 16) product_rows_kernel<T, LN, EPI, 1, SPLIT><<<count, 64 * rows_waves(1), 0, stream>>>(a);
-        else if (a.M <= 32) product_rows_kernel<T, LN, EPI, 2, SPLIT><<<count, 64 * rows_waves(2), 0, stream>>>(a);
-        else if (a.M <= 64) product_rows_kernel<T, LN, EPI, 4, SPLIT><<<count, 64 * rows_waves(4), 0, stream>>>(a);
-        else product_rows_kernel<T, LN, EPI, 8, SPLIT><<<count, 64 * rows_waves(8), 0, stream>>>(a);
+        if (a.M <= 16) product_rows_kernel<T, LN, EPI, 1><<<count, 64 * ROWS_WAVES, 0, stream>>>(a);
+        else product_rows_kernel<T, LN, EPI, 2><<<count, 64 * ROWS_WAVES, 0, stream>>>(a);
     });
 }
 

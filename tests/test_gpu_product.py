@@ -540,3 +540,52 @@ def test_short_backward_passes(size, q, kind):
     for t, key in got:
         assert_within(t, *want[key], key)
     assert_padding(dxbuf, wi)
+
+
+# 16-bit products that go in tiles of 256 x 256: cut sums, ends within a step and an odd number of steps, one tile of rows, a sum of many rows, columns behind a tile; and with
+# operands that are copied first
+LONG = [(513, 5000, 4104), (130, 9000, 9032), (8200, 9064, 136), (20_000, 72, 7000), (2500, 2056, 2000), (2050, 2003, 2521), (9001, 1026, 1101), (140, 8401, 9103)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("size", LONG, ids=str)
+def test_long_products(size, kind):
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    case = LONG.index(size)
+    gen = torch.Generator().manual_seed(300 + case)
+    ld = ("dense", "lines", "odd" if wi % 8 else "dense")[case % 3]
+    on_gpu = lambda t, t64: (t, t64.cuda())  # references in 64 bits on the device: 1e10 multiplications each
+    x, x64 = on_gpu(*rows(gen, n, wi, dtype, lds(n, wi, ld)))
+    (wg, wg64), (wu, wu64) = (on_gpu(*weights(gen, wi, wo, dtype)) for _ in range(2))
+    g, g64 = on_gpu(*rows(gen, n, wo, dtype, lds(n, wo, ld), std=1.5))
+    u, u64 = on_gpu(*rows(gen, n, wo, dtype, lds(n, wo, ld)))
+    d, d64 = on_gpu(*rows(gen, n, wo, dtype, lds(n, wo, ld)))
+    b = torch.randn(wo, generator=gen).cuda()
+    name = ACTS[case % 4]
+    y, ybuf = result(n, wo, dtype, lds(n, wo, ld))
+    p, pbuf = result(n, wo, dtype, lds(n, wo, "odd"))
+    dx, dxbuf = result(n, wi, dtype, lds(n, wi, ld))
+    dwg, dwu, db = torch.full_like(wg, 777.0), torch.full_like(wu, 777.0), torch.full((wo,), 777.0, device="cuda")
+
+    def check(got, want, key):
+        assert_within(got, *(t.cpu() for t in want[key]), key)
+    B.slicegcn_product_fwd(x, wg, y, workspace(B.slicegcn_product_fwd_workspace_bytes(n, wi, wo, dtype)), b=b, R=u, P=p, act=ACT[name], residual=0.5)
+    want = product_fwd(x64, wg64, b.to(F64), u64, 0.5, name, dtype)
+    check(y, want, "Y")
+    check(p, want, "P")
+    assert_padding(ybuf, wo)
+    assert_padding(pbuf, wo)
+    B.slicegcn_product_bwd(x, wg, g, d, workspace(B.slicegcn_product_bwd_workspace_bytes(n, wi, wo, dtype)), dX=dx, dW=dwg, db=db, act=ACT[name])
+    want = product_bwd(x64, wg64, g64, d64, 1.0, name, dtype)
+    for got, key in ((dx, "dX"), (dwg, "dW"), (db, "db")):
+        check(got, want, key)
+    assert_padding(dxbuf, wi)
+    B.slicegcn_gated_fwd(x, wg, wu, y, workspace(B.slicegcn_gated_fwd_workspace_bytes(n, wi, wo, dtype)), bg=b, act=ACT[name])
+    check(y, gated_fwd(x64, wg64, wu64, b.to(F64), None, name, dtype), "H")
+    assert_padding(ybuf, wo)
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, d, workspace(B.slicegcn_gated_bwd_workspace_bytes(n, wi, wo, dtype)), dX=dx, dWg=dwg, dWu=dwu, dbu=db, act=ACT[name])
+    want = gated_bwd(x64, wg64, wu64, g64, u64, d64, name, dtype)
+    for got, key in ((dx, "dX"), (dwg, "dWg"), (dwu, "dWu"), (db, "dbu")):
+        check(got, want, key)
+    assert_padding(dxbuf, wi)
