@@ -51,6 +51,10 @@ int kernel_for(const ProductShape &s, bool aligned)
 
 } // namespace
 
+// Where the tiles of 256 x 256 are more than one round of the CUs and the last round would leave half of them or more idle, its tiles are cut along k and joined: 8192 rows 4096 ->
+// 2304 161 us, whole 206; 8192 rows 2048 -> 2304 104 and 122; 20000 rows 1024 -> 1024 78 and 82, the shortest sum with which that was tried.
+constexpr int64_t TAIL_LEAST = 32; // steps
+
 // How k is cut: so that about `want` workgroups run, which are two a CU through registers (300 rows 4096 -> 512 bf16 14.6 us, with four 17.1; 300 rows 10240 -> 1024 31.5 and
 // with one 33.8), in parts of `least` steps or more (300 rows 4096 -> 1024 in tiles of 256: 16 steps 29 us, 4 33, 64 51; 300 rows 700 -> 500 fp32 through registers: 4 steps 12.2,
 // 1 14.4, 16 19.7).  Short sums are not cut, as the launch that joins the parts takes longer than they do (1000 rows 1024 -> 1024 bf16 11.7 us, in two parts 17.1; 2000 rows 256 ->
@@ -77,6 +81,18 @@ ProductPlan plan_product(const ProductShape &s, bool aligned)
     p.steps_per_split = (int32_t)(each > 0 ? each : 1);
     p.splits = (int32_t)(steps > 0 ? (steps + p.steps_per_split - 1) / p.steps_per_split : 1);
     p.bytes = p.splits > 1 ? (size_t)round_up(p.splits * one, 256) : 0;
+    if (p.kernel == BY_TILES && p.splits == 1 && tiles > CUS && steps >= TAIL_LEAST) {
+        const int64_t rest = tiles % CUS, most = steps / 16;
+        int64_t parts = rest > 0 ? CUS / rest : 0;
+        parts = parts < most ? parts : most;
+        parts = parts < 8 ? parts : 8;
+        if (parts > 1) {
+            p.tail = (int32_t)rest;
+            p.steps_per_split = (int32_t)((steps + parts - 1) / parts);
+            p.tail_splits = (int32_t)((steps + p.steps_per_split - 1) / p.steps_per_split);
+            p.bytes = (size_t)rest * p.tail_splits * DIRECT_TILE * DIRECT_TILE * 4;
+        }
+    }
     return p;
 }
 

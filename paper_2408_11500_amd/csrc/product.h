@@ -43,6 +43,7 @@ struct ProductArgs {
     float *partial;        // sums of parts of k: [set][split][M][N], where splits > 1
     int32_t splits;
     int32_t steps_per_split;
+    int32_t tail;          // BY_TILES: how many of the last tiles are formed by themselves, cut along k: [part][tile][DIRECT_TILE][DIRECT_TILE]
     int64_t first;         // first workgroup of this launch
     int32_t shares;        // threads that share the parts of a result out where they are joined
     int32_t on_words;      // whether buffers can read the operands: product_kernels.h
@@ -61,6 +62,7 @@ struct ProductPlan {
     int32_t kernel;
     int32_t tile; // BY_REGISTERS: index of a tile shape
     int32_t splits, steps_per_split;
+    int32_t tail, tail_splits; // BY_TILES, splits = 1: the last tiles, and in how many parts of steps_per_split they are cut
     size_t bytes; // of the sums of parts of k
 };
 ProductPlan plan_product(const ProductShape &s, bool aligned);

@@ -6,6 +6,8 @@
 // step a wavefront waits for its own loads of the step after this one and meets the others at a barrier: then that step is whole in LDS, and nobody reads the
 // buffer any more that the next loads are for.  During a step the operand registers for the next one are read: those of the N side into a second set, those of the M
 // side into the registers that the step is done with.
+// 8192 rows 4096 -> 10240 gated bf16: 1.03 ms, 1.34 PFLOP/s (a library's plain products of these sizes: 0.90 to 1.35); bound by the matrix instructions, which run 60 to 70 % of
+// the time at the clock that their power leaves.  With four wavefronts and tiles of 128 x 128, or with five buffers, slower.
 // The waits are counted by hand, since the compiler does not know which reads of LDS a load in flight has to do with; the loads are therefore inline assembly,
 // which has no register results.
 #pragma once
@@ -111,8 +113,11 @@ template <int LAYOUT, int R, int THREADS> struct DirectPiece {
     }
 };
 
+// What a launch forms: all tiles but the tail, parts of all tiles, or parts of the tail's tiles
+constexpr int WHOLE = 0, PARTS = 1, TAIL_PARTS = 2;
+
 // GATED: the N side is a piece of 128 columns of each of the two products
-template <class T, int LM, int LN, int EPI, bool SPLIT>
+template <class T, int LM, int LN, int EPI, int FORM>
 __global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const ProductArgs a)
 {
     constexpr bool TURNS = EPI == EPI_GATED, SEGMENTS = LM == LAYOUT_KC && LN == LAYOUT_KC;
@@ -122,11 +127,15 @@ __global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const
     __shared__ short8 lds[DIRECT_DEPTH * STEP_UNITS];
 
     const int64_t tile_rows = (a.M + BM - 1) / BM, tile_cols = (a.N + COLS - 1) / COLS, tiles = tile_rows * tile_cols;
-    int64_t id = tile_of(a.first + blockIdx.x, tiles * a.splits * a.sets), row_tile, col_tile;
-    const int set = a.sets > 1 ? (int)(id / (tiles * a.splits)) : 0;
-    id -= set * (tiles * a.splits);
-    const int split = SPLIT ? (int)(id / tiles) : 0;
-    tile_place(id - split * tiles, tile_rows, tile_cols, row_tile, col_tile);
+    const int64_t whole = tiles * a.sets - a.tail;
+    int64_t id = tile_of(a.first + blockIdx.x, FORM == WHOLE ? whole : FORM == PARTS ? tiles * a.splits * a.sets : (int64_t)a.tail * a.splits), row_tile, col_tile;
+    const int64_t part_of_tail = id; // TAIL_PARTS
+    if (FORM == TAIL_PARTS) id = whole + id % a.tail;
+    const int64_t each = FORM == PARTS ? tiles * a.splits : tiles;
+    const int set = a.sets > 1 ? (int)(id / each) : 0;
+    id -= set * each;
+    const int split = FORM == PARTS ? (int)(id / tiles) : FORM == TAIL_PARTS ? (int)(part_of_tail / a.tail) : 0;
+    tile_place(FORM == PARTS ? id - split * tiles : id, tile_rows, tile_cols, row_tile, col_tile);
     const int64_t m0 = row_tile * BM, n0 = col_tile * COLS;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), lane = threadIdx.x % 64, wm = wave / WN * 128, wn = wave % WN * 64;
 
@@ -137,8 +146,8 @@ __global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const
         for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
 
     const int32_t K = (int32_t)a.K, steps_each = (K + BK - 1) / BK, all = SEGMENTS ? steps_each * a.segments : steps_each;
-    const int32_t begin = SPLIT ? split * a.steps_per_split : 0;
-    const int32_t end = SPLIT && begin + a.steps_per_split < all ? begin + a.steps_per_split : all;
+    const int32_t begin = FORM != WHOLE ? split * a.steps_per_split : 0;
+    const int32_t end = FORM != WHOLE && begin + a.steps_per_split < all ? begin + a.steps_per_split : all;
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short8 *)lds;
     DirectPiece<LM, BM, DIRECT_THREADS> pm;
@@ -225,16 +234,74 @@ __global__ __launch_bounds__(DIRECT_THREADS, 2) void product_direct_kernel(const
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // no load into LDS outlives the workgroup
 
-    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, COLS, acc);
+    if constexpr (FORM == TAIL_PARTS) {
+        float *to = a.partial + (part_of_tail * BM + wm + lane % 16) * BN + wn + 4 * (lane / 16);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) *reinterpret_cast<float4v *>(to + 16 * i * BN + 16 * j) = acc[i][j];
+    } else {
+        finish_tile<T, EPI, FORM == PARTS, BM>(a, set, split, m0, n0, wm, wn, COLS, acc);
+    }
 }
 
-template <class T, int LM, int LN, int EPI, bool SPLIT> int launch_direct(ProductArgs &a, hipStream_t stream)
+// The parts of the tail's tiles added in fp64, in order, 16 rows of a tile a workgroup.  GATED: 16 columns of a tile are of the first product, 16 of the second, and so on.
+template <class T, int EPI> __global__ __launch_bounds__(256) void product_tail_kernel(const ProductArgs a)
+{
+    constexpr int Q = EPI == EPI_GATED ? 2 : 1, BM = DIRECT_TILE, BN = DIRECT_TILE, COLS = BN / Q, FOURS = COLS / 4, ROWS = 256 / FOURS;
+    const int64_t tile_rows = (a.M + BM - 1) / BM, tile_cols = (a.N + COLS - 1) / COLS, tiles = tile_rows * tile_cols;
+    const int tile = (int)((a.first + blockIdx.x) / (BM / 16)), rows16 = (int)((a.first + blockIdx.x) % (BM / 16));
+    const int64_t id = tiles * a.sets - a.tail + tile;
+    const int set = (int)(id / tiles);
+    int64_t row_tile, col_tile;
+    tile_place(id - set * tiles, tile_rows, tile_cols, row_tile, col_tile);
+    const int in_row = threadIdx.x % FOURS * 4, at = Q == 2 ? in_row / 16 * 32 + in_row % 16 : in_row;
+    const int64_t col = col_tile * COLS + in_row;
+    const int left = a.N - col < 4 ? (int)(a.N - col) : 4;
+    if (left <= 0) return;
+#pragma unroll
+    for (int r = 0; r < 16; r += ROWS) {
+        const int in = 16 * rows16 + r + threadIdx.x / FOURS;
+        const int64_t row = row_tile * BM + in;
+        if (row >= a.M) return;
+        double sum[Q][4] = {};
+        for (int s = 0; s < a.splits; ++s)
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const float4v v = *reinterpret_cast<const float4v *>(a.partial + (((int64_t)s * a.tail + tile) * BM + in) * BN + at + 16 * q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[q][i] += (double)v[i];
+            }
+        float s[Q][4];
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[q][i] = (float)sum[q][i];
+        finish4<T, EPI>(a, set, row, col, left, s[0], s[Q - 1]);
+    }
+}
+
+template <class T, int LM, int LN, int EPI, int FORM> int launch_direct(ProductArgs &a, hipStream_t stream)
 {
     constexpr int COLS = EPI == EPI_GATED ? DIRECT_TILE / 2 : DIRECT_TILE;
-    const int64_t blocks = (a.M + DIRECT_TILE - 1) / DIRECT_TILE * ((a.N + COLS - 1) / COLS) * a.splits * a.sets;
-    return launch_parts(blocks, [&](unsigned first, unsigned count) {
+    const int64_t tiles = (a.M + DIRECT_TILE - 1) / DIRECT_TILE * ((a.N + COLS - 1) / COLS) * a.sets;
+    return launch_parts(FORM == WHOLE ? tiles - a.tail : FORM == PARTS ? tiles * a.splits : (int64_t)a.tail * a.splits, [&](unsigned first, unsigned count) {
         a.first = first;
-        product_direct_kernel<T, LM, LN, EPI, SPLIT><<<count, DIRECT_THREADS, 0, stream>>>(a);
+        product_direct_kernel<T, LM, LN, EPI, FORM><<<count, DIRECT_THREADS, 0, stream>>>(a);
+    });
+}
+
+// All tiles of a product that is not cut, and those of a last round that would leave most CUs idle in parts
+template <class T, int LM, int LN, int EPI> int launch_whole(const ProductPlan &plan, ProductArgs &a, hipStream_t stream)
+{
+    a.tail = plan.tail;
+    if (int rc = launch_direct<T, LM, LN, EPI, WHOLE>(a, stream)) return rc;
+    if (!a.tail) return SLICEGCN_OK;
+    a.splits = plan.tail_splits;
+    if (int rc = launch_direct<T, LM, LN, EPI, TAIL_PARTS>(a, stream)) return rc;
+    return launch_parts((int64_t)a.tail * (DIRECT_TILE / 16), [&](unsigned first, unsigned count) {
+        a.first = first;
+        product_tail_kernel<T, EPI><<<count, 256, 0, stream>>>(a);
     });
 }
 

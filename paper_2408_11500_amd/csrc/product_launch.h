@@ -9,7 +9,10 @@ namespace {
 template <class T, int LM, int LN, int EPI, bool SPLIT> int launch_sums(const ProductPlan &plan, ProductArgs &a, hipStream_t stream)
 {
     if constexpr (sizeof(T) == 2) {
-        if (plan.kernel == BY_TILES) return launch_direct<T, LM, LN, EPI, SPLIT>(a, stream);
+        if (plan.kernel == BY_TILES) {
+            if constexpr (SPLIT) return launch_direct<T, LM, LN, EPI, PARTS>(a, stream);
+            else return launch_whole<T, LM, LN, EPI>(plan, a, stream);
+        }
         if constexpr (LM == LAYOUT_KC && !SPLIT)
             if (plan.kernel == BY_ROWS) return launch_rows<T, LN, EPI>(a, stream);
     }

@@ -544,7 +544,9 @@ def test_short_backward_passes(size, q, kind):
 
 # 16-bit products that go in tiles of 256 x 256: cut sums, ends within a step and an odd number of steps, one tile of rows, a sum of many rows, columns behind a tile; and with
 # operands that are copied first
-LONG = [(513, 5000, 4104), (130, 9000, 9032), (8200, 9064, 136), (20_000, 72, 7000), (2500, 2056, 2000), (2050, 2003, 2521), (9001, 1026, 1101), (140, 8401, 9103)]
+LONG = [(513, 5000, 4104), (130, 9000, 9032), (8200, 9064, 136), (20_000, 72, 7000), (2500, 2056, 2000), (2050, 2003, 2521), (9001, 1026, 1101), (140, 8401, 9103),
+        # more than a round of tiles, the last of which are cut: in dX and both dW of a gated projection, in all but the latter, and with an end within four columns
+        (4100, 4400, 3768), (4100, 4400, 4616), (4100, 4401, 4611)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
