@@ -383,7 +383,11 @@ SlopeGrid slope_grid(int64_t n, int32_t w, int32_t type)
     while (g.lanes < 64 && g.lanes < accesses) g.lanes *= 2;
     g.cols = (accesses + g.lanes - 1) / g.lanes;
     const int64_t rows = 256 / g.lanes;
-    g.parts = (8 * CUS + g.cols - 1) / g.cols;
+    // eight workgroups a CU where a thread has eight rows or more then, else two (each leaves column sums): 16 k rows 512 -> 512 gated bf16 with biases 99 us, with eight 113; 100 k
+    // rows 256 -> 688 495 and 460
+    const int64_t most = (8 * CUS + g.cols - 1) / g.cols, few = (2 * CUS + g.cols - 1) / g.cols, long_ones = n / (8 * rows);
+    g.parts = long_ones > few ? long_ones : few;
+    if (g.parts > most) g.parts = most;
     if (g.parts > (n + rows - 1) / rows) g.parts = (n + rows - 1) / rows;
     if (g.parts < 1) g.parts = 1;
     return g;
