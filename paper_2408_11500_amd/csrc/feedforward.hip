@@ -262,7 +262,7 @@ template <class T, bool GATED, int ACT> __global__ __launch_bounds__(256) void s
 {
     constexpr int V = 16 / sizeof(T), Q = GATED ? 2 : 1, ROWS = GATED ? 2 : 4;
     constexpr bool SLOPES = GATED || ACT != SLICEGCN_ACT_NONE;
-    __shared__ double sums[256][Q * V];
+    __shared__ double sums[Q * V][257];
     const int groups = 256 / a.lanes, lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
     const int64_t col = ((int64_t)blockIdx.x * a.lanes + lane) * V;
     const int left = a.w - col < V ? (int)(a.w - col) : V;
@@ -342,18 +342,17 @@ template <class T, bool GATED, int ACT> __global__ __launch_bounds__(256) void s
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
-        for (int i = 0; i < V; ++i) sums[threadIdx.x][q * V + i] = total[q][i] + (double)run[q][i];
+        for (int i = 0; i < V; ++i) sums[q * V + i][threadIdx.x] = total[q][i] + (double)run[q][i];
     __syncthreads();
-    if (group > 0 || left <= 0) return;
-#pragma unroll
-    for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (i >= left) continue;
-            double t = 0.0;
-            for (int w = 0; w < groups; ++w) t += sums[w * a.lanes + lane][q * V + i];
-            a.partial[((int64_t)blockIdx.y * Q + q) * a.w + col + i] = t;
-        }
+    const int here = a.lanes * V;
+    const int64_t col0 = (int64_t)blockIdx.x * here;
+    for (int o = threadIdx.x; o < Q * here; o += 256) {
+        const int q = o / here, c = o % here;
+        if (col0 + c >= a.w) continue;
+        double t = 0.0;
+        for (int w = 0; w < groups; ++w) t += sums[q * V + c % V][w * a.lanes + c / V];
+        a.partial[((int64_t)blockIdx.y * Q + q) * a.w + col0 + c] = t;
+    }
 }
 
 __global__ __launch_bounds__(1024) void bias_kernel(const BiasSums b)

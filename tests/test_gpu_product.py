@@ -391,12 +391,12 @@ def test_narrow_backward_passes_of_many_rows(size, kind, gated):
     assert_padding(buf, wi)
 
 
-# rows that are no whole units of 16 bytes, where the operands are copied: odd widths, even ones, one of the two
-COPIED = [(2050, 1003, 1021), (1500, 1026, 1401), (2100, 1016, 1001), (3000, 701, 1024), (140, 4001, 4103)]
+# rows that are no whole units of 16 bytes, through registers: odd widths, even ones, one of the two
+UNEVEN = [(2050, 1003, 1021), (1500, 1026, 1401), (2100, 1016, 1001), (3000, 701, 1024), (140, 4001, 4103)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
-@pytest.mark.parametrize("size", COPIED, ids=str)
+@pytest.mark.parametrize("size", UNEVEN, ids=str)
 @pytest.mark.parametrize("ld", ["dense", "lines", "odd"])
 def test_large_products_of_rows_that_lie_oddly(size, ld, kind):
     n, wi, wo = size
@@ -546,7 +546,9 @@ def test_short_backward_passes(size, q, kind):
 # operands that are copied first
 LONG = [(513, 5000, 4104), (130, 9000, 9032), (8200, 9064, 136), (20_000, 72, 7000), (2500, 2056, 2000), (2050, 2003, 2521), (9001, 1026, 1101), (140, 8401, 9103),
         # more than a round of tiles, the last of which are cut: in dX and both dW of a gated projection, in all but the latter, and with an end within four columns
-        (4100, 4400, 3768), (4100, 4400, 4616), (4100, 4401, 4611)]
+        (4100, 4400, 3768), (4100, 4400, 4616), (4100, 4401, 4611),
+        # copied: rows on odd elements, gradients without an activation
+        (1500, 3026, 2401), (2100, 2203, 2301)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
