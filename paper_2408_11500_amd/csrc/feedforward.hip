@@ -58,7 +58,7 @@ constexpr int64_t TAIL_LEAST = 32; // steps
 // How k is cut: so that about `want` workgroups run, which are two a CU through registers (300 rows 4096 -> 512 bf16 14.6 us, with four 17.1; 300 rows 10240 -> 1024 31.5 and
 // with one 33.8), in parts of `least` steps or more (300 rows 4096 -> 1024 in tiles of 256: 16 steps 29 us, 4 33, 64 51; 300 rows 700 -> 500 fp32 through registers: 4 steps 12.2,
 // 1 14.4, 16 19.7).  Short sums are not cut, as the launch that joins the parts takes longer than they do (1000 rows 1024 -> 1024 bf16 11.7 us, in two parts 17.1; 2000 rows 256 ->
-// 256 fp32 10.7 and 12.2); 16-bit operands that no buffer reads are slower by the step and cut all the same (300 rows 1001 -> 1203 bf16 17.2 us, in one part 29.9).
+// 256 fp32 10.7 and 12.2); 16-bit operands that lie oddly are slower by the step and cut sooner (one row 1001 -> 1203 bf16 12.3 us, in one part 16.3; 300 rows 501 -> 701 13.1 and 10.4).
 ProductPlan plan_product(const ProductShape &s, bool aligned)
 {
     ProductPlan p{};
@@ -73,7 +73,7 @@ ProductPlan plan_product(const ProductShape &s, bool aligned)
     const int64_t least = p.kernel == BY_REGISTERS ? 4 : 16; // steps of a part
     int64_t splits = 2 * tiles > want ? 1 : want / (tiles > 0 ? tiles : 1);
     if (splits > steps / least) splits = steps / least;
-    if (p.kernel == BY_REGISTERS && (s.type == SLICEGCN_F32 ? steps < 16 : aligned && steps < 24)) splits = 1;
+    if (p.kernel == BY_REGISTERS && steps < (s.type == SLICEGCN_F32 ? 16 : aligned ? 24 : 12)) splits = 1;
     if (splits * one > MOST_PARTIAL) splits = MOST_PARTIAL / one;
     if (splits < (steps + CHAIN - 1) / CHAIN) splits = (steps + CHAIN - 1) / CHAIN;
     if (splits < 1 || p.kernel == BY_ROWS) splits = 1;
@@ -210,7 +210,7 @@ int pack_operands(int layouts, const ProductShape &s, ProductArgs &a, char *room
     return SLICEGCN_OK;
 }
 
-// Whether buffers can read both operands: their range checks go by words, so no word may hold an element that exists and one that does not
+// Whether buffers can read both operands as they lie: their range checks go by words, so no word may hold an element that exists and one that does not
 bool on_words(const Operand &o, int32_t type)
 {
     return type == SLICEGCN_F32 || ((reinterpret_cast<uintptr_t>(o.p) & 3u) == 0 && o.ld % 2 == 0);
@@ -610,7 +610,9 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         y.segments = 1;
     }
     // one of two dW alone is cut like both, so that the workspace suffices and its bits are the same
-    if (paired(d.n, d.w_in, d.w_out, d.type, q) && (!want_x || product_on_words(PRODUCT_GWT, shape_x, x)) && (!want_w || product_on_words(PRODUCT_XTG, shape_w, y))) {
+    if (paired(d.n, d.w_in, d.w_out, d.type, q)) {
+        x.on_words = !want_x || product_on_words(PRODUCT_GWT, shape_x, x);
+        y.on_words = !want_w || product_on_words(PRODUCT_XTG, shape_w, y);
         const ProductPlan px = pair_plan(shape_x), pw = pair_plan(shape_w);
         x.splits = px.splits;
         x.steps_per_split = px.steps_per_split;

@@ -46,7 +46,7 @@ struct ProductArgs {
     int32_t tail;          // BY_TILES: how many of the last tiles are formed by themselves, cut along k: [part][tile][DIRECT_TILE][DIRECT_TILE]
     int64_t first;         // first workgroup of this launch
     int32_t shares;        // threads that share the parts of a result out where they are joined
-    int32_t on_words;      // whether buffers can read the operands: product_kernels.h
+    int32_t on_words;      // whether buffers can read the operands as they lie: product_kernels.h
 };
 
 // Sizes of a product and how it is cut: everything that a launch depends on follows from these

@@ -93,56 +93,6 @@ template <int LAYOUT, int R, int BK> __device__ inline int lds_unit(int outer_or
     }
 }
 
-// A piece of an operand on its way from memory to LDS, 8 elements a unit
-template <class T, int LAYOUT, int R, int BK, int THREADS, bool TURNS> struct Piece {
-    static constexpr int UNITS = R * BK / 8, EACH = (UNITS + THREADS - 1) / THREADS;
-    T v[EACH][8];
-
-    // outer indexes from o0 on (of `outer` in all), k from k0 on (of K).  TURNS: 16 columns of the first operand, 16 of the second, and so on.
-    __device__ void load(const Operand *op, int64_t o0, int64_t outer, int64_t k0, int64_t K)
-    {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int q = threadIdx.x + i * THREADS;
-            if (UNITS % THREADS != 0 && q >= UNITS) break;
-            int64_t o, k;
-            int which = 0;
-            if constexpr (LAYOUT == LAYOUT_KC) {
-                static_assert(!TURNS, "only columns take turns");
-                o = o0 + q / (BK / 8);
-                k = k0 + q % (BK / 8) * 8;
-            } else {
-                k = k0 + q / (R / 8);
-                const int c = q % (R / 8) * 8;
-                if (TURNS) {
-                    which = c / 16 % 2;
-                    o = o0 + c / 32 * 16 + c % 16;
-                } else {
-                    o = o0 + c;
-                }
-            }
-            const Operand m = op[which];
-            const T *p = reinterpret_cast<const T *>(m.p);
-            if constexpr (LAYOUT == LAYOUT_KC) load8(p + o * m.ld + k, o < outer ? K - k : 0, v[i]);
-            else load8(p + k * m.ld + o, k < K ? outer - o : 0, v[i]);
-        }
-    }
-
-    __device__ void store(short8 *lds) const
-    {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int q = threadIdx.x + i * THREADS;
-            if (UNITS % THREADS != 0 && q >= UNITS) break;
-            const int at = LAYOUT == LAYOUT_KC ? lds_unit<LAYOUT, R, BK>(q / (BK / 8), q % (BK / 8)) : lds_unit<LAYOUT, R, BK>(q % (R / 8), q / (R / 8));
-            short8 t[Planes<T>::count];
-            split8(v[i], t);
-#pragma unroll
-            for (int p = 0; p < Planes<T>::count; ++p) lds[p * UNITS + at] = t[p];
-        }
-    }
-};
-
 // The operand registers of 16 outer indexes from `base` on and 32 k from 32 * kk on: lane l holds 8 k of the index l % 16
 template <int LAYOUT, int R, int BK> __device__ inline short8 fragment(const short8 *lds, int base, int kk, int lane)
 {
@@ -408,81 +358,6 @@ __device__ inline void finish_tile(const ProductArgs &a, int set, int split, int
     }
 }
 
-// WM x WN wavefronts.  SPLIT: sums of a part of k go to a.partial.
-template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT>
-__global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs a)
-{
-    constexpr int P = Planes<T>::count, BK = P == 3 ? STEP_K_F32 : STEP_K_16, THREADS = 64 * WM * WN;
-    constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-    constexpr bool TURNS = EPI == EPI_GATED;
-    constexpr int COLS = TURNS ? BN / 2 : BN; // columns of results
-    static_assert(!TURNS || FN % 2 == 0, "a wavefront holds both products of its columns");
-    __shared__ short8 lds[P * (BM + BN) * BK / 8];
-    short8 *lds_m = lds, *lds_n = lds + P * BM * BK / 8;
-
-    const int64_t tile_rows = (a.M + BM - 1) / BM, tile_cols = (a.N + COLS - 1) / COLS, tiles = tile_rows * tile_cols;
-    int64_t id = tile_of(a.first + blockIdx.x, tiles * a.splits * a.sets), row_tile, col_tile;
-    const int set = a.sets > 1 ? (int)(id / (tiles * a.splits)) : 0;
-    id -= set * (tiles * a.splits);
-    const int split = SPLIT ? (int)(id / tiles) : 0;
-    tile_place(id - split * tiles, tile_rows, tile_cols, row_tile, col_tile);
-    const int64_t m0 = row_tile * BM, n0 = col_tile * COLS;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-
-    float4v acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
-
-    const int64_t steps_each = (a.K + BK - 1) / BK, steps = steps_each * a.segments;
-    int64_t step = SPLIT ? (int64_t)split * a.steps_per_split : 0;
-    const int64_t end = SPLIT && step + a.steps_per_split < steps ? step + a.steps_per_split : steps;
-    Piece<T, LM, BM, BK, THREADS, false> pm;
-    Piece<T, LN, BN, BK, THREADS, TURNS> pn;
-    auto load = [&](int64_t t) {
-        const int seg = t >= steps_each ? 1 : 0, which = seg + set; // one of them is 0
-        const int64_t k0 = (t - seg * steps_each) * BK;
-        pm.load(a.a + which, m0, a.M, k0, a.K);
-        pn.load(a.b + (TURNS ? 0 : which), n0, a.N, k0, a.K);
-    };
-    if (step < end) load(step);
-    for (; step < end; ++step) {
-        __syncthreads();
-        pm.store(lds_m);
-        pn.store(lds_n);
-        __syncthreads();
-        if (step + 1 < end) load(step + 1);
-#pragma unroll
-        for (int kk = 0; kk < BK / 32; ++kk) {
-            short8 fm[FM][P];
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int p = 0; p < P; ++p) fm[i][p] = fragment<LM, BM, BK>(lds_m + p * BM * BK / 8, wm + 16 * i, kk, lane);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                short8 fn[P];
-#pragma unroll
-                for (int p = 0; p < P; ++p) fn[p] = fragment<LN, BN, BK>(lds_n + p * BN * BK / 8, wn + 16 * j, kk, lane);
-                if constexpr (P == 3) {
-#pragma unroll
-                    for (int order = 2; order >= 0; --order) // terms of order 2, 1, 0: the sum of the two planes' numbers
-#pragma unroll
-                        for (int p = 0; p <= order; ++p)
-#pragma unroll
-                            for (int i = 0; i < FM; ++i) acc[i][j] = mfma<T>(fn[p], fm[i][order - p], acc[i][j]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < FM; ++i) acc[i][j] = mfma<T>(fn[0], fm[i][0], acc[i][j]);
-                }
-            }
-        }
-    }
-
-    finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, COLS, acc);
-}
-
 // The sums of all parts of k, in fp64: four columns a thread, and a.shares threads of a workgroup share the parts out (part s, s + shares, ... each), whose sums
 // are added in order.  GATED: the parts of the second product are those of set 1.  256 parts of 100 x 256 with one share 84 us.
 template <int EPI> constexpr int JOIN_SUMS = (EPI == EPI_GATED ? 2 : 1) * 4 + 1;
@@ -554,20 +429,23 @@ template <class T, int EPI> int launch_join(ProductArgs &a, hipStream_t stream)
     });
 }
 
-// ---- operands on boundaries of 4 bytes: through buffers -----------------------------------------------------------------
-
-
 // A piece of an operand (R outer indexes, BK of k) on its way from memory to LDS, 8 elements a unit.  It is read through a buffer whose range check takes care of rows, lines
 // and columns behind the last one, so that the loads of a step depend on no lane's branch and two steps can be in flight.  KC: the buffer of the tile's rows, of which a step
 // reads from its scalar offset on; OC: the buffer of the step's lines.
-template <class T, int LAYOUT, int R, int BK, int THREADS> struct BufferPiece {
+// The range check goes by words.  ODD: 16-bit elements of which a word may hold one that exists and one that does not, or whose rows begin within a word: a unit is read as
+// the five words that it lies in (a word with an element of the operand can be read whole) and shifted into place on its way to LDS, where elements that are not there turn
+// into zeros.  (2000 rows 4001 -> 557 bf16: 58 us, with
+// loads that branch by the lane 139; 2000 rows 1001 -> 1203 forward 26 and 37, backward 63 and 121.)
+template <class T, int LAYOUT, int R, int BK, int THREADS, bool ODD> struct BufferPiece {
     static constexpr int UNITS = R * BK / 8, EACH = (UNITS + THREADS - 1) / THREADS, V = sizeof(T) / 2; // accesses of 16 bytes a unit
+    static_assert(!ODD || V == 1, "elements of 16 bits");
     static constexpr uint32_t NOWHERE = 0xffffff00u;
     uint32_t offset[EACH];
     uint64_t base;
     uint32_t line, size; // bytes: of a line; KC: of the buffer, OC: of a line's part
     struct Regs {
         uint4v v[EACH][V];
+        uint32_t more[ODD ? EACH : 1];
     };
 
     __device__ static int unit(int i) { return (int)threadIdx.x + i * THREADS; }
@@ -602,25 +480,43 @@ template <class T, int LAYOUT, int R, int BK, int THREADS> struct BufferPiece {
             from += (uint64_t)(uint32_t)k0 * line;
             bytes += (uint32_t)(lines - 1) * line;
         }
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(from), 0, there ? (int)bytes : 0, 0x00020000);
+        const uint32_t within = ODD ? (uint32_t)from & 2u : 0u; // steps are whole words apart
+        if (ODD) bytes = (bytes + within + 3u) & ~3u;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(from - within), 0, there ? (int)bytes : 0, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < EACH; ++i)
+        for (int i = 0; i < EACH; ++i) {
+            const uint32_t at = ODD ? (offset[i] + within) & ~3u : offset[i];
 #pragma unroll
-            for (int v = 0; v < V; ++v) r.v[i][v] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(offset[i] + 16 * v), (int)scalar, 0);
+            for (int v = 0; v < V; ++v) r.v[i][v] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(at + 16 * v), (int)scalar, 0);
+            if (ODD) r.more[i] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, (int)(at + 16), (int)scalar, 0);
+        }
     }
 
-    // left: k that exist from the step's first one on (KC: what follows in the buffer is the next row)
-    __device__ static void store(const Regs &r, short8 *lds, int32_t left)
+    // left: k that exist from the step's first one on (KC: what follows in the buffer is the next row).  from: what base was for the step
+    __device__ void store(const Regs &r, short8 *lds, int32_t left, uint64_t from) const
     {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int q = unit(i);
             if (UNITS % THREADS != 0 && q >= UNITS) break;
             T v[8];
-            __builtin_memcpy(v, r.v[i], sizeof(v));
+            if constexpr (ODD) {
+                const uint32_t by = (offset[i] + (uint32_t)from) & 2u; // bytes into its first word
+                const uint32_t w[5] = {r.v[i][0][0], r.v[i][0][1], r.v[i][0][2], r.v[i][0][3], r.more[i]};
+                uint32_t x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_alignbyte(w[j + 1], w[j], by);
+                __builtin_memcpy(v, x, sizeof(v));
+            } else {
+                __builtin_memcpy(v, r.v[i], sizeof(v));
+            }
             if (LAYOUT == LAYOUT_KC && left < BK) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = unit_k(i) + j < left ? v[j] : (T)0.f;
+            }
+            if (ODD && LAYOUT == LAYOUT_OC && left < BK) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = q / (R / 8) < left ? v[j] : (T)0.f;
             }
             const int at = LAYOUT == LAYOUT_KC ? lds_unit<LAYOUT, R, BK>(q / (BK / 8), q % (BK / 8)) : lds_unit<LAYOUT, R, BK>(q % (R / 8), q / (R / 8));
             short8 t[Planes<T>::count];
@@ -636,7 +532,7 @@ template <class T, int BM, int BN> constexpr int buffer_units = Planes<T>::count
 
 // A tile of results of such operands, by workgroup `block` of a product: SETS steps on their way in registers, one in LDS.  (fp32: with two on their way 233 k rows 602 -> 256
 // take 500 us, with one 452; with three workgroups a CU instead of two 484.)
-template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT>
+template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT, bool ODD>
 __device__ inline void product_buffer_tile(const ProductArgs &a, int64_t block, short8 *lds)
 {
     constexpr int SETS = sizeof(T) == 4 ? 1 : 2;
@@ -645,8 +541,8 @@ __device__ inline void product_buffer_tile(const ProductArgs &a, int64_t block, 
     constexpr bool TURNS = EPI == EPI_GATED, SEGMENTS = LM == LAYOUT_KC && LN == LAYOUT_KC;
     constexpr int PIECES = TURNS ? 2 : 1, COLS = BN / PIECES; // columns of results; GATED: a piece of each product
     static_assert(!TURNS || FN % 2 == 0, "a wavefront holds both products of its columns");
-    typedef BufferPiece<T, LM, BM, BK, THREADS> PieceM;
-    typedef BufferPiece<T, LN, COLS, BK, THREADS> PieceN;
+    typedef BufferPiece<T, LM, BM, BK, THREADS, ODD> PieceM;
+    typedef BufferPiece<T, LN, COLS, BK, THREADS, ODD> PieceN;
     static_assert(P * (PieceM::UNITS + PIECES * PieceN::UNITS) == buffer_units<T, BM, BN>, "LDS of a step");
     short8 *lds_m = lds, *lds_n = lds + P * PieceM::UNITS;
 
@@ -693,9 +589,10 @@ __device__ inline void product_buffer_tile(const ProductArgs &a, int64_t block, 
     auto step = [&](Step &s, int32_t t) {
         const int32_t left = K - (SEGMENTS && t >= steps_each ? t - steps_each : t) * BK;
         __syncthreads();
-        PieceM::store(s.m, lds_m, left);
+        const bool second = SEGMENTS && t >= steps_each;
+        pm.store(s.m, lds_m, left, second ? second_m : base_m);
 #pragma unroll
-        for (int q = 0; q < PIECES; ++q) PieceN::store(s.n[q], lds_n + q * P * PieceN::UNITS, left);
+        for (int q = 0; q < PIECES; ++q) pn[q].store(s.n[q], lds_n + q * P * PieceN::UNITS, left, q ? pn[q].base : second ? second_n : base_n);
         __syncthreads();
         load(s, t + SETS);
 #pragma unroll
@@ -735,21 +632,21 @@ __device__ inline void product_buffer_tile(const ProductArgs &a, int64_t block, 
     finish_tile<T, EPI, SPLIT, BM>(a, set, split, m0, n0, wm, wn, COLS, acc);
 }
 
-// product_kernel for such operands
-template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT>
+// WM x WN wavefronts.  SPLIT: sums of a part of k go to a.partial.
+template <class T, int LM, int LN, int EPI, int BM, int BN, int WM, int WN, bool SPLIT, bool ODD>
 __global__ __launch_bounds__(64 * WM * WN, 2) void product_buffer_kernel(const ProductArgs a)
 {
     __shared__ short8 lds[buffer_units<T, BM, BN>];
-    product_buffer_tile<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT>(a, a.first + blockIdx.x, lds);
+    product_buffer_tile<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT, ODD>(a, a.first + blockIdx.x, lds);
 }
 
 // Both products of a backward pass in one launch, where they are short and launches would take longer than they: dX by the first workgroups, dW by the others, all as sums of
 // parts of k.
-template <class T> __global__ __launch_bounds__(256, 2) void product_pair_kernel(const ProductArgs x, const ProductArgs w, unsigned blocks_x)
+template <class T, bool ODD> __global__ __launch_bounds__(256, 2) void product_pair_kernel(const ProductArgs x, const ProductArgs w, unsigned blocks_x)
 {
     __shared__ short8 lds[buffer_units<T, PAIR_TILE, PAIR_TILE>];
-    if (blockIdx.x < blocks_x) product_buffer_tile<T, LAYOUT_KC, LAYOUT_KC, EPI_STORE, PAIR_TILE, PAIR_TILE, 2, 2, true>(x, blockIdx.x, lds);
-    else product_buffer_tile<T, LAYOUT_OC, LAYOUT_OC, EPI_STORE, PAIR_TILE, PAIR_TILE, 2, 2, true>(w, blockIdx.x - blocks_x, lds);
+    if (blockIdx.x < blocks_x) product_buffer_tile<T, LAYOUT_KC, LAYOUT_KC, EPI_STORE, PAIR_TILE, PAIR_TILE, 2, 2, true, ODD>(x, blockIdx.x, lds);
+    else product_buffer_tile<T, LAYOUT_OC, LAYOUT_OC, EPI_STORE, PAIR_TILE, PAIR_TILE, 2, 2, true, ODD>(w, blockIdx.x - blocks_x, lds);
 }
 
 // What is left of it: the parts of dX and of dW joined, and the column sums' parts
@@ -775,7 +672,11 @@ template <class T> int launch_pair(ProductArgs *x, ProductArgs *w, const BiasSum
     const ProductArgs none{};
     const int64_t x_tiles = tiles(x), w_tiles = tiles(w), x_joins = joins(x), w_joins = joins(w), bias_blocks = bias_workgroups(bias);
     if (x_tiles + w_tiles > 0) {
-        product_pair_kernel<T><<<(unsigned)(x_tiles + w_tiles), 256, 0, stream>>>(x ? *x : none, w ? *w : none, (unsigned)x_tiles);
+        const bool odd = (x && !x->on_words) || (w && !w->on_words);
+        const dim3 grid((unsigned)(x_tiles + w_tiles));
+        if constexpr (sizeof(T) == 2)
+            if (odd) product_pair_kernel<T, true><<<grid, 256, 0, stream>>>(x ? *x : none, w ? *w : none, (unsigned)x_tiles);
+        if (!odd) product_pair_kernel<T, false><<<grid, 256, 0, stream>>>(x ? *x : none, w ? *w : none, (unsigned)x_tiles);
         SG_LAUNCH_CHECK();
     }
     if (x_joins + w_joins + bias_blocks > 0) {
@@ -795,10 +696,10 @@ template <class T, int LM, int LN, int EPI, int TILE, bool SPLIT> int launch_til
         a.first = first;
         if constexpr (sizeof(T) == 2)
             if (!a.on_words) {
-                product_kernel<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT><<<count, 64 * WM * WN, 0, stream>>>(a);
+                product_buffer_kernel<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT, true><<<count, 64 * WM * WN, 0, stream>>>(a);
                 return;
             }
-        product_buffer_kernel<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT><<<count, 64 * WM * WN, 0, stream>>>(a);
+        product_buffer_kernel<T, LM, LN, EPI, BM, BN, WM, WN, SPLIT, false><<<count, 64 * WM * WN, 0, stream>>>(a);
     });
 }
 

@@ -593,3 +593,45 @@ def test_long_products(size, kind):
     for got, key in ((dx, "dX"), (dwg, "dWg"), (dwu, "dWu"), (db, "dbu")):
         check(got, want, key)
     assert_padding(dxbuf, wi)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [(33, 65, 129), (200, 131, 71), (7, 333, 45), (64, 63, 65), (300, 129, 201), (1, 1, 1), (1300, 901, 303)], ids=str)
+@pytest.mark.parametrize("offset", [0, 1])
+def test_operands_of_odd_widths_amid_nan(size, offset, kind):
+    """Elements before and behind an operand share words with its own: of a pair of weights one begins on a word, the other within one."""
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(400 + offset)
+
+    def amid(rows, width, offset, std=1.0):
+        buf = torch.full((rows * width + offset + 9,), float("nan"), dtype=dtype)
+        view = buf[offset:offset + rows * width].view(rows, width)
+        view.copy_((torch.randn((rows, width), generator=gen) * std).to(dtype))
+        return buf.cuda()[offset:offset + rows * width].view(rows, width), view.to(F64)
+    x, x64 = amid(n, wi, offset)
+    wg, wg64 = amid(wi, wo, offset, wi ** -0.5)
+    wu, wu64 = amid(wi, wo, 1 - offset, wi ** -0.5)
+    g, g64 = amid(n, wo, 1 - offset, 1.5)
+    u, u64 = amid(n, wo, offset)
+    d, d64 = amid(n, wo, 1)
+    ws = workspace(max(f(n, wi, wo, dtype) for f in (B.slicegcn_gated_fwd_workspace_bytes, B.slicegcn_gated_bwd_workspace_bytes,
+                                                     B.slicegcn_product_fwd_workspace_bytes, B.slicegcn_product_bwd_workspace_bytes)))
+    y, ybuf = result(n, wo, dtype, wo + 1)
+    dx, dxbuf = result(n, wi, dtype, wi + 2)
+    dwg, dwu, db = torch.full((wi, wo), 777.0, dtype=dtype, device="cuda"), torch.full((wi, wo), 777.0, dtype=dtype, device="cuda"), torch.zeros(wo, device="cuda")
+    B.slicegcn_product_fwd(x, wg, y, ws, R=u)
+    assert_within(y, *product_fwd(x64, wg64, None, u64, 1.0, "none", dtype)["Y"], "Y")
+    assert_padding(ybuf, wo)
+    B.slicegcn_gated_fwd(x, wg, wu, y, ws)
+    assert_within(y, *gated_fwd(x64, wg64, wu64, None, None, "silu", dtype)["H"], "H")
+    assert_padding(ybuf, wo)
+    B.slicegcn_product_bwd(x, wg, None, d, ws, dX=dx, dW=dwg, db=db)
+    want = product_bwd(x64, wg64, None, d64, 1.0, "none", dtype)
+    for got, key in ((dx, "dX"), (dwg, "dW"), (db, "db")):
+        assert_within(got, *want[key], key)
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, d, ws, dX=dx, dWg=dwg, dWu=dwu, dbg=db)
+    want = gated_bwd(x64, wg64, wu64, g64, u64, d64, "silu", dtype)
+    for got, key in ((dx, "dX"), (dwg, "dWg"), (dwu, "dWu"), (db, "dbg")):
+        assert_within(got, *want[key], key)
+    assert_padding(dxbuf, wi)
