@@ -238,7 +238,7 @@ size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_o
 int slicegcn_product_fwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream);
 
 /* dP = dY * act'(P);  dX = dP W^T;  dW = X^T dP;  db = column sums of dP;  dR = residual * dY.  Absent outputs are not formed (the inputs that only they
- * need may be absent too).  dP is rounded to the rows' type before the products; db is formed from it unrounded.
+ * need may be absent too).  dP is rounded to the rows' type before the products (short passes keep it in two terms); db is formed from it unrounded.
  * EINVAL, ERANGE, EWORKSPACE as above. */
 size_t slicegcn_product_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
 int slicegcn_product_bwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream);
@@ -250,7 +250,8 @@ size_t slicegcn_gated_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out
 int slicegcn_gated_fwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream);
 
 /* dG = dH * U * act'(G);  dU = dH * act(G);  dX = dG Wg^T + dU Wu^T;  dWg = X^T dG;  dWu = X^T dU;  dbg, dbu: column sums.  Absent outputs are not
- * formed.  dG and dU are rounded to the rows' type before the products; dbg and dbu are formed from them unrounded. */
+ * formed.  dG and dU are rounded to the rows' type before the products (short passes keep them in two terms); dbg and dbu are formed from them
+ * unrounded. */
 size_t slicegcn_gated_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
 int slicegcn_gated_bwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream);
 

@@ -122,6 +122,14 @@ ProductPlan pair_plan(const ProductShape &s)
     return p;
 }
 
+// Whether the gradients before the activation are kept in two 16-bit terms: where there are so few of them that the errors of rounding them do not level out over a sum, and both
+// products of them share a launch, in which the second term costs little (3 rows 2595 -> 8 gated bf16 gelu: errors of dX and dW 0.0031 of their norms in one term, 0.0017 in two).
+constexpr int64_t TERMS_MOST = (int64_t)1 << 15; // elements
+int terms_of(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q)
+{
+    return type != SLICEGCN_F32 && n * w_out * q <= TERMS_MOST && paired(n, w_in, w_out, type, q) ? 2 : 1;
+}
+
 // What a call may need, however its operands lie
 size_t partial_bytes(const ProductShape &s)
 {
@@ -250,6 +258,7 @@ struct SlopeArgs {
     int64_t ldg, ldu, ldr, n;
     int32_t w, lanes; // columns; threads that share a row out
     float residual;
+    int64_t rest;    // where not 0: what rounding dg and du leaves, rounded too, goes that many bytes behind them
     double *partial; // column sums of parts of the rows: [part][1 or 2][w], where biases have gradients
     int64_t rows_per_part;
 };
@@ -316,6 +325,19 @@ template <class T, bool GATED, int ACT> __global__ __launch_bounds__(256) void s
                 }
                 if (a.dg) write(a.dg, a.ldg, row, o[0], true);
                 if (GATED && a.du) write(a.du, a.ldu, row, o[Q - 1], true);
+                if constexpr (sizeof(T) == 2)
+                    if (a.rest) {
+                        float left_over[Q][V];
+#pragma unroll
+                        for (int q = 0; q < Q; ++q)
+#pragma unroll
+                            for (int i = 0; i < V; ++i) {
+                                const float h = (float)(T)o[q][i];
+                                left_over[q][i] = fabsf(h) < INFINITY ? o[q][i] - h : 0.f;
+                            }
+                        write(a.dg + a.rest, a.ldg, row, left_over[0], true);
+                        if (GATED) write(a.du + a.rest, a.ldu, row, left_over[Q - 1], true);
+                    }
                 if (a.dr) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) d[r][i] *= a.residual;
@@ -406,8 +428,9 @@ bool narrow_rows_fit(const Operand &o) { return !o.p || ((reinterpret_cast<uintp
 // Workspace of a backward pass: gradients before the activation, their column sums, sums of parts of k
 struct BwdWorkspace {
     int64_t ld; // of the gradients before the activation: rows on 16-byte boundaries
+    int terms;  // of them
     size_t rows, sums, partial, room;
-    size_t bytes(int q) const { return q * rows + sums + partial + room; }
+    size_t bytes(int q) const { return terms * q * rows + sums + partial + room; }
 };
 
 ProductShape dx_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q) { return ProductShape{n, w_out, w_in, q, 1, type, false, true}; }
@@ -417,6 +440,7 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
 {
     BwdWorkspace w;
     w.ld = round_up(w_out, 8);
+    w.terms = terms_of(n, w_in, w_out, type, q);
     w.rows = (size_t)round_up(n * w.ld * type_bytes(type), 256);
     const int64_t parts = slope_grid(n, w_out, type).parts, blocks = narrow_blocks(n, w_in, w_out, type, q);
     w.sums = (size_t)round_up((parts > blocks ? parts : blocks) * q * (int64_t)w_out * 8, 256);
@@ -425,7 +449,7 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     w.partial = x > y ? x : y;
     w.partial = w.partial > z ? w.partial : z;
     if (paired(n, w_in, w_out, type, q)) {
-        const size_t both = pair_plan(dx_shape(n, w_in, w_out, type, q)).bytes + pair_plan(dw_shape(n, w_in, w_out, type, q)).bytes;
+        const size_t both = w.terms * (pair_plan(dx_shape(n, w_in, w_out, type, q)).bytes + pair_plan(dw_shape(n, w_in, w_out, type, q)).bytes);
         w.partial = w.partial > both ? w.partial : both;
     }
     const size_t u = pack_bytes(PRODUCT_GWT, dx_shape(n, w_in, w_out, type, q), false, true), v = pack_bytes(PRODUCT_XTG, dw_shape(n, w_in, w_out, type, q), true, false);
@@ -521,12 +545,13 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         if (q == 2) s.du = at + w.rows;
         dg[0] = Operand{s.dg, w.ld, 1};
         dg[1] = Operand{s.du, w.ld, 1};
+        s.rest = w.terms == 2 ? (int64_t)(q * w.rows) : 0;
     }
     if (want_r) {
         s.dr = static_cast<char *>(c.dr.data);
         s.ldr = c.dr.ld;
     }
-    at += q * w.rows;
+    at += w.terms * q * w.rows;
     if (want_b) s.partial = reinterpret_cast<double *>(at);
     at += w.sums;
     float *partial = reinterpret_cast<float *>(at);
@@ -614,12 +639,15 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         x.on_words = !want_x || product_on_words(PRODUCT_GWT, shape_x, x);
         y.on_words = !want_w || product_on_words(PRODUCT_XTG, shape_w, y);
         const ProductPlan px = pair_plan(shape_x), pw = pair_plan(shape_w);
-        x.splits = px.splits;
+        const int terms = s.rest ? 2 : 1;
+        x.splits = terms * px.splits;
         x.steps_per_split = px.steps_per_split;
         x.partial = partial;
-        y.splits = pw.splits;
+        y.splits = terms * pw.splits;
         y.steps_per_split = pw.steps_per_split;
-        y.partial = partial + px.bytes / 4;
+        y.partial = partial + terms * px.bytes / 4;
+        x.terms = y.terms = terms;
+        x.rest_a = y.rest_b = s.rest;
         const auto launch = d.type == SLICEGCN_F32 ? launch_pair_f32 : d.type == SLICEGCN_BF16 ? launch_pair_bf16 : launch_pair_f16;
         return launch(want_x ? &x : nullptr, want_w ? &y : nullptr, bias, stream);
     }

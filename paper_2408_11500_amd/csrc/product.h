@@ -43,6 +43,8 @@ struct ProductArgs {
     float *partial;        // sums of parts of k: [set][split][M][N], where splits > 1
     int32_t splits;
     int32_t steps_per_split;
+    int32_t terms;         // 2, products of a pair alone: an operand is the sum of two, of which the second lies rest_a or rest_b bytes behind; its parts come behind the others
+    int64_t rest_a, rest_b;
     int32_t tail;          // BY_TILES: how many of the last tiles are formed by themselves, cut along k: [part][tile][DIRECT_TILE][DIRECT_TILE]
     int64_t first;         // first workgroup of this launch
     int32_t shares;        // threads that share the parts of a result out where they are joined

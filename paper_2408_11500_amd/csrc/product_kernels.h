@@ -562,12 +562,18 @@ __device__ inline void product_buffer_tile(const ProductArgs &a, int64_t block, 
         for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
 
     const int32_t K = (int32_t)a.K, steps_each = (K + BK - 1) / BK, all = SEGMENTS ? steps_each * a.segments : steps_each;
-    const int32_t begin = SPLIT ? split * a.steps_per_split : 0, end = SPLIT && begin + a.steps_per_split < all ? begin + a.steps_per_split : all;
+    const bool rest = SPLIT && a.terms == 2 && split >= a.splits / 2;
+    const int32_t begin = SPLIT ? (rest ? split - a.splits / 2 : split) * a.steps_per_split : 0;
+    const int32_t end = SPLIT && begin + a.steps_per_split < all ? begin + a.steps_per_split : all;
     PieceM pm;
     PieceN pn[PIECES];
     pm.aim(a.a[set], m0, a.M, K);
 #pragma unroll
     for (int q = 0; q < PIECES; ++q) pn[q].aim(a.b[TURNS ? q : set], n0, a.N, K);
+    if (rest) {
+        pm.base += a.rest_a;
+        pn[0].base += a.rest_b;
+    }
     // the second segment's operands have the leading dimensions of the first one's
     const uint64_t base_m = pm.base, base_n = pn[0].base, second_m = base_m + (uint64_t)(a.a[1].p - a.a[0].p), second_n = base_n + (uint64_t)(a.b[1].p - a.b[0].p);
     struct Step {

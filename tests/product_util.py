@@ -60,12 +60,12 @@ def gated_fwd(x, wg, wu, bg, bu, name, dtype):
     return dict(G=(g, eg), U=(u, eu), H=(a * u, ea * (u.abs() + eu) + a.abs() * eu + 2 * U * (a * u).abs()))
 
 
-def _products(x, pairs, dtype):
-    """Gradients of X and of the weights from [(dP, bound of dP, W)]: dP is rounded to the rows' type before the products."""
+def _products(x, pairs, dtype, terms):
+    """Gradients of X and of the weights from [(dP, bound of dP, W)]: dP is rounded to the rows' type before the products, or is the sum of two terms that are."""
     dx = ex = 0
     out = []
     for dp, ep, w in pairs:
-        ep = ep + half_step(dp, dtype)
+        ep = ep + (half_step(dp, dtype) if terms == 1 else half_step(half_step(dp, dtype), dtype))
         k = w.shape[1] * len(pairs)
         dx, ex = dx + dp @ w.t(), ex + (ep + depth(k, dtype) * (dp.abs() + ep)) @ w.abs().t()
         n = dp.shape[0]
@@ -78,19 +78,19 @@ def _columns(dp, ep):
     return dp.sum(0), (ep + 34 * U * dp.abs()).sum(0)
 
 
-def product_bwd(x, w, p, dy, residual, name, dtype):
+def product_bwd(x, w, p, dy, residual, name, dtype, terms=1):
     if name == "none":
         dp, ep = dy, torch.zeros_like(dy)
     else:
         _, slope = act(p, name)
         dp, ep = dy * slope, dy.abs() * U * (STEPS * (1 + p.abs()) + 2)
-    dx, (dw,) = _products(x, [(dp, ep, w)], dtype)
+    dx, (dw,) = _products(x, [(dp, ep, w)], dtype, terms)
     return dict(dX=dx, dW=dw, db=_columns(dp, ep), dR=(residual * dy, U * (residual * dy).abs()))
 
 
-def gated_bwd(x, wg, wu, g, u, dh, name, dtype):
+def gated_bwd(x, wg, wu, g, u, dh, name, dtype, terms=1):
     y, slope = act(g, name)
     dg, du = dh * u * slope, dh * y
     eg, eu = dh.abs() * u.abs() * U * (STEPS * (1 + g.abs()) + 2), dh.abs() * U * (STEPS + 2) * g.abs()
-    dx, (dwg, dwu) = _products(x, [(dg, eg, wg), (du, eu, wu)], dtype)
+    dx, (dwg, dwu) = _products(x, [(dg, eg, wg), (du, eu, wu)], dtype, terms)
     return dict(dX=dx, dWg=dwg, dWu=dwu, dbg=_columns(dg, eg), dbu=_columns(du, eu))

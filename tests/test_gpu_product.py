@@ -635,3 +635,41 @@ def test_operands_of_odd_widths_amid_nan(size, offset, kind):
     for got, key in ((dx, "dX"), (dwg, "dWg"), (dwu, "dWu"), (db, "dbg")):
         assert_within(got, *want[key], key)
     assert_padding(dxbuf, wi)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [(3, 259, 8), (1, 40, 24), (2, 15, 593), (60, 100, 200), (1300, 33, 12), (7, 1000, 501)], ids=str)
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+def test_gradients_of_few_elements_keep_two_terms(size, name, kind):
+    """Bounds without the rounding of the gradients before the activation: a sum of both terms has twice the products, in parts that are added in fp64."""
+    n, wi, wo = size
+    dtype = TYPES[kind]
+    gen = torch.Generator().manual_seed(15)
+    x, x64 = rows(gen, n, wi, dtype)
+    (wg, wg64), (wu, wu64) = weights(gen, wi, wo, dtype), weights(gen, wi, wo, dtype)
+    g, g64 = rows(gen, n, wo, dtype, wo + 3, std=1.5)
+    u, u64 = rows(gen, n, wo, dtype)
+    d, d64 = rows(gen, n, wo, dtype)
+    dx, dxbuf = result(n, wi, dtype, wi + 1)
+    dwg, dwu = torch.full_like(wg, 777.0), torch.full_like(wu, 777.0)
+    B.slicegcn_product_bwd(x, wg, g, d, workspace(B.slicegcn_product_bwd_workspace_bytes(n, wi, wo, dtype)), dX=dx, dW=dwg, act=ACT[name])
+    want = product_bwd(x64, wg64, g64, d64, 1.0, name, dtype, terms=2)
+    for got, key in ((dx, "dX"), (dwg, "dW")):
+        assert_within(got, *want[key], key)
+    ws = workspace(B.slicegcn_gated_bwd_workspace_bytes(n, wi, wo, dtype))
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, d, ws, dX=dx, dWg=dwg, dWu=dwu, act=ACT[name])
+    want = gated_bwd(x64, wg64, wu64, g64, u64, d64, name, dtype, terms=2)
+    for got, key in ((dx, "dX"), (dwg, "dWg"), (dwu, "dWu")):
+        assert_within(got, *want[key], key)
+    assert_padding(dxbuf, wi)
+    alone = torch.full_like(wu, 777.0)
+    B.slicegcn_gated_bwd(x, wg, wu, g, u, d, ws, dWu=alone, act=ACT[name])
+    assert torch.equal(alone, dwu)
+
+
+def test_gradients_beyond_fp16_stay_infinite():
+    one = lambda v, *shape: torch.full(shape, v, dtype=torch.float16, device="cuda")
+    x, w, g, u, d = one(2.0, 1, 8), one(0.5, 8, 16), one(3.0, 1, 16), one(60.0, 1, 16), one(-60000.0, 1, 16)
+    dx, dwg, dwu = one(0.0, 1, 8), one(0.0, 8, 16), one(0.0, 8, 16)
+    B.slicegcn_gated_bwd(x, w, w, g, u, d, workspace(B.slicegcn_gated_bwd_workspace_bytes(1, 8, 16, torch.float16)), dX=dx, dWg=dwg, dWu=dwu)
+    assert (dwg == -float("inf")).all() and (dx == -float("inf")).all()
