@@ -3,7 +3,7 @@
 //
 // A backward pass first forms the gradients before the activation in one pass over the rows (slope_kernel: dP, or dG and dU, rounded to the rows' type into
 // the workspace; the column sums for the biases from the same values unrounded), then dX as one product (over both dG and dU) and the
-// weights' gradients as one launch.
+// weights' gradients as one launch.  Short passes form both in one launch (paired), narrow layers of 16 bits on many rows everything in one sweep (product_narrow.h).
 #include "product.h"
 
 #include <cmath>
@@ -155,7 +155,7 @@ bool aligned_product(int layouts, const ProductShape &s, const ProductArgs &a)
 int64_t packed_bytes(int64_t rows, int64_t width) { return width % 8 == 0 ? 0 : round_up(rows * round_up(width, 8) * 2, 256); }
 int64_t rows_a(int layouts, const ProductShape &s) { return layouts == PRODUCT_XTG ? s.K : s.M; }
 int64_t rows_b(int layouts, const ProductShape &s) { return layouts == PRODUCT_GWT ? s.N : s.K; }
-// Room for copies of the operands whose width asks for one (`both`: of the M side too, which a backward pass has formed itself for dX)
+// Room for copies of the operands whose width asks for one (a, b: of the M side, of the N side; a backward pass has formed dP itself)
 size_t pack_bytes(int layouts, const ProductShape &s, bool a, bool b)
 {
     if (!long_product(s)) return 0;
