@@ -292,6 +292,12 @@ typedef struct {
 int slicegcn_adamw_step(const slicegcn_adam_tensor *tensors, int32_t count, int32_t states, double lr, double beta1, double beta2, double eps,
                         int32_t step, const float *factor, uint64_t seed, void *stream);
 
+/* The same with the steps counted on the device, so that one that is left out does not count: counter is a DEVICE array of 4, of which counter[0] is the number of steps
+ * taken before (zero to start with; the call adds one unless it leaves the step out) and the others belong to the call.  Calls that share a counter run one after
+ * another.  EINVAL as above, and for a counter that is NULL or not on a boundary of 4 bytes. */
+int slicegcn_adamw_step_counted(const slicegcn_adam_tensor *tensors, int32_t count, int32_t states, double lr, double beta1, double beta2, double eps,
+                                int32_t *counter, const float *factor, uint64_t seed, void *stream);
+
 /* further kinds of slicegcn_profile_entry */
 #define SLICEGCN_PROF_EMBED 11   /* lookup, sort and gradient; width = columns (0: sort) */
 #define SLICEGCN_PROF_RESNORM 12 /* norms around a block, forward and backward; width = columns */

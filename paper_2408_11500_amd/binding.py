@@ -228,6 +228,7 @@ def lib() -> ctypes.CDLL:
         for fn in (L.slicegcn_product_fwd, L.slicegcn_product_bwd, L.slicegcn_gated_fwd, L.slicegcn_gated_bwd):
             fn.argtypes = [vp, vp, vp, sz, vp]
         L.slicegcn_adamw_step.argtypes = [vp, i32, i32, f64, f64, f64, f64, i32, vp, ctypes.c_uint64, vp]
+        L.slicegcn_adamw_step_counted.argtypes = [vp, i32, i32, f64, f64, f64, f64, vp, vp, ctypes.c_uint64, vp]
         L.slicegcn_strerror.argtypes = [ctypes.c_int]
         L.slicegcn_strerror.restype = ctypes.c_char_p
         L.slicegcn_last_error.restype = ctypes.c_char_p
@@ -1003,6 +1004,16 @@ def slicegcn_adamw_step(tensors: AdamList, lr: float, step: int, beta1=0.9, beta
     step, where the states have 8 bits."""
     _check(lib().slicegcn_adamw_step(tensors.array, len(tensors), tensors.states, lr, beta1, beta2, eps, step, _vec(factor, "factor"),
                                      seed & 0xFFFFFFFFFFFFFFFF, _stream()))
+
+
+def slicegcn_adamw_step_counted(tensors: AdamList, lr: float, counter: torch.Tensor, beta1=0.9, beta2=0.999, eps=1e-8,
+                                factor: torch.Tensor | None = None, seed: int = 0):
+    """The same with the steps counted on the device, so that one that ``factor`` leaves out does not count.  ``counter``: int32 [4], whose first
+    element is the number of steps taken before."""
+    if counter.numel() != 4:
+        raise ValueError("counter must have 4 elements")
+    _check(lib().slicegcn_adamw_step_counted(tensors.array, len(tensors), tensors.states, lr, beta1, beta2, eps, _vec(counter, "counter", torch.int32),
+                                             _vec(factor, "factor"), seed & 0xFFFFFFFFFFFFFFFF, _stream()))
 
 
 def slicegcn_profile_reserve(scopes: int):

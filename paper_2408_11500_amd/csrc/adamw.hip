@@ -42,6 +42,7 @@ struct TensorList {
 };
 struct Step {
     const float *factor;
+    const float *counted; // NULL, or 1 / c1 and 1 / c2 where the steps are counted on the device
     float lr, beta1, omb1, beta2, omb2, eps, inv_c1, inv_c2; // omb = 1 - beta, rounded from fp64
     int32_t tensors;
     uint32_t tiles;
@@ -178,11 +179,23 @@ template <int SHIFT, bool SQUARE> __device__ inline codes2 encode(const float (&
     return c;
 }
 
+// One more step taken, where it is taken at all, and its corrections
+__global__ void count_kernel(int32_t *counter, const float *factor, double beta1, double beta2)
+{
+    if (factor && !(*factor > 0.f)) return;
+    const int32_t step = counter[0] < INT32_MAX ? counter[0] + 1 : counter[0];
+    counter[0] = step;
+    float *c = reinterpret_cast<float *>(counter);
+    c[1] = (float)(1.0 / (1.0 - pow(beta1, (double)step)));
+    c[2] = (float)(1.0 / (1.0 - pow(beta2, (double)step)));
+}
+
 template <int STATES> __global__ __launch_bounds__(THREADS) void adamw_kernel(const TensorList list, const Step s)
 {
 #pragma clang fp contract(off)
     const float f = s.factor ? *s.factor : 1.f;
     if (!(f > 0.f)) return;
+    const float inv_c1 = s.counted ? s.counted[0] : s.inv_c1, inv_c2 = s.counted ? s.counted[1] : s.inv_c2;
     int at = 0;
     for (uint32_t tile = blockIdx.x; tile < s.tiles; tile += gridDim.x) {
         int hi = s.tensors; // the tensor that holds the tile: the last one that starts at or before it
@@ -212,7 +225,7 @@ template <int STATES> __global__ __launch_bounds__(THREADS) void adamw_kernel(co
             g[i] = g[i] * f;
             m[i] = m[i] * s.beta1 + g[i] * s.omb1;
             v[i] = v[i] * s.beta2 + (g[i] * g[i]) * s.omb2;
-            const float update = (m[i] * s.inv_c1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * s.inv_c2) + s.eps);
+            const float update = (m[i] * inv_c1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * inv_c2) + s.eps);
             p[i] = p[i] - e.lr_decay * p[i] - s.lr * update;
         }
         if (e.master) store8(e.master + i0, left, p);
@@ -262,17 +275,13 @@ int check(const slicegcn_adam_tensor *ts, int32_t count, int32_t states, double 
     return SLICEGCN_OK;
 }
 
-} // namespace
-} // namespace slicegcn
-
-using namespace slicegcn;
-
-extern "C" int slicegcn_adamw_step(const slicegcn_adam_tensor *ts, int32_t count, int32_t states, double lr, double beta1, double beta2, double eps,
-                                   int32_t step, const float *factor, uint64_t seed, void *stream)
+// counter: NULL where `step` says which step it is
+int adamw(const slicegcn_adam_tensor *ts, int32_t count, int32_t states, double lr, double beta1, double beta2, double eps, int32_t step, int32_t *counter,
+          const float *factor, uint64_t seed, void *stream)
 {
-    if (int rc = check(ts, count, states, lr, beta1, beta2, eps, step)) return rc;
     Step s{};
     s.factor = factor;
+    s.counted = counter ? reinterpret_cast<const float *>(counter) + 1 : nullptr;
     s.lr = (float)lr;
     s.beta1 = (float)beta1;
     s.omb1 = (float)(1.0 - beta1);
@@ -284,6 +293,10 @@ extern "C" int slicegcn_adamw_step(const slicegcn_adam_tensor *ts, int32_t count
     const uint32_t key = (uint32_t)seed * 0x6A09E667u + (uint32_t)(seed >> 32) * 0xBB67AE85u;
     constexpr int64_t MOST_TILES = (int64_t)1 << 31;
     ProfScope prof(SLICEGCN_PROF_ADAMW, count, as_stream(stream));
+    if (counter) {
+        count_kernel<<<1, 1, 0, as_stream(stream)>>>(counter, factor, beta1, beta2);
+        SG_LAUNCH_CHECK();
+    }
     TensorList list;
     int64_t tiles = 0;
     int n = 0;
@@ -320,4 +333,24 @@ extern "C" int slicegcn_adamw_step(const slicegcn_adam_tensor *ts, int32_t count
         tiles += want;
     }
     return flush();
+}
+
+} // namespace
+} // namespace slicegcn
+
+using namespace slicegcn;
+
+extern "C" int slicegcn_adamw_step(const slicegcn_adam_tensor *ts, int32_t count, int32_t states, double lr, double beta1, double beta2, double eps,
+                                   int32_t step, const float *factor, uint64_t seed, void *stream)
+{
+    if (int rc = check(ts, count, states, lr, beta1, beta2, eps, step)) return rc;
+    return adamw(ts, count, states, lr, beta1, beta2, eps, step, nullptr, factor, seed, stream);
+}
+
+extern "C" int slicegcn_adamw_step_counted(const slicegcn_adam_tensor *ts, int32_t count, int32_t states, double lr, double beta1, double beta2, double eps,
+                                           int32_t *counter, const float *factor, uint64_t seed, void *stream)
+{
+    if (int rc = check(ts, count, states, lr, beta1, beta2, eps, 1)) return rc;
+    SG_REQUIRE(counter && (reinterpret_cast<uintptr_t>(counter) & 3u) == 0, SLICEGCN_EINVAL, "adamw_step_counted: NULL or misaligned counter");
+    return adamw(ts, count, states, lr, beta1, beta2, eps, 1, counter, factor, seed, stream);
 }

@@ -529,7 +529,8 @@ class AdamW:
     """AdamW (decoupled weight decay, on matrices alone) with a cosine-annealed learning rate over all learnable tensors of the given
     models, which stay where they are: one library call updates them all.  ``state_bits`` = 8: the means are kept as e4m3 numbers with a
     scale per 128 elements, 2 bytes a parameter instead of 8.  Tensors of 16 bits get fp32 masters.  ``max_norm`` as in ``Optimizer``;
-    where the gradients' norm is not finite, an update is left out."""
+    where the gradients' norm is not finite, an update is left out, and does not count among the steps that the means are corrected by
+    (``steps`` holds how many were taken, on the device)."""
 
     def __init__(self, models, lr_max: float, lr_min: float = 0.0, t_max: int = 1, beta1: float = 0.9, beta2: float = 0.999,
                  eps: float = 1e-8, weight_decay: float = 0.01, max_norm: float | None = None, state_bits: int = 32, seed: int = 0):
@@ -556,14 +557,18 @@ class AdamW:
             self.norm, self.factor = (torch.zeros(1, dtype=torch.float32, device=dev) for _ in range(2))
             self.gradients = B.TensorList(self.grads)
             self.norm_ws = torch.empty(B.slicegcn_global_norm_workspace_bytes(self.gradients), dtype=torch.uint8, device=dev)
+            self.counter = torch.zeros(4, dtype=torch.int32, device=dev)
+            self.steps = self.counter[:1]
 
     def step(self, epoch: int) -> float:
         """One update with the learning rate of ``epoch`` (0-based); returns that rate."""
         self.t += 1
         lr = B.slicegcn_cosine_lr(self.lr_max, self.lr_min, epoch, self.t_max)
-        if self.max_norm is not None:
+        if self.max_norm is None:
+            B.slicegcn_adamw_step(self.tensors, lr, self.t, seed=self.seed + self.t, **self.hyper)
+        else:
             B.slicegcn_global_norm(self.gradients, self.norm, self.norm_ws, max_norm=self.max_norm, factor=self.factor)
-        B.slicegcn_adamw_step(self.tensors, lr, self.t, factor=self.factor, seed=self.seed + self.t, **self.hyper)
+            B.slicegcn_adamw_step_counted(self.tensors, lr, self.counter, factor=self.factor, seed=self.seed + self.t, **self.hyper)
         return lr
 
 
