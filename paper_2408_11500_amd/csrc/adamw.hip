@@ -179,6 +179,14 @@ template <int SHIFT, bool SQUARE> __device__ inline codes2 encode(const float (&
     return c;
 }
 
+// The instruction takes a subnormal number for 0, and an update of 1 would become one of sqrt(v) / eps: 10^10 with v = 10^-40 and eps = 10^-30.  So it is given v 2^64 below 2^-96.
+// What it gives for all others is as before.  (v itself is 0 where g^2 is, below some 10^-23 |g|.)
+__device__ inline float root(float v)
+{
+    const bool small = v < 0x1p-96f;
+    return __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? 0x1p-32f : 1.f);
+}
+
 // One more step taken, where it is taken at all, and its corrections
 __global__ void count_kernel(int32_t *counter, const float *factor, double beta1, double beta2)
 {
@@ -225,7 +233,7 @@ template <int STATES> __global__ __launch_bounds__(THREADS) void adamw_kernel(co
             g[i] = g[i] * f;
             m[i] = m[i] * s.beta1 + g[i] * s.omb1;
             v[i] = v[i] * s.beta2 + (g[i] * g[i]) * s.omb2;
-            const float update = (m[i] * inv_c1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * inv_c2) + s.eps);
+            const float update = (m[i] * inv_c1) * __builtin_amdgcn_rcpf(root(v[i] * inv_c2) + s.eps);
             p[i] = p[i] - e.lr_decay * p[i] - s.lr * update;
         }
         if (e.master) store8(e.master + i0, left, p);
