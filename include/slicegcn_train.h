@@ -272,7 +272,8 @@ int slicegcn_gated_bwd(const slicegcn_product_desc *desc, const slicegcn_gated_i
  * tensors: HOST array of contiguous DEVICE tensors; count = 0 and empty tensors are valid; no two of them overlap.  factor: DEVICE scalar (slicegcn_global_norm's), or
  * NULL for 1; where it is not positive (0 or NaN: the norm was infinite or NaN) the step is left out: nothing is written.
  * EINVAL: NULL pointer, count < 0, step < 1, bad tensor (negative or too large count, unknown type, a master of fp32 parameters, no scales with 8 bits, misaligned:
- * every element on a boundary of its size, scales on one of 2 bytes), betas outside [0, 1), eps <= 0, lr or a decay not finite. */
+ * every element on a boundary of its size, scales on one of 2 bytes), betas outside [0, 1), eps below 2^-126, lr, eps or a decay
+ * not finite. */
 #define SLICEGCN_STATES_32 32
 #define SLICEGCN_STATES_8 8
 #define SLICEGCN_STATE_BLOCK 128

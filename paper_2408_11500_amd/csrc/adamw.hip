@@ -15,6 +15,7 @@
 #include "common.h"
 #include "values.h"
 
+#include <cfloat>
 #include <cmath>
 
 namespace slicegcn {
@@ -266,7 +267,8 @@ int check(const slicegcn_adam_tensor *ts, int32_t count, int32_t states, double 
     SG_REQUIRE(states == SLICEGCN_STATES_8 || states == SLICEGCN_STATES_32, SLICEGCN_EINVAL, "adamw_step: states of %d bits", states);
     SG_REQUIRE(step >= 1, SLICEGCN_EINVAL, "adamw_step: step must be >= 1");
     SG_REQUIRE(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0, SLICEGCN_EINVAL, "adamw_step: betas must lie in [0, 1)");
-    SG_REQUIRE(std::isfinite((float)lr) && (float)eps > 0.f && std::isfinite((float)eps), SLICEGCN_EINVAL, "adamw_step: lr must be finite and eps positive");
+    // 1 / eps is a number of fp32 then, and an m of 0 moves nothing where v is 0 too
+    SG_REQUIRE(std::isfinite((float)lr) && (float)eps >= FLT_MIN && std::isfinite((float)eps), SLICEGCN_EINVAL, "adamw_step: lr must be finite and eps at least 2^-126");
     for (int32_t i = 0; i < count; ++i) {
         const slicegcn_adam_tensor &t = ts[i];
         SG_REQUIRE(t.count >= 0 && t.count <= (int64_t)1 << 40, SLICEGCN_EINVAL, "adamw_step: tensor %d has %lld elements", i, (long long)t.count);

@@ -21,3 +21,10 @@ def test_the_binding_refuses_counters_that_do_not_fit():
         B.slicegcn_adamw_step_counted(tensors, 0.1, torch.zeros(1, dtype=torch.int32))
     with pytest.raises(TypeError):
         B.slicegcn_adamw_step_counted(tensors, 0.1, torch.zeros(4, dtype=torch.int32))  # on the host
+
+
+def test_eps_that_has_no_reciprocal_in_fp32_is_refused(L):  # noqa: F811
+    for eps in (1e-40, 1e-38, 2.0 ** -127):
+        assert L.slicegcn_adamw_step(adam(count=0), 1, 32, 0.1, 0.9, 0.999, eps, 1, None, 0, None) == B.EINVAL
+        assert L.slicegcn_adamw_step_counted(adam(count=0), 1, 32, 0.1, 0.9, 0.999, eps, ONE, None, 0, None) == B.EINVAL
+    assert L.slicegcn_adamw_step(adam(count=0), 1, 32, 0.1, 0.9, 0.999, 2.0 ** -126, 1, None, 0, None) == 0

@@ -27,3 +27,10 @@ def test_step(eps, beta1, beta2, step):
     # 16 roundings as for other numbers (square root and reciprocal are good to one place, eps and the corrections are rounded)
     tol = 16 * U * torch.stack([e.abs() for e in (want, *ends)]).amax(0) + (torch.stack([(e - want).abs() for e in ends]).amax(0) if step > 1 or beta2 else 0)
     assert ((-p.cpu().to(F64) - want).abs() <= tol + 2.0 ** -149).all()
+
+
+def test_zeros_stay_with_the_smallest_eps():
+    p, g, m, v = (torch.zeros(100, device="cuda") for _ in range(4))
+    g[1] = 1.0
+    B.slicegcn_adamw_step(B.AdamList([p], [g], [m], [v]), 1.0, 1, eps=2.0 ** -126)
+    assert p[0] == 0 and abs(float(p[1]) + 1) < 16 * U and (p[2:] == 0).all()
