@@ -5,6 +5,7 @@ library calls; every arithmetic step is a kernel of ``libslicegcn.so``.
 """
 from __future__ import annotations
 
+import sys
 from typing import NamedTuple
 
 import torch
@@ -551,7 +552,8 @@ class AdamW:
         self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps)
         self.lr_max, self.lr_min, self.t_max, self.seed = lr_max, lr_min, t_max, seed
         self.t = 0
-        self.max_norm = max_norm
+        # (with an infinite bound a norm that is infinite too would not be beyond it)
+        self.max_norm = None if max_norm is None else min(max_norm, sys.float_info.max)
         self.factor = None
         if max_norm is not None:
             self.norm, self.factor = (torch.zeros(1, dtype=torch.float32, device=dev) for _ in range(2))

@@ -90,3 +90,17 @@ def test_without_a_factor_every_step_counts():
     for i in range(3):
         B.slicegcn_adamw_step_counted(B.AdamList([p], [g], [m], [v]), 0.1, counter)
         assert int(counter[0]) == i + 1
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_without_a_bound_on_the_norm_updates_on_gradients_that_are_not_finite_are_left_out_too(bad):
+    m, same = Model(), Model()
+    opt, plain = AdamW([m], lr_max=0.1, max_norm=float("inf")), AdamW([same], lr_max=0.1)
+    before, good = m.w.clone(), m.g.clone()
+    m.g[3, 4] = bad
+    opt.step(0)
+    assert torch.equal(m.w, before) and int(opt.steps) == 0
+    m.g.copy_(good)
+    opt.step(0)
+    plain.step(0)
+    assert torch.equal(m.w, same.w) and int(opt.steps) == 1
