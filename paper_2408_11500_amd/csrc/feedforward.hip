@@ -416,11 +416,13 @@ SlopeGrid slope_grid(int64_t n, int32_t w, int32_t type)
 
 // Whether a backward pass may go in one sweep over the rows, by its sizes, and with how many workgroups (0: it may not).  Many rows, since every workgroup leaves a
 // dW of its own: 100 -> 256 columns bf16 gelu, 8192 rows 30 us, 22 in the general form; 16384 rows 28 and 37; 2.4 M rows 0.95 and 1.83 ms.
+// Each has at most CHAIN blocks of rows, so that its sums are as short as those of the other forms: one workgroup a CU up to 8.4 M rows, then some each.
 constexpr int64_t NARROW_LEAST = 16384;
 unsigned narrow_blocks(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q)
 {
     if (type == SLICEGCN_F32 || w_in > NARROW_WIDTH_IN || w_out * q > NARROW_WIDTH_OUT || w_in % 2 || w_out % 2 || n < NARROW_LEAST) return 0;
-    return CUS;
+    const int64_t rows = CHAIN * NARROW_ROWS * CUS;
+    return (unsigned)((n + rows - 1) / rows * CUS);
 }
 // ... and by how its rows lie: on boundaries of 4 bytes
 bool narrow_rows_fit(const Operand &o) { return !o.p || ((reinterpret_cast<uintptr_t>(o.p) & 3u) == 0 && o.ld % 2 == 0); }

@@ -109,6 +109,7 @@ int launch_pair_f16(ProductArgs *x, ProductArgs *w, const BiasSums &bias, hipStr
 
 // product_narrow.h: a backward pass in one sweep over the rows
 constexpr int NARROW_WIDTH_IN = 128, NARROW_WIDTH_OUT = 256; // at most; of all products together
+constexpr int NARROW_ROWS = 32;                              // of a block
 constexpr int NARROW_RUN = 32;                               // blocks of rows whose column sums a thread adds in fp32
 struct NarrowArgs {
     Operand x, w[2], g, u, d; // as in a backward pass

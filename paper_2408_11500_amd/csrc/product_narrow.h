@@ -10,7 +10,7 @@
 // wavefront's 64 x 64.  Nothing in the loop branches on a lane: rows and columns that are not there are read as zeros and not written by the buffers' range checks, so
 // that the compiler can count the loads in flight.
 // 2.4 M rows 100 -> 256 bf16 gelu: 0.95 ms, 3.7 TB/s; bound by the arithmetic of the gelu's slope (some 35 instructions an element).
-// Order of the sums: a workgroup's blocks in turn, the workgroups' sums in fp64 in order.
+// Order of the sums: a workgroup's blocks in turn (1024 at most), the workgroups' sums in fp64 in order.
 #pragma once
 
 #include "product_kernels.h"
@@ -18,7 +18,7 @@
 namespace slicegcn {
 namespace {
 
-constexpr int NARROW_THREADS = 512, NARROW_ROWS = 32, NARROW_X = NARROW_WIDTH_IN / 8, NARROW_G = NARROW_WIDTH_OUT / 8; // units of 8 columns
+constexpr int NARROW_THREADS = 512, NARROW_X = NARROW_WIDTH_IN / 8, NARROW_G = NARROW_WIDTH_OUT / 8; // units of 8 columns
 
 // A block's rows of a matrix as a buffer
 __device__ inline __amdgpu_buffer_rsrc_t rows_buffer(const char *p, int64_t ld, int64_t row0, int64_t n, int32_t w)
