@@ -81,3 +81,46 @@ def check(n, wi, wo, dtype, relu, seed=0, ld=0, forward=True, gated=True):
 @pytest.mark.parametrize("size", [(1024 * 32 * 256 + 1, 4, 8), (1024 * 32 * 256 + 32 * 256 + 5, 34, 6), (3 * 1024 * 32 * 256 - 31, 2, 2)], ids=str)
 def test_one_sweep_over_more_rows_than_a_workgroup_a_cu_takes(size, kind):
     check(*size, TYPES[kind], True, forward=False)
+
+
+# through registers in each tile shape, with sums whole and cut, on whole units, even and odd widths; few rows in strips; both products in one launch
+SIZES = [(1, 1, 1), (1, 64, 96), (1, 4104, 136), (3, 7, 5), (16, 40, 64), (17, 2304, 72), (24, 1024, 200), (32, 2048, 1001), (33, 65, 129), (65, 72, 200), (128, 1000, 40),
+         (257, 520, 384), (300, 264, 520), (300, 1003, 71), (1000, 72, 40), (2048, 64, 170), (2049, 512, 128), (5000, 24, 8), (5000, 1001, 333), (16_383, 100, 256),
+         (9000, 700, 260)]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("relu", [False, True])
+def test_short_and_middling_products(size, relu, kind):
+    check(*size, TYPES[kind], relu, seed=SIZES.index(size), ld=(0, 3, 8)[SIZES.index(size) % 3])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("size", [(16_384, 100, 256), (16_385, 100, 128), (33_333, 72, 40), (20_011, 128, 126), (17_000, 6, 2), (60_001, 34, 250)], ids=str)
+@pytest.mark.parametrize("relu", [False, True])
+def test_narrow_layers_of_many_rows(size, relu, kind):
+    check(*size, TYPES[kind], relu, ld=2)
+
+
+# tiles of 256 x 256: sums cut, whole, of an odd number of steps, a last round cut along k in dX, in one dW and in both, sums over many rows, operands that are copied
+LONG = [(513, 5000, 4104), (20_000, 72, 7000), (2500, 2056, 2000), (4100, 4400, 4616), (4100, 4400, 3768), (8200, 9064, 136), (2050, 2003, 2521), (9001, 1026, 1101), (40_000, 512, 520)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("size", LONG, ids=str)
+@pytest.mark.parametrize("relu", [False, True])
+def test_long_products(size, relu, kind):
+    check(*size, TYPES[kind], relu, seed=LONG.index(size))
+
+
+# widths in whole units, rows that are none: leading dimensions and bases off 16 bytes
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("size,ld", [((2500, 2056, 2000), 1), ((2500, 2056, 2000), 4), ((4100, 2400, 1808), 3)], ids=str)
+def test_long_products_of_rows_that_lie_oddly_at_widths_in_whole_units(size, ld, kind):
+    check(*size, TYPES[kind], True, ld=ld)
+
+
+@pytest.mark.parametrize("size", [(60_000, 300, 130), (3000, 1200, 700)], ids=str)
+def test_fp32_in_large_tiles(size):
+    check(*size, torch.float32, True, ld=1)
