@@ -236,13 +236,15 @@ bool product_on_words(int layouts, const ProductShape &s, const ProductArgs &a)
     }
 }
 
-// partial, room: parts of the workspace, for sums of parts of k and for copies of operands
-int launch_product(const ProductShape &s, int layouts, int epilogue, ProductArgs &a, void *partial, char *room, hipStream_t stream)
+// partial, room: parts of the workspace, for sums of parts of k and for copies of operands.  first_alone: the first set of two that s describes, without the second
+int launch_product(const ProductShape &s, int layouts, int epilogue, ProductArgs &a, void *partial, char *room, hipStream_t stream, bool first_alone = false)
 {
     const int32_t type = s.type;
     a.partial = static_cast<float *>(partial);
     if (int rc = pack_operands(layouts, s, a, room, stream)) return rc;
-    const ProductPlan plan = plan_product(s, aligned_product(layouts, s, a));
+    ProductPlan plan = plan_product(s, aligned_product(layouts, s, a));
+    // the tail is of the second set: of 2 t tiles, more than CUS, 2 t mod CUS are no more than t
+    if (first_alone) plan.tail = 0;
     a.on_words = product_on_words(layouts, s, a);
     return type == SLICEGCN_F32    ? launch_product_f32(layouts, epilogue, plan, a, stream)
            : type == SLICEGCN_BF16 ? launch_product_bf16(layouts, epilogue, plan, a, stream)
@@ -563,7 +565,7 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
     const Operand dx{static_cast<const char *>(c.dx.data), c.dx.ld, 0};
     const unsigned narrow = narrow_blocks(d.n, d.w_in, d.w_out, d.type, q);
     if (narrow && (want_x || want_w) && !want_r && narrow_rows_fit(c.x) && narrow_rows_fit(c.g) && narrow_rows_fit(c.u) && narrow_rows_fit(c.dy) &&
-        narrow_rows_fit(dx) && (q == 1 || !want_w || (c.dw[0] && c.dw[1]))) {
+        narrow_rows_fit(dx)) {
         NarrowArgs a{};
         a.x = c.x;
         a.w[0] = c.w[0];
@@ -579,16 +581,17 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         a.want_w = want_w;
         a.partial = partial;
         a.columns = s.partial;
+        // one of two dW alone: the sums of both are formed, and its are joined
         ProductArgs join{};
+        join.partial = c.dw[0] ? partial : partial + (int64_t)narrow * d.w_in * d.w_out;
         for (int i = 0; i < q; ++i) {
-            join.out[i] = static_cast<char *>(c.dw[i]);
-            join.ldo[i] = d.w_out;
+            if (!c.dw[i]) continue;
+            join.out[join.sets] = static_cast<char *>(c.dw[i]);
+            join.ldo[join.sets++] = d.w_out;
         }
         join.M = d.w_in;
         join.N = d.w_out;
-        join.sets = q;
         join.splits = (int32_t)narrow;
-        join.partial = partial;
         const auto launch = d.type == SLICEGCN_BF16 ? launch_narrow_bf16 : launch_narrow_f16;
         if (int rc = launch(a, join, d.act, q == 2, narrow, stream)) return rc;
         return launch_bias(BiasSums{s.partial, (int32_t)narrow, q, d.w_out, {c.db[0], c.db[1]}}, stream);
@@ -657,7 +660,7 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
     if (want_x)
         if (int rc = launch_product(shape_x, PRODUCT_GWT, EPI_STORE, x, partial, room, stream)) return rc;
     if (want_w)
-        if (int rc = launch_product(shape_w, PRODUCT_XTG, EPI_STORE, y, partial, room, stream)) return rc;
+        if (int rc = launch_product(shape_w, PRODUCT_XTG, EPI_STORE, y, partial, room, stream, q == 2 && !c.dw[1])) return rc;
     return SLICEGCN_OK;
 }
 
