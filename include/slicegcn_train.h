@@ -233,7 +233,7 @@ typedef struct {
 
 /* P = X W + b;  Y = residual * R + act(P).  b, R, P may be absent; P is kept for the backward pass, which needs it where there is an activation.
  * EINVAL: NULL descriptor, io, X, W or Y; n < 0, widths < 1, ld < width, unknown type or activation, misaligned base, residual not finite,
- * an output at the address of another operand; ERANGE: n, a width or an ld (beyond 2^21) too large; EWORKSPACE. */
+ * an output at the address of another operand; ERANGE: n, a width or an ld (beyond 2^21, of more than one row) too large; EWORKSPACE. */
 size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type); /* 0 on bad input, and where none is needed */
 int slicegcn_product_fwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream);
 

@@ -476,11 +476,12 @@ int check(const char *what, const slicegcn_product_desc *d, const void *io)
     return SLICEGCN_OK;
 }
 
-int check_rows(const char *what, const char *name, const slicegcn_matrix &m, int32_t width, int32_t type, bool needed)
+constexpr int64_t MOST_LD = 1 << 21; // offsets within a tile fit 31 bits
+int check_rows(const char *what, const char *name, const slicegcn_matrix &m, int64_t n, int32_t width, int32_t type, bool needed)
 {
     SG_REQUIRE(!needed || m.data, SLICEGCN_EINVAL, "%s: NULL %s", what, name);
     SG_REQUIRE(!m.data || (m.ld >= width && aligned_for(m.data, type)), SLICEGCN_EINVAL, "%s: %s has an ld smaller than its width, or a misaligned base", what, name);
-    SG_REQUIRE(!m.data || m.ld <= 1 << 21, SLICEGCN_ERANGE, "%s: %s has an ld beyond 2^21", what, name); // offsets within a tile fit 31 bits
+    SG_REQUIRE(!m.data || n <= 1 || m.ld <= MOST_LD, SLICEGCN_ERANGE, "%s: %s has an ld beyond 2^21", what, name);
     return SLICEGCN_OK;
 }
 
@@ -509,7 +510,9 @@ int check_workspace(const char *what, const void *ws, size_t ws_bytes, size_t ne
     return SLICEGCN_OK;
 }
 
-Operand operand(const slicegcn_matrix &m) { return Operand{static_cast<const char *>(m.data), m.ld, 0}; }
+// One row alone (the last token of a long sequence, say) may be said to be any distance from a next one that does not exist
+int64_t ld_of(const slicegcn_matrix &m, int32_t width) { return m.ld <= MOST_LD ? m.ld : width; }
+Operand operand(const slicegcn_matrix &m, int32_t width) { return Operand{static_cast<const char *>(m.data), ld_of(m, width), 0}; }
 Operand weights(const void *w, int32_t w_out) { return Operand{static_cast<const char *>(w), w_out, 0}; }
 
 ProductShape fwd_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, bool gated) { return ProductShape{n, w_in, w_out, 1, 1, type, gated, true}; }
@@ -680,10 +683,10 @@ extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const sliceg
     const char *what = "product_fwd";
     if (int rc = check(what, d, io)) return rc;
     SG_REQUIRE(io->W, SLICEGCN_EINVAL, "%s: NULL W", what);
-    if (int rc = check_rows(what, "X", io->X, d->w_in, d->type, true)) return rc;
-    if (int rc = check_rows(what, "Y", io->Y, d->w_out, d->type, true)) return rc;
-    if (int rc = check_rows(what, "R", io->R, d->w_out, d->type, false)) return rc;
-    if (int rc = check_rows(what, "P", io->P, d->w_out, d->type, false)) return rc;
+    if (int rc = check_rows(what, "X", io->X, d->n, d->w_in, d->type, true)) return rc;
+    if (int rc = check_rows(what, "Y", io->Y, d->n, d->w_out, d->type, true)) return rc;
+    if (int rc = check_rows(what, "R", io->R, d->n, d->w_out, d->type, false)) return rc;
+    if (int rc = check_rows(what, "P", io->P, d->n, d->w_out, d->type, false)) return rc;
     if (int rc = check_params(what, d->type, {io->W}, {io->b})) return rc;
     if (d->n == 0) return SLICEGCN_OK;
     if (int rc = check_apart(what, {io->Y.data, io->P.data}, {io->X.data, io->W, io->b})) return rc;
@@ -692,18 +695,18 @@ extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const sliceg
     const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, false);
     if (int rc = check_workspace(what, ws, ws_bytes, fwd_bytes(shape))) return rc;
     ProductArgs a{};
-    a.a[0] = operand(io->X);
+    a.a[0] = operand(io->X, d->w_in);
     a.b[0] = weights(io->W, d->w_out);
     a.M = d->n;
     a.K = d->w_in;
     a.N = d->w_out;
     a.segments = a.sets = 1;
     a.out[0] = static_cast<char *>(io->Y.data);
-    a.ldo[0] = io->Y.ld;
+    a.ldo[0] = ld_of(io->Y, d->w_out);
     a.bias[0] = io->b;
-    a.r = operand(io->R);
+    a.r = operand(io->R, d->w_out);
     a.keep[0] = static_cast<char *>(io->P.data);
-    a.ldk[0] = io->P.ld;
+    a.ldk[0] = ld_of(io->P, d->w_out);
     a.residual = (float)d->residual;
     a.act = d->act;
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d->w_out, as_stream(stream));
@@ -721,23 +724,23 @@ extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *d, const sliceg
     const char *what = "product_bwd";
     if (int rc = check(what, d, io)) return rc;
     const bool rows = d->n > 0, slope = d->act != SLICEGCN_ACT_NONE && (io->dX.data || io->dW || io->db);
-    if (int rc = check_rows(what, "X", io->X, d->w_in, d->type, rows && io->dW)) return rc;
-    if (int rc = check_rows(what, "P", io->P, d->w_out, d->type, rows && slope)) return rc;
-    if (int rc = check_rows(what, "dY", io->dY, d->w_out, d->type, rows)) return rc;
-    if (int rc = check_rows(what, "dX", io->dX, d->w_in, d->type, false)) return rc;
-    if (int rc = check_rows(what, "dR", io->dR, d->w_out, d->type, false)) return rc;
+    if (int rc = check_rows(what, "X", io->X, d->n, d->w_in, d->type, rows && io->dW)) return rc;
+    if (int rc = check_rows(what, "P", io->P, d->n, d->w_out, d->type, rows && slope)) return rc;
+    if (int rc = check_rows(what, "dY", io->dY, d->n, d->w_out, d->type, rows)) return rc;
+    if (int rc = check_rows(what, "dX", io->dX, d->n, d->w_in, d->type, false)) return rc;
+    if (int rc = check_rows(what, "dR", io->dR, d->n, d->w_out, d->type, false)) return rc;
     SG_REQUIRE(io->W || !io->dX.data || !rows, SLICEGCN_EINVAL, "%s: NULL W", what);
     if (int rc = check_params(what, d->type, {io->W, io->dW}, {io->db})) return rc;
     if (rows)
         if (int rc = check_apart(what, {io->dX.data, io->dW, io->db, io->dR.data}, {io->X.data, io->W, io->P.data, io->dY.data})) return rc;
     BwdCall c{};
     c.d = d;
-    c.x = operand(io->X);
+    c.x = operand(io->X, d->w_in);
     c.w[0] = weights(io->W, d->w_out);
-    c.g = operand(io->P);
-    c.dy = operand(io->dY);
-    c.dx = io->dX;
-    c.dr = io->dR;
+    c.g = operand(io->P, d->w_out);
+    c.dy = operand(io->dY, d->w_out);
+    c.dx = slicegcn_matrix{io->dX.data, ld_of(io->dX, d->w_in)};
+    c.dr = slicegcn_matrix{io->dR.data, ld_of(io->dR, d->w_out)};
     c.dw[0] = io->dW;
     c.db[0] = io->db;
     return backward(what, c, 1, ws, ws_bytes, as_stream(stream));
@@ -754,10 +757,10 @@ extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn
     const char *what = "gated_fwd";
     if (int rc = check(what, d, io)) return rc;
     SG_REQUIRE(io->Wg && io->Wu, SLICEGCN_EINVAL, "%s: NULL Wg or Wu", what);
-    if (int rc = check_rows(what, "X", io->X, d->w_in, d->type, true)) return rc;
-    if (int rc = check_rows(what, "H", io->H, d->w_out, d->type, true)) return rc;
-    if (int rc = check_rows(what, "G", io->G, d->w_out, d->type, false)) return rc;
-    if (int rc = check_rows(what, "U", io->U, d->w_out, d->type, false)) return rc;
+    if (int rc = check_rows(what, "X", io->X, d->n, d->w_in, d->type, true)) return rc;
+    if (int rc = check_rows(what, "H", io->H, d->n, d->w_out, d->type, true)) return rc;
+    if (int rc = check_rows(what, "G", io->G, d->n, d->w_out, d->type, false)) return rc;
+    if (int rc = check_rows(what, "U", io->U, d->n, d->w_out, d->type, false)) return rc;
     SG_REQUIRE(!io->G.data == !io->U.data, SLICEGCN_EINVAL, "%s: G without U, or U without G", what);
     if (int rc = check_params(what, d->type, {io->Wg, io->Wu}, {io->bg, io->bu})) return rc;
     if (d->n == 0) return SLICEGCN_OK;
@@ -765,7 +768,7 @@ extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn
     const ProductShape shape = fwd_shape(d->n, d->w_in, d->w_out, d->type, true);
     if (int rc = check_workspace(what, ws, ws_bytes, fwd_bytes(shape))) return rc;
     ProductArgs a{};
-    a.a[0] = operand(io->X);
+    a.a[0] = operand(io->X, d->w_in);
     a.b[0] = weights(io->Wg, d->w_out);
     a.b[1] = weights(io->Wu, d->w_out);
     a.M = d->n;
@@ -773,13 +776,13 @@ extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn
     a.N = d->w_out;
     a.segments = a.sets = 1;
     a.out[0] = static_cast<char *>(io->H.data);
-    a.ldo[0] = io->H.ld;
+    a.ldo[0] = ld_of(io->H, d->w_out);
     a.bias[0] = io->bg;
     a.bias[1] = io->bu;
     a.keep[0] = static_cast<char *>(io->G.data);
-    a.ldk[0] = io->G.ld;
+    a.ldk[0] = ld_of(io->G, d->w_out);
     a.keep[1] = static_cast<char *>(io->U.data);
-    a.ldk[1] = io->U.ld;
+    a.ldk[1] = ld_of(io->U, d->w_out);
     a.act = d->act;
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d->w_out, as_stream(stream));
     return launch_product(shape, PRODUCT_XW, EPI_GATED, a, ws, static_cast<char *>(ws) + partial_bytes(shape), as_stream(stream));
@@ -796,24 +799,24 @@ extern "C" int slicegcn_gated_bwd(const slicegcn_product_desc *d, const slicegcn
     const char *what = "gated_bwd";
     if (int rc = check(what, d, io)) return rc;
     const bool rows = d->n > 0;
-    if (int rc = check_rows(what, "X", io->X, d->w_in, d->type, rows && (io->dWg || io->dWu))) return rc;
-    if (int rc = check_rows(what, "G", io->G, d->w_out, d->type, rows)) return rc;
-    if (int rc = check_rows(what, "U", io->U, d->w_out, d->type, rows)) return rc;
-    if (int rc = check_rows(what, "dH", io->dH, d->w_out, d->type, rows)) return rc;
-    if (int rc = check_rows(what, "dX", io->dX, d->w_in, d->type, false)) return rc;
+    if (int rc = check_rows(what, "X", io->X, d->n, d->w_in, d->type, rows && (io->dWg || io->dWu))) return rc;
+    if (int rc = check_rows(what, "G", io->G, d->n, d->w_out, d->type, rows)) return rc;
+    if (int rc = check_rows(what, "U", io->U, d->n, d->w_out, d->type, rows)) return rc;
+    if (int rc = check_rows(what, "dH", io->dH, d->n, d->w_out, d->type, rows)) return rc;
+    if (int rc = check_rows(what, "dX", io->dX, d->n, d->w_in, d->type, false)) return rc;
     SG_REQUIRE((io->Wg && io->Wu) || !io->dX.data || !rows, SLICEGCN_EINVAL, "%s: NULL Wg or Wu", what);
     if (int rc = check_params(what, d->type, {io->Wg, io->Wu, io->dWg, io->dWu}, {io->dbg, io->dbu})) return rc;
     if (rows)
         if (int rc = check_apart(what, {io->dX.data, io->dWg, io->dWu, io->dbg, io->dbu}, {io->X.data, io->Wg, io->Wu, io->G.data, io->U.data, io->dH.data})) return rc;
     BwdCall c{};
     c.d = d;
-    c.x = operand(io->X);
+    c.x = operand(io->X, d->w_in);
     c.w[0] = weights(io->Wg, d->w_out);
     c.w[1] = weights(io->Wu, d->w_out);
-    c.g = operand(io->G);
-    c.u = operand(io->U);
-    c.dy = operand(io->dH);
-    c.dx = io->dX;
+    c.g = operand(io->G, d->w_out);
+    c.u = operand(io->U, d->w_out);
+    c.dy = operand(io->dH, d->w_out);
+    c.dx = slicegcn_matrix{io->dX.data, ld_of(io->dX, d->w_in)};
     c.dw[0] = io->dWg;
     c.dw[1] = io->dWu;
     c.db[0] = io->dbg;
