@@ -176,8 +176,8 @@ int slicegcn_adam_step_scaled(float *param, const float *grad, const float *fact
 /* ---------------------------------------------------------------------------------------
  * Products of rows with a weight matrix, and feed-forward blocks.  Rows, weights and the weights' gradients are of one type (fp32, bf16 or
  * fp16); biases and their gradients are fp32.  Sums are fp32 on the matrix cores, and a result is rounded once; fp32 operands go
- * through them as three 16-bit terms each (a relative error of 2^-22 of a product at most; an operand that is infinite, or above 2^128 (1 - 2^-9), makes its
- * sums NaN).
+ * through them as three 16-bit terms each (a relative error of 2^-22 of a product at most; of an operand below 2^-110 what lies below 2^-134 is lost too; an
+ * operand that is infinite, or above 2^128 (1 - 2^-9), makes its sums NaN).
  *   X: n x w_in;  W, Wg, Wu: w_in x w_out, contiguous;  all other matrices have n rows, of w_out columns (dX: of w_in)
  *   act: SLICEGCN_ACT_NONE v;  _RELU max(v, 0);  _SILU v / (1 + exp(-v));  _GELU v Phi(v), Phi the normal distribution
  * n = 0 is a valid batch (gradients of weights and biases are zeros then).  Outputs overlap nothing else of the call, with one exception: Y may
@@ -238,7 +238,8 @@ size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_o
 int slicegcn_product_fwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream);
 
 /* dP = dY * act'(P);  dX = dP W^T;  dW = X^T dP;  db = column sums of dP;  dR = residual * dY.  Absent outputs are not formed (the inputs that only they
- * need may be absent too).  dP is rounded to the rows' type before the products (short passes keep it in two terms); db is formed from it unrounded.
+ * need may be absent too).  dP is rounded to the rows' type before the products (short passes keep it in two terms); db is formed from it unrounded.  So what is
+ * beyond the type's range in dP is infinite in dX and dW (fp16: above 65504, which a smaller factor of the loss avoids), and what is below it is lost; rows of fp32 keep dP whole.
  * EINVAL, ERANGE, EWORKSPACE as above. */
 size_t slicegcn_product_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
 int slicegcn_product_bwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream);
@@ -250,7 +251,7 @@ size_t slicegcn_gated_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out
 int slicegcn_gated_fwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream);
 
 /* dG = dH * U * act'(G);  dU = dH * act(G);  dX = dG Wg^T + dU Wu^T;  dWg = X^T dG;  dWu = X^T dU;  dbg, dbu: column sums.  Absent outputs are not
- * formed.  dG and dU are rounded to the rows' type before the products (short passes keep them in two terms); dbg and dbu are formed from them
+ * formed.  dG and dU are rounded to the rows' type before the products (short passes keep them in two terms), with the range of dP above; dbg and dbu are formed from them
  * unrounded. */
 size_t slicegcn_gated_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
 int slicegcn_gated_bwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream);
