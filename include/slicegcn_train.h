@@ -186,11 +186,14 @@ int slicegcn_adam_step_scaled(float *param, const float *grad, const float *fact
  * graphs that may run at the same time too). */
 #define SLICEGCN_ACT_SILU 2
 #define SLICEGCN_ACT_GELU 3
+/* Added to the type of a call's descriptor and of its query: a backward pass keeps the gradients before the activation in two terms of the type, whose sum is within 2^-16 (bf16) or
+ * 2^-22 (fp16, and 2^-25 by itself) of them, for twice the products.  Nothing else changes by it. */
+#define SLICEGCN_TWO_TERMS 0x100
 typedef struct {
     int64_t n;    /* at most 2^31 - 2^16 */
     int32_t w_in; /* both widths: at most 2^20 */
     int32_t w_out;
-    int32_t type;
+    int32_t type; /* with or without SLICEGCN_TWO_TERMS */
     int32_t act;
     double residual; /* factor of R; products alone */
 } slicegcn_product_desc;
@@ -238,7 +241,8 @@ size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_o
 int slicegcn_product_fwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream);
 
 /* dP = dY * act'(P);  dX = dP W^T;  dW = X^T dP;  db = column sums of dP;  dR = residual * dY.  Absent outputs are not formed (the inputs that only they
- * need may be absent too).  dP is rounded to the rows' type before the products (short passes keep it in two terms); db is formed from it unrounded.  So what is
+ * need may be absent too).  dP is rounded to the rows' type before the products (short passes, and those with SLICEGCN_TWO_TERMS, keep it in two terms); db is formed
+ * from it unrounded.  What is
  * beyond the type's range in dP is infinite in dX and dW (fp16: above 65504, which a smaller factor of the loss avoids), and what is below it is lost; rows of fp32 keep dP whole.
  * EINVAL, ERANGE, EWORKSPACE as above. */
 size_t slicegcn_product_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
@@ -251,7 +255,7 @@ size_t slicegcn_gated_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out
 int slicegcn_gated_fwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream);
 
 /* dG = dH * U * act'(G);  dU = dH * act(G);  dX = dG Wg^T + dU Wu^T;  dWg = X^T dG;  dWu = X^T dU;  dbg, dbu: column sums.  Absent outputs are not
- * formed.  dG and dU are rounded to the rows' type before the products (short passes keep them in two terms), with the range of dP above; dbg and dbu are formed from them
+ * formed.  dG and dU are rounded to the rows' type before the products (or kept in two terms, as dP is), with the range of dP above; dbg and dbu are formed from them
  * unrounded. */
 size_t slicegcn_gated_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type);
 int slicegcn_gated_bwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream);

@@ -30,6 +30,7 @@ ACT_NONE = 0
 ACT_RELU = 1
 ACT_SILU = 2  # products and gated projections
 ACT_GELU = 3
+TWO_TERMS = 0x100
 LAYER_Z_VALID = 1
 LAYER_TRANSFORM_FIRST = 2
 LAYER_ORDER_AUTO = 4
@@ -890,10 +891,10 @@ def _weights(t, name: str, shape, dtype):
     return t.data_ptr()
 
 
-def _workspace_bytes(fn, n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
+def _workspace_bytes(fn, n: int, w_in: int, w_out: int, dtype: torch.dtype, two_terms: bool = False) -> int:
     if dtype not in VALUE_TYPES:
         raise TypeError(f"expected fp32, bf16 or fp16, not {dtype}")
-    return int(fn(n, w_in, w_out, VALUE_TYPES[dtype]))
+    return int(fn(n, w_in, w_out, VALUE_TYPES[dtype] | (TWO_TERMS if two_terms else 0)))
 
 
 def slicegcn_product_fwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
@@ -911,16 +912,18 @@ def slicegcn_product_fwd(X, W, Y, ws=None, b=None, R=None, P=None, act: int = AC
     return Y
 
 
-def slicegcn_product_bwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
-    return _workspace_bytes(lib().slicegcn_product_bwd_workspace_bytes, n, w_in, w_out, dtype)
+def slicegcn_product_bwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype, two_terms: bool = False) -> int:
+    return _workspace_bytes(lib().slicegcn_product_bwd_workspace_bytes, n, w_in, w_out, dtype, two_terms)
 
 
-def slicegcn_product_bwd(X, W, P, dY, ws=None, dX=None, dW=None, db=None, dR=None, act: int = ACT_NONE, residual: float = 1.0):
+def slicegcn_product_bwd(X, W, P, dY, ws=None, dX=None, dW=None, db=None, dR=None, act: int = ACT_NONE, residual: float = 1.0,
+                         two_terms: bool = False):
     """dP = dY * act'(P);  dX = dP W^T;  dW = X^T dP;  db (fp32) = column sums of dP;  dR = residual * dY.  Gradients that are None are not
-    formed; ``P`` is needed where there is an activation, ``X`` for dW."""
+    formed; ``P`` is needed where there is an activation, ``X`` for dW.  ``two_terms``: a dP of 16 bits is kept in two terms rather than rounded once, for
+    twice the products (the workspace's size has to be that of ``two_terms`` then)."""
     (w_in, w_out), wsh, dtype, ys = W.shape, W.shape, W.dtype, dY.shape
     xs = (ys[0], w_in)
-    desc = _PRODUCT_DESC.pack(ys[0], w_in, w_out, _value_type(W, "W"), act, residual)
+    desc = _PRODUCT_DESC.pack(ys[0], w_in, w_out, _value_type(W, "W") | (TWO_TERMS if two_terms else 0), act, residual)
     io = _PRODUCT_IO.pack(*_rows(X, "X", xs, dtype), _weights(W, "W", wsh, dtype), 0, 0, 0, *_rows(P, "P", ys, dtype), 0, 0,
                           *_rows(dY, "dY", (ys[0], w_out), dtype), *_rows(dX, "dX", xs, dtype), _weights(dW, "dW", wsh, dtype),
                           _columns(db, "db", w_out), *_rows(dR, "dR", ys, dtype))
@@ -943,15 +946,17 @@ def slicegcn_gated_fwd(X, Wg, Wu, H, ws=None, bg=None, bu=None, G=None, U=None, 
     return H
 
 
-def slicegcn_gated_bwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype) -> int:
-    return _workspace_bytes(lib().slicegcn_gated_bwd_workspace_bytes, n, w_in, w_out, dtype)
+def slicegcn_gated_bwd_workspace_bytes(n: int, w_in: int, w_out: int, dtype: torch.dtype, two_terms: bool = False) -> int:
+    return _workspace_bytes(lib().slicegcn_gated_bwd_workspace_bytes, n, w_in, w_out, dtype, two_terms)
 
 
-def slicegcn_gated_bwd(X, Wg, Wu, G, U, dH, ws=None, dX=None, dWg=None, dWu=None, dbg=None, dbu=None, act: int = ACT_SILU):
-    """Gradients of slicegcn_gated_fwd from ``dH`` and the G and U that it kept; those that are None are not formed."""
+def slicegcn_gated_bwd(X, Wg, Wu, G, U, dH, ws=None, dX=None, dWg=None, dWu=None, dbg=None, dbu=None, act: int = ACT_SILU,
+                       two_terms: bool = False):
+    """Gradients of slicegcn_gated_fwd from ``dH`` and the G and U that it kept; those that are None are not formed.  ``two_terms``: as in
+    slicegcn_product_bwd."""
     (w_in, w_out), wsh, dtype, ys = Wg.shape, Wg.shape, Wg.dtype, dH.shape
     xs = (ys[0], w_in)
-    desc = _PRODUCT_DESC.pack(ys[0], w_in, w_out, _value_type(Wg, "Wg"), act, 0.0)
+    desc = _PRODUCT_DESC.pack(ys[0], w_in, w_out, _value_type(Wg, "Wg") | (TWO_TERMS if two_terms else 0), act, 0.0)
     io = _GATED_IO.pack(*_rows(X, "X", xs, dtype), _weights(Wg, "Wg", wsh, dtype), _weights(Wu, "Wu", wsh, dtype), 0, 0,
                         *_rows(G, "G", ys, dtype), *_rows(U, "U", ys, dtype), 0, 0, *_rows(dH, "dH", (ys[0], w_out), dtype),
                         *_rows(dX, "dX", xs, dtype), _weights(dWg, "dWg", wsh, dtype), _weights(dWu, "dWu", wsh, dtype),

@@ -125,9 +125,11 @@ ProductPlan pair_plan(const ProductShape &s)
 // Whether the gradients before the activation are kept in two 16-bit terms: where there are so few of them that the errors of rounding them do not level out over a sum, and both
 // products of them share a launch, in which the second term costs little (3 rows 2595 -> 8 gated bf16 gelu: errors of dX and dW 0.0031 of their norms in one term, 0.0017 in two).
 constexpr int64_t TERMS_MOST = (int64_t)1 << 15; // elements
-int terms_of(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q)
+// Elsewhere a caller may ask for them, for twice the products (in one sweep over narrow layers they would need more registers than there are: 2.4 M rows 100 -> 256 bf16 gelu
+// 0.96 ms in one term, 1.40 in two; gated 100 -> 128 0.69 and 1.87).
+int terms_of(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q, bool two)
 {
-    return type != SLICEGCN_F32 && n * w_out * q <= TERMS_MOST && paired(n, w_in, w_out, type, q) ? 2 : 1;
+    return type != SLICEGCN_F32 && (two || (n * w_out * q <= TERMS_MOST && paired(n, w_in, w_out, type, q))) ? 2 : 1;
 }
 
 // What a call may need, however its operands lie
@@ -249,6 +251,81 @@ int launch_product(const ProductShape &s, int layouts, int epilogue, ProductArgs
     return type == SLICEGCN_F32    ? launch_product_f32(layouts, epilogue, plan, a, stream)
            : type == SLICEGCN_BF16 ? launch_product_bf16(layouts, epilogue, plan, a, stream)
                                    : launch_product_f16(layouts, epilogue, plan, a, stream);
+}
+
+// Products of gradients in two terms: the sums of either term's products, whole or in parts of k, are parts that are joined.  Each dW by itself; dX some rows at a time,
+// so that the parts stay bounded.  Bound as the products are, of which there are twice as many, and by the parts' bytes: 8192 rows 4096 -> 10240 gated bf16 5.04 ms (one term 2.28; errors of
+// dX and dW 0.0017 of their norms, 0.0023), 2.4 M rows 100 -> 256 gelu 3.79 ms (in one sweep and one term 0.96), 2048 rows 64 -> 170 gated 19.3 us (15.8).
+int64_t rows_at_once(int64_t n, int32_t w_in)
+{
+    const int64_t most = MOST_PARTIAL / (8 * (int64_t)w_in) / DIRECT_TILE * DIRECT_TILE;
+    return n <= most ? n : most > 0 ? most : DIRECT_TILE;
+}
+ProductPlan plan_terms(const ProductShape &s, bool aligned)
+{
+    ProductPlan p = plan_product(s, aligned);
+    if (p.kernel == BY_ROWS) p = plan_product(s, false); // strips form whole results alone
+    if (p.tail) p.steps_per_split = (int32_t)((s.K + DIRECT_K - 1) / DIRECT_K * s.segments);
+    p.tail = p.tail_splits = 0;
+    p.bytes = (size_t)round_up(2 * p.splits * s.M * s.N * 4, 256);
+    return p;
+}
+size_t terms_bytes(ProductShape s, int layouts)
+{
+    s.sets = 1;
+    const int64_t rows = s.M;
+    if (layouts == PRODUCT_GWT) s.M = rows_at_once(rows, s.N);
+    size_t most = 0;
+    for (int last = 0; last < 2; ++last) {
+        for (int aligned = 0; aligned < 2; ++aligned) {
+            const size_t here = plan_terms(s, aligned).bytes;
+            most = here > most ? here : most;
+        }
+        if (s.M == rows || rows % s.M == 0) break;
+        s.M = rows % s.M;
+    }
+    return most;
+}
+// rest: how far the second term lies behind the first; it is that of the M side of dX (GWT), and of the N side of dW (XTG)
+int launch_terms(ProductShape s, int layouts, ProductArgs &all, int64_t rest, void *partial, char *room, hipStream_t stream)
+{
+    if (int rc = pack_operands(layouts, s, all, room, stream)) return rc;
+    const bool dx = layouts == PRODUCT_GWT;
+    const auto launch = s.type == SLICEGCN_BF16 ? launch_product_bf16 : launch_product_f16;
+    s.sets = 1;
+    const int64_t rows = all.M, at_once = dx ? rows_at_once(rows, all.N) : rows;
+    for (int set = 0; set < all.sets; ++set) {
+        for (int64_t first = 0; first < rows; first += at_once) {
+            ProductArgs a = all;
+            s.M = a.M = rows - first < at_once ? rows - first : at_once;
+            a.sets = 1;
+            a.out[0] = all.out[set] + first * all.ldo[set] * 2;
+            a.ldo[0] = all.ldo[set];
+            if (dx) {
+                for (int i = 0; i < a.segments; ++i) a.a[i].p += first * a.a[i].ld * 2;
+            } else {
+                a.a[0] = all.a[set];
+                a.b[0] = all.b[set];
+            }
+            ProductPlan plan = plan_terms(s, aligned_product(layouts, s, a));
+            a.on_words = product_on_words(layouts, s, a);
+            plan.stage = SUMS_ALONE;
+            for (int term = 0; term < 2; ++term) {
+                a.partial = static_cast<float *>(partial) + term * plan.splits * a.M * a.N;
+                if (int rc = launch(layouts, EPI_STORE, plan, a, stream)) return rc;
+                if (dx) {
+                    for (int i = 0; i < a.segments; ++i) a.a[i].p += rest;
+                } else {
+                    a.b[0].p += rest;
+                }
+            }
+            plan.stage = JOIN_ALONE;
+            plan.splits *= 2;
+            a.partial = static_cast<float *>(partial);
+            if (int rc = launch(layouts, EPI_STORE, plan, a, stream)) return rc;
+        }
+    }
+    return SLICEGCN_OK;
 }
 
 // ---- gradients before the activation ----------------------------------------------------------------------------------
@@ -440,11 +517,11 @@ struct BwdWorkspace {
 ProductShape dx_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q) { return ProductShape{n, w_out, w_in, q, 1, type, false, true}; }
 ProductShape dw_shape(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q) { return ProductShape{w_in, n, w_out, 1, q, type, false, false}; }
 
-BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q)
+BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type, int q, bool two)
 {
     BwdWorkspace w;
     w.ld = round_up(w_out, 8);
-    w.terms = terms_of(n, w_in, w_out, type, q);
+    w.terms = terms_of(n, w_in, w_out, type, q, two);
     w.rows = (size_t)round_up(n * w.ld * type_bytes(type), 256);
     const int64_t parts = slope_grid(n, w_out, type).parts, blocks = narrow_blocks(n, w_in, w_out, type, q);
     w.sums = (size_t)round_up((parts > blocks ? parts : blocks) * q * (int64_t)w_out * 8, 256);
@@ -455,6 +532,10 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
     if (paired(n, w_in, w_out, type, q)) {
         const size_t both = w.terms * (pair_plan(dx_shape(n, w_in, w_out, type, q)).bytes + pair_plan(dw_shape(n, w_in, w_out, type, q)).bytes);
         w.partial = w.partial > both ? w.partial : both;
+    } else if (w.terms == 2) {
+        const size_t a = terms_bytes(dx_shape(n, w_in, w_out, type, q), PRODUCT_GWT), b = terms_bytes(dw_shape(n, w_in, w_out, type, q), PRODUCT_XTG);
+        w.partial = w.partial > a ? w.partial : a;
+        w.partial = w.partial > b ? w.partial : b;
     }
     const size_t u = pack_bytes(PRODUCT_GWT, dx_shape(n, w_in, w_out, type, q), false, true), v = pack_bytes(PRODUCT_XTG, dw_shape(n, w_in, w_out, type, q), true, false);
     w.room = u > v ? u : v;
@@ -465,11 +546,19 @@ BwdWorkspace bwd_workspace(int64_t n, int32_t w_in, int32_t w_out, int32_t type,
 constexpr int64_t MOST_ROWS = ((int64_t)1 << 31) - (1 << 16);
 bool sizes_fit(int64_t n, int32_t w_in, int32_t w_out) { return n >= 0 && n <= MOST_ROWS && w_in >= 1 && w_out >= 1 && w_in <= 1 << 20 && w_out <= 1 << 20; }
 
+// The type of the elements alone
+int32_t one_type(int32_t type) { return type & ~SLICEGCN_TWO_TERMS; }
+slicegcn_product_desc of_one_type(slicegcn_product_desc d)
+{
+    d.type = one_type(d.type);
+    return d;
+}
+
 int check(const char *what, const slicegcn_product_desc *d, const void *io)
 {
     SG_REQUIRE(d && io, SLICEGCN_EINVAL, "%s: NULL descriptor or io", what);
     SG_REQUIRE(d->n >= 0 && d->w_in >= 1 && d->w_out >= 1, SLICEGCN_EINVAL, "%s: need n >= 0 and widths >= 1", what);
-    SG_REQUIRE(known_type(d->type), SLICEGCN_EINVAL, "%s: unknown type", what);
+    SG_REQUIRE(known_type(one_type(d->type)), SLICEGCN_EINVAL, "%s: unknown type", what);
     SG_REQUIRE(d->act >= SLICEGCN_ACT_NONE && d->act <= SLICEGCN_ACT_GELU, SLICEGCN_EINVAL, "%s: unknown activation", what);
     SG_REQUIRE(std::isfinite((float)d->residual), SLICEGCN_EINVAL, "%s: residual is not finite", what);
     SG_REQUIRE(sizes_fit(d->n, d->w_in, d->w_out), SLICEGCN_ERANGE, "%s: n or a width too large", what);
@@ -522,6 +611,7 @@ size_t fwd_bytes(const ProductShape &s) { return partial_bytes(s) + pack_bytes(P
 // Both backward passes.  q = 2: gated
 struct BwdCall {
     const slicegcn_product_desc *d;
+    bool two; // whether the caller asks for two terms
     Operand x, w[2], g, u, dy;
     slicegcn_matrix dx, dr;
     void *dw[2];
@@ -531,7 +621,8 @@ struct BwdCall {
 int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_bytes, hipStream_t stream)
 {
     const slicegcn_product_desc &d = *c.d;
-    const BwdWorkspace w = bwd_workspace(d.n, d.w_in, d.w_out, d.type, q);
+    const bool two = c.two && d.type != SLICEGCN_F32 && (q == 2 || d.act != SLICEGCN_ACT_NONE); // else dP is whole in one
+    const BwdWorkspace w = bwd_workspace(d.n, d.w_in, d.w_out, d.type, q, two);
     if (int rc = check_workspace(what, ws, ws_bytes, w.bytes(q))) return rc;
     const bool want_x = c.dx.data && d.n > 0, want_w = c.dw[0] || c.dw[1], want_b = c.db[0] || c.db[1], want_r = c.dr.data && d.n > 0;
     char *at = static_cast<char *>(ws);
@@ -567,7 +658,7 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
     ProfScope prof(SLICEGCN_PROF_PRODUCT, d.w_out, stream);
     const Operand dx{static_cast<const char *>(c.dx.data), c.dx.ld, 0};
     const unsigned narrow = narrow_blocks(d.n, d.w_in, d.w_out, d.type, q);
-    if (narrow && (want_x || want_w) && !want_r && narrow_rows_fit(c.x) && narrow_rows_fit(c.g) && narrow_rows_fit(c.u) && narrow_rows_fit(c.dy) &&
+    if (narrow && !two && (want_x || want_w) && !want_r && narrow_rows_fit(c.x) && narrow_rows_fit(c.g) && narrow_rows_fit(c.u) && narrow_rows_fit(c.dy) &&
         narrow_rows_fit(dx)) {
         NarrowArgs a{};
         a.x = c.x;
@@ -660,6 +751,11 @@ int backward(const char *what, const BwdCall &c, int q, void *ws, size_t ws_byte
         return launch(want_x ? &x : nullptr, want_w ? &y : nullptr, bias, stream);
     }
     if (int rc = launch_bias(bias, stream)) return rc;
+    if (s.rest) {
+        if (want_x)
+            if (int rc = launch_terms(shape_x, PRODUCT_GWT, x, s.rest, partial, room, stream)) return rc;
+        return want_w ? launch_terms(shape_w, PRODUCT_XTG, y, s.rest, partial, room, stream) : SLICEGCN_OK;
+    }
     if (want_x)
         if (int rc = launch_product(shape_x, PRODUCT_GWT, EPI_STORE, x, partial, room, stream)) return rc;
     if (want_w)
@@ -674,14 +770,15 @@ using namespace slicegcn;
 
 extern "C" size_t slicegcn_product_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
 {
-    if (!sizes_fit(n, w_in, w_out) || !known_type(type) || n == 0) return 0;
-    return fwd_bytes(fwd_shape(n, w_in, w_out, type, false));
+    if (!sizes_fit(n, w_in, w_out) || !known_type(one_type(type)) || n == 0) return 0;
+    return fwd_bytes(fwd_shape(n, w_in, w_out, one_type(type), false));
 }
 
-extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream)
+extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream)
 {
     const char *what = "product_fwd";
-    if (int rc = check(what, d, io)) return rc;
+    if (int rc = check(what, desc, io)) return rc;
+    const slicegcn_product_desc one = of_one_type(*desc), *d = &one;
     SG_REQUIRE(io->W, SLICEGCN_EINVAL, "%s: NULL W", what);
     if (int rc = check_rows(what, "X", io->X, d->n, d->w_in, d->type, true)) return rc;
     if (int rc = check_rows(what, "Y", io->Y, d->n, d->w_out, d->type, true)) return rc;
@@ -715,14 +812,15 @@ extern "C" int slicegcn_product_fwd(const slicegcn_product_desc *d, const sliceg
 
 extern "C" size_t slicegcn_product_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
 {
-    if (!sizes_fit(n, w_in, w_out) || !known_type(type)) return 0;
-    return bwd_workspace(n, w_in, w_out, type, 1).bytes(1);
+    if (!sizes_fit(n, w_in, w_out) || !known_type(one_type(type))) return 0;
+    return bwd_workspace(n, w_in, w_out, one_type(type), 1, type != one_type(type)).bytes(1);
 }
 
-extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *d, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream)
+extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *desc, const slicegcn_product_io *io, void *ws, size_t ws_bytes, void *stream)
 {
     const char *what = "product_bwd";
-    if (int rc = check(what, d, io)) return rc;
+    if (int rc = check(what, desc, io)) return rc;
+    const slicegcn_product_desc one = of_one_type(*desc), *d = &one;
     const bool rows = d->n > 0, slope = d->act != SLICEGCN_ACT_NONE && (io->dX.data || io->dW || io->db);
     if (int rc = check_rows(what, "X", io->X, d->n, d->w_in, d->type, rows && io->dW)) return rc;
     if (int rc = check_rows(what, "P", io->P, d->n, d->w_out, d->type, rows && slope)) return rc;
@@ -735,6 +833,7 @@ extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *d, const sliceg
         if (int rc = check_apart(what, {io->dX.data, io->dW, io->db, io->dR.data}, {io->X.data, io->W, io->P.data, io->dY.data})) return rc;
     BwdCall c{};
     c.d = d;
+    c.two = desc->type != d->type;
     c.x = operand(io->X, d->w_in);
     c.w[0] = weights(io->W, d->w_out);
     c.g = operand(io->P, d->w_out);
@@ -748,14 +847,15 @@ extern "C" int slicegcn_product_bwd(const slicegcn_product_desc *d, const sliceg
 
 extern "C" size_t slicegcn_gated_fwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
 {
-    if (!sizes_fit(n, w_in, w_out) || !known_type(type) || n == 0) return 0;
-    return fwd_bytes(fwd_shape(n, w_in, w_out, type, true));
+    if (!sizes_fit(n, w_in, w_out) || !known_type(one_type(type)) || n == 0) return 0;
+    return fwd_bytes(fwd_shape(n, w_in, w_out, one_type(type), true));
 }
 
-extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream)
+extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream)
 {
     const char *what = "gated_fwd";
-    if (int rc = check(what, d, io)) return rc;
+    if (int rc = check(what, desc, io)) return rc;
+    const slicegcn_product_desc one = of_one_type(*desc), *d = &one;
     SG_REQUIRE(io->Wg && io->Wu, SLICEGCN_EINVAL, "%s: NULL Wg or Wu", what);
     if (int rc = check_rows(what, "X", io->X, d->n, d->w_in, d->type, true)) return rc;
     if (int rc = check_rows(what, "H", io->H, d->n, d->w_out, d->type, true)) return rc;
@@ -790,14 +890,15 @@ extern "C" int slicegcn_gated_fwd(const slicegcn_product_desc *d, const slicegcn
 
 extern "C" size_t slicegcn_gated_bwd_workspace_bytes(int64_t n, int32_t w_in, int32_t w_out, int32_t type)
 {
-    if (!sizes_fit(n, w_in, w_out) || !known_type(type)) return 0;
-    return bwd_workspace(n, w_in, w_out, type, 2).bytes(2);
+    if (!sizes_fit(n, w_in, w_out) || !known_type(one_type(type))) return 0;
+    return bwd_workspace(n, w_in, w_out, one_type(type), 2, type != one_type(type)).bytes(2);
 }
 
-extern "C" int slicegcn_gated_bwd(const slicegcn_product_desc *d, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream)
+extern "C" int slicegcn_gated_bwd(const slicegcn_product_desc *desc, const slicegcn_gated_io *io, void *ws, size_t ws_bytes, void *stream)
 {
     const char *what = "gated_bwd";
-    if (int rc = check(what, d, io)) return rc;
+    if (int rc = check(what, desc, io)) return rc;
+    const slicegcn_product_desc one = of_one_type(*desc), *d = &one;
     const bool rows = d->n > 0;
     if (int rc = check_rows(what, "X", io->X, d->n, d->w_in, d->type, rows && (io->dWg || io->dWu))) return rc;
     if (int rc = check_rows(what, "G", io->G, d->n, d->w_out, d->type, rows)) return rc;
@@ -810,6 +911,7 @@ extern "C" int slicegcn_gated_bwd(const slicegcn_product_desc *d, const slicegcn
         if (int rc = check_apart(what, {io->dX.data, io->dWg, io->dWu, io->dbg, io->dbu}, {io->X.data, io->Wg, io->Wu, io->G.data, io->U.data, io->dH.data})) return rc;
     BwdCall c{};
     c.d = d;
+    c.two = desc->type != d->type;
     c.x = operand(io->X, d->w_in);
     c.w[0] = weights(io->Wg, d->w_out);
     c.w[1] = weights(io->Wu, d->w_out);

@@ -60,8 +60,10 @@ struct ProductShape {
     bool by_rows; // rows of the M side lie along k
 };
 constexpr int BY_REGISTERS = 0, BY_TILES = 1, BY_ROWS = 2; // product_kernels.h, product_direct.h, product_rows.h
+constexpr int ALL = 0, SUMS_ALONE = 1, JOIN_ALONE = 2;     // of a product that is cut: sums of parts and their join, either by itself
 struct ProductPlan {
     int32_t kernel;
+    int32_t stage;
     int32_t tile; // BY_REGISTERS: index of a tile shape
     int32_t splits, steps_per_split;
     int32_t tail, tail_splits; // BY_TILES, splits = 1: the last tiles, and in how many parts of steps_per_split they are cut

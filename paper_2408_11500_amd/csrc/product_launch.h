@@ -28,6 +28,10 @@ template <class T, int LM, int LN, int EPI> int launch_layouts(const ProductPlan
 {
     a.splits = plan.splits;
     a.steps_per_split = plan.steps_per_split;
+    if constexpr (EPI == EPI_STORE) {
+        if (plan.stage == SUMS_ALONE) return launch_sums<T, LM, LN, EPI_STORE, true>(plan, a, stream);
+        if (plan.stage == JOIN_ALONE) return launch_join<T, EPI_STORE>(a, stream);
+    }
     if (plan.splits == 1) return launch_sums<T, LM, LN, EPI, false>(plan, a, stream);
     const int32_t sets = a.sets;
     if (EPI == EPI_GATED) { // each product by itself, and both joined

@@ -97,16 +97,18 @@ class BlockNorm:
 
 class GatedFeedForward:
     """x' = x + (act(u Wg) * (u Wu)) Wd on rows of fp32, bf16 or fp16: gated projections to ``inner`` columns and the way back with the
-    residual in its epilogue.  ``u``: x behind the norm before the block."""
+    residual in its epilogue.  ``u``: x behind the norm before the block.  ``two_terms``: gradients before the activation are kept in two terms of a
+    16-bit type."""
 
-    def __init__(self, n: int, width: int, inner: int, act: int = B.ACT_SILU, dtype: torch.dtype = torch.float32, device="cuda"):
-        self.act = act
+    def __init__(self, n: int, width: int, inner: int, act: int = B.ACT_SILU, dtype: torch.dtype = torch.float32, device="cuda",
+                 two_terms: bool = False):
+        self.act, self.two_terms = act, two_terms
         like = dict(dtype=dtype, device=device)
         self.Wg, self.Wu, self.dWg, self.dWu = (torch.zeros((width, inner), **like) for _ in range(4))
         self.Wd, self.dWd = (torch.zeros((inner, width), **like) for _ in range(2))
         self.G, self.U, self.H, self.dH = (torch.empty((n, inner), **like) for _ in range(4))
         self.x, self.du = (torch.empty((n, width), **like) for _ in range(2))
-        self.ws = torch.empty(max(B.slicegcn_gated_fwd_workspace_bytes(n, width, inner, dtype), B.slicegcn_gated_bwd_workspace_bytes(n, width, inner, dtype),
+        self.ws = torch.empty(max(B.slicegcn_gated_fwd_workspace_bytes(n, width, inner, dtype), B.slicegcn_gated_bwd_workspace_bytes(n, width, inner, dtype, two_terms),
                                   B.slicegcn_product_fwd_workspace_bytes(n, inner, width, dtype),
                                   B.slicegcn_product_bwd_workspace_bytes(n, inner, width, dtype)), dtype=torch.uint8, device=device)
 
@@ -121,7 +123,8 @@ class GatedFeedForward:
     def backward(self, u: torch.Tensor, dx: torch.Tensor) -> torch.Tensor:
         """Gradient of u from that of x'; the gradient of x is that of x' (and what reaches it through u)."""
         B.slicegcn_product_bwd(self.H, self.Wd, None, dx, self.ws, dX=self.dH, dW=self.dWd)
-        B.slicegcn_gated_bwd(u, self.Wg, self.Wu, self.G, self.U, self.dH, self.ws, dX=self.du, dWg=self.dWg, dWu=self.dWu, act=self.act)
+        B.slicegcn_gated_bwd(u, self.Wg, self.Wu, self.G, self.U, self.dH, self.ws, dX=self.du, dWg=self.dWg, dWu=self.dWu, act=self.act,
+                             two_terms=self.two_terms)
         return self.du
 
     def parameter_slots(self):
