@@ -98,19 +98,23 @@ class BlockNorm:
 class GatedFeedForward:
     """x' = x + (act(u Wg) * (u Wu)) Wd on rows of fp32, bf16 or fp16: gated projections to ``inner`` columns and the way back with the
     residual in its epilogue.  ``u``: x behind the norm before the block.  ``two_terms``: gradients before the activation are kept in two terms of a
-    16-bit type."""
+    16-bit type.  Without ``training`` nothing is kept for a backward pass and there are no gradients."""
 
     def __init__(self, n: int, width: int, inner: int, act: int = B.ACT_SILU, dtype: torch.dtype = torch.float32, device="cuda",
-                 two_terms: bool = False):
-        self.act, self.two_terms = act, two_terms
+                 two_terms: bool = False, training: bool = True):
+        self.act, self.two_terms, self.training = act, two_terms, training
         like = dict(dtype=dtype, device=device)
-        self.Wg, self.Wu, self.dWg, self.dWu = (torch.zeros((width, inner), **like) for _ in range(4))
-        self.Wd, self.dWd = (torch.zeros((inner, width), **like) for _ in range(2))
-        self.G, self.U, self.H, self.dH = (torch.empty((n, inner), **like) for _ in range(4))
-        self.x, self.du = (torch.empty((n, width), **like) for _ in range(2))
-        self.ws = torch.empty(max(B.slicegcn_gated_fwd_workspace_bytes(n, width, inner, dtype), B.slicegcn_gated_bwd_workspace_bytes(n, width, inner, dtype, two_terms),
-                                  B.slicegcn_product_fwd_workspace_bytes(n, inner, width, dtype),
-                                  B.slicegcn_product_bwd_workspace_bytes(n, inner, width, dtype)), dtype=torch.uint8, device=device)
+        self.Wg, self.Wu = (torch.zeros((width, inner), **like) for _ in range(2))
+        self.Wd = torch.zeros((inner, width), **like)
+        self.H, self.x = torch.empty((n, inner), **like), torch.empty((n, width), **like)
+        self.G = self.U = None
+        sizes = [B.slicegcn_gated_fwd_workspace_bytes(n, width, inner, dtype), B.slicegcn_product_fwd_workspace_bytes(n, inner, width, dtype)]
+        if training:
+            self.dWg, self.dWu, self.dWd = (torch.zeros_like(w) for w in (self.Wg, self.Wu, self.Wd))
+            self.G, self.U, self.dH = (torch.empty((n, inner), **like) for _ in range(3))
+            self.du = torch.empty((n, width), **like)
+            sizes += [B.slicegcn_gated_bwd_workspace_bytes(n, width, inner, dtype, two_terms), B.slicegcn_product_bwd_workspace_bytes(n, inner, width, dtype)]
+        self.ws = torch.empty(max(sizes), dtype=torch.uint8, device=device)
 
     def set_params(self, Wg, Wu, Wd):
         for dst, src in ((self.Wg, Wg), (self.Wu, Wu), (self.Wd, Wd)):
@@ -122,13 +126,15 @@ class GatedFeedForward:
 
     def backward(self, u: torch.Tensor, dx: torch.Tensor) -> torch.Tensor:
         """Gradient of u from that of x'; the gradient of x is that of x' (and what reaches it through u)."""
+        if not self.training:
+            raise RuntimeError("a feed-forward block without training keeps nothing for a backward pass")
         B.slicegcn_product_bwd(self.H, self.Wd, None, dx, self.ws, dX=self.dH, dW=self.dWd)
         B.slicegcn_gated_bwd(u, self.Wg, self.Wu, self.G, self.U, self.dH, self.ws, dX=self.du, dWg=self.dWg, dWu=self.dWu, act=self.act,
                              two_terms=self.two_terms)
         return self.du
 
     def parameter_slots(self):
-        return [(self, w, self, "d" + w) for w in ("Wg", "Wu", "Wd")]
+        return [(self, w, self, "d" + w) for w in ("Wg", "Wu", "Wd")] if self.training else []
 
 
 class TokenTrainer:
