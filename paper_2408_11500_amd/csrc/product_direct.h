@@ -6,7 +6,7 @@
 // step a wavefront waits for its own loads of the step after this one and meets the others at a barrier: then that step is whole in LDS, and nobody reads the
 // buffer any more that the next loads are for.  During a step the operand registers for the next one are read: those of the N side into a second set, those of the M
 // side into the registers that the step is done with.
-// 8192 rows 4096 -> 10240 gated bf16: 1.03 ms, 1.34 PFLOP/s (a library's plain products of these sizes: 0.90 to 1.35); bound by the matrix instructions, which run 60 to 70 % of
+// 8192 rows 4096 -> 10240 gated bf16: 1.05 ms, 1.31 PFLOP/s (a library's plain products of these sizes: 0.90 to 1.35); bound by the matrix instructions, which run 60 to 70 % of
 // the time at the clock that their power leaves.  With four wavefronts of 128 x 128 each, with five buffers or with 32 x 32 x 16
 // instructions (1.81 PFLOP/s by themselves, these 2.05) slower.
 // The waits are counted by hand, since the compiler does not know which reads of LDS a load in flight has to do with; the loads are therefore inline assembly,

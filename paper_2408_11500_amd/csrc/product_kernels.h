@@ -6,7 +6,7 @@
 // transposing read ds_read_b64_tr_b16, of which 16 lanes together take 4 k of 16 columns and get 4 k of a column each.
 // fp32 operands are split into three bf16 terms each, x = x0 + x1 + x2, every term the rest rounded to 8 bits: |x1| <= 2^-8 |x|, |x2| <= 2^-16 |x|, and what
 // is left is at most 2^-24 |x|.  Six products are added, smallest first; the three that are left out are below 2^-23 of the product together.  Six bf16
-// instructions take 96 cycles for what the fp32 instruction takes 256 for.  fp32, 233 k rows 602 -> 256 with gelu: 440 us, 164 TFLOP/s (a library's product of 8192^3 reaches 154);
+// instructions take 96 cycles for what the fp32 instruction takes 256 for.  fp32, 233 k rows 602 -> 256 with gelu: 447 us, 161 TFLOP/s (a library's product of 8192^3 reaches 154);
 // bound by the matrix instructions (53 % of the time), the reads of LDS and the splitting, which three workgroups a CU overlap in part, and by the stores of results.
 #pragma once
 

@@ -9,7 +9,7 @@
 // N side of dW (k across the rows: transposing reads).  The weights for dX stay in registers, a wavefront's for 16 columns of dX, and so do the sums of dW, a
 // wavefront's 64 x 64.  Nothing in the loop branches on a lane: rows and columns that are not there are read as zeros and not written by the buffers' range checks, so
 // that the compiler can count the loads in flight.
-// 2.4 M rows 100 -> 256 bf16 gelu: 0.95 ms, 3.7 TB/s; bound by the arithmetic of the gelu's slope (some 35 instructions an element).
+// 2.4 M rows 100 -> 256 bf16 gelu: 0.96 ms, 3.6 TB/s; bound by the arithmetic of the gelu's slope (some 35 instructions an element).
 // Order of the sums: a workgroup's blocks in turn (1024 at most), the workgroups' sums in fp64 in order.
 #pragma once
 
