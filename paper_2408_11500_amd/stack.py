@@ -531,7 +531,8 @@ class AdamW:
     models, which stay where they are: one library call updates them all.  ``state_bits`` = 8: the means are kept as e4m3 numbers with a
     scale per 128 elements, 2 bytes a parameter instead of 8.  Tensors of 16 bits get fp32 masters.  ``max_norm`` as in ``Optimizer``;
     where the gradients' norm is not finite, an update is left out, and does not count among the steps that the means are corrected by
-    (``steps`` holds how many were taken, on the device)."""
+    (with ``max_norm`` ``steps`` holds how many were taken, on the device).  ``t``: the calls of ``step`` so far; who goes on with the states of an earlier
+    run sets it to the steps that these have seen."""
 
     def __init__(self, models, lr_max: float, lr_min: float = 0.0, t_max: int = 1, beta1: float = 0.9, beta2: float = 0.999,
                  eps: float = 1e-8, weight_decay: float = 0.01, max_norm: float | None = None, state_bits: int = 32, seed: int = 0):
@@ -551,7 +552,6 @@ class AdamW:
                                   decays=[weight_decay if p.dim() > 1 else 0.0 for p in self.params])
         self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps)
         self.lr_max, self.lr_min, self.t_max, self.seed = lr_max, lr_min, t_max, seed
-        self.t = 0
         # (with an infinite bound a norm that is infinite too would not be beyond it)
         self.max_norm = None if max_norm is None else min(max_norm, sys.float_info.max)
         self.factor = None
@@ -561,10 +561,21 @@ class AdamW:
             self.norm_ws = torch.empty(B.slicegcn_global_norm_workspace_bytes(self.gradients), dtype=torch.uint8, device=dev)
             self.counter = torch.zeros(4, dtype=torch.int32, device=dev)
             self.steps = self.counter[:1]
+        self.t = 0
+
+    @property
+    def t(self) -> int:
+        return self._t
+
+    @t.setter
+    def t(self, steps: int):
+        self._t = steps
+        if self.max_norm is not None:
+            self.steps.fill_(steps)
 
     def step(self, epoch: int) -> float:
         """One update with the learning rate of ``epoch`` (0-based); returns that rate."""
-        self.t += 1
+        self._t += 1
         lr = B.slicegcn_cosine_lr(self.lr_max, self.lr_min, epoch, self.t_max)
         if self.max_norm is None:
             B.slicegcn_adamw_step(self.tensors, lr, self.t, seed=self.seed + self.t, **self.hyper)

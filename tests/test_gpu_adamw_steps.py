@@ -35,7 +35,7 @@ def test_updates_after_one_that_was_left_out(left_out, bad, bits):
         if t in left_out:
             a.g[3, 4] = bad
         opt.step(t)
-        plain.t += 1
+        plain._t += 1
         if t not in left_out:
             B.slicegcn_global_norm(B.TensorList([g]), plain.norm, plain.norm_ws, max_norm=1.0, factor=plain.factor)
             b.g.copy_(g)
@@ -104,3 +104,26 @@ def test_without_a_bound_on_the_norm_updates_on_gradients_that_are_not_finite_ar
     opt.step(0)
     plain.step(0)
     assert torch.equal(m.w, same.w) and int(opt.steps) == 1
+
+
+@pytest.mark.parametrize("max_norm", [None, 1.0])
+def test_going_on_with_the_states_of_an_earlier_run(max_norm):
+    """With t set to the steps that they have seen, as one run."""
+    a, b, grads = Model(), Model(), [torch.randn((50, 33), generator=torch.Generator().manual_seed(t)).cuda() for t in range(6)]
+    make = lambda m: AdamW([m], lr_max=0.01, max_norm=max_norm)
+    one, first = make(a), make(b)
+    for t in range(6):
+        a.g.copy_(grads[t])
+        one.step(t)
+    for t in range(3):
+        b.g.copy_(grads[t])
+        first.step(t)
+    second = make(b)
+    for name in ("m", "v"):
+        for to, of in zip(getattr(second, name), getattr(first, name)):
+            to.copy_(of)
+    second.t = first.t
+    for t in range(3, 6):
+        b.g.copy_(grads[t])
+        second.step(t)
+    assert torch.equal(a.w, b.w) and second.t == 6

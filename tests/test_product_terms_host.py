@@ -31,3 +31,11 @@ def test_workspaces(L, n, w_in, w_out):  # noqa: F811
             assert two % 256 == 0 and two >= one and two >= 2 * rows
             # the second term, sums of two parts of a turn of dX, and two for one of each part of dW
             assert two <= 2 * one + rows + (512 << 20) + 2 * q * 4 * w_in * w_out * (1 + n // 32768) + 4096
+
+
+@pytest.mark.parametrize("op", ["product", "gated"])
+def test_a_workspace_for_one_term_is_refused(L, op):  # noqa: F811
+    n, w_in, w_out = 3000, 300, 136
+    one = getattr(L, f"slicegcn_{op}_bwd_workspace_bytes")(n, w_in, w_out, B.BF16)
+    d = desc(n, w_in, w_out, B.BF16 | B.TWO_TERMS, act=B.ACT_GELU)
+    assert call(L, op, "bwd", d=d, ld=300, ws_bytes=one) == B.EWORKSPACE
